@@ -272,6 +272,96 @@ int grf_masked_attn_mhat(grf_ctx* ctx, const grf_features* feat, int32_t G, int3
                          int dtype, const void* phiQ, const void* phiK, const void* V, void* out, float* den_out);
 
 /*
+ * Softmax attention over tokens in an order (Eq. 1, with what Eq. 2 multiplies by added to the scores instead): for sequence b, head h
+ * (its keys: head h / (heads / kv_heads)), query i at position p = q_start[b] + i, key j:
+ *   x = scale q_i . k_j,   c = cap tanh(x / cap) (cap > 0) or x (cap = 0),   s_ij = c + bias_h(j - p)
+ *   out_i = sum_j exp(s_ij - lse_i) v_j,   lse_i = log sum_j exp(s_ij)       over the keys j that query i sees
+ * A query sees key j when all of these hold:
+ *   j < k_len[b];   mask FULL, or CAUSAL: j <= p, or PREFIX: j <= p or j < prefix[b];
+ *   no documents, or q_doc[b][i] == k_doc[b][j] >= 0 (a token whose document is negative sees and is seen by none).
+ * A query that sees no key, or only keys with s = -inf, gets out = 0 and lse = -inf, and its gradients are 0.
+ * bias_h: NONE; SLOPES: -slopes[h] |j - p|; BUCKETS: table[h][bucket(j - p)], where the distance n = max(p - j, 0), or |j - p| when
+ * two_sided, falls into the last bucket y with first[y] <= n, and two_sided keys behind the query (j > p) use a second half of the
+ * table, columns n_buckets .. 2 n_buckets - 1.  grf_relative_buckets makes the usual choice of first[].
+ *
+ * What a token that nobody sees holds (infinities, NaN) does not matter, and in grf_softmax_attn what a key that a query does not see
+ * holds does not matter to that query.  An infinity or NaN in what it does see makes its results infinite or NaN; in a row of dout it
+ * may reach all dim columns of the gradients that the row enters.
+ */
+#define GRF_ORDER_FULL   0
+#define GRF_ORDER_CAUSAL 1
+#define GRF_ORDER_PREFIX 2
+#define GRF_BIAS_NONE    0
+#define GRF_BIAS_SLOPES  1
+#define GRF_BIAS_BUCKETS 2
+#define GRF_MAX_BUCKETS  64
+#define GRF_MAX_TOKENS   (1 << 22)   /* largest n_q and n_k */
+
+/* Zero the whole structure first: a zero field means "not used" (a stride triple of zeros: contiguous [batch][heads][tokens][dim]). */
+typedef struct grf_softmax_desc {
+    int32_t batch, heads, kv_heads, n_q, n_k;  /* kv_heads divides heads                                                     */
+    int32_t dim;                       /* of Q, K and V: a multiple of 8, 8 .. 128                                           */
+    int32_t dtype;                     /* of Q, K, V, out, their gradients, and the bucket table and its gradient            */
+    float scale, cap;                  /* finite; cap >= 0                                                                   */
+    int32_t order;                     /* GRF_ORDER_*                                                                        */
+    int32_t bias;                      /* GRF_BIAS_*                                                                         */
+    int32_t n_buckets, two_sided;      /* BUCKETS: 1 .. GRF_MAX_BUCKETS                                                      */
+    int32_t first[GRF_MAX_BUCKETS];    /* smallest distance of each bucket: first[0] = 0, ascending                          */
+    const float* slopes;               /* DEVICE [heads]                                                                     */
+    const void* table;                 /* DEVICE [heads][n_buckets * (1 + two_sided)], dtype                                 */
+    const int32_t* k_len;              /* DEVICE [batch] or NULL: n_k each; values are clipped to 0 .. n_k                   */
+    const int32_t* q_start;            /* DEVICE [batch] or NULL: n_k - n_q each (the queries are the last tokens)           */
+    const int32_t* prefix;             /* DEVICE [batch], with GRF_ORDER_PREFIX                                              */
+    const int32_t* q_doc;              /* DEVICE [batch][n_q] and                                                            */
+    const int32_t* k_doc;              /* DEVICE [batch][n_k]: both or neither; any order of documents                       */
+    /* element strides (batch, head, token) of [batch][heads or kv_heads][tokens][dim]; dim itself is contiguous.  Multiples of 16
+     * bytes, not negative.  Q, K, V and dout may have strides of 0 (a broadcast); written arrays must not overlap themselves. */
+    int64_t q_stride[3], k_stride[3], v_stride[3], out_stride[3];
+    int64_t dout_stride[3], dq_stride[3], dk_stride[3], dv_stride[3];
+} grf_softmax_desc;
+
+/* first[0 .. n_buckets-1] (HOST): half of the buckets hold one distance each, 0, 1, ..; the others split the distances from h =
+ * n_buckets / 2 to max_distance evenly by their logarithm, and the last goes on without end: first[h + y] is the smallest n with
+ * (n / h)^(n_buckets - h) >= (max_distance / h)^y, found in integers, and at least one more than the one before.
+ * GRF_ERR_INVALID unless 2 <= n_buckets <= GRF_MAX_BUCKETS and n_buckets / 2 < max_distance <= 2^24. */
+int grf_relative_buckets(int32_t n_buckets, int32_t max_distance, int32_t* first);
+
+/* Bytes of DEVICE workspace that the call below needs for this descriptor (its pointers may still be NULL, except that it
+ * matters which are): grf_softmax_attn (backward = 0) or grf_softmax_attn_backward (1).  May be 0; 0 also on invalid arguments. */
+size_t grf_softmax_attn_workspace_bytes(const grf_ctx* ctx, const grf_softmax_desc* desc, int backward);
+
+/* Q, K, V, out: DEVICE, 16-byte aligned.  lse: optional DEVICE fp32 [batch][heads][n_q].  rest: optional, bf16 only: DEVICE [batch][heads]
+ * [n_q][dim] contiguous, 16-byte aligned, receives what rounding to bf16 took from out (rounded to bf16 itself): the backward pass uses it
+ * so that D_i, a difference of nearly equal terms where a row looks at few keys, does not inherit that rounding.  workspace: DEVICE, 256-byte aligned (may be
+ * NULL where 0 bytes are needed); its contents are scratch of this call alone, so calls that may run at the same time, captured ones
+ * among them, need one each.  Few queries (n_q <= 16) are served by kernels that split the keys.  bf16 products have their probabilities
+ * rounded to bf16 (by at most 2^-8 relative each), sums are fp32; summation order is fixed.  Asynchronous; can be captured.
+ * GRF_ERR_TOO_LARGE: more than GRF_MAX_TOKENS tokens, or more than 65535 (batch, head) pairs. */
+int grf_softmax_attn(grf_ctx* ctx, const grf_softmax_desc* desc, const void* Q, const void* K, const void* V, void* out, float* lse,
+                     void* rest, void* workspace, size_t workspace_bytes);
+
+/* Gradients of grf_softmax_attn for dout = d(loss)/d(out), from its out, lse and (or NULL) rest, with the same descriptor:
+ *   D_i = dout_i . (out_i + rest_i),  dS_ij = P_ij (dout_i . v_j - D_i),  dX_ij = dS_ij (1 - (c_ij / cap)^2)  (cap = 0: dS_ij)
+ *   dQ_i = scale sum_j dX_ij k_j,  dK_j = scale sum_i dX_ij q_i,  dV_j = sum_i P_ij dout_i,  dtable[h][y] = sum of dS_ij over bucket y
+ * dK and dV are sums over the heads that share them; dtable (dtype, [heads][n_buckets * (1 + two_sided)], optional, BUCKETS only) over the
+ * batch.  All outputs are overwritten, rows that nothing reaches with zeros; dQ, dK, dV are all required.  No atomic additions: equal
+ * calls give equal bits.  Scores of magnitude beyond 1e30 in a row's largest place leave P_ij of that row undefined in 0 .. 1. */
+int grf_softmax_attn_backward(grf_ctx* ctx, const grf_softmax_desc* desc, const void* Q, const void* K, const void* V, const void* out,
+                              const float* lse, const void* rest, const void* dout, void* dQ, void* dK, void* dV, void* dtable, void* workspace,
+                              size_t workspace_bytes);
+
+/* The learned relative position bias by itself, as rows of a matrix (compare grf_mask_rows): rows[h][i][j] = table[h][bucket(j - (q_start
+ * + i))], buckets as above; first: HOST [n_buckets].  table [heads][n_buckets * (1 + two_sided)] and rows [heads][n_q][n_k]: DEVICE, dtype.
+ * The backward call sums drows [batch][heads][n_q][n_k] into dtable (fp32 sums in a fixed order, one rounding to dtype), for which it
+ * needs the workspace.  Asynchronous.  At most GRF_MAX_TOKENS tokens and 65535 heads. */
+int grf_relative_bias(grf_ctx* ctx, int32_t heads, int32_t n_q, int32_t n_k, int32_t q_start, int32_t n_buckets, int two_sided,
+                      const int32_t* first, int dtype, const void* table, void* rows);
+size_t grf_relative_bias_workspace_bytes(int32_t heads, int32_t n_q, int32_t n_k, int32_t n_buckets, int two_sided);
+int grf_relative_bias_backward(grf_ctx* ctx, int32_t batch, int32_t heads, int32_t n_q, int32_t n_k, int32_t q_start,
+                               int32_t n_buckets, int two_sided, const int32_t* first, int dtype, const void* drows, void* dtable,
+                               void* workspace, size_t workspace_bytes);
+
+/*
  * The whole path of Alg. 1 from HOST buffers, for callers that keep nothing on the device:
  * copies the graph and phi(Q), phi(K), V to the device, samples features, evaluates the attention and
  * copies `out` ([G][N][d], dtype) back; returns after the result is in `out`, with an error after its copies have ended.  Device buffers and the

@@ -1,6 +1,8 @@
 """Object layer over the binding: owns torch device tensors and handles, computes nothing itself."""
 from __future__ import annotations
 
+from typing import NamedTuple
+
 import numpy as np
 import torch
 
@@ -130,3 +132,148 @@ def masked_attn_mhat(ctx: Context, feat: Features, phiQ, phiK, V, want_den=False
     den = torch.empty((G, N), dtype=torch.float32, device=V.device) if want_den else None
     B.grf_masked_attn_mhat(ctx.handle, feat.handle, G, N, m, d, B.dtype_code(phiQ), phiQ, phiK, V, out, den)
     return (out, den) if want_den else out
+
+
+ORDERS = {"full": B.GRF_ORDER_FULL, "causal": B.GRF_ORDER_CAUSAL, "prefix": B.GRF_ORDER_PREFIX}
+
+
+def relative_buckets(n_buckets: int = 32, max_distance: int = 128) -> np.ndarray:
+    """Smallest distance of each bucket of a learned relative position bias (half of them exact, half logarithmic)."""
+    return B.grf_relative_buckets(n_buckets, max_distance)
+
+
+class SoftmaxSaved(NamedTuple):
+    """What softmax_attn keeps of its rows for softmax_attn_backward."""
+    lse: torch.Tensor                   # [B, H, Nq] fp32
+    rest: torch.Tensor | None           # [B, H, Nq, d] bf16: what rounding took from out (None in fp32)
+
+
+def _tokens(t, device, shape, name):
+    """Address of an int32 device array of the given shape; None -> None."""
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or t.device != device or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous int32 tensor {shape} on {device}")
+    return t.data_ptr()
+
+
+def _stride3(t, name):
+    """Strides of [batch, heads, tokens, dim] whose last axis is contiguous."""
+    s = t.stride()
+    if s[3] != 1 and t.shape[3] > 1:
+        raise ValueError(f"{name}: the last axis must be contiguous")
+    # (all zeros would mean "contiguous": an axis of one token, head or sequence is never stepped over, so any stride does)
+    if s[0] == s[1] == s[2] == 0 and t.shape[0] * t.shape[1] * t.shape[2] > 1:
+        raise ValueError(f"{name}: a tensor broadcast along every axis")
+    return s[:3]
+
+
+def _softmax_desc(ctx, q, k, v, scale, cap, mask, k_len, q_start, prefix, q_doc, k_doc, slopes, table, first, two_sided):
+    if q.dim() != 4 or k.dim() != 4 or v.shape != k.shape:
+        raise ValueError("expected q [B, H, Nq, d] and k, v [B, KV, Nk, d]")
+    batch, heads, n_q, dim = q.shape
+    kv_heads, n_k = k.shape[1], k.shape[2]
+    device = torch.device("cuda", ctx.device)
+    if k.shape[0] != batch or k.shape[3] != dim or k.dtype != q.dtype or v.dtype != q.dtype:
+        raise ValueError("q, k and v disagree in batch, dim or type")
+    if q.device != device or k.device != device or v.device != device:
+        raise ValueError(f"expected tensors on {device}")
+    s = B.SoftmaxDesc()
+    s.batch, s.heads, s.kv_heads, s.n_q, s.n_k, s.dim, s.dtype = batch, heads, kv_heads, n_q, n_k, dim, B.dtype_code(q)
+    s.scale, s.cap, s.order = dim ** -0.5 if scale is None else scale, cap, ORDERS[mask]
+    s.q_stride[:], s.k_stride[:], s.v_stride[:] = _stride3(q, "q"), _stride3(k, "k"), _stride3(v, "v")
+    s.k_len = _tokens(k_len, device, (batch,), "k_len")
+    s.q_start = _tokens(q_start, device, (batch,), "q_start")
+    s.prefix = _tokens(prefix, device, (batch,), "prefix")
+    s.q_doc = _tokens(q_doc, device, (batch, n_q), "q_doc")
+    s.k_doc = _tokens(k_doc, device, (batch, n_k), "k_doc")
+    if slopes is not None and table is not None:
+        raise ValueError("slopes or a table, not both")
+    if slopes is not None:
+        if slopes.dtype != torch.float32 or slopes.device != device or tuple(slopes.shape) != (heads,) or not slopes.is_contiguous():
+            raise ValueError(f"slopes: expected a contiguous float32 tensor ({heads},) on {device}")
+        s.bias, s.slopes = B.GRF_BIAS_SLOPES, slopes.data_ptr()
+    if table is not None:
+        if first is None or not 1 <= len(first) <= B.GRF_MAX_BUCKETS:
+            raise ValueError(f"a table needs first, the smallest distance of each of 1 .. {B.GRF_MAX_BUCKETS} buckets")
+        n = len(first)
+        shape = (heads, n * (2 if two_sided else 1))
+        if table.dtype != q.dtype or table.device != device or tuple(table.shape) != shape or not table.is_contiguous():
+            raise ValueError(f"table: expected a contiguous {q.dtype} tensor {shape} on {device}")
+        s.bias, s.table, s.n_buckets, s.two_sided = B.GRF_BIAS_BUCKETS, table.data_ptr(), n, int(two_sided)
+        s.first[:n] = [int(y) for y in first]
+    return s
+
+
+def _scratch(nbytes, device):
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+
+
+def softmax_attn(ctx: Context, q, k, v, scale=None, cap=0.0, mask="full", k_len=None, q_start=None, prefix=None, q_doc=None,
+                 k_doc=None, slopes=None, table=None, first=None, two_sided=False, want_lse=False, out=None, workspace=None):
+    """Softmax attention over tokens in an order (grf_softmax_attn).  q [B, H, Nq, d], k, v [B, KV, Nk, d]: CUDA tensors (fp32 or bf16)
+    of any strides with a contiguous last axis; KV divides H.  mask: "full", "causal", "prefix" (with prefix [B]).  k_len, q_start,
+    prefix [B], q_doc [B, Nq], k_doc [B, Nk]: int32.  A bias by distance: slopes [H] (fp32), or table [H, len(first)] (twice as many
+    columns when two_sided) with first as relative_buckets gives it.  Returns out [B, H, Nq, d]; with want_lse (out, SoftmaxSaved),
+    which the backward pass takes."""
+    s = _softmax_desc(ctx, q, k, v, scale, cap, mask, k_len, q_start, prefix, q_doc, k_doc, slopes, table, first, two_sided)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    elif out.shape != q.shape or out.dtype != q.dtype or out.device != q.device:
+        raise ValueError("out: expected the shape, type and device of q")
+    else:
+        s.out_stride[:] = _stride3(out, "out")
+    lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device) if want_lse else None
+    if workspace is None:
+        workspace = _scratch(B.grf_softmax_attn_workspace_bytes(ctx.handle, s, False), q.device)
+    rest = torch.empty(q.shape, dtype=q.dtype, device=q.device) if want_lse and q.dtype == torch.bfloat16 else None
+    B.grf_softmax_attn(ctx.handle, s, q, k, v, out, lse, rest, workspace, workspace.numel() if workspace is not None else 0)
+    return (out, SoftmaxSaved(lse, rest)) if want_lse else out
+
+
+def softmax_attn_backward(ctx: Context, q, k, v, out, saved, dout, scale=None, cap=0.0, mask="full", k_len=None, q_start=None,
+                          prefix=None, q_doc=None, k_doc=None, slopes=None, table=None, first=None, two_sided=False,
+                          want_dtable=True, workspace=None):
+    """Gradients of softmax_attn from its out and SoftmaxSaved and the gradient dout of out (any strides): (dq, dk, dv, dtable), dtable None
+    without a table.  Gradients of broadcast or shared k, v are those of the tensors as they are passed."""
+    s = _softmax_desc(ctx, q, k, v, scale, cap, mask, k_len, q_start, prefix, q_doc, k_doc, slopes, table, first, two_sided)
+    for name, t in (("out", out), ("dout", dout)):
+        if t.shape != q.shape or t.dtype != q.dtype or t.device != q.device:
+            raise ValueError(f"{name}: expected the shape, type and device of q")
+    lse, rest = saved
+    if lse.shape != q.shape[:3] or lse.dtype != torch.float32 or lse.device != q.device:
+        raise ValueError("lse: expected float32 [B, H, Nq]")
+    if rest is not None and (rest.shape != q.shape or rest.dtype != q.dtype or rest.device != q.device):
+        raise ValueError("rest: expected the shape, type and device of q")
+    s.out_stride[:], s.dout_stride[:] = _stride3(out, "out"), _stride3(dout, "dout")
+    dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+    dtable = torch.empty_like(table) if table is not None and want_dtable else None
+    if workspace is None:
+        workspace = _scratch(B.grf_softmax_attn_workspace_bytes(ctx.handle, s, True), q.device)
+    B.grf_softmax_attn_backward(ctx.handle, s, q, k, v, out, lse, rest, dout, dq, dk, dv, dtable, workspace, workspace.numel())
+    return dq, dk, dv, dtable
+
+
+def relative_bias(ctx: Context, table, first, n_q, n_k, two_sided=False, q_start=None):
+    """Rows [H, n_q, n_k] of the learned relative position bias table [H, len(first)] (twice as many columns when two_sided); the
+    queries are the last of the n_k tokens unless q_start says where they begin."""
+    heads = table.shape[0]
+    if tuple(table.shape) != (heads, len(first) * (2 if two_sided else 1)):
+        raise ValueError("table: expected one column per bucket and side")
+    rows = torch.empty((heads, n_q, n_k), dtype=table.dtype, device=table.device)
+    B.grf_relative_bias(ctx.handle, heads, n_q, n_k, n_k - n_q if q_start is None else q_start, first, two_sided,
+                        B.dtype_code(table), table, rows)
+    return rows
+
+
+def relative_bias_backward(ctx: Context, drows, first, two_sided=False, q_start=None, workspace=None):
+    """Gradient [H, columns] of relative_bias's table from drows [B, H, n_q, n_k] (or [H, n_q, n_k]), summed over the batch."""
+    if drows.dim() == 3:
+        drows = drows[None]
+    batch, heads, n_q, n_k = drows.shape
+    dtable = torch.empty((heads, len(first) * (2 if two_sided else 1)), dtype=drows.dtype, device=drows.device)
+    if workspace is None:
+        workspace = _scratch(B.grf_relative_bias_workspace_bytes(heads, n_q, n_k, len(first), two_sided), drows.device)
+    B.grf_relative_bias_backward(ctx.handle, batch, heads, n_q, n_k, n_k - n_q if q_start is None else q_start, first, two_sided,
+                                 B.dtype_code(drows), drows, dtable, workspace, workspace.numel())
+    return dtable

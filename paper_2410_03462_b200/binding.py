@@ -17,6 +17,9 @@ GRF_ERR_INVALID, GRF_ERR_TOO_LARGE, GRF_ERR_WORKSPACE, GRF_ERR_CUDA, GRF_ERR_NOM
 GRF_ERR_TIMEOUT = -7
 GRF_DTYPE_F32, GRF_DTYPE_BF16 = 0, 1
 GRF_KERNEL_LINEAR, GRF_KERNEL_SOFTMAX = 0, 1
+GRF_ORDER_FULL, GRF_ORDER_CAUSAL, GRF_ORDER_PREFIX = 0, 1, 2
+GRF_BIAS_NONE, GRF_BIAS_SLOPES, GRF_BIAS_BUCKETS = 0, 1, 2
+GRF_MAX_BUCKETS = 64
 
 _LIB_PATH = _build.LIB
 if not os.path.exists(_LIB_PATH):
@@ -25,6 +28,18 @@ lib = ctypes.CDLL(_LIB_PATH)
 
 _vp, _i32, _i64, _u64, _f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_float
 _sz, _int = ctypes.c_size_t, ctypes.c_int
+
+
+class SoftmaxDesc(ctypes.Structure):
+    """grf_softmax_desc; pointers as device addresses."""
+    _fields_ = [("batch", _i32), ("heads", _i32), ("kv_heads", _i32), ("n_q", _i32), ("n_k", _i32), ("dim", _i32), ("dtype", _i32),
+                ("scale", _f32), ("cap", _f32), ("order", _i32), ("bias", _i32), ("n_buckets", _i32), ("two_sided", _i32),
+                ("first", _i32 * GRF_MAX_BUCKETS), ("slopes", _vp), ("table", _vp), ("k_len", _vp), ("q_start", _vp),
+                ("prefix", _vp), ("q_doc", _vp), ("k_doc", _vp)] + [
+                    (name + "_stride", _i64 * 3) for name in ("q", "k", "v", "out", "dout", "dq", "dk", "dv")]
+
+
+_desc = ctypes.POINTER(SoftmaxDesc)
 
 _SIGNATURES = {
     "grf_ctx_create": (_int, [ctypes.POINTER(_vp), _int, _vp]),
@@ -49,6 +64,13 @@ _SIGNATURES = {
     "grf_mask_stats": (_int, [_vp, ctypes.POINTER(_i32), ctypes.POINTER(_i64), ctypes.POINTER(_i64)]),
     "grf_mask_rows": (_int, [_vp, _vp, _i32, _vp, _vp]),
     "grf_masked_attn_mhat": (_int, [_vp, _vp, _i32, _i32, _i32, _i32, _int, _vp, _vp, _vp, _vp, _vp]),
+    "grf_relative_buckets": (_int, [_i32, _i32, _vp]),
+    "grf_softmax_attn_workspace_bytes": (_sz, [_vp, _desc, _int]),
+    "grf_softmax_attn": (_int, [_vp, _desc] + [_vp] * 7 + [_sz]),
+    "grf_softmax_attn_backward": (_int, [_vp, _desc] + [_vp] * 12 + [_sz]),
+    "grf_relative_bias": (_int, [_vp, _i32, _i32, _i32, _i32, _i32, _int, _vp, _int, _vp, _vp]),
+    "grf_relative_bias_workspace_bytes": (_sz, [_i32, _i32, _i32, _i32, _int]),
+    "grf_relative_bias_backward": (_int, [_vp, _i32, _i32, _i32, _i32, _i32, _i32, _int, _vp, _int, _vp, _vp, _vp, _sz]),
     "grf_step_host": (_int, [_vp, _i32, _vp, _vp, _vp, _u64, _i32, _f32, _i32, _vp, _vp,
                              _i32, _i32, _i32, _int, _vp, _vp, _vp, _vp]),
     "grf_plan_stats": (_int, [_vp, _vp, ctypes.POINTER(_i32), ctypes.POINTER(_i64)]),
@@ -278,6 +300,55 @@ def grf_mask_rows(ctx, features, n, rows, out):
 def grf_masked_attn_mhat(ctx, features, G, N, m, d, dtype, phiQ, phiK, V, out, den_out):
     _check(lib.grf_masked_attn_mhat(ctx, features, G, N, m, d, dtype, _dev(phiQ), _dev(phiK), _dev(V), _dev(out),
                                     _dev(den_out)), "grf_masked_attn_mhat")
+
+
+def grf_relative_buckets(n_buckets: int, max_distance: int) -> np.ndarray:
+    """Smallest distance of each bucket, int32 [n_buckets]."""
+    first = np.empty(max(n_buckets, 1), dtype=np.int32)
+    _check(lib.grf_relative_buckets(n_buckets, max_distance, first.ctypes.data), "grf_relative_buckets")
+    return first
+
+
+def _strided(x):
+    """Device address of a torch CUDA tensor of any strides (the descriptor states them), or an int; None -> NULL."""
+    if x is None or isinstance(x, int):
+        return x
+    if not x.is_cuda:
+        raise ValueError("expected a CUDA tensor")
+    return x.data_ptr()
+
+
+def grf_softmax_attn_workspace_bytes(ctx, desc: SoftmaxDesc, backward: bool) -> int:
+    return int(lib.grf_softmax_attn_workspace_bytes(ctx, desc, int(backward)))
+
+
+def grf_softmax_attn(ctx, desc: SoftmaxDesc, Q, K, V, out, lse, rest, workspace, workspace_bytes):
+    _check(lib.grf_softmax_attn(ctx, desc, _strided(Q), _strided(K), _strided(V), _strided(out), _dev(lse), _dev(rest),
+                                _dev(workspace), workspace_bytes), "grf_softmax_attn")
+
+
+def grf_softmax_attn_backward(ctx, desc: SoftmaxDesc, Q, K, V, out, lse, rest, dout, dQ, dK, dV, dtable, workspace,
+                              workspace_bytes):
+    _check(lib.grf_softmax_attn_backward(ctx, desc, _strided(Q), _strided(K), _strided(V), _strided(out), _dev(lse),
+                                         _dev(rest), _strided(dout), _strided(dQ), _strided(dK), _strided(dV), _dev(dtable), _dev(workspace),
+                                         workspace_bytes), "grf_softmax_attn_backward")
+
+
+def grf_relative_bias(ctx, heads, n_q, n_k, q_start, first, two_sided, dtype, table, rows):
+    p, keep = _host(first, np.int32)
+    _check(lib.grf_relative_bias(ctx, heads, n_q, n_k, q_start, keep.shape[0], int(two_sided), p, dtype, _dev(table), _dev(rows)),
+           "grf_relative_bias")
+
+
+def grf_relative_bias_workspace_bytes(heads, n_q, n_k, n_buckets, two_sided) -> int:
+    return int(lib.grf_relative_bias_workspace_bytes(heads, n_q, n_k, n_buckets, int(two_sided)))
+
+
+def grf_relative_bias_backward(ctx, batch, heads, n_q, n_k, q_start, first, two_sided, dtype, drows, dtable, workspace,
+                               workspace_bytes):
+    p, keep = _host(first, np.int32)
+    _check(lib.grf_relative_bias_backward(ctx, batch, heads, n_q, n_k, q_start, keep.shape[0], int(two_sided), p, dtype, _dev(drows),
+                                          _dev(dtable), _dev(workspace), workspace_bytes), "grf_relative_bias_backward")
 
 
 def grf_step_host(ctx, N, rowptr, col, w, seed, n_walks, p_halt, max_len, f_phi, f_psi, G, m, d, dtype,

@@ -1,0 +1,475 @@
+// Softmax attention over ordered tokens and its gradients in plain fp32 arithmetic: what serves fp32, and bf16 when the context keeps off
+// the tensor cores.
+//
+// Forward: a CTA has 64 queries of one head and goes over the keys in tiles of 64 with the running maximum and sum of each row
+// (s in units of log 2): m' = max(m, max s), l' = l 2^(m - m') + sum 2^(s - m'), O' = O 2^(m - m') + P V, out = O / l.
+// Backward, in two kernels so that nothing is added atomically: a CTA of 64 queries recomputes P = 2^(s - lse) and dS = P (dP - D) tile by
+// tile for dQ (and the sums of dS along the tile's diagonals for the bias table); a CTA of 64 keys does the same over the queries of
+// all heads that share it for dK and dV.
+//
+// 256 threads hold 4 x 4 scores each; operands lie in shared memory as rows with four words of padding, read 16 bytes at a time: two reads
+// for sixteen multiply-adds, which leaves the fp32 pipe as the bound.
+#include "softmax.cuh"
+
+namespace {
+
+constexpr int BT = 64;                  // queries, and keys, of a tile
+constexpr int THREADS = 256;
+constexpr int PS = BT + 4;              // row of a score tile
+
+template <int DP> struct Alu {
+    static constexpr int ROW = DP + 4;
+    static constexpr int TILE = BT * ROW;
+    static constexpr int W = DP / 16 < 4 ? DP / 16 : 4;        // neighbouring output columns of a thread
+    static constexpr int NC = DP / 16 / W;                      // and groups of them, 16 W apart
+};
+
+__device__ __forceinline__ bool finite(float x) { return fabsf(x) <= 3.4028235e38f; }
+
+// Rows r0 .. r0 + 63 of [tokens][d] as floats: zeros behind `rows`, behind d, and for tokens whose document is negative.  clean: what is not
+// finite becomes 0 too and sets *bad.
+template <typename T, int DP>
+__device__ __forceinline__ void load_rows(float* tile, const T* base, int64_t stride, int32_t r0, int32_t rows, int32_t d, const int32_t* doc,
+                                          bool clean, int* bad)
+{
+    constexpr int CH = 16 / (int)sizeof(T), PER = DP / CH;
+    for (int x = threadIdx.x; x < BT * PER; x += THREADS) {
+        const int r = x / PER, c = x % PER * CH;
+        float v[CH];
+#pragma unroll
+        for (int e = 0; e < CH; ++e) v[e] = 0.0f;
+        if (r0 + r < rows && c < d && (!doc || doc[r0 + r] >= 0)) {
+            const uint4 w = *reinterpret_cast<const uint4*>(base + (int64_t)(r0 + r) * stride + c);
+            const T* t = reinterpret_cast<const T*>(&w);
+#pragma unroll
+            for (int e = 0; e < CH; ++e) {
+                v[e] = grf_to_float(t[e]);
+                if (clean && !finite(v[e])) {
+                    v[e] = 0.0f;
+                    if (bad) *bad = 1;
+                }
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < CH; e += 4) *reinterpret_cast<float4*>(tile + r * Alu<DP>::ROW + c + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+    }
+}
+
+// acc[r][c] = sum over d of a[4 ty + r][.] b[tx + 16 c][.]
+template <int DP>
+__device__ __forceinline__ void products(float (&acc)[4][4], const float* a, const float* b, int ty, int tx)
+{
+    constexpr int ROW = Alu<DP>::ROW;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) acc[r][c] = 0.0f;
+#pragma unroll 4
+    for (int k = 0; k < DP; k += 4) {
+        float4 x[4], y[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[r] = *reinterpret_cast<const float4*>(a + (4 * ty + r) * ROW + k);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) y[c] = *reinterpret_cast<const float4*>(b + (tx + 16 * c) * ROW + k);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                acc[r][c] = fmaf(x[r].x, y[c].x, acc[r][c]);
+                acc[r][c] = fmaf(x[r].y, y[c].y, acc[r][c]);
+                acc[r][c] = fmaf(x[r].z, y[c].z, acc[r][c]);
+                acc[r][c] = fmaf(x[r].w, y[c].w, acc[r][c]);
+            }
+    }
+}
+
+template <int W> __device__ __forceinline__ void load_w(float (&v)[W], const float* at)
+{
+    if constexpr (W == 4) {
+        const float4 x = *reinterpret_cast<const float4*>(at);
+        v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+    } else {
+        const float2 x = *reinterpret_cast<const float2*>(at);
+        v[0] = x.x; v[1] = x.y;
+    }
+}
+
+// acc[r][.] += sum over x of w[x][4 ty + r] rows[x][this thread's columns]
+template <int DP>
+__device__ __forceinline__ void accumulate(float (&acc)[4][DP / 16], const float* w, const float* rows, int ty, int tx)
+{
+    using A = Alu<DP>;
+#pragma unroll 4
+    for (int x = 0; x < BT; ++x) {
+        const float4 p = *reinterpret_cast<const float4*>(w + x * PS + 4 * ty);
+        const float pr[4] = {p.x, p.y, p.z, p.w};
+#pragma unroll
+        for (int g = 0; g < A::NC; ++g) {
+            float v[A::W];
+            load_w<A::W>(v, rows + x * A::ROW + A::W * tx + 16 * A::W * g);
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int e = 0; e < A::W; ++e) acc[r][g * A::W + e] = fmaf(pr[r], v[e], acc[r][g * A::W + e]);
+        }
+    }
+}
+
+template <typename T, int DP>
+__device__ __forceinline__ void store_row(T* dst, const float (&v)[DP / 16], int tx, int32_t d)
+{
+    using A = Alu<DP>;
+#pragma unroll
+    for (int g = 0; g < A::NC; ++g) {
+        const int c = A::W * tx + 16 * A::W * g;
+        if (c < d) {
+#pragma unroll
+            for (int e = 0; e < A::W; ++e) dst[c + e] = grf_from_float<T>(v[g * A::W + e]);
+        }
+    }
+}
+
+// Where a row of a head lies; heads of keys and values: h / group.
+template <typename T> __device__ __forceinline__ const T* at_head(const void* base, const int64_t (&s)[3], int32_t b, int32_t h)
+{
+    return reinterpret_cast<const T*>(base) + b * s[0] + h * s[1];
+}
+template <typename T> __device__ __forceinline__ T* at_head_w(void* base, const int64_t (&s)[3], int32_t b, int32_t h)
+{
+    return reinterpret_cast<T*>(base) + b * s[0] + h * s[1];
+}
+
+__device__ __forceinline__ int4 all_docs() { return make_int4(0, 0, 0, 0); }
+
+// Bias of every diagonal of a tile, index (j - j0) - (i - i0) + BT - 1.
+template <typename T> __device__ __forceinline__ void load_bias(float* lut, const grf_softmax_params& p, int32_t h, int32_t j0, int32_t pos0)
+{
+    if (p.bias == GRF_BIAS_NONE) return;
+    for (int x = threadIdx.x; x < 2 * BT - 1; x += THREADS) lut[x] = grf_bias2<T>(p, h, j0 - pos0 + x - (BT - 1));
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(THREADS) softmax_alu_forward_kernel(const __grid_constant__ grf_softmax_params p)
+{
+    using A = Alu<DP>;
+    extern __shared__ float smem[];
+    float *qs = smem, *ks = qs + A::TILE, *vs = ks + A::TILE, *pt = vs + A::TILE;
+    __shared__ float lut[2 * BT];
+    __shared__ int bad;
+    const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
+    const int32_t b = blockIdx.y / p.H, h = blockIdx.y % p.H, i0 = (gridDim.x - 1 - blockIdx.x) * BT, kvh = h / p.group;
+    const grf_sight sight(p, b);
+    const int32_t *qdoc = sight.docs ? p.q_doc + (int64_t)b * p.Nq : nullptr, *kdoc = sight.docs ? p.k_doc + (int64_t)b * p.Nk : nullptr;
+    const int32_t kblocks = (p.Nk + BT - 1) / BT, i1 = min(i0 + BT, p.Nq);
+    const int4 qr = sight.docs ? p.q_range[(int64_t)b * gridDim.x + i0 / BT] : all_docs();
+    const T *K = at_head<T>(p.k, p.ks, b, kvh), *V = at_head<T>(p.v, p.vs, b, kvh);
+    if (tid == 0) bad = 0;
+    load_rows<T, DP>(qs, at_head<T>(p.q, p.qs, b, h), p.qs[2], i0, p.Nq, p.d, nullptr, false, nullptr);
+    float o[4][DP / 16], m[4], l[4];
+    int32_t doc[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        m[r] = -CUDART_INF_F;
+        l[r] = 0.0f;
+        doc[r] = qdoc && i0 + 4 * ty + r < p.Nq ? qdoc[i0 + 4 * ty + r] : -1;
+#pragma unroll
+        for (int c = 0; c < DP / 16; ++c) o[r][c] = 0.0f;
+    }
+    const float to2 = p.scale * GRF_LOG2E, cap2 = p.cap * GRF_LOG2E, by_cap = p.cap > 0.0f ? p.scale / p.cap : 0.0f;
+    const int32_t end = sight.end(i1);
+    for (int32_t j0 = 0; j0 < end; j0 += BT) {
+        const int what = sight.tile(i0, i1, j0, j0 + BT, qr, sight.docs ? __ldg(p.k_range + (int64_t)b * kblocks + j0 / BT) : all_docs());
+        if (what == 0) continue;
+        __syncthreads();
+        load_rows<T, DP>(ks, K, p.ks[2], j0, sight.len, p.d, kdoc, false, nullptr);
+        load_rows<T, DP>(vs, V, p.vs[2], j0, sight.len, p.d, kdoc, what == 1, &bad);
+        load_bias<T>(lut, p, h, j0, sight.position(i0));
+        __syncthreads();
+        float s[4][4];
+        products<DP>(s, qs, ks, ty, tx);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int i = 4 * ty + r;
+            float top = m[r];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const int j = tx + 16 * c;
+                float x = p.cap > 0.0f ? cap2 * tanhf(s[r][c] * by_cap) : s[r][c] * to2;
+                if (p.bias != GRF_BIAS_NONE) x += lut[j - i + BT - 1];
+                if (what == 1) {
+                    const bool seen = sight.sees(sight.position(i0 + i), j0 + j) && (!kdoc || (doc[r] >= 0 && kdoc[j0 + j] == doc[r]));
+                    if (!seen) x = -CUDART_INF_F;
+                }
+                s[r][c] = x;
+                top = fmaxf(top, x);
+            }
+#pragma unroll
+            for (int y = 1; y < 16; y <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, y));
+            const float base = top == -CUDART_INF_F ? 0.0f : top, alpha = exp2f(m[r] - base);
+            float sum = 0.0f;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                s[r][c] = exp2f(s[r][c] - base);
+                sum += s[r][c];
+            }
+#pragma unroll
+            for (int y = 1; y < 16; y <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, y);
+            l[r] = l[r] * alpha + sum;
+            m[r] = top;
+#pragma unroll
+            for (int c = 0; c < DP / 16; ++c) o[r][c] *= alpha;
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            *reinterpret_cast<float4*>(pt + (tx + 16 * c) * PS + 4 * ty) = make_float4(s[0][c], s[1][c], s[2][c], s[3][c]);
+        __syncthreads();
+        accumulate<DP>(o, pt, vs, ty, tx);
+    }
+    __syncthreads();
+    // Values that are not finite, in tiles that not every query sees whole, were left out above: they go to the queries that see them.
+    if (bad) {
+        for (int32_t j = 0; j < end; ++j) {
+            const int32_t j0 = j & ~(BT - 1);
+            const int what = sight.tile(i0, i1, j0, j0 + BT, qr, sight.docs ? p.k_range[(int64_t)b * kblocks + j0 / BT] : all_docs());
+            if (what != 1) { j = j0 + BT - 1; continue; }
+#pragma unroll
+            for (int c = 0; c < DP / 16; ++c) {
+                const int col = c / A::W * 16 * A::W + A::W * tx + c % A::W;
+                if (col >= p.d) continue;
+                const float v = grf_to_float(V[(int64_t)j * p.vs[2] + col]);
+                if (finite(v)) continue;
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (sight.sees(sight.position(i0 + 4 * ty + r), j) && (!kdoc || (doc[r] >= 0 && kdoc[j] == doc[r]))) o[r][c] += v;
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int32_t i = i0 + 4 * ty + r;
+        if (i >= p.Nq) continue;
+        const float inv = l[r] == 0.0f ? 0.0f : 1.0f / l[r];
+#pragma unroll
+        for (int c = 0; c < DP / 16; ++c) o[r][c] = l[r] == 0.0f ? 0.0f : o[r][c] * inv;
+        store_row<T, DP>(at_head_w<T>(p.out_w, p.os, b, h) + (int64_t)i * p.os[2], o[r], tx, p.d);
+        if (p.rest_w) {
+#pragma unroll
+            for (int c = 0; c < DP / 16; ++c) {
+                const int col = c / A::W * 16 * A::W + A::W * tx + c % A::W;
+                if (col < p.d) p.rest_w[(((int64_t)b * p.H + h) * p.Nq + i) * p.d + col] = grf_rest(o[r][c], grf_from_float<T>(o[r][c]));
+            }
+        }
+        if (p.lse_w && tx == 0)
+            p.lse_w[((int64_t)b * p.H + h) * p.Nq + i] = l[r] == 0.0f ? -CUDART_INF_F : (m[r] + log2f(l[r])) * GRF_LN2;
+    }
+}
+
+// P and dS of one tile from its products: on entry s = q.k and dp = dout.v; on return s = P, dp = dX (dS through the cap), ds = dS.
+struct alu_row { float lse2, dsum; int32_t doc, pos; bool any; };
+template <typename T>
+__device__ __forceinline__ alu_row load_alu_row(const grf_softmax_params& p, const grf_sight& sight, const int32_t* qdoc, int32_t b, int32_t h, int32_t i)
+{
+    alu_row w;
+    const bool in = i < p.Nq;
+    const int64_t x = ((int64_t)b * p.H + h) * p.Nq + i;
+    const float lse = in ? p.lse[x] : -CUDART_INF_F;
+    w.any = lse != -CUDART_INF_F;
+    w.lse2 = lse * GRF_LOG2E;
+    w.dsum = in ? p.dsum[x] : 0.0f;
+    w.doc = qdoc && in ? qdoc[i] : -1;
+    w.pos = sight.position(i);
+    return w;
+}
+__device__ __forceinline__ void score_gradient(const grf_softmax_params& p, const grf_sight& sight, const alu_row& w, const int32_t* kdoc, int what,
+                                               int32_t j, float bias2, float& s, float& dp, float& ds)
+{
+    float t = 0.0f, x;
+    if (p.cap > 0.0f) { t = tanhf(s * (p.scale / p.cap)); x = p.cap * GRF_LOG2E * t; }
+    else x = s * (p.scale * GRF_LOG2E);
+    x += bias2;
+    bool seen = w.any;
+    if (what == 1) seen = seen && sight.sees(w.pos, j) && (!kdoc || (w.doc >= 0 && kdoc[j] == w.doc));
+    float e = x - w.lse2;
+    e = e > 0.0f ? 0.0f : e;                                    // (NaN stays)
+    s = seen ? exp2f(e) : 0.0f;
+    ds = seen ? s * (dp - w.dsum) : 0.0f;
+    dp = p.cap > 0.0f ? (seen ? ds * (1.0f - t * t) : 0.0f) : ds;
+    // a row of dout that is not finite was left out of the products of a tile that is not seen whole
+    if (seen && !finite(w.dsum)) s = CUDART_NAN_F;
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(THREADS) softmax_alu_dq_kernel(const __grid_constant__ grf_softmax_params p)
+{
+    using A = Alu<DP>;
+    extern __shared__ float smem[];
+    float *qs = smem, *gs = qs + A::TILE, *ks = gs + A::TILE, *vs = ks + A::TILE, *xt = vs + A::TILE, *st = xt + BT * PS;
+    __shared__ float lut[2 * BT], diagonal[2 * BT];
+    const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
+    const int32_t b = blockIdx.y / p.H, h = blockIdx.y % p.H, i0 = (gridDim.x - 1 - blockIdx.x) * BT, kvh = h / p.group;
+    const grf_sight sight(p, b);
+    const int32_t *qdoc = sight.docs ? p.q_doc + (int64_t)b * p.Nq : nullptr, *kdoc = sight.docs ? p.k_doc + (int64_t)b * p.Nk : nullptr;
+    const int32_t kblocks = (p.Nk + BT - 1) / BT, i1 = min(i0 + BT, p.Nq), columns = grf_softmax_columns(p);
+    const int4 qr = sight.docs ? p.q_range[(int64_t)b * gridDim.x + i0 / BT] : all_docs();
+    const T *K = at_head<T>(p.k, p.ks, b, kvh), *V = at_head<T>(p.v, p.vs, b, kvh);
+    load_rows<T, DP>(qs, at_head<T>(p.q, p.qs, b, h), p.qs[2], i0, p.Nq, p.d, nullptr, false, nullptr);
+    load_rows<T, DP>(gs, at_head<T>(p.dout, p.dos, b, h), p.dos[2], i0, p.Nq, p.d, nullptr, false, nullptr);
+    alu_row row[4];
+    float dq[4][DP / 16];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        row[r] = load_alu_row<T>(p, sight, qdoc, b, h, i0 + 4 * ty + r);
+#pragma unroll
+        for (int c = 0; c < DP / 16; ++c) dq[r][c] = 0.0f;
+    }
+    float table_sum = 0.0f;                                     // bucket tid's
+    const int32_t end = sight.end(i1);
+    for (int32_t j0 = 0; j0 < end; j0 += BT) {
+        const int what = sight.tile(i0, i1, j0, j0 + BT, qr, sight.docs ? __ldg(p.k_range + (int64_t)b * kblocks + j0 / BT) : all_docs());
+        if (what == 0) continue;
+        __syncthreads();
+        load_rows<T, DP>(ks, K, p.ks[2], j0, sight.len, p.d, kdoc, what == 1, nullptr);
+        load_rows<T, DP>(vs, V, p.vs[2], j0, sight.len, p.d, kdoc, false, nullptr);
+        load_bias<T>(lut, p, h, j0, sight.position(i0));
+        __syncthreads();
+        float s[4][4], dp[4][4];
+        products<DP>(s, qs, ks, ty, tx);
+        products<DP>(dp, gs, vs, ty, tx);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const int i = 4 * ty + r, j = tx + 16 * c;
+                float ds;
+                score_gradient(p, sight, row[r], kdoc, what, j0 + j, p.bias != GRF_BIAS_NONE ? lut[j - i + BT - 1] : 0.0f, s[r][c], dp[r][c], ds);
+                if (p.dtable_part) st[i * PS + j] = ds;
+            }
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            *reinterpret_cast<float4*>(xt + (tx + 16 * c) * PS + 4 * ty) = make_float4(dp[0][c], dp[1][c], dp[2][c], dp[3][c]);
+        __syncthreads();
+        accumulate<DP>(dq, xt, ks, ty, tx);
+        if (p.dtable_part) {
+            if (tid < 2 * BT - 1) {
+                float sum = 0.0f;
+                const int delta = tid - (BT - 1);               // j - i
+                for (int i = max(0, -delta); i < min(BT, BT - delta); ++i) sum += st[i * PS + i + delta];
+                diagonal[tid] = sum;
+            }
+            __syncthreads();
+            if (tid < columns) {
+                float sum = 0.0f;
+                for (int x = 0; x < 2 * BT - 1; ++x)
+                    if (grf_bucket(p, j0 - sight.position(i0) + x - (BT - 1)) == tid) sum += diagonal[x];
+                table_sum += sum;
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int32_t i = i0 + 4 * ty + r;
+        if (i >= p.Nq) continue;
+#pragma unroll
+        for (int c = 0; c < DP / 16; ++c) dq[r][c] *= p.scale;
+        store_row<T, DP>(at_head_w<T>(p.dq, p.dqs, b, h) + (int64_t)i * p.dqs[2], dq[r], tx, p.d);
+    }
+    if (p.dtable_part && tid < columns) p.dtable_part[((int64_t)blockIdx.y * gridDim.x + i0 / BT) * columns + tid] = table_sum;
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(THREADS) softmax_alu_dkv_kernel(const __grid_constant__ grf_softmax_params p)
+{
+    using A = Alu<DP>;
+    extern __shared__ float smem[];
+    float *qs = smem, *gs = qs + A::TILE, *ks = gs + A::TILE, *vs = ks + A::TILE, *ps = vs + A::TILE, *xs = ps + BT * PS;
+    __shared__ float lut[2 * BT];
+    const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
+    const int32_t b = blockIdx.y / p.KV, kvh = blockIdx.y % p.KV, j0 = blockIdx.x * BT, j1 = j0 + BT;
+    const grf_sight sight(p, b);
+    const int32_t *qdoc = sight.docs ? p.q_doc + (int64_t)b * p.Nq : nullptr, *kdoc = sight.docs ? p.k_doc + (int64_t)b * p.Nk : nullptr;
+    const int32_t qblocks = (p.Nq + BT - 1) / BT;
+    const int4 kr = sight.docs ? p.k_range[(int64_t)b * gridDim.x + blockIdx.x] : all_docs();
+    load_rows<T, DP>(ks, at_head<T>(p.k, p.ks, b, kvh), p.ks[2], j0, sight.len, p.d, kdoc, false, nullptr);
+    load_rows<T, DP>(vs, at_head<T>(p.v, p.vs, b, kvh), p.vs[2], j0, sight.len, p.d, kdoc, false, nullptr);
+    float dk[4][DP / 16], dv[4][DP / 16];
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int c = 0; c < DP / 16; ++c) dk[r][c] = dv[r][c] = 0.0f;
+    for (int32_t x = 0; x < p.group * qblocks; ++x) {
+        const int32_t h = kvh * p.group + x / qblocks, i0 = x % qblocks * BT;
+        const int what = sight.tile(i0, min(i0 + BT, p.Nq), j0, j1, sight.docs ? __ldg(p.q_range + (int64_t)b * qblocks + i0 / BT) : all_docs(), kr);
+        if (what == 0) continue;
+        __syncthreads();
+        load_rows<T, DP>(qs, at_head<T>(p.q, p.qs, b, h), p.qs[2], i0, p.Nq, p.d, qdoc, what == 1, nullptr);
+        load_rows<T, DP>(gs, at_head<T>(p.dout, p.dos, b, h), p.dos[2], i0, p.Nq, p.d, qdoc, what == 1, nullptr);
+        load_bias<T>(lut, p, h, j0, sight.position(i0));
+        __syncthreads();
+        float s[4][4], dp[4][4];
+        products<DP>(s, qs, ks, ty, tx);
+        products<DP>(dp, gs, vs, ty, tx);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int i = 4 * ty + r;
+            const alu_row w = load_alu_row<T>(p, sight, qdoc, b, h, i0 + i);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const int j = tx + 16 * c;
+                float ds;
+                score_gradient(p, sight, w, kdoc, what, j0 + j, p.bias != GRF_BIAS_NONE ? lut[j - i + BT - 1] : 0.0f, s[r][c], dp[r][c], ds);
+                ps[i * PS + j] = s[r][c];
+                xs[i * PS + j] = dp[r][c];
+            }
+        }
+        __syncthreads();
+        accumulate<DP>(dv, ps, gs, ty, tx);
+        accumulate<DP>(dk, xs, qs, ty, tx);
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int32_t j = j0 + 4 * ty + r;
+        if (j >= p.Nk) continue;
+#pragma unroll
+        for (int c = 0; c < DP / 16; ++c) dk[r][c] *= p.scale;
+        store_row<T, DP>(at_head_w<T>(p.dk, p.dks, b, kvh) + (int64_t)j * p.dks[2], dk[r], tx, p.d);
+        store_row<T, DP>(at_head_w<T>(p.dv, p.dvs, b, kvh) + (int64_t)j * p.dvs[2], dv[r], tx, p.d);
+    }
+}
+
+template <typename T, int DP> int forward(grf_ctx* ctx, const grf_softmax_params& p)
+{
+    const size_t smem = sizeof(float) * (3 * Alu<DP>::TILE + BT * PS);
+    GRF_CUDA_TRY(cudaFuncSetAttribute(softmax_alu_forward_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    grf_softmax_scope scope(ctx, "grf:softmax_attention");
+    softmax_alu_forward_kernel<T, DP><<<dim3(grf_ceil_div(p.Nq, BT), p.B * p.H), THREADS, smem, ctx->stream>>>(p);
+    return cudaGetLastError() == cudaSuccess ? GRF_OK : GRF_ERR_CUDA;
+}
+
+template <typename T, int DP> int backward(grf_ctx* ctx, const grf_softmax_params& p)
+{
+    const size_t smem = sizeof(float) * (4 * Alu<DP>::TILE + 2 * BT * PS);
+    GRF_CUDA_TRY(cudaFuncSetAttribute(softmax_alu_dq_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    GRF_CUDA_TRY(cudaFuncSetAttribute(softmax_alu_dkv_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    grf_softmax_scope scope(ctx, "grf:softmax_gradients", 2);
+    softmax_alu_dq_kernel<T, DP><<<dim3(grf_ceil_div(p.Nq, BT), p.B * p.H), THREADS, smem, ctx->stream>>>(p);
+    softmax_alu_dkv_kernel<T, DP><<<dim3(grf_ceil_div(p.Nk, BT), p.B * p.KV), THREADS, smem, ctx->stream>>>(p);
+    return cudaGetLastError() == cudaSuccess ? GRF_OK : GRF_ERR_CUDA;
+}
+
+}  // namespace
+
+int grf_softmax_alu_forward(grf_ctx* ctx, const grf_softmax_params& p, int dtype)
+{
+    const bool wide = dtype == GRF_DTYPE_F32;
+    if (p.d <= 32) return wide ? forward<float, 32>(ctx, p) : forward<__nv_bfloat16, 32>(ctx, p);
+    if (p.d <= 64) return wide ? forward<float, 64>(ctx, p) : forward<__nv_bfloat16, 64>(ctx, p);
+    return wide ? forward<float, 128>(ctx, p) : forward<__nv_bfloat16, 128>(ctx, p);
+}
+
+int grf_softmax_alu_backward(grf_ctx* ctx, const grf_softmax_params& p, int dtype)
+{
+    const bool wide = dtype == GRF_DTYPE_F32;
+    if (p.d <= 32) return wide ? backward<float, 32>(ctx, p) : backward<__nv_bfloat16, 32>(ctx, p);
+    if (p.d <= 64) return wide ? backward<float, 64>(ctx, p) : backward<__nv_bfloat16, 64>(ctx, p);
+    return wide ? backward<float, 128>(ctx, p) : backward<__nv_bfloat16, 128>(ctx, p);
+}
