@@ -168,22 +168,20 @@ struct room {
     size_t take(size_t n) { const size_t at = bytes; bytes += align256(n); return at; }
 };
 
-constexpr int RANGE_BLOCK = 64;
+constexpr int RANGE_BLOCK = 64;         // the smallest block that a route takes: sizes of the workspace
 
 struct doc_room {
     size_t q = 0, k = 0;
-    int32_t q_blocks = 0, k_blocks = 0, block = 0;
-    doc_room(room& r, const grf_softmax_params& p, int32_t block_) : block(block_)
+    doc_room(room& r, const grf_softmax_params& p)
     {
         if (!p.q_doc) return;
-        q_blocks = grf_ceil_div(p.Nq, block);
-        k_blocks = grf_ceil_div(p.Nk, block);
-        q = r.take(sizeof(int4) * (size_t)p.B * q_blocks);
-        k = r.take(sizeof(int4) * (size_t)p.B * k_blocks);
+        q = r.take(sizeof(int4) * (size_t)p.B * grf_ceil_div(p.Nq, RANGE_BLOCK));
+        k = r.take(sizeof(int4) * (size_t)p.B * grf_ceil_div(p.Nk, RANGE_BLOCK));
     }
-    int fill(grf_ctx* ctx, grf_softmax_params& p, char* ws) const
+    int fill(grf_ctx* ctx, grf_softmax_params& p, char* ws, int32_t block) const
     {
         if (!p.q_doc) return GRF_OK;
+        const int32_t q_blocks = grf_ceil_div(p.Nq, block), k_blocks = grf_ceil_div(p.Nk, block);
         p.q_range = (const int4*)(ws + q);
         p.k_range = (const int4*)(ws + k);
         const bool same = p.q_doc == p.k_doc && p.Nq == p.Nk;
@@ -200,7 +198,7 @@ size_t forward_bytes(const grf_ctx* ctx, const grf_softmax_params& p, int dtype)
 {
     if (by_few(p)) return grf_softmax_few_workspace(ctx, p, dtype);
     room r;
-    doc_room docs(r, p, RANGE_BLOCK);
+    doc_room docs(r, p);
     return r.bytes;
 }
 
@@ -208,7 +206,7 @@ struct backward_room : room {
     doc_room docs;
     size_t dsum, table;
     int32_t q_blocks;
-    explicit backward_room(const grf_softmax_params& p) : docs(*this, p, RANGE_BLOCK)
+    explicit backward_room(const grf_softmax_params& p) : docs(*this, p)
     {
         dsum = take(sizeof(float) * (size_t)p.B * p.H * p.Nq);
         q_blocks = grf_ceil_div(p.Nq, RANGE_BLOCK);
@@ -281,8 +279,13 @@ extern "C" int grf_softmax_attn(grf_ctx* ctx, const grf_softmax_desc* desc, cons
     p.error_word = ctx->error_word;
     if (by_few(p)) return grf_softmax_few(ctx, p, desc->dtype, workspace);
     room r;
-    const doc_room docs(r, p, RANGE_BLOCK);
-    GRF_TRY(docs.fill(ctx, p, (char*)workspace));
+    const doc_room docs(r, p);
+    if (desc->dtype == GRF_DTYPE_BF16 && ctx->use_tensor_cores) {
+        GRF_TRY(docs.fill(ctx, p, (char*)workspace, 128));
+        const int rc = grf_softmax_tc_forward(ctx, p);
+        if (rc <= 0) return rc;
+    }
+    GRF_TRY(docs.fill(ctx, p, (char*)workspace, 64));
     return grf_softmax_alu_forward(ctx, p, desc->dtype);
 }
 
@@ -306,7 +309,7 @@ extern "C" int grf_softmax_attn_backward(grf_ctx* ctx, const grf_softmax_desc* d
     p.dsum = (const float*)(ws + r.dsum);
     p.dtable_part = dtable ? (float*)(ws + r.table) : nullptr;
     p.error_word = ctx->error_word;
-    GRF_TRY(r.docs.fill(ctx, p, ws));
+    GRF_TRY(r.docs.fill(ctx, p, ws, 64));
     {
         grf_softmax_scope scope(ctx, "grf:output_products");
         const int lanes = (int)(p.d * elem(desc->dtype) / 16);

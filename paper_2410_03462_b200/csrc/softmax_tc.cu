@@ -1,0 +1,526 @@
+// Softmax attention over ordered tokens on the tensor cores (bf16): the forward pass.
+//
+// S = Q K^T of 128 queries and 128 keys comes out in tensor memory, a query per lane; a thread reads its query's 128 scores, keeps the
+// running maximum m and sum l (in units of log 2), and writes P = 2^(s - m) back to tensor memory as bf16 pairs, where it is the left operand
+// of O += P V.  O stays in tensor memory; it is rescaled only when a maximum grows by more than 2^8 (until then P <= 2^8, which costs no
+// precision: bf16 has the same relative step everywhere and l is fp32), so almost never after the first tiles.
+//   d > 64   a CTA per SM, two groups of 128 queries: while one group's softmax runs, the other one's products do.  P overwrites S
+//   d <= 64  two CTAs per SM of one group; P has its own place, so the next S is made while P is
+//   warps of the last warpgroup: copies of K and V (two stages, boxes by the copy engine), one issuing warp per group, and one that
+//   clears rows of V which nobody sees (behind a length, of no document): 0 times an infinity there would reach every query of the tile.
+// A value that some queries see and others do not, and that is not finite, does reach the others' accumulators: a row that ends up not finite
+// has its columns summed again from what it does see (redo_row).
+#include <type_traits>
+
+#include "softmax_tc.cuh"
+
+namespace {
+
+using namespace grf_softmax_tc;
+
+template <int DP> struct Fwd {
+    static constexpr int QT = DP == 64 ? 1 : 2;                 // groups
+    static constexpr int CTAS = DP == 64 ? 2 : 1;
+    static constexpr bool SEP = DP == 64;                       // P beside S
+    static constexpr int THREADS = 128 * (QT + 1);
+    static constexpr int NS = 2;
+    static constexpr uint32_t TILE = HALF * (DP / 64);
+    static constexpr uint32_t TMEM = DP == 64 ? 256 : 512;
+    static constexpr uint32_t P_COL = SEP ? 128 : 0, O_COL = SEP ? 192 : 256;
+    static constexpr size_t SMEM = 1024 + (size_t)TILE * (QT + 2 * NS);    // then the tiles' bits
+    static constexpr int MORE = DP == 64 ? 200 : 208, LESS = DP == 64 ? 56 : 88;   // registers: QT * MORE + LESS = the launch's
+};
+
+struct forward_tiles {
+    const grf_softmax_params& p;
+    const grf_sight& sight;
+    const uint32_t* bits;                                       // [seen, whole] per group, then of any group, then tiles with a token of no document
+    int32_t i0, tiles, words;
+    // queries of group g
+    __device__ __forceinline__ int32_t from(int g) const { return i0 + g * BT; }
+    __device__ __forceinline__ int what(int g, int32_t t) const
+    {
+        if (from(g) >= p.Nq) return 0;
+        if (sight.docs) return bit(bits + 2 * g * words, t) ? (bit(bits + (2 * g + 1) * words, t) ? 2 : 1) : 0;
+        return sight.tile(from(g), min(from(g) + BT, p.Nq), t * BT, t * BT + BT, make_int4(0, 0, 0, 0), make_int4(0, 0, 0, 0));
+    }
+    // the first tile from t on that any group sees
+    template <int QT> __device__ __forceinline__ int32_t next(int32_t t) const
+    {
+        if (!sight.docs) return t;
+        const uint32_t* any = bits + 2 * QT * words;
+        while (t < tiles) {
+            const uint32_t w = any[t >> 5] >> (t & 31);
+            if (w) return min(t + __ffs(w) - 1, tiles);
+            t = (t | 31) + 1;
+        }
+        return tiles;
+    }
+    template <int QT> __device__ __forceinline__ bool unclean(int32_t t) const
+    {
+        return (sight.len < p.Nk && t * BT + BT > sight.len) || (sight.docs && bit(bits + (2 * QT + 1) * words, t));
+    }
+};
+
+// The outputs of row i from the keys that it sees, where a value that it does not see has spoilt them: the warp together, lanes take keys for
+// the scores and columns for the sums.  Rare, and only columns that are not finite are replaced.
+template <bool CAP>
+__device__ __noinline__ void redo_row(const grf_softmax_params& p, int32_t b, int32_t h, int32_t i, float m, float l)
+{
+    const grf_sight sight(p, b);
+    const int lane = threadIdx.x & 31;
+    const int32_t kvh = h / p.group, pos = sight.position(i), end = sight.end(i + 1);
+    const __nv_bfloat16* Q = reinterpret_cast<const __nv_bfloat16*>(p.q) + b * p.qs[0] + h * p.qs[1] + (int64_t)i * p.qs[2];
+    const __nv_bfloat16* K = reinterpret_cast<const __nv_bfloat16*>(p.k) + b * p.ks[0] + kvh * p.ks[1];
+    const __nv_bfloat16* V = reinterpret_cast<const __nv_bfloat16*>(p.v) + b * p.vs[0] + kvh * p.vs[1];
+    const int32_t doc = sight.docs ? p.q_doc[(int64_t)b * p.Nq + i] : 0;
+    const int32_t* kdoc = sight.docs ? p.k_doc + (int64_t)b * p.Nk : nullptr;
+    float o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int32_t j0 = 0; j0 < end; j0 += 32) {
+        const int32_t j = j0 + lane;
+        const bool seen = j < end && sight.sees(pos, j) && (!kdoc || (doc >= 0 && kdoc[j] == doc));
+        float w = 0.0f;
+        if (seen) {
+            for (int c = 0; c < p.d; ++c) w = fmaf(__bfloat162float(Q[c]), __bfloat162float(K[(int64_t)j * p.ks[2] + c]), w);
+            w = CAP ? p.cap * GRF_LOG2E * tanh_any(w * (p.scale / p.cap)) : w * (p.scale * GRF_LOG2E);
+            if (p.bias != GRF_BIAS_NONE) w += grf_bias2<__nv_bfloat16>(p, h, j - pos);
+            w = __bfloat162float(__float2bfloat16_rn(ex2(w - m)));
+        }
+        const uint32_t who = __ballot_sync(0xffffffffu, seen);
+        for (int y = 0; y < 32; ++y) {
+            const float wy = __shfl_sync(0xffffffffu, w, y);
+            if (!(who >> y & 1u)) continue;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const int c = lane + 32 * x;
+                if (c < p.d) o[x] = fmaf(wy, __bfloat162float(V[(int64_t)(j0 + y) * p.vs[2] + c]), o[x]);
+            }
+        }
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.out_w) + b * p.os[0] + h * p.os[1] + (int64_t)i * p.os[2];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+        const int c = lane + 32 * x;
+        if (c >= p.d || fabsf(__bfloat162float(out[c])) <= 3.4028235e38f) continue;
+        const float y = o[x] * inv;
+        out[c] = __float2bfloat16_rn(y);
+        if (p.rest_w) p.rest_w[(((int64_t)b * p.H + h) * p.Nq + i) * p.d + c] = grf_rest(y, __float2bfloat16_rn(y));
+    }
+}
+
+template <int DP, bool CAP, int BIAS>
+__global__ void __launch_bounds__(Fwd<DP>::THREADS, Fwd<DP>::CTAS)
+softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                          const __grid_constant__ CUtensorMap map_v, const __grid_constant__ grf_softmax_params p)
+{
+    using Sh = Fwd<DP>;
+    constexpr int QT = Sh::QT, NS = Sh::NS;
+    extern __shared__ unsigned char smem_dyn[];
+    __shared__ __align__(8) unsigned long long bars[5 * NS + 7 * QT];
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_flag;
+    __shared__ float lut[BIAS == GRF_BIAS_BUCKETS ? QT * 2 * 256 : 1];
+    const int tid = threadIdx.x, lane = tid & 31, warp = uniform(tid >> 5);
+    const uint32_t smem = (smem_u32(smem_dyn) + 1023u) & ~1023u;
+    uint32_t* bits = reinterpret_cast<uint32_t*>(smem_dyn + (smem - smem_u32(smem_dyn)) + Sh::TILE * (QT + 2 * NS));
+    const uint32_t q_at = smem, k_at = q_at + QT * Sh::TILE, v_at = k_at + NS * Sh::TILE, bar0 = smem_u32(bars);
+    auto k_full = [&](int s) { return bar0 + 8u * s; };
+    auto v_full = [&](int s) { return bar0 + 8u * (NS + s); };
+    auto k_empty = [&](int s) { return bar0 + 8u * (2 * NS + s); };
+    auto v_empty = [&](int s) { return bar0 + 8u * (3 * NS + s); };
+    auto v_clean = [&](int s) { return bar0 + 8u * (4 * NS + s); };
+    auto of_group = [&](int g, int what) { return bar0 + 8u * (5 * NS + 7 * g + what); };
+    auto q_full = [&](int g) { return of_group(g, 0); };
+    auto s_full = [&](int g) { return of_group(g, 1); };
+    auto s_read = [&](int g) { return of_group(g, 2); };
+    auto p_full = [&](int g) { return of_group(g, 3); };
+    auto pv_done = [&](int g) { return of_group(g, 4); };
+    auto drain = [&](int g) { return of_group(g, 5); };
+    auto lut_full = [&](int g) { return of_group(g, 6); };
+
+    const int32_t b = (int32_t)blockIdx.x / p.H, h = (int32_t)blockIdx.x % p.H, kvh = h / p.group;
+    const grf_sight sight(p, b);
+    const int32_t i0 = ((int32_t)gridDim.y - 1 - (int32_t)blockIdx.y) * (QT * BT);           // the longest rows first
+    const int32_t tiles = (sight.end(min(i0 + QT * BT, p.Nq)) + BT - 1) / BT;
+    const forward_tiles T{p, sight, bits, i0, tiles, (tiles + 31) / 32};
+    constexpr int COPY = 4 * QT, ISSUE = 4 * QT + 1, CLEAN = 4 * QT + 3;
+
+    if (tid == 0) {
+        abort_flag = 0;
+        for (int s = 0; s < NS; ++s) {
+            mbar_init(k_full(s), 1); mbar_init(v_full(s), 1); mbar_init(v_clean(s), 1);
+            mbar_init(k_empty(s), QT); mbar_init(v_empty(s), QT + 1);
+        }
+        for (int g = 0; g < QT; ++g) {
+            mbar_init(q_full(g), 1); mbar_init(s_full(g), 1); mbar_init(pv_done(g), 1); mbar_init(drain(g), 1);
+            mbar_init(s_read(g), 4); mbar_init(p_full(g), 4); mbar_init(lut_full(g), 4);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == COPY) tmem_alloc(&tmem_slot, Sh::TMEM);
+    if (sight.docs) {
+        const int32_t kblocks = (p.Nk + BT - 1) / BT, qblocks = (p.Nq + BT - 1) / BT;
+        for (int32_t w = warp; w < T.words; w += Sh::THREADS / 32) {
+            const int32_t t = w * 32 + lane;
+            const int4 kr = t < tiles ? p.k_range[(int64_t)b * kblocks + t] : make_int4(INT32_MAX, -1, 0, 0);
+            uint32_t any = 0u;
+            for (int g = 0; g < QT; ++g) {
+                int what = 0;
+                if (t < tiles && T.from(g) < p.Nq)
+                    what = sight.tile(T.from(g), min(T.from(g) + BT, p.Nq), t * BT, t * BT + BT, p.q_range[(int64_t)b * qblocks + T.from(g) / BT], kr);
+                const uint32_t seen = __ballot_sync(0xffffffffu, what != 0), whole = __ballot_sync(0xffffffffu, what == 2);
+                any |= seen;
+                if (lane == 0) { bits[2 * g * T.words + w] = seen; bits[(2 * g + 1) * T.words + w] = whole; }
+            }
+            const uint32_t hole = __ballot_sync(0xffffffffu, kr.z != 0);
+            if (lane == 0) { bits[2 * QT * T.words + w] = any; bits[(2 * QT + 1) * T.words + w] = hole; }
+        }
+    }
+    fence_before_sync();
+    __syncthreads();
+    fence_after_sync();
+    const uint32_t tmem = (uint32_t)uniform((int32_t)tmem_slot);
+    auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, &abort_flag)) != 0; };
+
+    if (warp >= 4 * QT) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Sh::LESS));
+        if (warp == COPY) {
+            // ------------------------------------------------------------ copies
+            const int32_t qb = p.qs[0] ? b : 0, qh = p.qs[1] ? h : 0, kb = p.ks[0] ? b : 0, kh = p.ks[1] ? kvh : 0, vb = p.vs[0] ? b : 0, vh = p.vs[1] ? kvh : 0;
+            bool ok = true;
+            int32_t n = 0;
+            for (int g = 0; g < QT; ++g) {
+                if (T.from(g) >= p.Nq || tiles == 0) continue;
+                expect_tx_elected(q_full(g), Sh::TILE);
+                for (int y = 0; y < DP / 64; ++y) load_box(q_at + g * Sh::TILE + y * HALF, &map_q, 64 * y, T.from(g), qh, qb, q_full(g));
+            }
+            for (int32_t t = T.next<QT>(0); t < tiles && ok; t = T.next<QT>(t + 1), ++n) {
+                const int s = n % NS;
+                const uint32_t before = (uint32_t)(n / NS - 1) & 1u;
+                if (n >= NS && !(ok = wait(k_empty(s), before))) break;
+                expect_tx_elected(k_full(s), Sh::TILE);
+                for (int y = 0; y < DP / 64; ++y) load_box(k_at + s * Sh::TILE + y * HALF, &map_k, 64 * y, t * BT, kh, kb, k_full(s));
+                if (n >= NS && !(ok = wait(v_empty(s), before))) {
+                    mbar_drain(k_full(s), (uint32_t)(n / NS) & 1u, 20000000ll);
+                    break;
+                }
+                expect_tx_elected(v_full(s), Sh::TILE);
+                for (int y = 0; y < DP / 64; ++y) load_box(v_at + s * Sh::TILE + y * HALF, &map_v, 64 * y, t * BT, vh, vb, v_full(s));
+            }
+            // after an abort nobody may have waited for the last copies: they end before the CTA does
+            if (!ok || *(volatile int*)&abort_flag) {
+                for (int32_t x = max(0, n - NS); x < n; ++x) {
+                    mbar_drain(k_full(x % NS), (uint32_t)(x / NS) & 1u, 20000000ll);
+                    mbar_drain(v_full(x % NS), (uint32_t)(x / NS) & 1u, 20000000ll);
+                }
+                for (int g = 0; g < QT; ++g)
+                    if (T.from(g) < p.Nq && tiles > 0) mbar_drain(q_full(g), 0u, 20000000ll);
+            }
+        } else if (warp >= ISSUE && warp < ISSUE + QT) {
+            // ------------------------------------------------------------ products of one group
+            const int g = warp - ISSUE;
+            const int32_t steps = (p.d + 15) / 16;
+            const uint64_t q_op = rows_operand(q_at + g * Sh::TILE), k_op = rows_operand(k_at), v_op = columns_operand(v_at);
+            const uint32_t scores = tmem + g * BT, probs = scores + Sh::P_COL, acc = tmem + Sh::O_COL + g * DP;
+            bool ok = true;
+            int32_t n = 0, c = 0;
+            uint32_t cleaned = 0u;                              // parity of each stage's cleanings
+            auto make_scores = [&](int s, int32_t n_) {
+                if (!wait(k_full(s), (uint32_t)(n_ / NS) & 1u)) return false;
+                fence_after_sync();
+                product_over_columns<DP>(scores, lo32(q_op), hi32(q_op), lo32(k_op) + s * (Sh::TILE / 16), hi32(k_op), steps);
+                mma_commit(s_full(g));
+                mma_commit(k_empty(s));
+                return true;
+            };
+            auto values_ready = [&](int s, int32_t n_, int32_t t) {
+                if (!wait(v_full(s), (uint32_t)(n_ / NS) & 1u)) return false;
+                if (T.unclean<QT>(t)) {
+                    if (!wait(v_clean(s), cleaned >> s & 1u)) return false;
+                    cleaned ^= 1u << s;
+                }
+                return true;
+            };
+            int32_t t = T.next<QT>(0);
+            if (t < tiles && T.from(g) < p.Nq) ok = wait(q_full(g), 0u);
+            if (Sh::SEP && t < tiles && ok) ok = make_scores(0, 0);
+            for (; t < tiles && ok; ++n) {
+                const int s = n % NS;
+                const int32_t t_next = T.next<QT>(t + 1);
+                if (!Sh::SEP) {
+                    if (T.what(g, t) == 0) {
+                        if (!(ok = wait(k_full(s), (uint32_t)(n / NS) & 1u))) break;
+                        arrive_elected(k_empty(s));
+                        if (!(ok = values_ready(s, n, t))) break;
+                        arrive_elected(v_empty(s));
+                        t = t_next;
+                        continue;
+                    }
+                    if (!(ok = make_scores(s, n))) break;
+                } else if (t_next < tiles) {
+                    if (!(ok = wait(s_read(g), (uint32_t)c & 1u))) break;
+                    fence_after_sync();
+                    if (!(ok = make_scores((n + 1) % NS, n + 1))) break;
+                }
+                if (!(ok = wait(p_full(g), (uint32_t)c & 1u))) break;
+                if (!(ok = values_ready(s, n, t))) break;
+                fence_after_sync();
+                product_over_rows<DP>(acc, probs, lo32(v_op) + s * (Sh::TILE / 16), hi32(v_op), c > 0 ? 1u : 0u);
+                mma_commit(v_empty(s));
+                mma_commit(pv_done(g));
+                ++c;
+                t = t_next;
+            }
+            if (!ok) {
+                mma_commit(drain(g));
+                mbar_drain(drain(g), 0u, 20000000ll);
+            }
+        } else if (warp == CLEAN) {
+            // ------------------------------------------------------------ rows of V that nobody sees
+            int32_t n = 0;
+            for (int32_t t = T.next<QT>(0); t < tiles; t = T.next<QT>(t + 1), ++n) {
+                // (it waits for every tile, and holds the stage until then: a parity only tells a phase from the one before it)
+                const int s = n % NS;
+                if (!wait(v_full(s), (uint32_t)(n / NS) & 1u)) break;
+                if (!T.unclean<QT>(t)) {
+                    arrive_elected(v_empty(s));
+                    continue;
+                }
+                for (int r = lane; r < BT; r += 32) {
+                    const int32_t j = t * BT + r;
+                    if (j >= p.Nk || (j < sight.len && !(sight.docs && p.k_doc[(int64_t)b * p.Nk + j] < 0))) continue;
+                    for (int y = 0; y < DP / 64; ++y)
+                        for (int x = 0; x < 8; ++x)
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(v_at + s * Sh::TILE + y * HALF + r * 128 + x * 16), "r"(0u) : "memory");
+                }
+                fence_async_smem();                             // the products read through the asynchronous proxy
+                __syncwarp();
+                arrive_elected(v_clean(s));
+                arrive_elected(v_empty(s));
+            }
+        }
+    } else {
+        // ---------------------------------------------------------------- a thread per query
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Sh::MORE));
+        const int g = warp >> 2, r = (warp & 3) * 32 + lane;
+        const int32_t i = T.from(g) + r, pos = sight.position(i), pos0 = sight.position(T.from(g));
+        const int32_t limit = sight.order == GRF_ORDER_FULL ? sight.len : min(sight.len, max(pos + 1, sight.prefix));
+        const int32_t doc = sight.docs && i < p.Nq ? p.q_doc[(int64_t)b * p.Nq + i] : -1;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t s_addr = tmem + g * BT + lanes, p_addr = s_addr + Sh::P_COL, o_addr = tmem + Sh::O_COL + g * DP + lanes;
+        const float to2 = p.scale * GRF_LOG2E, by_cap = CAP ? p.scale / p.cap : 0.0f, cap2 = p.cap * GRF_LOG2E;
+        const float slope2 = BIAS == GRF_BIAS_SLOPES ? p.slopes[h] * GRF_LOG2E : 0.0f;
+        float m = -CUDART_INF_F;
+        uint64_t sum2[2] = {0ull, 0ull};
+        int32_t c = 0, luts = 0;
+        bool ok = true;
+        for (int32_t t = T.next<QT>(0); t < tiles; t = T.next<QT>(t + 1)) {
+            const int what = T.what(g, t);
+            if (what == 0) continue;
+            const int32_t j0 = t * BT;
+            // the bias of this tile: one value, or one per diagonal
+            float bias2 = 0.0f;
+            bool diagonals = false;
+            const float* mine = lut;
+            if (BIAS == GRF_BIAS_BUCKETS) {
+                const int32_t near = grf_bucket(p, j0 - pos0 - (BT - 1)), far = grf_bucket(p, j0 + BT - 1 - pos0);
+                diagonals = near != far;
+                if (diagonals) {
+                    float* at = lut + (g * 2 + (luts & 1)) * 256;
+                    at[r] = grf_bias2<__nv_bfloat16>(p, h, j0 - pos0 + r - (BT - 1));
+                    at[r + BT] = grf_bias2<__nv_bfloat16>(p, h, j0 - pos0 + r + 1);
+                    mine = at + (BT - 1 - r);
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(lut_full(g));
+                    if (!(ok = wait(lut_full(g), (uint32_t)luts & 1u))) break;
+                    ++luts;
+                } else bias2 = grf_bias2<__nv_bfloat16>(p, h, j0 - pos0);
+            }
+            if (!(ok = wait(s_full(g), (uint32_t)c & 1u))) break;
+            fence_after_sync();
+            uint32_t sv[8][16];
+#pragma unroll
+            for (int y = 0; y < 8; ++y) tmem_ld16_nowait(s_addr + 16 * y, sv[y]);
+            tmem_ld_wait();
+            if (Sh::SEP) {
+                fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(s_read(g));
+            }
+            float top = -CUDART_INF_F;
+            const uint64_t to22 = pack2(to2, to2), bias22 = pack2(bias2, bias2);
+#pragma unroll
+            for (int y = 0; y < 8; ++y)
+#pragma unroll
+                for (int e = 0; e < 16; e += 2) {
+                    const int col = 16 * y + e;
+                    float x0, x1;
+                    if (CAP) {
+                        x0 = cap2 * tanh_any(__uint_as_float(sv[y][e]) * by_cap) + bias2;
+                        x1 = cap2 * tanh_any(__uint_as_float(sv[y][e + 1]) * by_cap) + bias2;
+                    } else unpack2(fma2(pack2(sv[y][e], sv[y][e + 1]), to22, bias22), x0, x1);
+                    if (BIAS == GRF_BIAS_SLOPES) {
+                        x0 = fmaf(-slope2, fabsf((float)(j0 - pos + col)), x0);
+                        x1 = fmaf(-slope2, fabsf((float)(j0 - pos + col + 1)), x1);
+                    }
+                    if (BIAS == GRF_BIAS_BUCKETS) {
+                        if (diagonals) { x0 += mine[col]; x1 += mine[col + 1]; }
+                    }
+                    sv[y][e] = __float_as_uint(x0);
+                    sv[y][e + 1] = __float_as_uint(x1);
+                }
+            if (what == 1) {
+                if (sight.docs) {
+                    const int32_t* kd = p.k_doc + (int64_t)b * p.Nk + j0;
+#pragma unroll
+                    for (int y = 0; y < 8; ++y)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            if (!(j0 + 16 * y + e < limit && doc >= 0 && __ldg(kd + 16 * y + e) == doc)) sv[y][e] = 0xff800000u;
+                } else {
+#pragma unroll
+                    for (int y = 0; y < 8; ++y)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            if (j0 + 16 * y + e >= limit) sv[y][e] = 0xff800000u;
+                }
+            }
+#pragma unroll
+            for (int y = 0; y < 8; ++y)
+#pragma unroll
+                for (int e = 0; e < 16; e += 2) top = max3(top, __uint_as_float(sv[y][e]), __uint_as_float(sv[y][e + 1]));
+            // a new maximum only when it matters: 2^8 above the one in use (or the first)
+            const bool grow = top > m + 8.0f;
+            if (__any_sync(0xffffffffu, grow)) {
+                const float alpha = grow ? ex2(m - top) : 1.0f;
+                if (grow) m = top;
+                if (c > 0) {
+                    if (!(ok = wait(pv_done(g), (uint32_t)(c - 1) & 1u))) break;
+                    fence_after_sync();
+                    const uint64_t a2 = pack2(alpha, alpha);
+                    sum2[0] = mul2(sum2[0], a2);
+                    sum2[1] = mul2(sum2[1], a2);
+#pragma unroll
+                    for (int y = 0; y < DP / 16; ++y) {
+                        uint32_t o[16];
+                        tmem_ld16(o_addr + 16 * y, o);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+                        tmem_st16(o_addr + 16 * y, o);
+                    }
+                }
+            }
+            if (Sh::SEP && c > 0) {
+                if (!(ok = wait(pv_done(g), (uint32_t)(c - 1) & 1u))) break;
+                fence_after_sync();
+            }
+            const float base = m == -CUDART_INF_F ? 0.0f : m;
+            const uint64_t minus = pack2(-base, -base);
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                uint32_t w[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int a = 2 * y + (e >> 3), z = (2 * e) & 15;
+                    float x0, x1;
+                    unpack2(add2(pack2(sv[a][z], sv[a][z + 1]), minus), x0, x1);
+                    x0 = ex2(x0);
+                    x1 = ex2(x1);
+                    sum2[e & 1] = add2(sum2[e & 1], pack2(x0, x1));
+                    w[e] = pack_bf16(x0, x1);
+                }
+                tmem_st16(p_addr + 16 * y, w);
+            }
+            tmem_st_wait();
+            fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(p_full(g));
+            ++c;
+        }
+        ok = __all_sync(0xffffffffu, ok) != 0;
+        if (ok && c > 0) ok = wait(pv_done(g), (uint32_t)(c - 1) & 1u);
+        fence_after_sync();
+        float l0, l1, l2, l3;
+        unpack2(sum2[0], l0, l1);
+        unpack2(sum2[1], l2, l3);
+        const float l = (l0 + l1) + (l2 + l3), inv = l == 0.0f ? 0.0f : 1.0f / l;
+        bool spoilt = false;
+        if (ok) {
+            __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.out_w) + b * p.os[0] + h * p.os[1] + (int64_t)i * p.os[2];
+            __nv_bfloat16* rest = p.rest_w ? p.rest_w + (((int64_t)b * p.H + h) * p.Nq + i) * p.d : nullptr;
+#pragma unroll
+            for (int y = 0; y < DP / 16; ++y) {
+                uint32_t o[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[e] = 0u;
+                if (c > 0) tmem_ld16(o_addr + 16 * y, o);
+                if (i >= p.Nq) continue;
+#pragma unroll
+                for (int z = 0; z < 2; ++z) {
+                    if (16 * y + 8 * z >= p.d) continue;
+                    uint32_t w[4], u[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        // (no key seen: 0, whatever the accumulator holds)
+                        const float x0 = l == 0.0f ? 0.0f : __uint_as_float(o[8 * z + 2 * e]) * inv, x1 = l == 0.0f ? 0.0f : __uint_as_float(o[8 * z + 2 * e + 1]) * inv;
+                        spoilt |= !(fabsf(x0) <= 3.4028235e38f) || !(fabsf(x1) <= 3.4028235e38f);
+                        w[e] = pack_bf16(x0, x1);
+                        if (rest) {
+                            const __nv_bfloat16 r0 = grf_rest(x0, __float2bfloat16_rn(x0)), r1 = grf_rest(x1, __float2bfloat16_rn(x1));
+                            u[e] = pack_bf16(__bfloat162float(r0), __bfloat162float(r1));
+                        }
+                    }
+                    *reinterpret_cast<uint4*>(out + 16 * y + 8 * z) = make_uint4(w[0], w[1], w[2], w[3]);
+                    if (rest) *reinterpret_cast<uint4*>(rest + 16 * y + 8 * z) = make_uint4(u[0], u[1], u[2], u[3]);
+                }
+            }
+            if (p.lse_w && i < p.Nq) p.lse_w[((int64_t)b * p.H + h) * p.Nq + i] = l == 0.0f ? -CUDART_INF_F : (m + log2f(l)) * GRF_LN2;
+            // rows whose scores are finite but whose outputs are not
+            uint32_t again = __ballot_sync(0xffffffffu, spoilt && l <= 3.4028235e38f && fabsf(m) <= 3.4028235e38f);
+            __syncwarp();
+            while (again) {
+                const int y = __ffs(again) - 1;
+                again &= again - 1;
+                redo_row<CAP>(p, b, h, __shfl_sync(0xffffffffu, i, y), __shfl_sync(0xffffffffu, m, y), __shfl_sync(0xffffffffu, l, y));
+            }
+        }
+        fence_before_sync();
+    }
+    fence_before_sync();
+    __syncthreads();
+    if (warp == COPY) tmem_dealloc(tmem, Sh::TMEM);
+    if (tid == 0 && abort_flag) atomicExch(p.error_word, 1);
+}
+
+template <int DP, bool CAP, int BIAS> int launch(grf_ctx* ctx, const grf_softmax_params& p, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv)
+{
+    using Sh = Fwd<DP>;
+    const size_t smem = Sh::SMEM + (p.q_doc ? 4 * (size_t)(2 * Sh::QT + 2) * (grf_ceil_div(p.Nk, BT) / 32 + 1) : 0);
+    GRF_CUDA_TRY(cudaFuncSetAttribute(softmax_tc_forward_kernel<DP, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    grf_softmax_scope scope(ctx, "grf:softmax_attention");
+    softmax_tc_forward_kernel<DP, CAP, BIAS><<<dim3(p.B * p.H, grf_ceil_div(p.Nq, Sh::QT * BT)), Sh::THREADS, smem, ctx->stream>>>(mq, mk, mv, p);
+    return cudaGetLastError() == cudaSuccess ? GRF_OK : GRF_ERR_CUDA;
+}
+
+template <int DP> int choose(grf_ctx* ctx, const grf_softmax_params& p, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv)
+{
+    if (p.cap > 0.0f) {
+        if (p.bias == GRF_BIAS_NONE) return launch<DP, true, GRF_BIAS_NONE>(ctx, p, mq, mk, mv);
+        if (p.bias == GRF_BIAS_SLOPES) return launch<DP, true, GRF_BIAS_SLOPES>(ctx, p, mq, mk, mv);
+        return launch<DP, true, GRF_BIAS_BUCKETS>(ctx, p, mq, mk, mv);
+    }
+    if (p.bias == GRF_BIAS_NONE) return launch<DP, false, GRF_BIAS_NONE>(ctx, p, mq, mk, mv);
+    if (p.bias == GRF_BIAS_SLOPES) return launch<DP, false, GRF_BIAS_SLOPES>(ctx, p, mq, mk, mv);
+    return launch<DP, false, GRF_BIAS_BUCKETS>(ctx, p, mq, mk, mv);
+}
+
+}  // namespace
+
+int grf_softmax_tc_forward(grf_ctx* ctx, const grf_softmax_params& p)
+{
+    CUtensorMap mq, mk, mv;
+    if (!grf_make_token_box_map(&mq, p.q, p.qs, p.B, p.H, p.Nq, p.d) || !grf_make_token_box_map(&mk, p.k, p.ks, p.B, p.KV, p.Nk, p.d) ||
+        !grf_make_token_box_map(&mv, p.v, p.vs, p.B, p.KV, p.Nk, p.d)) return 1;
+    return p.d <= 64 ? choose<64>(ctx, p, mq, mk, mv) : choose<128>(ctx, p, mq, mk, mv);
+}

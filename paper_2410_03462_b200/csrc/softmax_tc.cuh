@@ -1,0 +1,98 @@
+// What the tensor-core kernels of softmax attention share: boxes of rows by the copy engine, which tiles a block visits, scores from raw products.
+#pragma once
+
+#include "softmax.cuh"
+#include "tc_common.cuh"
+
+namespace grf_softmax_tc {
+
+using namespace grf_tc;
+
+constexpr int BT = 128;                 // queries, and keys, of a tile
+constexpr uint32_t HALF = BT * 128;     // bytes of 64 columns of a tile: rows of 128 bytes, swizzled over a row
+
+// A box of 64 columns and BT rows of (columns, tokens, heads, sequences), by one elected lane of a converged warp.
+__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, int32_t col, int32_t row, int32_t head, int32_t batch, uint32_t bar)
+{
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "elect.sync _|q, 0xffffffff;\n\t"
+        "@q cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];\n\t}"
+        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(col), "r"(row), "r"(head), "r"(batch), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void arrive_elected(uint32_t bar)
+{
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "elect.sync _|q, 0xffffffff;\n\t"
+        "@q mbarrier.arrive.shared::cta.b64 _, [%0];\n\t}" ::"r"(bar) : "memory");
+}
+
+// A tile as the operand whose rows are the product's rows or columns (K-major): 32 bytes along a row per step of 16, HALF per 64.
+__device__ __forceinline__ uint64_t rows_operand(uint32_t base) { return swizzled_desc(base, 16, 1024, 2); }
+// A tile as the right operand summed over its rows (MN-major): 64 columns every HALF bytes, eight rows every 1024; 2048 per step of 16 rows.
+__device__ __forceinline__ uint64_t columns_operand(uint32_t base) { return swizzled_desc(base, HALF, 1024, 2); }
+__device__ __forceinline__ uint32_t lo32(uint64_t x) { return (uint32_t)x; }
+__device__ __forceinline__ uint32_t hi32(uint64_t x) { return (uint32_t)(x >> 32); }
+
+// D[128][128] = A B^T over d columns (rounded up to 16), both operands rows in shared memory.
+template <int DP>
+__device__ __forceinline__ void product_over_columns(uint32_t acc, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, int32_t steps)
+{
+    constexpr uint32_t idesc = instr_desc(BT, false, false);
+#pragma unroll
+    for (int y = 0; y < DP / 16; ++y) {
+        if (y < steps) {
+            const uint32_t at = (uint32_t)(y / 4) * (HALF / 16) + (uint32_t)(y % 4) * 2;
+            if (y == 0) mma_bf16_ss_halves<false>(acc, a_lo + at, a_hi, b_lo + at, b_hi, idesc);
+            else mma_bf16_ss_halves<true>(acc, a_lo + at, a_hi, b_lo + at, b_hi, idesc);
+        }
+    }
+}
+// acc[128][DP] (+)= A[128][128] B[128][DP]: A in tensor memory (bf16 pairs), B's rows in shared memory.
+template <int DP>
+__device__ __forceinline__ void product_over_rows(uint32_t acc, uint32_t a_tmem, uint32_t b_lo, uint32_t b_hi, uint32_t accumulate)
+{
+    constexpr uint32_t idesc = instr_desc(DP, false, true);
+#pragma unroll
+    for (int y = 0; y < BT / 16; ++y) mma_bf16_ts_halves(acc, a_tmem + y * 8, b_lo + y * (2048 / 16), b_hi, idesc, y > 0 ? 1u : accumulate);
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float ex2(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// tanh within 2e-7 (absolute): 1 - 2 / (1 + e^2y).
+__device__ __forceinline__ float tanh_any(float y)
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + ex2(y * (2.0f * GRF_LOG2E))));
+    return fmaf(-2.0f, r, 1.0f);
+}
+
+__device__ __forceinline__ int32_t uniform(int32_t x) { return __shfl_sync(0xffffffffu, x, 0); }
+
+// Bits of a block's tiles, in shared memory; only with documents, as otherwise the tiles follow from positions alone.
+struct tile_bits {
+    const uint32_t *seen, *whole;
+};
+__device__ __forceinline__ bool bit(const uint32_t* w, int32_t t) { return w[t >> 5] >> (t & 31) & 1u; }
+
+}  // namespace grf_softmax_tc
+
+// [B][heads][tokens][d] bf16 by strides (0: that axis is not stepped along): boxes of 64 columns and 128 rows, swizzled.
+bool grf_make_token_box_map(CUtensorMap* map, const void* base, const int64_t (&stride)[3], int32_t batch, int32_t heads, int32_t tokens, int32_t d);

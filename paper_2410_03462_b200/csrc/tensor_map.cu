@@ -45,3 +45,21 @@ bool grf_make_row_box_map(CUtensorMap* map, const void* base, uint32_t problems,
     return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
                CU_TENSOR_MAP_INTERLEAVE_NONE, sw, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+
+bool grf_make_token_box_map(CUtensorMap* map, const void* base, const int64_t (&stride)[3], int32_t batch, int32_t heads, int32_t tokens, int32_t d)
+{
+    encode_tiled_fn enc = tensor_map_encoder();
+    if (!enc || (reinterpret_cast<uintptr_t>(base) & 15u) != 0) return false;
+    // heads or sequences with stride 0 are one place, at which the kernels stay
+    if (stride[2] == 0 && tokens > 1) return false;
+    const int32_t extent[3] = {tokens, heads, batch};
+    cuuint64_t dims[4] = {(cuuint64_t)d, 1, 1, 1}, strides[3];
+    for (int x = 0; x < 3; ++x) {
+        const int64_t s = stride[2 - x];
+        if (s != 0) dims[x + 1] = (cuuint64_t)extent[x];
+        strides[x] = s != 0 ? (cuuint64_t)s * 2 : 16;
+    }
+    const cuuint32_t box[4] = {64, 128, 1, 1}, estr[4] = {1, 1, 1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}

@@ -250,7 +250,13 @@ def test_what_nobody_sees_does_not_matter(lib, route, dtype, bad, nq):
     hit = np.zeros(out.shape, bool)
     hit[0, 2:, :, 5] = see[0][:, j]
     assert not np.isfinite(out[hit]).any()
-    assert np.array_equal(out[~hit], clean[0].float().cpu().numpy()[~hit])
+    same = clean[0].float().cpu().numpy()
+    # (a spoilt column of a row that does not see the value may be summed again, in another order: one rounding to storage)
+    again = np.zeros(out.shape, bool)
+    again[0, 2:, :, 5] = True
+    assert np.array_equal(out[~again], same[~again])
+    again &= ~hit
+    assert (np.abs(out[again] - same[again]) <= (2 * R.HALF_STEP[DT[dtype]] + 2 * 200 * R.U) * np.abs(same[again]) + 1e-4).all()
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
