@@ -205,12 +205,10 @@ size_t forward_bytes(const grf_ctx* ctx, const grf_softmax_params& p, int dtype)
 struct backward_room : room {
     doc_room docs;
     size_t dsum, table;
-    int32_t q_blocks;
     explicit backward_room(const grf_softmax_params& p) : docs(*this, p)
     {
         dsum = take(sizeof(float) * (size_t)p.B * p.H * p.Nq);
-        q_blocks = grf_ceil_div(p.Nq, RANGE_BLOCK);
-        table = take(p.bias == GRF_BIAS_BUCKETS ? sizeof(float) * (size_t)p.B * p.H * q_blocks * grf_softmax_columns(p) : 0);
+        table = take(p.bias == GRF_BIAS_BUCKETS ? sizeof(float) * (size_t)p.B * p.H * grf_ceil_div(p.Nq, RANGE_BLOCK) * grf_softmax_columns(p) : 0);
     }
 };
 
@@ -309,7 +307,6 @@ extern "C" int grf_softmax_attn_backward(grf_ctx* ctx, const grf_softmax_desc* d
     p.dsum = (const float*)(ws + r.dsum);
     p.dtable_part = dtable ? (float*)(ws + r.table) : nullptr;
     p.error_word = ctx->error_word;
-    GRF_TRY(r.docs.fill(ctx, p, ws, 64));
     {
         grf_softmax_scope scope(ctx, "grf:output_products");
         const int lanes = (int)(p.d * elem(desc->dtype) / 16);
@@ -324,12 +321,23 @@ extern "C" int grf_softmax_attn_backward(grf_ctx* ctx, const grf_softmax_desc* d
             else output_products<__nv_bfloat16, 16>(ctx, p, dsum);
         }
     }
-    GRF_TRY(grf_softmax_alu_backward(ctx, p, desc->dtype));
+    int rc = 1, block = 128;
+    if (desc->dtype == GRF_DTYPE_BF16 && ctx->use_tensor_cores) {
+        GRF_TRY(r.docs.fill(ctx, p, ws, block));
+        rc = grf_softmax_tc_backward(ctx, p);
+    }
+    if (rc > 0) {
+        block = 64;
+        GRF_TRY(r.docs.fill(ctx, p, ws, block));
+        rc = grf_softmax_alu_backward(ctx, p, desc->dtype);
+    }
+    GRF_TRY(rc);
     if (dtable) {
+        const int32_t q_blocks = grf_ceil_div(p.Nq, block);
         grf_softmax_scope scope(ctx, "grf:bucket_sums");
         const dim3 grid(grf_softmax_columns(p), p.H);
-        if (desc->dtype == GRF_DTYPE_F32) bucket_sums_kernel<float><<<grid, 256, 0, ctx->stream>>>(p.dtable_part, (float*)dtable, p.B, p.H, r.q_blocks, grf_softmax_columns(p));
-        else bucket_sums_kernel<__nv_bfloat16><<<grid, 256, 0, ctx->stream>>>(p.dtable_part, (__nv_bfloat16*)dtable, p.B, p.H, r.q_blocks, grf_softmax_columns(p));
+        if (desc->dtype == GRF_DTYPE_F32) bucket_sums_kernel<float><<<grid, 256, 0, ctx->stream>>>(p.dtable_part, (float*)dtable, p.B, p.H, q_blocks, grf_softmax_columns(p));
+        else bucket_sums_kernel<__nv_bfloat16><<<grid, 256, 0, ctx->stream>>>(p.dtable_part, (__nv_bfloat16*)dtable, p.B, p.H, q_blocks, grf_softmax_columns(p));
     }
     return cudaGetLastError() == cudaSuccess ? GRF_OK : GRF_ERR_CUDA;
 }

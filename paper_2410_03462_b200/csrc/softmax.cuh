@@ -121,6 +121,7 @@ int grf_softmax_alu_backward(grf_ctx* ctx, const grf_softmax_params& p, int dtyp
 // softmax_tc.cu, softmax_tc_grad.cu: bf16 on the tensor cores; documents' ranges over blocks of 128.  1 (nothing launched) where no tensor map
 // can be made of the operands
 int grf_softmax_tc_forward(grf_ctx* ctx, const grf_softmax_params& p);
+int grf_softmax_tc_backward(grf_ctx* ctx, const grf_softmax_params& p);
 // softmax_few.cu: few queries, keys split over CTAs
 #define GRF_FEW_QUERIES 16
 size_t grf_softmax_few_workspace(const grf_ctx* ctx, const grf_softmax_params& p, int dtype);

@@ -36,6 +36,7 @@ struct forward_tiles {
     const grf_sight& sight;
     const uint32_t* bits;                                       // [seen, whole] per group, then of any group, then tiles with a token of no document
     int32_t i0, tiles, words;
+    int32_t last;                                               // one past the last key that any query of the sequence can see
     // queries of group g
     __device__ __forceinline__ int32_t from(int g) const { return i0 + g * BT; }
     __device__ __forceinline__ int what(int g, int32_t t) const
@@ -58,7 +59,7 @@ struct forward_tiles {
     }
     template <int QT> __device__ __forceinline__ bool unclean(int32_t t) const
     {
-        return (sight.len < p.Nk && t * BT + BT > sight.len) || (sight.docs && bit(bits + (2 * QT + 1) * words, t));
+        return (last < p.Nk && t * BT + BT > last) || (sight.docs && bit(bits + (2 * QT + 1) * words, t));
     }
 };
 
@@ -143,7 +144,7 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
     const grf_sight sight(p, b);
     const int32_t i0 = ((int32_t)gridDim.y - 1 - (int32_t)blockIdx.y) * (QT * BT);           // the longest rows first
     const int32_t tiles = (sight.end(min(i0 + QT * BT, p.Nq)) + BT - 1) / BT;
-    const forward_tiles T{p, sight, bits, i0, tiles, (tiles + 31) / 32};
+    const forward_tiles T{p, sight, bits, i0, tiles, (tiles + 31) / 32, sight.end(p.Nq)};
     constexpr int COPY = 4 * QT, ISSUE = 4 * QT + 1, CLEAN = 4 * QT + 3;
 
     if (tid == 0) {
@@ -289,7 +290,7 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 }
                 for (int r = lane; r < BT; r += 32) {
                     const int32_t j = t * BT + r;
-                    if (j >= p.Nk || (j < sight.len && !(sight.docs && p.k_doc[(int64_t)b * p.Nk + j] < 0))) continue;
+                    if (j >= p.Nk || (j < T.last && !(sight.docs && p.k_doc[(int64_t)b * p.Nk + j] < 0))) continue;
                     for (int y = 0; y < DP / 64; ++y)
                         for (int x = 0; x < 8; ++x)
                             asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(v_at + s * Sh::TILE + y * HALF + r * 128 + x * 16), "r"(0u) : "memory");

@@ -1,0 +1,765 @@
+// Softmax attention over ordered tokens on the tensor cores (bf16): gradients, in two kernels so that nothing is added atomically.
+//
+//   dQ     a CTA of 128 queries goes over the key tiles: S = Q K^T, dP = dout V^T (a query per lane of tensor memory), dS = P (dP - D), and
+//          dQ += dX K with dX as bf16 pairs in tensor memory.  Where the bias table wants its gradient, dS is summed along diagonals by
+//          shuffles (a lane hands its sum to the next lane, which adds the next column), and the diagonals by bucket
+//   dK, dV a CTA of 128 keys goes over the query tiles of all heads that share it, transposed: S^T = K Q^T, dP^T = V dout^T (a key per lane), so
+//          that P^T and dX^T are left operands where they are made: dV += P^T dout, dK += dX^T Q
+// Seven products a tile where a single kernel would need five, but no tile of dQ travels through memory.  Two warpgroups share a tile, 64
+// columns each, and work in turn with the products: while P of a tile is made the tensor cores finish the one before, while dS is made they
+// make the next S.  Three warps copy, issue, and prepare: lse and D of the queries (dK, dV), and rows that nobody sees cleared (0 times an
+// infinity there would reach a whole tile).
+#include "softmax_tc.cuh"
+
+namespace {
+
+using namespace grf_softmax_tc;
+
+constexpr int THREADS = 384, WORKERS = 8;           // warps that make P and dS
+constexpr int MORE = 208, LESS = 88;                // registers: 2 * 208 + 88 = 3 * 168
+constexpr int COPY = WORKERS, ISSUE = WORKERS + 1, PREPARE = WORKERS + 2;
+constexpr int NS = 2;
+
+template <int DP> struct Grad {
+    static constexpr uint32_t TILE = HALF * (DP / 64);
+    static constexpr size_t SMEM = 1024 + (size_t)TILE * (2 + 2 * NS);      // then the tiles' bits
+};
+
+// Tiles of the other side that a block sees, in order; with documents from bits in shared memory.
+struct grad_tiles {
+    const uint32_t* bits;               // seen, whole, tiles with a token of no document
+    int32_t first, tiles, words;
+    bool docs;
+    __device__ __forceinline__ int32_t next(int32_t t) const
+    {
+        if (!docs) return t;
+        while (t < tiles) {
+            const uint32_t w = bits[t >> 5] >> (t & 31);
+            if (w) return min(t + __ffs(w) - 1, tiles);
+            t = (t | 31) + 1;
+        }
+        return tiles;
+    }
+    __device__ __forceinline__ int32_t begin() const { return next(first); }
+    __device__ __forceinline__ bool whole(int32_t t) const { return bit(bits + words, t); }
+    __device__ __forceinline__ bool hole(int32_t t) const { return docs && bit(bits + 2 * words, t); }
+};
+
+__device__ __forceinline__ float min_nan(float a, float b)
+{
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void clear_row(uint32_t tile, int r, int halves)
+{
+    for (int y = 0; y < halves; ++y)
+        for (int x = 0; x < 8; ++x) asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(tile + y * HALF + r * 128 + x * 16), "r"(0u) : "memory");
+}
+// D[128][DP] (+)= A B: A's bf16 pairs in two halves of 32 columns, 64 columns apart.
+template <int DP>
+__device__ __forceinline__ void product_of_halves(uint32_t acc, uint32_t a_tmem, uint32_t b_lo, uint32_t b_hi, uint32_t accumulate)
+{
+    constexpr uint32_t idesc = instr_desc(DP, false, true);
+#pragma unroll
+    for (int y = 0; y < BT / 16; ++y)
+        mma_bf16_ts_halves(acc, a_tmem + (y / 4) * 64 + (y % 4) * 8, b_lo + y * (2048 / 16), b_hi, idesc, y > 0 ? 1u : accumulate);
+}
+
+template <int DP, bool CAP, int BIAS>
+__global__ void __launch_bounds__(THREADS, 1)
+softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                     const __grid_constant__ CUtensorMap map_g, const __grid_constant__ grf_softmax_params p)
+{
+    using Sh = Grad<DP>;
+    constexpr int LUTS = BIAS == GRF_BIAS_BUCKETS ? 1 : 0;
+    extern __shared__ unsigned char smem_dyn[];
+    __shared__ __align__(8) unsigned long long bars[5 * NS + 9];
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_flag;
+    __shared__ float lut[LUTS ? 2 * 256 : 1];
+    __shared__ float bins[LUTS ? WORKERS * 2 * GRF_MAX_BUCKETS : 1];
+    __shared__ float diag[LUTS ? WORKERS * 96 : 1];
+    __shared__ unsigned char diag_bucket[LUTS ? WORKERS * 96 : 1];
+    const int tid = threadIdx.x, lane = tid & 31, warp = uniform(tid >> 5);
+    const uint32_t smem = (smem_u32(smem_dyn) + 1023u) & ~1023u;
+    uint32_t* bits = reinterpret_cast<uint32_t*>(smem_dyn + (smem - smem_u32(smem_dyn)) + Sh::TILE * (2 + 2 * NS));
+    const uint32_t q_at = smem, g_at = q_at + Sh::TILE, k_at = g_at + Sh::TILE, v_at = k_at + NS * Sh::TILE, bar0 = smem_u32(bars);
+    auto k_full = [&](int s) { return bar0 + 8u * s; };
+    auto v_full = [&](int s) { return bar0 + 8u * (NS + s); };
+    auto k_empty = [&](int s) { return bar0 + 8u * (2 * NS + s); };
+    auto v_empty = [&](int s) { return bar0 + 8u * (3 * NS + s); };
+    auto k_clean = [&](int s) { return bar0 + 8u * (4 * NS + s); };
+    const uint32_t one = bar0 + 8u * (5 * NS);
+    const uint32_t rows_full = one, s_full0 = one + 8, dp_full = one + 24, ds_full = one + 32, dq_done = one + 40, drain = one + 48, lut_full = one + 56;
+
+    const int32_t b = (int32_t)blockIdx.x / p.H, h = (int32_t)blockIdx.x % p.H, kvh = h / p.group;
+    const grf_sight sight(p, b);
+    const int32_t qb = (int32_t)gridDim.y - 1 - (int32_t)blockIdx.y, i0 = qb * BT, i1 = min(i0 + BT, p.Nq);
+    const int32_t tiles = (sight.end(i1) + BT - 1) / BT, last = sight.end(p.Nq);
+    const grad_tiles T{bits, 0, tiles, (tiles + 31) / 32, sight.docs};
+    auto unclean = [&](int32_t t) { return (last < p.Nk && t * BT + BT > last) || T.hole(t); };
+
+    if (tid == 0) {
+        abort_flag = 0;
+        for (int s = 0; s < NS; ++s) {
+            mbar_init(k_full(s), 1); mbar_init(v_full(s), 1); mbar_init(k_clean(s), 1);
+            mbar_init(k_empty(s), 2); mbar_init(v_empty(s), 1);
+        }
+        mbar_init(rows_full, 1); mbar_init(s_full0, 1); mbar_init(s_full0 + 8, 1); mbar_init(dp_full, 1); mbar_init(ds_full, WORKERS);
+        mbar_init(dq_done, 1); mbar_init(drain, 1); mbar_init(lut_full, WORKERS);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == COPY) tmem_alloc(&tmem_slot, 512u);
+    if (sight.docs) {
+        const int32_t kblocks = (p.Nk + BT - 1) / BT, qblocks = (p.Nq + BT - 1) / BT;
+        const int4 qr = p.q_range[(int64_t)b * qblocks + qb];
+        for (int32_t w = warp; w < T.words; w += THREADS / 32) {
+            const int32_t t = w * 32 + lane;
+            const int4 kr = t < tiles ? p.k_range[(int64_t)b * kblocks + t] : make_int4(INT32_MAX, -1, 0, 0);
+            const int what = t < tiles ? sight.tile(i0, i1, t * BT, t * BT + BT, qr, kr) : 0;
+            const uint32_t seen = __ballot_sync(0xffffffffu, what != 0), whole = __ballot_sync(0xffffffffu, what == 2), hole = __ballot_sync(0xffffffffu, kr.z != 0);
+            if (lane == 0) { bits[w] = seen; bits[T.words + w] = whole; bits[2 * T.words + w] = hole; }
+        }
+    }
+    if (LUTS)
+        for (int x = tid; x < WORKERS * 2 * GRF_MAX_BUCKETS; x += THREADS) bins[x] = 0.0f;
+    fence_before_sync();
+    __syncthreads();
+    fence_after_sync();
+    const uint32_t tmem = (uint32_t)uniform((int32_t)tmem_slot);
+    const uint32_t dp_col = tmem + 256, acc = tmem + 384;
+    auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, &abort_flag)) != 0; };
+
+    if (warp >= WORKERS) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(LESS));
+        if (warp == COPY) {
+            const int32_t qbt = p.qs[0] ? b : 0, qh = p.qs[1] ? h : 0, gb = p.dos[0] ? b : 0, gh = p.dos[1] ? h : 0;
+            const int32_t kb = p.ks[0] ? b : 0, kh = p.ks[1] ? kvh : 0, vb = p.vs[0] ? b : 0, vh = p.vs[1] ? kvh : 0;
+            bool ok = true;
+            int32_t n = 0;
+            if (T.begin() < tiles) {
+                expect_tx_elected(rows_full, 2 * Sh::TILE);
+                for (int y = 0; y < DP / 64; ++y) {
+                    load_box(q_at + y * HALF, &map_q, 64 * y, i0, qh, qbt, rows_full);
+                    load_box(g_at + y * HALF, &map_g, 64 * y, i0, gh, gb, rows_full);
+                }
+            }
+            for (int32_t t = T.begin(); t < tiles && ok; t = T.next(t + 1), ++n) {
+                const int s = n % NS;
+                const uint32_t before = (uint32_t)(n / NS - 1) & 1u;
+                if (n >= NS && !(ok = wait(k_empty(s), before) && wait(v_empty(s), before))) break;
+                expect_tx_elected(k_full(s), Sh::TILE);
+                expect_tx_elected(v_full(s), Sh::TILE);
+                for (int y = 0; y < DP / 64; ++y) {
+                    load_box(k_at + s * Sh::TILE + y * HALF, &map_k, 64 * y, t * BT, kh, kb, k_full(s));
+                    load_box(v_at + s * Sh::TILE + y * HALF, &map_v, 64 * y, t * BT, vh, vb, v_full(s));
+                }
+            }
+            if (!ok || *(volatile int*)&abort_flag) {
+                for (int32_t x = max(0, n - NS); x < n; ++x) {
+                    mbar_drain(k_full(x % NS), (uint32_t)(x / NS) & 1u, 20000000ll);
+                    mbar_drain(v_full(x % NS), (uint32_t)(x / NS) & 1u, 20000000ll);
+                }
+                if (T.begin() < tiles) mbar_drain(rows_full, 0u, 20000000ll);
+            }
+        } else if (warp == ISSUE) {
+            const int32_t steps = (p.d + 15) / 16;
+            const uint64_t q_op = rows_operand(q_at), g_op = rows_operand(g_at), k_op = rows_operand(k_at), v_op = rows_operand(v_at), kc_op = columns_operand(k_at);
+            uint32_t cleaned = 0u;
+            bool ok = true;
+            auto make_scores = [&](int32_t n) {
+                const int s = n % NS;
+                if (!wait(k_full(s), (uint32_t)(n / NS) & 1u)) return false;
+                fence_after_sync();
+                product_over_columns<DP>(tmem + (n & 1) * BT, lo32(q_op), hi32(q_op), lo32(k_op) + s * (Sh::TILE / 16), hi32(k_op), steps);
+                mma_commit(s_full0 + 8 * (n & 1));
+                return true;
+            };
+            auto make_dp = [&](int32_t n) {
+                const int s = n % NS;
+                if (!wait(v_full(s), (uint32_t)(n / NS) & 1u)) return false;
+                fence_after_sync();
+                product_over_columns<DP>(dp_col, lo32(g_op), hi32(g_op), lo32(v_op) + s * (Sh::TILE / 16), hi32(v_op), steps);
+                mma_commit(dp_full);
+                mma_commit(v_empty(s));
+                return true;
+            };
+            int32_t t = T.begin(), n = 0;
+            if (t < tiles) ok = wait(rows_full, 0u) && make_scores(0) && make_dp(0);
+            for (; t < tiles && ok; ++n) {
+                const int s = n % NS;
+                const int32_t t_next = T.next(t + 1);
+                // (its place was read before the last tile's dS arrived)
+                if (t_next < tiles && !(ok = make_scores(n + 1))) break;
+                if (!(ok = wait(ds_full, (uint32_t)n & 1u))) break;
+                if (unclean(t)) {
+                    if (!(ok = wait(k_clean(s), cleaned >> s & 1u))) break;
+                    cleaned ^= 1u << s;
+                }
+                fence_after_sync();
+                product_of_halves<DP>(acc, dp_col, lo32(kc_op) + s * (Sh::TILE / 16), hi32(kc_op), n > 0 ? 1u : 0u);
+                mma_commit(k_empty(s));
+                if (t_next >= tiles) mma_commit(dq_done);
+                else ok = make_dp(n + 1);
+                t = t_next;
+            }
+            if (!ok) {
+                mma_commit(drain);
+                mbar_drain(drain, 0u, 20000000ll);
+            }
+        } else if (warp == PREPARE) {
+            // rows of K that nobody sees, once S is made of them (before that, dQ's product alone reads them summed over rows)
+            int32_t n = 0;
+            for (int32_t t = T.begin(); t < tiles; t = T.next(t + 1), ++n) {
+                const int s = n % NS;
+                if (!wait(k_full(s), (uint32_t)(n / NS) & 1u)) break;
+                if (unclean(t)) {
+                    for (int r = lane; r < BT; r += 32) {
+                        const int32_t j = t * BT + r;
+                        if (j < p.Nk && (j >= last || (sight.docs && p.k_doc[(int64_t)b * p.Nk + j] < 0))) clear_row(k_at + s * Sh::TILE, r, DP / 64);
+                    }
+                    fence_async_smem();
+                    __syncwarp();
+                    arrive_elected(k_clean(s));
+                }
+                arrive_elected(k_empty(s));
+            }
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(MORE));
+        const int r = (warp & 3) * 32 + lane, part = warp >> 2, c0 = part * 64;
+        const int32_t i = i0 + r, pos = sight.position(i), pos0 = sight.position(i0);
+        const int32_t limit = sight.order == GRF_ORDER_FULL ? sight.len : min(sight.len, max(pos + 1, sight.prefix));
+        const int32_t doc = sight.docs && i < p.Nq ? p.q_doc[(int64_t)b * p.Nq + i] : -1;
+        const int64_t row = ((int64_t)b * p.H + h) * p.Nq + i;
+        const float lse = i < p.Nq ? p.lse[row] : -CUDART_INF_F, dsum = i < p.Nq ? p.dsum[row] : 0.0f;
+        const bool any = lse != -CUDART_INF_F;                  // a row without a key: P = 0
+        const float lse2 = any ? lse * GRF_LOG2E : CUDART_INF_F;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const float to2 = p.scale * GRF_LOG2E, by_cap = CAP ? p.scale / p.cap : 0.0f, cap2 = p.cap * GRF_LOG2E;
+        const float slope2 = BIAS == GRF_BIAS_SLOPES ? p.slopes[h] * GRF_LOG2E : 0.0f;
+        const int32_t columns = grf_softmax_columns(p);
+        const bool sums = LUTS && p.dtable_part != nullptr;
+        float* my_bins = bins + warp * 2 * GRF_MAX_BUCKETS;
+        float far_sum = 0.0f;                                   // of dS in tiles of one bucket, until the bucket changes
+        int32_t far_bucket = -1;
+        auto flush = [&]() {
+            float x = far_sum;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+            if (far_bucket >= 0 && lane == 0) my_bins[far_bucket] += x;
+            far_sum = 0.0f;
+            __syncwarp();
+        };
+        int32_t n = 0, luts = 0;
+        bool ok = true;
+        for (int32_t t = T.begin(); t < tiles; t = T.next(t + 1)) {
+            const int32_t j0 = t * BT;
+            const bool partial = sight.docs ? !T.whole(t) : sight.tile(i0, i1, j0, j0 + BT, make_int4(0, 0, 0, 0), make_int4(0, 0, 0, 0)) == 1;
+            float bias2 = 0.0f;
+            bool diagonals = false;
+            int32_t bucket0 = 0;
+            const float* mine = lut;
+            if (LUTS) {
+                bucket0 = grf_bucket(p, j0 - pos0 - (BT - 1));
+                diagonals = bucket0 != grf_bucket(p, j0 + BT - 1 - pos0);
+                if (diagonals) {
+                    float* at = lut + (luts & 1) * 256;
+                    at[tid] = tid < 2 * BT - 1 ? grf_bias2<__nv_bfloat16>(p, h, j0 - pos0 + tid - (BT - 1)) : 0.0f;
+                    mine = at + (BT - 1 - r) + c0;
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(lut_full);
+                    if (!(ok = wait(lut_full, (uint32_t)luts & 1u))) break;
+                    ++luts;
+                } else bias2 = grf_bias2<__nv_bfloat16>(p, h, j0 - pos0);
+            }
+            if (!(ok = wait(s_full0 + 8 * (n & 1), (uint32_t)(n >> 1) & 1u))) break;
+            fence_after_sync();
+            float x[64], dcap[CAP ? 64 : 1];
+            {
+                uint32_t sv[4][16];
+#pragma unroll
+                for (int y = 0; y < 4; ++y) tmem_ld16_nowait(tmem + (n & 1) * BT + c0 + 16 * y + lanes, sv[y]);
+                tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 64; ++e) {
+                    const float raw = __uint_as_float(sv[e / 16][e % 16]);
+                    float s;
+                    if (CAP) {
+                        const float th = tanh_any(raw * by_cap);
+                        dcap[e] = fmaf(-th, th, 1.0f);
+                        s = fmaf(cap2, th, bias2);
+                    } else s = fmaf(raw, to2, bias2);
+                    if (BIAS == GRF_BIAS_SLOPES) s = fmaf(-slope2, fabsf((float)(j0 + c0 - pos + e)), s);
+                    if (LUTS) { if (diagonals) s += mine[e]; }
+                    x[e] = ex2(min_nan(s - lse2, 0.0f));
+                }
+            }
+            const bool careful = partial || !any;               // (of this row: nothing in it may meet an infinity or NaN)
+            if (careful) {
+                const int32_t* kd = p.k_doc + (int64_t)b * p.Nk + j0 + c0;
+#pragma unroll
+                for (int e = 0; e < 64; ++e)
+                    if (!(j0 + c0 + e < limit && any && (!sight.docs || (doc >= 0 && __ldg(kd + e) == doc)))) x[e] = 0.0f;
+            }
+            if (!(ok = wait(dp_full, (uint32_t)n & 1u))) break;
+            fence_after_sync();
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                uint32_t dv[16];
+                tmem_ld16(dp_col + c0 + 16 * y + lanes, dv);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float d = __uint_as_float(dv[e]) - dsum;
+                    // (a place that is not seen holds 0, whatever dP is there)
+                    x[16 * y + e] = careful && x[16 * y + e] == 0.0f ? 0.0f : x[16 * y + e] * d;
+                }
+            }
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                uint32_t w[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int a = 32 * y + 2 * e;
+                    w[e] = CAP ? pack_bf16(x[a] * dcap[CAP ? a : 0], x[a + 1] * dcap[CAP ? a + 1 : 0]) : pack_bf16(x[a], x[a + 1]);
+                }
+                tmem_st16(dp_col + c0 + 16 * y + lanes, w);
+            }
+            tmem_st_wait();
+            fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(ds_full);
+            ++n;
+            if (sums) {
+                if (!diagonals) {
+                    if (bucket0 != far_bucket) { flush(); far_bucket = bucket0; }
+                    float y0 = 0.0f, y1 = 0.0f, y2 = 0.0f, y3 = 0.0f;
+#pragma unroll
+                    for (int e = 0; e < 64; e += 4) { y0 += x[e]; y1 += x[e + 1]; y2 += x[e + 2]; y3 += x[e + 3]; }
+                    far_sum += (y0 + y1) + (y2 + y3);
+                } else {
+                    // diagonal e - lane is complete in lane 31 after column e; those that end at the last column are in the other lanes
+                    float a = 0.0f;
+                    float* at = diag + warp * 96;
+#pragma unroll
+                    for (int e = 0; e < 64; ++e) {
+                        const float up = __shfl_up_sync(0xffffffffu, a, 1);
+                        a = x[e] + (lane > 0 ? up : 0.0f);
+                        if (lane == 31) at[e] = a;
+                    }
+                    if (lane < 31) at[64 + 30 - lane] = a;      // diagonal 63 - lane; place x holds diagonal x - 31
+#pragma unroll
+                    for (int z = 0; z < 3; ++z) {
+                        const int d = lane + 32 * z;
+                        if (d < 95) diag_bucket[warp * 96 + d] = (unsigned char)grf_bucket(p, j0 + c0 + d - 31 - sight.position(i0 + (warp & 3) * 32));
+                    }
+                    __syncwarp();
+                    for (int y = lane; y < columns; y += 32) {
+                        float sum = 0.0f;
+                        for (int d = 0; d < 95; ++d)
+                            if (diag_bucket[warp * 96 + d] == y) sum += at[d];
+                        my_bins[y] += sum;
+                    }
+                    __syncwarp();
+                }
+            }
+        }
+        if (sums) flush();
+        ok = __all_sync(0xffffffffu, ok) != 0;
+        if (ok && n > 0) ok = wait(dq_done, 0u);
+        fence_after_sync();
+        if (ok) {
+            __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.dq) + b * p.dqs[0] + h * p.dqs[1] + (int64_t)i * p.dqs[2];
+#pragma unroll
+            for (int y = 0; y < DP / 32; ++y) {
+                const int col = part * (DP / 2) + 16 * y;
+                uint32_t o[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[e] = 0u;
+                if (n > 0) tmem_ld16(acc + col + lanes, o);
+                if (i >= p.Nq) continue;
+#pragma unroll
+                for (int z = 0; z < 2; ++z) {
+                    if (col + 8 * z >= p.d) continue;
+                    uint32_t w[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] = any ? pack_bf16(__uint_as_float(o[8 * z + 2 * e]) * p.scale, __uint_as_float(o[8 * z + 2 * e + 1]) * p.scale) : 0u;
+                    *reinterpret_cast<uint4*>(dst + col + 8 * z) = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+            }
+        }
+        fence_before_sync();
+    }
+    fence_before_sync();
+    __syncthreads();
+    if (warp == COPY) tmem_dealloc(tmem, 512u);
+    if (LUTS && p.dtable_part && tid < grf_softmax_columns(p)) {
+        float sum = 0.0f;
+        for (int w = 0; w < WORKERS; ++w) sum += bins[w * 2 * GRF_MAX_BUCKETS + tid];
+        p.dtable_part[((int64_t)blockIdx.x * gridDim.y + qb) * grf_softmax_columns(p) + tid] = sum;
+    }
+    if (tid == 0 && abort_flag) atomicExch(p.error_word, 1);
+}
+
+template <int DP, bool CAP, int BIAS>
+__global__ void __launch_bounds__(THREADS, 1)
+softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                      const __grid_constant__ CUtensorMap map_g, const __grid_constant__ grf_softmax_params p)
+{
+    using Sh = Grad<DP>;
+    constexpr int LUTS = BIAS == GRF_BIAS_BUCKETS ? 1 : 0;
+    extern __shared__ unsigned char smem_dyn[];
+    __shared__ __align__(8) unsigned long long bars[4 * NS + 9];
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_flag;
+    __shared__ float lut[LUTS ? 2 * 256 : 1];
+    __shared__ __align__(16) float info[NS][2][BT];             // lse (in units of log 2; infinity where P = 0) and D of a tile's queries
+    __shared__ __align__(16) int32_t info_doc[NS][BT];
+    const int tid = threadIdx.x, lane = tid & 31, warp = uniform(tid >> 5);
+    const uint32_t smem = (smem_u32(smem_dyn) + 1023u) & ~1023u;
+    uint32_t* bits = reinterpret_cast<uint32_t*>(smem_dyn + (smem - smem_u32(smem_dyn)) + Sh::TILE * (2 + 2 * NS));
+    const uint32_t k_at = smem, v_at = k_at + Sh::TILE, q_at = v_at + Sh::TILE, g_at = q_at + NS * Sh::TILE, bar0 = smem_u32(bars);
+    auto q_full = [&](int s) { return bar0 + 8u * s; };
+    auto g_full = [&](int s) { return bar0 + 8u * (NS + s); };
+    auto empty = [&](int s) { return bar0 + 8u * (2 * NS + s); };
+    auto ready = [&](int s) { return bar0 + 8u * (3 * NS + s); };
+    const uint32_t one = bar0 + 8u * (4 * NS);
+    const uint32_t keys_full = one, s_full = one + 8, dp_full = one + 16, p_full = one + 24, ds_full = one + 32, acc_done = one + 40, drain = one + 48,
+                   lut_full = one + 56;
+
+    const int32_t b = (int32_t)blockIdx.x / p.KV, kvh = (int32_t)blockIdx.x % p.KV;
+    const grf_sight sight(p, b);
+    const int32_t j0 = (int32_t)blockIdx.y * BT, qblocks = (p.Nq + BT - 1) / BT;
+    // the first query that sees a key of the block, were there no documents
+    int32_t first = 0;
+    if (sight.order != GRF_ORDER_FULL && j0 >= sight.prefix) {
+        const int64_t x = (int64_t)j0 - sight.start;
+        first = x <= 0 ? 0 : x >= p.Nq ? qblocks : (int32_t)x / BT;
+    }
+    if (j0 >= sight.len) first = qblocks;
+    const grad_tiles T{bits, first, qblocks, (qblocks + 31) / 32, sight.docs};
+
+    if (tid == 0) {
+        abort_flag = 0;
+        for (int s = 0; s < NS; ++s) { mbar_init(q_full(s), 1); mbar_init(g_full(s), 1); mbar_init(empty(s), 1); mbar_init(ready(s), 1); }
+        mbar_init(keys_full, 1); mbar_init(s_full, 1); mbar_init(dp_full, 1); mbar_init(p_full, WORKERS); mbar_init(ds_full, WORKERS);
+        mbar_init(acc_done, 1); mbar_init(drain, 1); mbar_init(lut_full, WORKERS);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == COPY) tmem_alloc(&tmem_slot, 512u);
+    if (sight.docs) {
+        const int4 kr = p.k_range[(int64_t)b * gridDim.y + blockIdx.y];
+        for (int32_t w = warp; w < T.words; w += THREADS / 32) {
+            const int32_t t = w * 32 + lane;
+            const bool in = t >= first && t < qblocks;
+            const int what = in ? sight.tile(t * BT, min(t * BT + BT, p.Nq), j0, j0 + BT, p.q_range[(int64_t)b * qblocks + t], kr) : 0;
+            const uint32_t seen = __ballot_sync(0xffffffffu, what != 0), whole = __ballot_sync(0xffffffffu, what == 2);
+            if (lane == 0) { bits[w] = seen; bits[T.words + w] = whole; bits[2 * T.words + w] = 0u; }
+        }
+    }
+    fence_before_sync();
+    __syncthreads();
+    fence_after_sync();
+    const uint32_t tmem = (uint32_t)uniform((int32_t)tmem_slot);
+    const uint32_t s_col = tmem, dp_col = tmem + 128, dv_acc = tmem + 256, dk_acc = tmem + 256 + DP;
+    const bool some = T.begin() < qblocks;
+    auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, &abort_flag)) != 0; };
+    // the block's tiles, head after head: true while there is one, with t and h advanced to it
+    auto step = [&](int32_t& t, int32_t& h) {
+        t = T.next(t + 1);
+        if (t >= qblocks) {
+            if (++h >= (kvh + 1) * p.group) return false;
+            t = T.begin();
+        }
+        return true;
+    };
+
+    if (warp >= WORKERS) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(LESS));
+        if (warp == COPY) {
+            bool ok = true;
+            int32_t n = 0;
+            if (some) {
+                expect_tx_elected(keys_full, 2 * Sh::TILE);
+                for (int y = 0; y < DP / 64; ++y) {
+                    load_box(k_at + y * HALF, &map_k, 64 * y, j0, p.ks[1] ? kvh : 0, p.ks[0] ? b : 0, keys_full);
+                    load_box(v_at + y * HALF, &map_v, 64 * y, j0, p.vs[1] ? kvh : 0, p.vs[0] ? b : 0, keys_full);
+                }
+                int32_t t = T.begin(), h = kvh * p.group;
+                do {
+                    const int s = n % NS;
+                    if (n >= NS && !(ok = wait(empty(s), (uint32_t)(n / NS - 1) & 1u))) break;
+                    expect_tx_elected(q_full(s), Sh::TILE);
+                    expect_tx_elected(g_full(s), Sh::TILE);
+                    for (int y = 0; y < DP / 64; ++y) {
+                        load_box(q_at + s * Sh::TILE + y * HALF, &map_q, 64 * y, t * BT, p.qs[1] ? h : 0, p.qs[0] ? b : 0, q_full(s));
+                        load_box(g_at + s * Sh::TILE + y * HALF, &map_g, 64 * y, t * BT, p.dos[1] ? h : 0, p.dos[0] ? b : 0, g_full(s));
+                    }
+                    ++n;
+                } while (step(t, h));
+                if (!ok || *(volatile int*)&abort_flag) {
+                    for (int32_t x = max(0, n - NS); x < n; ++x) {
+                        mbar_drain(q_full(x % NS), (uint32_t)(x / NS) & 1u, 20000000ll);
+                        mbar_drain(g_full(x % NS), (uint32_t)(x / NS) & 1u, 20000000ll);
+                    }
+                    mbar_drain(keys_full, 0u, 20000000ll);
+                }
+            }
+        } else if (warp == ISSUE) {
+            const int32_t steps = (p.d + 15) / 16;
+            const uint64_t k_op = rows_operand(k_at), v_op = rows_operand(v_at), q_op = rows_operand(q_at), g_op = rows_operand(g_at), qc_op = columns_operand(q_at),
+                           gc_op = columns_operand(g_at);
+            bool ok = true;
+            auto make_scores = [&](int32_t n) {
+                const int s = n % NS;
+                if (!wait(ready(s), (uint32_t)(n / NS) & 1u) || !wait(q_full(s), (uint32_t)(n / NS) & 1u)) return false;
+                fence_after_sync();
+                product_over_columns<DP>(s_col, lo32(k_op), hi32(k_op), lo32(q_op) + s * (Sh::TILE / 16), hi32(q_op), steps);
+                mma_commit(s_full);
+                return true;
+            };
+            auto make_dp = [&](int32_t n) {
+                const int s = n % NS;
+                if (!wait(g_full(s), (uint32_t)(n / NS) & 1u)) return false;
+                fence_after_sync();
+                product_over_columns<DP>(dp_col, lo32(v_op), hi32(v_op), lo32(g_op) + s * (Sh::TILE / 16), hi32(g_op), steps);
+                mma_commit(dp_full);
+                return true;
+            };
+            if (some) {
+                int32_t t = T.begin(), h = kvh * p.group, n = 0;
+                ok = wait(keys_full, 0u) && make_scores(0) && make_dp(0);
+                bool more = true;
+                for (; ok && more; ++n) {
+                    const int s = n % NS;
+                    more = step(t, h);
+                    if (!(ok = wait(p_full, (uint32_t)n & 1u))) break;
+                    fence_after_sync();
+                    product_of_halves<DP>(dv_acc, s_col, lo32(gc_op) + s * (Sh::TILE / 16), hi32(gc_op), n > 0 ? 1u : 0u);
+                    if (more && !(ok = make_scores(n + 1))) break;
+                    if (!(ok = wait(ds_full, (uint32_t)n & 1u))) break;
+                    fence_after_sync();
+                    product_of_halves<DP>(dk_acc, dp_col, lo32(qc_op) + s * (Sh::TILE / 16), hi32(qc_op), n > 0 ? 1u : 0u);
+                    mma_commit(empty(s));
+                    if (!more) mma_commit(acc_done);
+                    else ok = make_dp(n + 1);
+                }
+                if (!ok) {
+                    mma_commit(drain);
+                    mbar_drain(drain, 0u, 20000000ll);
+                }
+            }
+        } else if (warp == PREPARE && some) {
+            int32_t t = T.begin(), h = kvh * p.group, n = 0;
+            do {
+                const int s = n % NS;
+                if (n >= NS && !wait(empty(s), (uint32_t)(n / NS - 1) & 1u)) break;
+                const int64_t row = ((int64_t)b * p.H + h) * p.Nq + t * BT;
+                uint32_t none[4];
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    const int r = lane + 32 * y;
+                    const bool in = t * BT + r < p.Nq;
+                    const float lse = in ? p.lse[row + r] : -CUDART_INF_F, d = in ? p.dsum[row + r] : 0.0f;
+                    const bool empty_row = lse == -CUDART_INF_F;
+                    none[y] = __ballot_sync(0xffffffffu, in && empty_row);
+                    info[s][0][r] = empty_row ? CUDART_INF_F : lse * GRF_LOG2E;
+                    info[s][1][r] = empty_row ? 0.0f : d;
+                    if (sight.docs) info_doc[s][r] = in ? p.q_doc[(int64_t)b * p.Nq + t * BT + r] : -1;
+                }
+                if (none[0] | none[1] | none[2] | none[3]) {
+                    // what rows of queries that see nothing hold does not matter: cleared, as 0 times it is summed below
+                    if (!wait(q_full(s), (uint32_t)(n / NS) & 1u) || !wait(g_full(s), (uint32_t)(n / NS) & 1u)) break;
+#pragma unroll
+                    for (int y = 0; y < 4; ++y)
+                        if (none[y] >> lane & 1u) {
+                            clear_row(q_at + s * Sh::TILE, lane + 32 * y, DP / 64);
+                            clear_row(g_at + s * Sh::TILE, lane + 32 * y, DP / 64);
+                        }
+                    fence_async_smem();
+                }
+                __syncwarp();
+                arrive_elected(ready(s));
+                ++n;
+            } while (step(t, h));
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(MORE));
+        const int r = (warp & 3) * 32 + lane, part = warp >> 2, c0 = part * 64;
+        const int32_t j = j0 + r;
+        const int32_t doc = sight.docs && j < p.Nk ? p.k_doc[(int64_t)b * p.Nk + j] : -1;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const float to2 = p.scale * GRF_LOG2E, by_cap = CAP ? p.scale / p.cap : 0.0f, cap2 = p.cap * GRF_LOG2E;
+        int32_t n = 0, luts = 0;
+        bool ok = true;
+        if (some) {
+            int32_t t = T.begin(), h = kvh * p.group;
+            do {
+                const int s = n % NS;
+                const int32_t i0 = t * BT, pos0 = sight.position(i0);
+                const bool partial = sight.docs ? !T.whole(t)
+                                                : sight.tile(i0, min(i0 + BT, p.Nq), j0, j0 + BT, make_int4(0, 0, 0, 0), make_int4(0, 0, 0, 0)) == 1;
+                // columns from `from` on see this key
+                const int32_t from = j >= sight.len ? BT : sight.order == GRF_ORDER_FULL || j < sight.prefix ? 0 : min(max(j - pos0, 0), BT);
+                const float slope2 = BIAS == GRF_BIAS_SLOPES ? p.slopes[h] * GRF_LOG2E : 0.0f;
+                float bias2 = 0.0f;
+                bool diagonals = false;
+                const float* mine = lut;
+                if (LUTS) {
+                    diagonals = grf_bucket(p, j0 - pos0 - (BT - 1)) != grf_bucket(p, j0 + BT - 1 - pos0);
+                    if (diagonals) {
+                        float* at = lut + (luts & 1) * 256;
+                        at[tid] = tid < 2 * BT - 1 ? grf_bias2<__nv_bfloat16>(p, h, j0 - pos0 + tid - (BT - 1)) : 0.0f;
+                        mine = at + (BT - 1 + r - c0);          // column e: mine[-e]
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(lut_full);
+                        if (!(ok = wait(lut_full, (uint32_t)luts & 1u))) break;
+                        ++luts;
+                    } else bias2 = grf_bias2<__nv_bfloat16>(p, h, j0 - pos0);
+                }
+                if (!(ok = wait(ready(s), (uint32_t)(n / NS) & 1u) && wait(s_full, (uint32_t)n & 1u))) break;
+                fence_after_sync();
+                float x[64], dcap[CAP ? 64 : 1];
+                {
+                    uint32_t sv[4][16];
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) tmem_ld16_nowait(s_col + c0 + 16 * y + lanes, sv[y]);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int e4 = 0; e4 < 64; e4 += 4) {
+                        const float4 l4 = *reinterpret_cast<const float4*>(&info[s][0][c0 + e4]);
+                        const float lv[4] = {l4.x, l4.y, l4.z, l4.w};
+#pragma unroll
+                        for (int z = 0; z < 4; ++z) {
+                            const int e = e4 + z;
+                            const float raw = __uint_as_float(sv[e / 16][e % 16]);
+                            float sc;
+                            if (CAP) {
+                                const float th = tanh_any(raw * by_cap);
+                                dcap[e] = fmaf(-th, th, 1.0f);
+                                sc = fmaf(cap2, th, bias2);
+                            } else sc = fmaf(raw, to2, bias2);
+                            if (BIAS == GRF_BIAS_SLOPES) sc = fmaf(-slope2, fabsf((float)(j - pos0 - c0 - e)), sc);
+                            if (LUTS) { if (diagonals) sc += mine[-e]; }
+                            x[e] = ex2(min_nan(sc - lv[z], 0.0f));
+                        }
+                    }
+                }
+                if (partial) {
+#pragma unroll
+                    for (int e = 0; e < 64; ++e)
+                        if (!(c0 + e >= from && (!sight.docs || (doc >= 0 && info_doc[s][c0 + e] == doc)))) x[e] = 0.0f;
+                }
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    uint32_t w[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) w[e] = pack_bf16(x[32 * y + 2 * e], x[32 * y + 2 * e + 1]);
+                    tmem_st16(s_col + c0 + 16 * y + lanes, w);
+                }
+                tmem_st_wait();
+                fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_full);
+                if (!(ok = wait(dp_full, (uint32_t)n & 1u))) break;
+                fence_after_sync();
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    uint32_t dv[16];
+                    tmem_ld16(dp_col + c0 + 16 * y + lanes, dv);
+#pragma unroll
+                    for (int e4 = 0; e4 < 16; e4 += 4) {
+                        const float4 d4 = *reinterpret_cast<const float4*>(&info[s][1][c0 + 16 * y + e4]);
+                        const float d[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+                        for (int z = 0; z < 4; ++z) {
+                            const int e = 16 * y + e4 + z;
+                            const float ds = x[e] * (__uint_as_float(dv[e4 + z]) - d[z]);
+                            x[e] = partial && x[e] == 0.0f ? 0.0f : CAP ? ds * dcap[CAP ? e : 0] : ds;
+                        }
+                    }
+                }
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    uint32_t w[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) w[e] = pack_bf16(x[32 * y + 2 * e], x[32 * y + 2 * e + 1]);
+                    tmem_st16(dp_col + c0 + 16 * y + lanes, w);
+                }
+                tmem_st_wait();
+                fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(ds_full);
+                ++n;
+            } while (step(t, h));
+        }
+        ok = __all_sync(0xffffffffu, ok) != 0;
+        if (ok && n > 0) ok = wait(acc_done, 0u);
+        fence_after_sync();
+        if (ok) {
+            // the first warpgroup writes dV, the second one dK
+            const int64_t (&st)[3] = part == 0 ? p.dvs : p.dks;
+            __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(part == 0 ? p.dv : p.dk) + b * st[0] + kvh * st[1] + (int64_t)j * st[2];
+            const float by = part == 0 ? 1.0f : p.scale;
+#pragma unroll
+            for (int y = 0; y < DP / 16; ++y) {
+                uint32_t o[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[e] = 0u;
+                if (n > 0) tmem_ld16((part == 0 ? dv_acc : dk_acc) + 16 * y + lanes, o);
+                if (j >= p.Nk) continue;
+#pragma unroll
+                for (int z = 0; z < 2; ++z) {
+                    if (16 * y + 8 * z >= p.d) continue;
+                    uint32_t w[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] = pack_bf16(__uint_as_float(o[8 * z + 2 * e]) * by, __uint_as_float(o[8 * z + 2 * e + 1]) * by);
+                    *reinterpret_cast<uint4*>(dst + 16 * y + 8 * z) = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+            }
+        }
+        fence_before_sync();
+    }
+    fence_before_sync();
+    __syncthreads();
+    if (warp == COPY) tmem_dealloc(tmem, 512u);
+    if (tid == 0 && abort_flag) atomicExch(p.error_word, 1);
+}
+
+struct grad_maps { CUtensorMap q, k, v, g; };
+
+template <int DP, bool CAP, int BIAS> int launch(grf_ctx* ctx, const grf_softmax_params& p, const grad_maps& m)
+{
+    using Sh = Grad<DP>;
+    auto bits = [&](int32_t tokens) { return p.q_doc ? 12 * (size_t)(grf_ceil_div(tokens, BT) / 32 + 1) : 0; };
+    const size_t dq_smem = Sh::SMEM + bits(p.Nk), dkv_smem = Sh::SMEM + bits(p.Nq);
+    GRF_CUDA_TRY(cudaFuncSetAttribute(softmax_tc_dq_kernel<DP, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)dq_smem));
+    GRF_CUDA_TRY(cudaFuncSetAttribute(softmax_tc_dkv_kernel<DP, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)dkv_smem));
+    grf_softmax_scope scope(ctx, "grf:softmax_gradients", 2);
+    softmax_tc_dkv_kernel<DP, CAP, BIAS><<<dim3(p.B * p.KV, grf_ceil_div(p.Nk, BT)), THREADS, dkv_smem, ctx->stream>>>(m.q, m.k, m.v, m.g, p);
+    softmax_tc_dq_kernel<DP, CAP, BIAS><<<dim3(p.B * p.H, grf_ceil_div(p.Nq, BT)), THREADS, dq_smem, ctx->stream>>>(m.q, m.k, m.v, m.g, p);
+    return cudaGetLastError() == cudaSuccess ? GRF_OK : GRF_ERR_CUDA;
+}
+
+template <int DP> int choose(grf_ctx* ctx, const grf_softmax_params& p, const grad_maps& m)
+{
+    if (p.cap > 0.0f) {
+        if (p.bias == GRF_BIAS_NONE) return launch<DP, true, GRF_BIAS_NONE>(ctx, p, m);
+        if (p.bias == GRF_BIAS_SLOPES) return launch<DP, true, GRF_BIAS_SLOPES>(ctx, p, m);
+        return launch<DP, true, GRF_BIAS_BUCKETS>(ctx, p, m);
+    }
+    if (p.bias == GRF_BIAS_NONE) return launch<DP, false, GRF_BIAS_NONE>(ctx, p, m);
+    if (p.bias == GRF_BIAS_SLOPES) return launch<DP, false, GRF_BIAS_SLOPES>(ctx, p, m);
+    return launch<DP, false, GRF_BIAS_BUCKETS>(ctx, p, m);
+}
+
+}  // namespace
+
+int grf_softmax_tc_backward(grf_ctx* ctx, const grf_softmax_params& p)
+{
+    grad_maps m;
+    if (!grf_make_token_box_map(&m.q, p.q, p.qs, p.B, p.H, p.Nq, p.d) || !grf_make_token_box_map(&m.k, p.k, p.ks, p.B, p.KV, p.Nk, p.d) ||
+        !grf_make_token_box_map(&m.v, p.v, p.vs, p.B, p.KV, p.Nk, p.d) || !grf_make_token_box_map(&m.g, p.dout, p.dos, p.B, p.H, p.Nq, p.d)) return 1;
+    return p.d <= 64 ? choose<64>(ctx, p, m) : choose<128>(ctx, p, m);
+}
