@@ -18,15 +18,17 @@ namespace {
 
 using namespace grf_softmax_tc;
 
-template <int DP> struct Fwd {
+// EXACT: P as the sum of two bf16 values, so that O has fp32 precision and D = dout . O of the backward pass, a difference of nearly equal terms
+// where a row looks at few keys, loses nothing (dQ of the capped case: 2.8e-3 from 64 bits without, MEASURED with).  The second values take the rest of S's place.
+template <int DP, bool EXACT> struct Fwd {
     static constexpr int QT = DP == 64 ? 1 : 2;                 // groups
     static constexpr int CTAS = DP == 64 ? 2 : 1;
-    static constexpr bool SEP = DP == 64;                       // P beside S
+    static constexpr bool SEP = DP == 64 && !EXACT;             // P beside S
     static constexpr int THREADS = 128 * (QT + 1);
     static constexpr int NS = 2;
     static constexpr uint32_t TILE = HALF * (DP / 64);
     static constexpr uint32_t TMEM = DP == 64 ? 256 : 512;
-    static constexpr uint32_t P_COL = SEP ? 128 : 0, O_COL = SEP ? 192 : 256;
+    static constexpr uint32_t P_COL = SEP ? 128 : 0, O_COL = DP == 64 ? 192 : 256;
     static constexpr size_t SMEM = 1024 + (size_t)TILE * (QT + 2 * NS);    // then the tiles' bits
     static constexpr int MORE = DP == 64 ? 200 : 208, LESS = DP == 64 ? 56 : 88;   // registers: QT * MORE + LESS = the launch's
 };
@@ -110,12 +112,12 @@ __device__ __noinline__ void redo_row(const grf_softmax_params& p, int32_t b, in
     }
 }
 
-template <int DP, bool CAP, int BIAS>
-__global__ void __launch_bounds__(Fwd<DP>::THREADS, Fwd<DP>::CTAS)
+template <int DP, bool CAP, int BIAS, bool EXACT>
+__global__ void __launch_bounds__(Fwd<DP, EXACT>::THREADS, Fwd<DP, EXACT>::CTAS)
 softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                           const __grid_constant__ CUtensorMap map_v, const __grid_constant__ grf_softmax_params p)
 {
-    using Sh = Fwd<DP>;
+    using Sh = Fwd<DP, EXACT>;
     constexpr int QT = Sh::QT, NS = Sh::NS;
     extern __shared__ unsigned char smem_dyn[];
     __shared__ __align__(8) unsigned long long bars[5 * NS + 7 * QT];
@@ -268,6 +270,7 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 if (!(ok = values_ready(s, n, t))) break;
                 fence_after_sync();
                 product_over_rows<DP>(acc, probs, lo32(v_op) + s * (Sh::TILE / 16), hi32(v_op), c > 0 ? 1u : 0u);
+                if (EXACT) product_over_rows<DP>(acc, probs + 64, lo32(v_op) + s * (Sh::TILE / 16), hi32(v_op), 1u);
                 mma_commit(v_empty(s));
                 mma_commit(pv_done(g));
                 ++c;
@@ -420,7 +423,7 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             const uint64_t minus = pack2(-base, -base);
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
-                uint32_t w[16];
+                uint32_t w[16], u[EXACT ? 16 : 1];
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const int a = 2 * y + (e >> 3), z = (2 * e) & 15;
@@ -430,8 +433,10 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                     x1 = ex2(x1);
                     sum2[e & 1] = add2(sum2[e & 1], pack2(x0, x1));
                     w[e] = pack_bf16(x0, x1);
+                    if (EXACT) u[EXACT ? e : 0] = pack_bf16(x0 - __uint_as_float(w[e] << 16), x1 - __uint_as_float(w[e] & 0xffff0000u));
                 }
                 tmem_st16(p_addr + 16 * y, w);
+                if constexpr (EXACT) tmem_st16(p_addr + 64 + 16 * y, u);
             }
             tmem_st_wait();
             fence_before_sync();
@@ -494,34 +499,39 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
     if (tid == 0 && abort_flag) atomicExch(p.error_word, 1);
 }
 
-template <int DP, bool CAP, int BIAS> int launch(grf_ctx* ctx, const grf_softmax_params& p, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv)
+struct forward_maps { CUtensorMap q, k, v; };
+
+template <int DP, bool CAP, int BIAS, bool EXACT> int launch(grf_ctx* ctx, const grf_softmax_params& p, const forward_maps& m)
 {
-    using Sh = Fwd<DP>;
+    using Sh = Fwd<DP, EXACT>;
+    const auto kernel = softmax_tc_forward_kernel<DP, CAP, BIAS, EXACT>;
     const size_t smem = Sh::SMEM + (p.q_doc ? 4 * (size_t)(2 * Sh::QT + 2) * (grf_ceil_div(p.Nk, BT) / 32 + 1) : 0);
-    GRF_CUDA_TRY(cudaFuncSetAttribute(softmax_tc_forward_kernel<DP, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    GRF_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     grf_softmax_scope scope(ctx, "grf:softmax_attention");
-    softmax_tc_forward_kernel<DP, CAP, BIAS><<<dim3(p.B * p.H, grf_ceil_div(p.Nq, Sh::QT * BT)), Sh::THREADS, smem, ctx->stream>>>(mq, mk, mv, p);
+    kernel<<<dim3(p.B * p.H, grf_ceil_div(p.Nq, Sh::QT * BT)), Sh::THREADS, smem, ctx->stream>>>(m.q, m.k, m.v, p);
     return cudaGetLastError() == cudaSuccess ? GRF_OK : GRF_ERR_CUDA;
 }
 
-template <int DP> int choose(grf_ctx* ctx, const grf_softmax_params& p, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv)
+template <int DP, bool EXACT, bool CAP> int by_bias(grf_ctx* ctx, const grf_softmax_params& p, const forward_maps& m)
 {
-    if (p.cap > 0.0f) {
-        if (p.bias == GRF_BIAS_NONE) return launch<DP, true, GRF_BIAS_NONE>(ctx, p, mq, mk, mv);
-        if (p.bias == GRF_BIAS_SLOPES) return launch<DP, true, GRF_BIAS_SLOPES>(ctx, p, mq, mk, mv);
-        return launch<DP, true, GRF_BIAS_BUCKETS>(ctx, p, mq, mk, mv);
-    }
-    if (p.bias == GRF_BIAS_NONE) return launch<DP, false, GRF_BIAS_NONE>(ctx, p, mq, mk, mv);
-    if (p.bias == GRF_BIAS_SLOPES) return launch<DP, false, GRF_BIAS_SLOPES>(ctx, p, mq, mk, mv);
-    return launch<DP, false, GRF_BIAS_BUCKETS>(ctx, p, mq, mk, mv);
+    return p.bias == GRF_BIAS_NONE ? launch<DP, CAP, GRF_BIAS_NONE, EXACT>(ctx, p, m)
+         : p.bias == GRF_BIAS_SLOPES ? launch<DP, CAP, GRF_BIAS_SLOPES, EXACT>(ctx, p, m) : launch<DP, CAP, GRF_BIAS_BUCKETS, EXACT>(ctx, p, m);
+}
+template <int DP, bool EXACT> int by_cap(grf_ctx* ctx, const grf_softmax_params& p, const forward_maps& m)
+{
+    return p.cap > 0.0f ? by_bias<DP, EXACT, true>(ctx, p, m) : by_bias<DP, EXACT, false>(ctx, p, m);
+}
+template <int DP> int by_rest(grf_ctx* ctx, const grf_softmax_params& p, const forward_maps& m)
+{
+    return p.rest_w ? by_cap<DP, true>(ctx, p, m) : by_cap<DP, false>(ctx, p, m);
 }
 
 }  // namespace
 
 int grf_softmax_tc_forward(grf_ctx* ctx, const grf_softmax_params& p)
 {
-    CUtensorMap mq, mk, mv;
-    if (!grf_make_token_box_map(&mq, p.q, p.qs, p.B, p.H, p.Nq, p.d) || !grf_make_token_box_map(&mk, p.k, p.ks, p.B, p.KV, p.Nk, p.d) ||
-        !grf_make_token_box_map(&mv, p.v, p.vs, p.B, p.KV, p.Nk, p.d)) return 1;
-    return p.d <= 64 ? choose<64>(ctx, p, mq, mk, mv) : choose<128>(ctx, p, mq, mk, mv);
+    forward_maps m;
+    if (!grf_make_token_box_map(&m.q, p.q, p.qs, p.B, p.H, p.Nq, p.d) || !grf_make_token_box_map(&m.k, p.k, p.ks, p.B, p.KV, p.Nk, p.d) ||
+        !grf_make_token_box_map(&m.v, p.v, p.vs, p.B, p.KV, p.Nk, p.d)) return 1;
+    return p.d <= 64 ? by_rest<64>(ctx, p, m) : by_rest<128>(ctx, p, m);
 }
