@@ -345,16 +345,19 @@ extern "C" int grf_softmax_attn_backward(grf_ctx* ctx, const grf_softmax_desc* d
 // ------------------------------------------------------------------------------------------------ the bias by itself
 //
 // Both directions are bound by the matrix's bytes.  The rows are written, and read, as one long run of 16-byte pieces per head (rows of
-// any length, so a piece may pass a row's end).  The bucket of a distance comes from a table in shared memory when the last bucket
-// starts before BIAS_NEAR, from a search otherwise.  Gradient: every lane adds into bins of its own in shared memory, a piece whose
-// distances share a bucket with one addition (all but a band around the diagonal: the two far buckets), so that nothing is atomic.
+// any length, so a piece may pass a row's end).  Beyond the distance F at which the last bucket starts there is one value to either side: most
+// pieces lie there whole and take no look-up.  The others look their distances up in shared memory (F < BIAS_NEAR; a search otherwise).
+// Gradient: pieces beyond F are added into two registers, the others into bins that every thread has for itself in shared memory, so nothing is
+// atomic; four pieces are loaded before the first is used.
 namespace {
 
 constexpr int BIAS_NEAR = 2048, BIAS_THREADS = 256;
 
 struct bias_shape {
-    int32_t heads, n_q, n_k, start, n_first, two_sided, near;   // near: distances in the table, 0: none
+    int32_t heads, n_q, n_k, start, n_first, two_sided, near;   // near: whether distances are looked up
     int32_t strips;
+    uint32_t by_n_k;                                            // n / n_k = (t + ((n - t) >> 1)) >> shift with t the upper half of n * by_n_k
+    int32_t shift;                                              // -1: a plane of 2^31 places or more, or n_k = 1: divided as it is
     int32_t first[GRF_MAX_BUCKETS];
     __host__ __device__ int32_t columns() const { return n_first * (1 + two_sided); }
 };
@@ -369,16 +372,41 @@ __device__ __forceinline__ int32_t searched(const bias_shape& s, int32_t n)
     }
     return lo;
 }
-__device__ __forceinline__ int32_t bucket_of(const bias_shape& s, const unsigned char* near, int64_t delta)
+// relative positions are kept within +-2^30
+__device__ __forceinline__ int32_t relative(const bias_shape& s, int32_t i, int32_t j)
 {
-    const int64_t far = s.two_sided ? (delta < 0 ? -delta : delta) : (delta < 0 ? -delta : 0);
-    const int32_t n = (int32_t)(far < INT32_MAX ? far : INT32_MAX);
-    const int32_t y = s.near ? near[min(n, s.near - 1)] : searched(s, n);
+    const int64_t x = (int64_t)j - s.start - i;
+    return (int32_t)(x < -(1 << 30) ? -(1 << 30) : x > (1 << 30) ? (1 << 30) : x);
+}
+__device__ __forceinline__ int32_t bucket_of(const bias_shape& s, const unsigned char* near, int32_t delta)
+{
+    const int32_t n = s.two_sided ? abs(delta) : max(-delta, 0), F = s.first[s.n_first - 1];
+    const int32_t y = s.near ? near[min(n, F)] : searched(s, n);
     return s.two_sided && delta > 0 ? y + s.n_first : y;
 }
 __device__ __forceinline__ void load_near(const bias_shape& s, unsigned char* near)
 {
-    for (int x = threadIdx.x; x < s.near; x += BIAS_THREADS) near[x] = (unsigned char)searched(s, x);
+    if (s.near)
+        for (int x = threadIdx.x; x <= s.first[s.n_first - 1]; x += BIAS_THREADS) near[x] = (unsigned char)searched(s, x);
+}
+// row and column of place e of a plane
+__device__ __forceinline__ void place_of(const bias_shape& s, int64_t e, int32_t& i, int32_t& j)
+{
+    if (s.shift >= 0) {
+        const uint32_t n = (uint32_t)e, t = __umulhi(n, s.by_n_k), q = (t + ((n - t) >> 1)) >> s.shift;
+        i = (int32_t)q;
+        j = (int32_t)(n - q * (uint32_t)s.n_k);
+    } else {
+        i = (int32_t)(e / s.n_k);
+        j = (int32_t)(e - (int64_t)i * s.n_k);
+    }
+}
+// 0: the piece of CH places at (i, j) lies beyond F before the diagonal, 1: behind it (or where one-sided distances are 0), -1: neither
+template <int CH> __device__ __forceinline__ int side_of(const bias_shape& s, int32_t F, int32_t i, int32_t j)
+{
+    if (j + CH > s.n_k) return -1;
+    const int32_t delta = relative(s, i, j);
+    return delta + CH - 1 <= -F ? 0 : delta >= (s.two_sided ? max(F, 1) : 0) ? 1 : -1;
 }
 
 template <typename T>
@@ -387,20 +415,28 @@ __global__ void __launch_bounds__(BIAS_THREADS) relative_rows_kernel(const __gri
     constexpr int CH = 16 / (int)sizeof(T);
     __shared__ unsigned char near[BIAS_NEAR];
     __shared__ T value[2 * GRF_MAX_BUCKETS];
-    const int32_t h = blockIdx.y;
+    const int32_t h = blockIdx.y, F = s.first[s.n_first - 1];
     load_near(s, near);
     for (int x = threadIdx.x; x < s.columns(); x += BIAS_THREADS) value[x] = table[(int64_t)h * s.columns() + x];
     __syncthreads();
+    const T before = value[s.n_first - 1], behind = value[s.two_sided ? 2 * s.n_first - 1 : 0];
     const int64_t plane = (int64_t)s.n_q * s.n_k, from = h * plane, to = from + plane;
     for (int64_t c = from / CH + (int64_t)blockIdx.x * BIAS_THREADS + threadIdx.x; c * CH < to; c += (int64_t)s.strips * BIAS_THREADS) {
         const int64_t e0 = c * CH > from ? c * CH : from, e1 = (c + 1) * CH < to ? (c + 1) * CH : to;
-        int32_t i = (int32_t)((e0 - from) / s.n_k), j = (int32_t)((e0 - from) - (int64_t)i * s.n_k);
+        int32_t i, j;
+        place_of(s, e0 - from, i, j);
+        const int side = side_of<CH>(s, F, i, j);
         __align__(16) T v[CH];
+        if (side >= 0) {
 #pragma unroll
-        for (int e = 0; e < CH; ++e) {
-            if (e0 + e < e1) {
-                v[e] = value[bucket_of(s, near, (int64_t)j - s.start - i)];
-                if (++j == s.n_k) { j = 0; ++i; }
+            for (int e = 0; e < CH; ++e) v[e] = side ? behind : before;
+        } else {
+#pragma unroll
+            for (int e = 0; e < CH; ++e) {
+                if (e0 + e < e1) {
+                    v[e] = value[bucket_of(s, near, relative(s, i, j))];
+                    if (++j == s.n_k) { j = 0; ++i; }
+                }
             }
         }
         if (e1 - e0 == CH) *reinterpret_cast<uint4*>(rows + e0) = *reinterpret_cast<const uint4*>(v);
@@ -414,44 +450,59 @@ __global__ void __launch_bounds__(BIAS_THREADS) relative_rows_kernel(const __gri
 template <typename T>
 __global__ void __launch_bounds__(BIAS_THREADS) relative_sums_kernel(const __grid_constant__ bias_shape s, int32_t batch, const T* __restrict__ drows, float* __restrict__ part)
 {
-    constexpr int CH = 16 / (int)sizeof(T);
+    constexpr int CH = 16 / (int)sizeof(T), AHEAD = 4;
     extern __shared__ float bins[];                             // [column][thread]
     __shared__ unsigned char near[BIAS_NEAR];
-    const int32_t h = blockIdx.y, columns = s.columns(), tid = threadIdx.x;
+    const int32_t h = blockIdx.y, columns = s.columns(), tid = threadIdx.x, F = s.first[s.n_first - 1];
     load_near(s, near);
     for (int x = tid; x < columns * BIAS_THREADS; x += BIAS_THREADS) bins[x] = 0.0f;
     __syncthreads();
     const int64_t plane = (int64_t)s.n_q * s.n_k;
+    float far[2] = {0.0f, 0.0f};
     for (int32_t b = 0; b < batch; ++b) {
-        const int64_t from = ((int64_t)b * s.heads + h) * plane, to = from + plane;
-        for (int64_t c = from / CH + (int64_t)blockIdx.x * BIAS_THREADS + tid; c * CH < to; c += (int64_t)s.strips * BIAS_THREADS) {
-            const int64_t e0 = c * CH > from ? c * CH : from, e1 = (c + 1) * CH < to ? (c + 1) * CH : to;
-            int32_t i = (int32_t)((e0 - from) / s.n_k), j = (int32_t)((e0 - from) - (int64_t)i * s.n_k);
-            if (e1 - e0 == CH) {
-                const uint4 w = *reinterpret_cast<const uint4*>(drows + e0);
-                const T* v = reinterpret_cast<const T*>(&w);
-                const int32_t y0 = bucket_of(s, near, (int64_t)j - s.start - i), y1 = bucket_of(s, near, (int64_t)j + CH - 1 - s.start - i);
-                // (buckets follow each other along a row; a row's other side of the diagonal lies between them only if it has both)
-                if (j + CH <= s.n_k && y0 == y1) {
-                    float sum = 0.0f;
+        const int64_t from = ((int64_t)b * s.heads + h) * plane, to = from + plane, step = (int64_t)s.strips * BIAS_THREADS;
+        for (int64_t c0 = from / CH + (int64_t)blockIdx.x * BIAS_THREADS + tid; c0 * CH < to; c0 += AHEAD * step) {
+            uint4 w[AHEAD];
 #pragma unroll
-                    for (int e = 0; e < CH; ++e) sum += grf_to_float(v[e]);
-                    bins[y0 * BIAS_THREADS + tid] += sum;
-                    continue;
-                }
+            for (int x = 0; x < AHEAD; ++x) {
+                const int64_t c = c0 + x * step;
+                if (c * CH >= from && (c + 1) * CH <= to) w[x] = __ldcs(reinterpret_cast<const uint4*>(drows + c * CH));
+            }
 #pragma unroll
-                for (int e = 0; e < CH; ++e) {
-                    bins[bucket_of(s, near, (int64_t)j - s.start - i) * BIAS_THREADS + tid] += grf_to_float(v[e]);
-                    if (++j == s.n_k) { j = 0; ++i; }
-                }
-            } else {
-                for (int64_t e = e0; e < e1; ++e) {
-                    bins[bucket_of(s, near, (int64_t)j - s.start - i) * BIAS_THREADS + tid] += grf_to_float(drows[e]);
-                    if (++j == s.n_k) { j = 0; ++i; }
+            for (int x = 0; x < AHEAD; ++x) {
+                const int64_t c = c0 + x * step;
+                if (c * CH >= to) continue;
+                int32_t i, j;
+                if (c * CH >= from && (c + 1) * CH <= to) {
+                    place_of(s, c * CH - from, i, j);
+                    const T* v = reinterpret_cast<const T*>(&w[x]);
+                    const int side = side_of<CH>(s, F, i, j);
+                    if (side >= 0) {
+                        float sum = 0.0f;
+#pragma unroll
+                        for (int e = 0; e < CH; ++e) sum += grf_to_float(v[e]);
+                        far[0] += side == 0 ? sum : 0.0f;
+                        far[1] += side == 1 ? sum : 0.0f;
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < CH; ++e) {
+                            bins[bucket_of(s, near, relative(s, i, j)) * BIAS_THREADS + tid] += grf_to_float(v[e]);
+                            if (++j == s.n_k) { j = 0; ++i; }
+                        }
+                    }
+                } else {
+                    const int64_t e0 = c * CH > from ? c * CH : from, e1 = (c + 1) * CH < to ? (c + 1) * CH : to;
+                    place_of(s, e0 - from, i, j);
+                    for (int64_t e = e0; e < e1; ++e) {
+                        bins[bucket_of(s, near, relative(s, i, j)) * BIAS_THREADS + tid] += grf_to_float(drows[e]);
+                        if (++j == s.n_k) { j = 0; ++i; }
+                    }
                 }
             }
         }
     }
+    bins[(s.n_first - 1) * BIAS_THREADS + tid] += far[0];
+    bins[(s.two_sided ? 2 * s.n_first - 1 : 0) * BIAS_THREADS + tid] += far[1];
     __syncthreads();
     const int lane = tid & 31, warp = tid >> 5;
     for (int y = warp; y < columns; y += BIAS_THREADS / 32) {
@@ -472,7 +523,14 @@ int read_bias(bias_shape* s, int32_t heads, int32_t n_q, int32_t n_k, int32_t q_
     memset(s, 0, sizeof *s);
     s->heads = heads; s->n_q = n_q; s->n_k = n_k; s->start = q_start; s->n_first = n_buckets; s->two_sided = two_sided;
     memcpy(s->first, first, sizeof(int32_t) * n_buckets);
-    s->near = first[n_buckets - 1] < BIAS_NEAR ? first[n_buckets - 1] + 1 : 0;
+    s->near = first[n_buckets - 1] < BIAS_NEAR;
+    s->shift = -1;
+    if (n_k > 1 && (int64_t)n_q * n_k < ((int64_t)1 << 31)) {
+        int32_t bits = 1;                                       // 2^(bits - 1) < n_k <= 2^bits
+        while (((int64_t)1 << bits) < n_k) ++bits;
+        s->by_n_k = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << bits) - n_k)) / n_k + 1);
+        s->shift = bits - 1;
+    }
     return GRF_OK;
 }
 

@@ -71,6 +71,22 @@ __device__ __forceinline__ float grf_bias2(const grf_softmax_params& p, int32_t 
     return fabsf(b) <= 3.4028235e38f ? fminf(fmaxf(b2, -GRF_BIAS_MOST), GRF_BIAS_MOST) : b2;
 }
 
+// bins[b] += v of every lane, by one converged warp and in a fixed order: equal b lie in neighbouring lanes (buckets follow each other along
+// diagonals), so a scan within runs leaves a run's sum in its last lane.  b < 0: nothing to add.
+__device__ __forceinline__ void grf_add_runs(float* bins, int32_t b, float v)
+{
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const float u = __shfl_up_sync(0xffffffffu, v, o);
+        const int32_t c = __shfl_up_sync(0xffffffffu, b, o);
+        if (lane >= o && c == b) v += u;
+    }
+    const int32_t next = __shfl_down_sync(0xffffffffu, b, 1);
+    if (b >= 0 && (lane == 31 || next != b)) bins[b] += v;
+    __syncwarp();
+}
+
 // What a sequence's queries see.
 struct grf_sight {
     int32_t start, len, prefix, order;      // prefix: keys before it are seen whatever the order

@@ -304,7 +304,7 @@ __global__ void __launch_bounds__(THREADS) softmax_alu_dq_kernel(const __grid_co
     using A = Alu<DP>;
     extern __shared__ float smem[];
     float *qs = smem, *gs = qs + A::TILE, *ks = gs + A::TILE, *vs = ks + A::TILE, *xt = vs + A::TILE, *st = xt + BT * PS;
-    __shared__ float lut[2 * BT], diagonal[2 * BT];
+    __shared__ float lut[2 * BT], bins[4][2 * GRF_MAX_BUCKETS];   // sums by bucket, of diagonals 32 w .. 32 w + 31 of each tile
     const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
     const int32_t b = blockIdx.y / p.H, h = blockIdx.y % p.H, i0 = (gridDim.x - 1 - blockIdx.x) * BT, kvh = h / p.group;
     const grf_sight sight(p, b);
@@ -322,7 +322,7 @@ __global__ void __launch_bounds__(THREADS) softmax_alu_dq_kernel(const __grid_co
 #pragma unroll
         for (int c = 0; c < DP / 16; ++c) dq[r][c] = 0.0f;
     }
-    float table_sum = 0.0f;                                     // bucket tid's
+    for (int x = tid; x < 4 * 2 * GRF_MAX_BUCKETS; x += THREADS) (&bins[0][0])[x] = 0.0f;
     const int32_t end = sight.end(i1);
     for (int32_t j0 = 0; j0 < end; j0 += BT) {
         const int what = sight.tile(i0, i1, j0, j0 + BT, qr, sight.docs ? __ldg(p.k_range + (int64_t)b * kblocks + j0 / BT) : all_docs());
@@ -350,21 +350,15 @@ __global__ void __launch_bounds__(THREADS) softmax_alu_dq_kernel(const __grid_co
         __syncthreads();
         accumulate<DP>(dq, xt, ks, ty, tx);
         if (p.dtable_part) {
-            if (tid < 2 * BT - 1) {
+            if (tid < 2 * BT) {
                 float sum = 0.0f;
                 const int delta = tid - (BT - 1);               // j - i
                 for (int i = max(0, -delta); i < min(BT, BT - delta); ++i) sum += st[i * PS + i + delta];
-                diagonal[tid] = sum;
-            }
-            __syncthreads();
-            if (tid < columns) {
-                float sum = 0.0f;
-                for (int x = 0; x < 2 * BT - 1; ++x)
-                    if (grf_bucket(p, j0 - sight.position(i0) + x - (BT - 1)) == tid) sum += diagonal[x];
-                table_sum += sum;
+                grf_add_runs(bins[tid >> 5], tid < 2 * BT - 1 ? grf_bucket(p, j0 - sight.position(i0) + delta) : -1, sum);
             }
         }
     }
+    __syncthreads();
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         const int32_t i = i0 + 4 * ty + r;
@@ -373,7 +367,7 @@ __global__ void __launch_bounds__(THREADS) softmax_alu_dq_kernel(const __grid_co
         for (int c = 0; c < DP / 16; ++c) dq[r][c] *= p.scale;
         store_row<T, DP>(at_head_w<T>(p.dq, p.dqs, b, h) + (int64_t)i * p.dqs[2], dq[r], tx, p.d);
     }
-    if (p.dtable_part && tid < columns) p.dtable_part[((int64_t)blockIdx.y * gridDim.x + i0 / BT) * columns + tid] = table_sum;
+    if (p.dtable_part && tid < columns) p.dtable_part[((int64_t)blockIdx.y * gridDim.x + i0 / BT) * columns + tid] = (bins[0][tid] + bins[1][tid]) + (bins[2][tid] + bins[3][tid]);
 }
 
 template <typename T, int DP>

@@ -353,6 +353,7 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 if (lane == 0) mbar_arrive(s_read(g));
             }
             float top = -CUDART_INF_F;
+            const float ahead = (float)(j0 - pos);              // (exact, as are its sums: below 2^24; beyond, off by half a step as the distance itself)
             const uint64_t to22 = pack2(to2, to2), bias22 = pack2(bias2, bias2);
 #pragma unroll
             for (int y = 0; y < 8; ++y)
@@ -365,8 +366,8 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                         x1 = cap2 * tanh_any(__uint_as_float(sv[y][e + 1]) * by_cap) + bias2;
                     } else unpack2(fma2(pack2(sv[y][e], sv[y][e + 1]), to22, bias22), x0, x1);
                     if (BIAS == GRF_BIAS_SLOPES) {
-                        x0 = fmaf(-slope2, fabsf((float)(j0 - pos + col)), x0);
-                        x1 = fmaf(-slope2, fabsf((float)(j0 - pos + col + 1)), x1);
+                        x0 = fmaf(-slope2, fabsf(ahead + (float)col), x0);
+                        x1 = fmaf(-slope2, fabsf(ahead + (float)(col + 1)), x1);
                     }
                     if (BIAS == GRF_BIAS_BUCKETS) {
                         if (diagonals) { x0 += mine[col]; x1 += mine[col + 1]; }

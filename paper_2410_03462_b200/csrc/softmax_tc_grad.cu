@@ -80,7 +80,6 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     __shared__ float lut[LUTS ? 2 * 256 : 1];
     __shared__ float bins[LUTS ? WORKERS * 2 * GRF_MAX_BUCKETS : 1];
     __shared__ float diag[LUTS ? WORKERS * 96 : 1];
-    __shared__ unsigned char diag_bucket[LUTS ? WORKERS * 96 : 1];
     const int tid = threadIdx.x, lane = tid & 31, warp = uniform(tid >> 5);
     const uint32_t smem = (smem_u32(smem_dyn) + 1023u) & ~1023u;
     uint32_t* bits = reinterpret_cast<uint32_t*>(smem_dyn + (smem - smem_u32(smem_dyn)) + Sh::TILE * (2 + 2 * NS));
@@ -239,7 +238,6 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const float to2 = p.scale * GRF_LOG2E, by_cap = CAP ? p.scale / p.cap : 0.0f, cap2 = p.cap * GRF_LOG2E;
         const float slope2 = BIAS == GRF_BIAS_SLOPES ? p.slopes[h] * GRF_LOG2E : 0.0f;
-        const int32_t columns = grf_softmax_columns(p);
         const bool sums = LUTS && p.dtable_part != nullptr;
         float* my_bins = bins + warp * 2 * GRF_MAX_BUCKETS;
         float far_sum = 0.0f;                                   // of dS in tiles of one bucket, until the bucket changes
@@ -276,6 +274,7 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             }
             if (!(ok = wait(s_full0 + 8 * (n & 1), (uint32_t)(n >> 1) & 1u))) break;
             fence_after_sync();
+            const float ahead = (float)(j0 + c0 - pos);
             float x[64], dcap[CAP ? 64 : 1];
             {
                 uint32_t sv[4][16];
@@ -291,7 +290,7 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                         dcap[e] = fmaf(-th, th, 1.0f);
                         s = fmaf(cap2, th, bias2);
                     } else s = fmaf(raw, to2, bias2);
-                    if (BIAS == GRF_BIAS_SLOPES) s = fmaf(-slope2, fabsf((float)(j0 + c0 - pos + e)), s);
+                    if (BIAS == GRF_BIAS_SLOPES) s = fmaf(-slope2, fabsf(ahead + (float)e), s);
                     if (LUTS) { if (diagonals) s += mine[e]; }
                     x[e] = ex2(min_nan(s - lse2, 0.0f));
                 }
@@ -349,17 +348,11 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                         if (lane == 31) at[e] = a;
                     }
                     if (lane < 31) at[64 + 30 - lane] = a;      // diagonal 63 - lane; place x holds diagonal x - 31
+                    __syncwarp();
 #pragma unroll
                     for (int z = 0; z < 3; ++z) {
                         const int d = lane + 32 * z;
-                        if (d < 95) diag_bucket[warp * 96 + d] = (unsigned char)grf_bucket(p, j0 + c0 + d - 31 - sight.position(i0 + (warp & 3) * 32));
-                    }
-                    __syncwarp();
-                    for (int y = lane; y < columns; y += 32) {
-                        float sum = 0.0f;
-                        for (int d = 0; d < 95; ++d)
-                            if (diag_bucket[warp * 96 + d] == y) sum += at[d];
-                        my_bins[y] += sum;
+                        grf_add_runs(my_bins, d < 95 ? grf_bucket(p, j0 + c0 + d - 31 - sight.position(i0 + (warp & 3) * 32)) : -1, d < 95 ? at[d] : 0.0f);
                     }
                     __syncwarp();
                 }
@@ -620,6 +613,7 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                 }
                 if (!(ok = wait(ready(s), (uint32_t)(n / NS) & 1u) && wait(s_full, (uint32_t)n & 1u))) break;
                 fence_after_sync();
+                const float ahead = (float)(j - pos0 - c0);
                 float x[64], dcap[CAP ? 64 : 1];
                 {
                     uint32_t sv[4][16];
@@ -640,7 +634,7 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                                 dcap[e] = fmaf(-th, th, 1.0f);
                                 sc = fmaf(cap2, th, bias2);
                             } else sc = fmaf(raw, to2, bias2);
-                            if (BIAS == GRF_BIAS_SLOPES) sc = fmaf(-slope2, fabsf((float)(j - pos0 - c0 - e)), sc);
+                            if (BIAS == GRF_BIAS_SLOPES) sc = fmaf(-slope2, fabsf(ahead - (float)e), sc);
                             if (LUTS) { if (diagonals) sc += mine[-e]; }
                             x[e] = ex2(min_nan(sc - lv[z], 0.0f));
                         }
