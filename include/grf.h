@@ -306,7 +306,7 @@ typedef struct grf_softmax_desc {
     int32_t order;                     /* GRF_ORDER_*                                                                        */
     int32_t bias;                      /* GRF_BIAS_*                                                                         */
     int32_t n_buckets, two_sided;      /* BUCKETS: 1 .. GRF_MAX_BUCKETS                                                      */
-    int32_t first[GRF_MAX_BUCKETS];    /* smallest distance of each bucket: first[0] = 0, ascending                          */
+    int32_t first[GRF_MAX_BUCKETS];    /* smallest distance of each bucket: first[0] = 0, ascending, at most 2^29             */
     const float* slopes;               /* DEVICE [heads]                                                                     */
     const void* table;                 /* DEVICE [heads][n_buckets * (1 + two_sided)], dtype                                 */
     const int32_t* k_len;              /* DEVICE [batch] or NULL: n_k each; values are clipped to 0 .. n_k                   */

@@ -91,7 +91,7 @@ int first_ok(int32_t n, const int32_t* first)
     if (n < 1 || n > GRF_MAX_BUCKETS || !first || first[0] != 0) return GRF_ERR_INVALID;
     for (int32_t y = 1; y < n; ++y)
         if (first[y] <= first[y - 1]) return GRF_ERR_INVALID;
-    return GRF_OK;
+    return first[n - 1] <= (1 << 29) ? GRF_OK : GRF_ERR_INVALID;   // relative positions are kept within +-2^30
 }
 
 // Strides of one array (a triple of zeros: contiguous), checked; zero where the extent is 1, so that it is never used.
@@ -357,152 +357,160 @@ struct bias_shape {
     int32_t heads, n_q, n_k, start, n_first, two_sided, near;   // near: whether distances are looked up
     int32_t strips;
     uint32_t by_n_k;                                            // n / n_k = (t + ((n - t) >> 1)) >> shift with t the upper half of n * by_n_k
-    int32_t shift;                                              // -1: a plane of 2^31 places or more, or n_k = 1: divided as it is
+    int32_t shift;                                              // -1: n_k = 1 or a plane that 64 bits count: divided as it is
     int32_t first[GRF_MAX_BUCKETS];
     __host__ __device__ int32_t columns() const { return n_first * (1 + two_sided); }
 };
 
-__device__ __forceinline__ int32_t searched(const bias_shape& s, int32_t n)
+// column of the table for a relative position (|delta| < 2^31: starts are kept within +-2^30)
+__device__ __forceinline__ int32_t column_of(const bias_shape& s, int32_t delta)
 {
+    const int32_t n = s.two_sided ? abs(delta) : max(-delta, 0);
     int lo = 0, hi = s.n_first;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (s.first[mid] <= n) lo = mid;
         else hi = mid;
     }
-    return lo;
+    return s.two_sided && delta > 0 ? lo + s.n_first : lo;
 }
-// relative positions are kept within +-2^30
-__device__ __forceinline__ int32_t relative(const bias_shape& s, int32_t i, int32_t j)
-{
-    const int64_t x = (int64_t)j - s.start - i;
-    return (int32_t)(x < -(1 << 30) ? -(1 << 30) : x > (1 << 30) ? (1 << 30) : x);
-}
-__device__ __forceinline__ int32_t bucket_of(const bias_shape& s, const unsigned char* near, int32_t delta)
-{
-    const int32_t n = s.two_sided ? abs(delta) : max(-delta, 0), F = s.first[s.n_first - 1];
-    const int32_t y = s.near ? near[min(n, F)] : searched(s, n);
-    return s.two_sided && delta > 0 ? y + s.n_first : y;
-}
-__device__ __forceinline__ void load_near(const bias_shape& s, unsigned char* near)
+// columns of the distances -F .. F, if they are looked up
+__device__ __forceinline__ void load_near(const bias_shape& s, int32_t F, unsigned char* near)
 {
     if (s.near)
-        for (int x = threadIdx.x; x <= s.first[s.n_first - 1]; x += BIAS_THREADS) near[x] = (unsigned char)searched(s, x);
+        for (int x = threadIdx.x; x <= 2 * F; x += BIAS_THREADS) near[x] = (unsigned char)column_of(s, x - F);
+}
+__device__ __forceinline__ int32_t column_at(const bias_shape& s, int32_t F, const unsigned char* near, int32_t delta)
+{
+    return s.near ? near[min(max(delta + F, 0), 2 * F)] : column_of(s, delta);
 }
 // row and column of place e of a plane
-__device__ __forceinline__ void place_of(const bias_shape& s, int64_t e, int32_t& i, int32_t& j)
+template <typename I> __device__ __forceinline__ void place_of(const bias_shape& s, I e, int32_t& i, int32_t& j)
 {
-    if (s.shift >= 0) {
+    if (sizeof(I) == 4 && s.shift >= 0) {
         const uint32_t n = (uint32_t)e, t = __umulhi(n, s.by_n_k), q = (t + ((n - t) >> 1)) >> s.shift;
         i = (int32_t)q;
         j = (int32_t)(n - q * (uint32_t)s.n_k);
     } else {
         i = (int32_t)(e / s.n_k);
-        j = (int32_t)(e - (int64_t)i * s.n_k);
+        j = (int32_t)(e - (I)i * s.n_k);
     }
 }
-// 0: the piece of CH places at (i, j) lies beyond F before the diagonal, 1: behind it (or where one-sided distances are 0), -1: neither
-template <int CH> __device__ __forceinline__ int side_of(const bias_shape& s, int32_t F, int32_t i, int32_t j)
-{
-    if (j + CH > s.n_k) return -1;
-    const int32_t delta = relative(s, i, j);
-    return delta + CH - 1 <= -F ? 0 : delta >= (s.two_sided ? max(F, 1) : 0) ? 1 : -1;
-}
+// A plane as pieces of 16 bytes: piece x holds the plane's places x CH - head .. + CH - 1, the first and the last one maybe not whole.
+template <typename T, typename I> struct plane_pieces {
+    static constexpr int CH = 16 / (int)sizeof(T);
+    I places, count;
+    int head;
+    __device__ __forceinline__ plane_pieces(const bias_shape& s, int64_t plane)
+    {
+        const int64_t all = (int64_t)s.n_q * s.n_k;
+        places = (I)all;
+        head = (int)(plane * all % CH);
+        count = (I)((head + all + CH - 1) / CH);
+    }
+    __device__ __forceinline__ I first(I x) const { return x * CH - head; }
+    __device__ __forceinline__ bool whole(I x) const { return first(x) >= 0 && first(x) + CH <= places; }
+};
 
-template <typename T>
+template <typename T, typename I>
 __global__ void __launch_bounds__(BIAS_THREADS) relative_rows_kernel(const __grid_constant__ bias_shape s, const T* __restrict__ table, T* __restrict__ rows)
 {
-    constexpr int CH = 16 / (int)sizeof(T);
-    __shared__ unsigned char near[BIAS_NEAR];
+    using P = plane_pieces<T, I>;
+    __shared__ unsigned char near[2 * BIAS_NEAR];
     __shared__ T value[2 * GRF_MAX_BUCKETS];
-    const int32_t h = blockIdx.y, F = s.first[s.n_first - 1];
-    load_near(s, near);
+    const int32_t h = blockIdx.y, F = s.first[s.n_first - 1], right = s.two_sided ? max(F, 1) : 0;
+    load_near(s, F, near);
     for (int x = threadIdx.x; x < s.columns(); x += BIAS_THREADS) value[x] = table[(int64_t)h * s.columns() + x];
     __syncthreads();
     const T before = value[s.n_first - 1], behind = value[s.two_sided ? 2 * s.n_first - 1 : 0];
-    const int64_t plane = (int64_t)s.n_q * s.n_k, from = h * plane, to = from + plane;
-    for (int64_t c = from / CH + (int64_t)blockIdx.x * BIAS_THREADS + threadIdx.x; c * CH < to; c += (int64_t)s.strips * BIAS_THREADS) {
-        const int64_t e0 = c * CH > from ? c * CH : from, e1 = (c + 1) * CH < to ? (c + 1) * CH : to;
+    const P at(s, h);
+    T* base = rows + (int64_t)h * s.n_q * s.n_k - at.head;
+    for (I x = (I)blockIdx.x * BIAS_THREADS + threadIdx.x; x < at.count; x += (I)s.strips * BIAS_THREADS) {
         int32_t i, j;
-        place_of(s, e0 - from, i, j);
-        const int side = side_of<CH>(s, F, i, j);
-        __align__(16) T v[CH];
-        if (side >= 0) {
+        T v[P::CH];
+        if (at.whole(x)) {
+            place_of(s, at.first(x), i, j);
+            const int32_t delta = j - s.start - i;
+            if (j + P::CH <= s.n_k && (delta + P::CH - 1 <= -F || delta >= right)) {
 #pragma unroll
-            for (int e = 0; e < CH; ++e) v[e] = side ? behind : before;
-        } else {
+                for (int e = 0; e < P::CH; ++e) v[e] = delta < 0 ? before : behind;
+            } else {
 #pragma unroll
-            for (int e = 0; e < CH; ++e) {
-                if (e0 + e < e1) {
-                    v[e] = value[bucket_of(s, near, relative(s, i, j))];
+                for (int e = 0; e < P::CH; ++e) {
+                    v[e] = value[column_at(s, F, near, j - s.start - i)];
                     if (++j == s.n_k) { j = 0; ++i; }
                 }
             }
+            uint4 w;
+            memcpy(&w, v, 16);
+            *reinterpret_cast<uint4*>(base + (int64_t)x * P::CH) = w;
+        } else {
+            for (I e = max(at.first(x), (I)0); e < min(at.first(x) + P::CH, at.places); ++e) {
+                place_of(s, e, i, j);
+                base[at.head + (int64_t)e] = value[column_at(s, F, near, j - s.start - i)];
+            }
         }
-        if (e1 - e0 == CH) *reinterpret_cast<uint4*>(rows + e0) = *reinterpret_cast<const uint4*>(v);
-        else
-#pragma unroll
-            for (int e = 0; e < CH; ++e)
-                if (e0 + e < e1) rows[e0 + e] = v[e];
     }
 }
 
-template <typename T>
+template <typename T, typename I>
 __global__ void __launch_bounds__(BIAS_THREADS) relative_sums_kernel(const __grid_constant__ bias_shape s, int32_t batch, const T* __restrict__ drows, float* __restrict__ part)
 {
-    constexpr int CH = 16 / (int)sizeof(T), AHEAD = 4;
+    using P = plane_pieces<T, I>;
+    constexpr int AHEAD = 4;
     extern __shared__ float bins[];                             // [column][thread]
-    __shared__ unsigned char near[BIAS_NEAR];
-    const int32_t h = blockIdx.y, columns = s.columns(), tid = threadIdx.x, F = s.first[s.n_first - 1];
-    load_near(s, near);
+    __shared__ unsigned char near[2 * BIAS_NEAR];
+    const int32_t h = blockIdx.y, columns = s.columns(), tid = threadIdx.x, F = s.first[s.n_first - 1], right = s.two_sided ? max(F, 1) : 0;
+    load_near(s, F, near);
     for (int x = tid; x < columns * BIAS_THREADS; x += BIAS_THREADS) bins[x] = 0.0f;
     __syncthreads();
-    const int64_t plane = (int64_t)s.n_q * s.n_k;
+    float* mine = bins + tid;
     float far[2] = {0.0f, 0.0f};
     for (int32_t b = 0; b < batch; ++b) {
-        const int64_t from = ((int64_t)b * s.heads + h) * plane, to = from + plane, step = (int64_t)s.strips * BIAS_THREADS;
-        for (int64_t c0 = from / CH + (int64_t)blockIdx.x * BIAS_THREADS + tid; c0 * CH < to; c0 += AHEAD * step) {
+        const int64_t plane = (int64_t)b * s.heads + h;
+        const P at(s, plane);
+        const T* base = drows + plane * s.n_q * s.n_k - at.head;
+        const I step = (I)s.strips * BIAS_THREADS;
+        for (I x0 = (I)blockIdx.x * BIAS_THREADS + tid; x0 < at.count; x0 += AHEAD * step) {
             uint4 w[AHEAD];
 #pragma unroll
-            for (int x = 0; x < AHEAD; ++x) {
-                const int64_t c = c0 + x * step;
-                if (c * CH >= from && (c + 1) * CH <= to) w[x] = __ldcs(reinterpret_cast<const uint4*>(drows + c * CH));
+            for (int y = 0; y < AHEAD; ++y) {
+                const I x = x0 + y * step;
+                if (x < at.count && at.whole(x)) w[y] = __ldcs(reinterpret_cast<const uint4*>(base + (int64_t)x * P::CH));
             }
 #pragma unroll
-            for (int x = 0; x < AHEAD; ++x) {
-                const int64_t c = c0 + x * step;
-                if (c * CH >= to) continue;
+            for (int y = 0; y < AHEAD; ++y) {
+                const I x = x0 + y * step;
+                if (x >= at.count) break;
                 int32_t i, j;
-                if (c * CH >= from && (c + 1) * CH <= to) {
-                    place_of(s, c * CH - from, i, j);
-                    const T* v = reinterpret_cast<const T*>(&w[x]);
-                    const int side = side_of<CH>(s, F, i, j);
-                    if (side >= 0) {
+                if (at.whole(x)) {
+                    place_of(s, at.first(x), i, j);
+                    const T* v = reinterpret_cast<const T*>(&w[y]);
+                    const int32_t delta = j - s.start - i;
+                    if (j + P::CH <= s.n_k && (delta + P::CH - 1 <= -F || delta >= right)) {
                         float sum = 0.0f;
 #pragma unroll
-                        for (int e = 0; e < CH; ++e) sum += grf_to_float(v[e]);
-                        far[0] += side == 0 ? sum : 0.0f;
-                        far[1] += side == 1 ? sum : 0.0f;
+                        for (int e = 0; e < P::CH; ++e) sum += grf_to_float(v[e]);
+                        if (delta < 0) far[0] += sum;
+                        else far[1] += sum;
                     } else {
 #pragma unroll
-                        for (int e = 0; e < CH; ++e) {
-                            bins[bucket_of(s, near, relative(s, i, j)) * BIAS_THREADS + tid] += grf_to_float(v[e]);
+                        for (int e = 0; e < P::CH; ++e) {
+                            mine[column_at(s, F, near, j - s.start - i) * BIAS_THREADS] += grf_to_float(v[e]);
                             if (++j == s.n_k) { j = 0; ++i; }
                         }
                     }
                 } else {
-                    const int64_t e0 = c * CH > from ? c * CH : from, e1 = (c + 1) * CH < to ? (c + 1) * CH : to;
-                    place_of(s, e0 - from, i, j);
-                    for (int64_t e = e0; e < e1; ++e) {
-                        bins[bucket_of(s, near, relative(s, i, j)) * BIAS_THREADS + tid] += grf_to_float(drows[e]);
-                        if (++j == s.n_k) { j = 0; ++i; }
+                    for (I e = max(at.first(x), (I)0); e < min(at.first(x) + P::CH, at.places); ++e) {
+                        place_of(s, e, i, j);
+                        mine[column_at(s, F, near, j - s.start - i) * BIAS_THREADS] += grf_to_float(base[at.head + (int64_t)e]);
                     }
                 }
             }
         }
     }
-    bins[(s.n_first - 1) * BIAS_THREADS + tid] += far[0];
-    bins[(s.two_sided ? 2 * s.n_first - 1 : 0) * BIAS_THREADS + tid] += far[1];
+    mine[(s.n_first - 1) * BIAS_THREADS] += far[0];
+    mine[(s.two_sided ? 2 * s.n_first - 1 : 0) * BIAS_THREADS] += far[1];
     __syncthreads();
     const int lane = tid & 31, warp = tid >> 5;
     for (int y = warp; y < columns; y += BIAS_THREADS / 32) {
@@ -515,17 +523,22 @@ __global__ void __launch_bounds__(BIAS_THREADS) relative_sums_kernel(const __gri
     }
 }
 
+// places that 32 bits do not count (and the threads' strides behind the last one)
+bool big_plane(const bias_shape& s) { return (int64_t)s.n_q * s.n_k > ((int64_t)1 << 30); }
+
 int read_bias(bias_shape* s, int32_t heads, int32_t n_q, int32_t n_k, int32_t q_start, int32_t n_buckets, int two_sided, const int32_t* first, int dtype)
 {
     if (heads <= 0 || n_q <= 0 || n_k <= 0 || (two_sided & ~1) != 0 || (dtype != GRF_DTYPE_F32 && dtype != GRF_DTYPE_BF16)) return GRF_ERR_INVALID;
     GRF_TRY(first_ok(n_buckets, first));
     if (n_q > GRF_MAX_TOKENS || n_k > GRF_MAX_TOKENS || heads > 65535) return GRF_ERR_TOO_LARGE;
     memset(s, 0, sizeof *s);
-    s->heads = heads; s->n_q = n_q; s->n_k = n_k; s->start = q_start; s->n_first = n_buckets; s->two_sided = two_sided;
+    s->heads = heads; s->n_q = n_q; s->n_k = n_k;
+    s->start = q_start < -(1 << 30) ? -(1 << 30) : q_start > (1 << 30) ? 1 << 30 : q_start;      // (no bucket starts beyond 2^29)
+    s->n_first = n_buckets; s->two_sided = two_sided;
     memcpy(s->first, first, sizeof(int32_t) * n_buckets);
     s->near = first[n_buckets - 1] < BIAS_NEAR;
     s->shift = -1;
-    if (n_k > 1 && (int64_t)n_q * n_k < ((int64_t)1 << 31)) {
+    if (n_k > 1 && !big_plane(*s)) {
         int32_t bits = 1;                                       // 2^(bits - 1) < n_k <= 2^bits
         while (((int64_t)1 << bits) < n_k) ++bits;
         s->by_n_k = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << bits) - n_k)) / n_k + 1);
@@ -546,15 +559,17 @@ constexpr int32_t ROW_CTAS = 1184, SUM_CTAS = 444;
 template <typename T> int bias_rows(grf_ctx* ctx, const bias_shape& s, const void* table, void* rows)
 {
     grf_softmax_scope scope(ctx, "grf:relative_rows");
-    relative_rows_kernel<T><<<dim3(s.strips, s.heads), BIAS_THREADS, 0, ctx->stream>>>(s, (const T*)table, (T*)rows);
+    const auto kernel = big_plane(s) ? relative_rows_kernel<T, int64_t> : relative_rows_kernel<T, int32_t>;
+    kernel<<<dim3(s.strips, s.heads), BIAS_THREADS, 0, ctx->stream>>>(s, (const T*)table, (T*)rows);
     return cudaGetLastError() == cudaSuccess ? GRF_OK : GRF_ERR_CUDA;
 }
 template <typename T> int bias_sums(grf_ctx* ctx, const bias_shape& s, int32_t batch, const void* drows, void* dtable, float* part)
 {
     const size_t smem = sizeof(float) * (size_t)s.columns() * BIAS_THREADS;
-    GRF_CUDA_TRY(cudaFuncSetAttribute(relative_sums_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    const auto kernel = big_plane(s) ? relative_sums_kernel<T, int64_t> : relative_sums_kernel<T, int32_t>;
+    GRF_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     grf_softmax_scope scope(ctx, "grf:relative_sums", 2);
-    relative_sums_kernel<T><<<dim3(s.strips, s.heads), BIAS_THREADS, smem, ctx->stream>>>(s, batch, (const T*)drows, part);
+    kernel<<<dim3(s.strips, s.heads), BIAS_THREADS, smem, ctx->stream>>>(s, batch, (const T*)drows, part);
     bucket_sums_kernel<T><<<dim3(s.columns(), s.heads), 256, 0, ctx->stream>>>(part, (T*)dtable, 1, s.heads, s.strips, s.columns());
     return cudaGetLastError() == cudaSuccess ? GRF_OK : GRF_ERR_CUDA;
 }

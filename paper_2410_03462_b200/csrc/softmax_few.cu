@@ -332,11 +332,12 @@ __global__ void __launch_bounds__(THREADS) softmax_few_bf16_kernel(const __grid_
     join<__nv_bfloat16, ROWS, DP>(sh, p, f, b, kvh, r0);
 }
 
-// fp32: thread (g, t) holds dimensions 16 c + 4 t .. + 3 of key g of a tile of eight.
+// fp32: thread (g, t) holds dimensions 16 c + 4 t .. + 3 of key g of a tile of eight.  Every g has running maxima and sums of its own, so nothing
+// is exchanged but a score's four parts; U tiles at a time, whose chains overlap.
 template <int DG, int ROWS>
 __global__ void __launch_bounds__(THREADS) softmax_few_f32_kernel(const __grid_constant__ grf_softmax_params p, const few_shape f)
 {
-    constexpr int DP = 32 * DG, NC = 2 * DG;
+    constexpr int DP = 32 * DG, NC = 2 * DG, U = DG <= 2 ? 2 : 1;
     extern __shared__ __align__(16) unsigned char smem[];
     FewShared<ROWS, DP>& sh = *reinterpret_cast<FewShared<ROWS, DP>*>(smem);
     __shared__ float4 q[ROWS][DP / 4];
@@ -350,17 +351,20 @@ __global__ void __launch_bounds__(THREADS) softmax_few_f32_kernel(const __grid_c
     const int32_t t0 = (int32_t)((int64_t)tiles * split / f.splits), t1 = (int32_t)((int64_t)tiles * (split + 1) / f.splits);
     const int32_t whole = sight.docs ? 0 : sight.order == GRF_ORDER_FULL ? sight.len : min(sight.len, max(sight.position(0) + 1, sight.prefix));
 
-    float4 kr[NC], vr[NC];
-    auto load = [&](float4 (&x)[NC], const float* base, int64_t stride, int32_t tile) {
-        const int32_t j = tile * 8 + g;
+    float4 kr[U][NC], vr[U][NC];
+    auto load = [&](float4 (&x)[U][NC], const float* base, int64_t stride, int32_t tile) {
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const uint4 w = tile < t1 && j < end && 16 * c + 4 * t < p.d ? load16(base + (int64_t)j * stride + 16 * c) : make_uint4(0, 0, 0, 0);
-            x[c] = make_float4(__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w));
+        for (int u = 0; u < U; ++u) {
+            const int32_t j = (tile + u) * 8 + g;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const uint4 w = tile + u < t1 && j < end && 16 * c + 4 * t < p.d ? load16(base + (int64_t)j * stride + 16 * c) : make_uint4(0, 0, 0, 0);
+                x[u][c] = make_float4(__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w));
+            }
         }
     };
-    load(kr, K, p.ks[2], t0 + warp);
-    load(vr, V, p.vs[2], t0 + warp);
+    load(kr, K, p.ks[2], t0 + warp * U);
+    load(vr, V, p.vs[2], t0 + warp * U);
     for (int x = threadIdx.x; x < ROWS * (DP / 4); x += THREADS) {
         const int r = x / (DP / 4), c = x % (DP / 4);
         few_row w;
@@ -370,11 +374,12 @@ __global__ void __launch_bounds__(THREADS) softmax_few_f32_kernel(const __grid_c
     }
     __syncthreads();
     few_row row[ROWS];
-    float m[ROWS], l[ROWS];
+    float m[ROWS], l[ROWS], slope2[ROWS];
     float4 o[ROWS][NC];
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
         row[r].set(p, sight, qdoc, kvh, r0 + r, f.rows);
+        slope2[r] = p.bias == GRF_BIAS_SLOPES ? -p.slopes[row[r].h] * GRF_LOG2E : 0.0f;
         m[r] = -CUDART_INF_F;
         l[r] = 0.0f;
 #pragma unroll
@@ -384,72 +389,107 @@ __global__ void __launch_bounds__(THREADS) softmax_few_f32_kernel(const __grid_c
     auto clean = [&](float& x) {
         if (!(fabsf(x) <= 3.4028235e38f)) { x = 0.0f; bad = true; }
     };
-    for (int32_t tile = t0 + warp; tile < t1; tile += WARPS) {
-        const int32_t j = tile * 8 + g;
-        const bool partial = tile * 8 + 8 > whole;
-        float s[ROWS];
+    for (int32_t tile = t0 + warp * U; tile < t1; tile += WARPS * U) {
+        float x[U][ROWS];
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
-            s[r] = 0.0f;
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                const float4 y = q[r][4 * c + t];
-                s[r] = fmaf(kr[c].x, y.x, fmaf(kr[c].y, y.y, fmaf(kr[c].z, y.z, fmaf(kr[c].w, y.w, s[r]))));
+            for (int r = 0; r < ROWS; ++r) {
+                float a0 = 0.0f, a1 = 0.0f;
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    const float4 y = q[r][4 * c + t];
+                    a0 = fmaf(kr[u][c].x, y.x, fmaf(kr[u][c].y, y.y, a0));
+                    a1 = fmaf(kr[u][c].z, y.z, fmaf(kr[u][c].w, y.w, a1));
+                }
+                x[u][r] = a0 + a1;
+            }
+        load(kr, K, p.ks[2], tile + WARPS * U);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) x[u][r] += __shfl_xor_sync(0xffffffffu, x[u][r], 1);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) x[u][r] += __shfl_xor_sync(0xffffffffu, x[u][r], 2);
+        bool grow = false;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int32_t j = (tile + u) * 8 + g;
+            const bool partial = (tile + u) * 8 + 8 > whole;
+            if (partial) {
+#pragma unroll
+                for (int c = 0; c < NC; ++c) { clean(vr[u][c].x); clean(vr[u][c].y); clean(vr[u][c].z); clean(vr[u][c].w); }
+            }
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                float y = capped2(p, x[u][r]);
+                if (p.bias == GRF_BIAS_SLOPES) y = fmaf(slope2[r], fabsf((float)(j - row[r].pos)), y);
+                if (p.bias == GRF_BIAS_BUCKETS) y += grf_bias2<float>(p, row[r].h, j - row[r].pos);
+                if (tile + u >= t1 || (partial && !row[r].sees(sight, kdoc, j))) y = -CUDART_INF_F;
+                x[u][r] = y;
+                grow |= y > m[r] + 8.0f;
             }
         }
-        load(kr, K, p.ks[2], tile + WARPS);
-        if (partial) {
+        // a new maximum only where it matters (see the tensor-core kernels), or for the first key
+        if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
-            for (int c = 0; c < NC; ++c) { clean(vr[c].x); clean(vr[c].y); clean(vr[c].z); clean(vr[c].w); }
-        }
+            for (int r = 0; r < ROWS; ++r) {
+                float top = m[r];
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
-            s[r] += __shfl_xor_sync(0xffffffffu, s[r], 1);
-            s[r] += __shfl_xor_sync(0xffffffffu, s[r], 2);
-            float x = capped2(p, s[r]);
-            if (p.bias != GRF_BIAS_NONE) x += grf_bias2<float>(p, row[r].h, j - row[r].pos);
-            if (partial && !row[r].sees(sight, kdoc, j)) x = -CUDART_INF_F;
-            float top = fmaxf(m[r], x);
-#pragma unroll
-            for (int y = 4; y < 32; y <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, y));
-            const float base = top == -CUDART_INF_F ? 0.0f : top, alpha = exp2f(m[r] - base), w = exp2f(x - base);
-            m[r] = top;
-            l[r] = l[r] * alpha + w;
-            if (__any_sync(0xffffffffu, alpha != 1.0f)) {
+                for (int u = 0; u < U; ++u) top = fmaxf(top, x[u][r]);
+                const float alpha = m[r] == -CUDART_INF_F ? 0.0f : exp2f(m[r] - top);
+                m[r] = top;
+                l[r] *= alpha;
 #pragma unroll
                 for (int c = 0; c < NC; ++c) { o[r][c].x *= alpha; o[r][c].y *= alpha; o[r][c].z *= alpha; o[r][c].w *= alpha; }
             }
-#pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                o[r][c].x = fmaf(w, vr[c].x, o[r][c].x); o[r][c].y = fmaf(w, vr[c].y, o[r][c].y);
-                o[r][c].z = fmaf(w, vr[c].z, o[r][c].z); o[r][c].w = fmaf(w, vr[c].w, o[r][c].w);
-            }
         }
-        load(vr, V, p.vs[2], tile + WARPS);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                const float w = exp2f(x[u][r] - (m[r] == -CUDART_INF_F ? 0.0f : m[r]));
+                l[r] += w;
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    o[r][c].x = fmaf(w, vr[u][c].x, o[r][c].x); o[r][c].y = fmaf(w, vr[u][c].y, o[r][c].y);
+                    o[r][c].z = fmaf(w, vr[u][c].z, o[r][c].z); o[r][c].w = fmaf(w, vr[u][c].w, o[r][c].w);
+                }
+            }
+        load(vr, V, p.vs[2], tile + WARPS * U);
     }
     if (__any_sync(0xffffffffu, bad)) {
-        for (int32_t tile = t0 + warp; tile < t1; tile += WARPS) {
-            const int32_t j = tile * 8 + g;
-            if (tile * 8 + 8 <= whole || j >= end) continue;
+        for (int32_t tile0 = t0 + warp * U; tile0 < t1; tile0 += WARPS * U)
+            for (int32_t tile = tile0; tile < min(tile0 + U, t1); ++tile) {
+                const int32_t j = tile * 8 + g;
+                if (tile * 8 + 8 <= whole || j >= end) continue;
 #pragma unroll
-            for (int c = 0; c < NC; ++c)
-                for (int e = 0; e < 4; ++e) {
-                    if (16 * c + 4 * t >= p.d) continue;
-                    const float v = V[(int64_t)j * p.vs[2] + 16 * c + e];
-                    if (fabsf(v) <= 3.4028235e38f) continue;
+                for (int c = 0; c < NC; ++c)
+                    for (int e = 0; e < 4; ++e) {
+                        if (16 * c + 4 * t >= p.d) continue;
+                        const float v = V[(int64_t)j * p.vs[2] + 16 * c + e];
+                        if (fabsf(v) <= 3.4028235e38f) continue;
 #pragma unroll
-                    for (int r = 0; r < ROWS; ++r)
-                        if (row[r].sees(sight, kdoc, j)) (&o[r][c].x)[e] += v;
-                }
-        }
+                        for (int r = 0; r < ROWS; ++r)
+                            if (row[r].sees(sight, kdoc, j)) (&o[r][c].x)[e] += v;
+                    }
+            }
     }
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
+        float top = m[r];
+#pragma unroll
+        for (int y = 4; y < 32; y <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, y));
+        // (a lane without a key has zeros, or NaN beside a maximum that is not one)
+        const float a = m[r] == -CUDART_INF_F ? 1.0f : exp2f(m[r] - top);
+        l[r] *= a;
 #pragma unroll
         for (int y = 4; y < 32; y <<= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], y);
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            float v[4] = {o[r][c].x, o[r][c].y, o[r][c].z, o[r][c].w};
+            float v[4] = {o[r][c].x * a, o[r][c].y * a, o[r][c].z * a, o[r][c].w * a};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
 #pragma unroll
@@ -457,7 +497,7 @@ __global__ void __launch_bounds__(THREADS) softmax_few_f32_kernel(const __grid_c
             }
             if (g == 0) *reinterpret_cast<float4*>(&sh.o[warp][r][16 * c + 4 * t]) = make_float4(v[0], v[1], v[2], v[3]);
         }
-        if (lane == 0) { sh.m[warp][r] = m[r]; sh.l[warp][r] = l[r]; }
+        if (lane == 0) { sh.m[warp][r] = top; sh.l[warp][r] = l[r]; }
     }
     join<float, ROWS, DP>(sh, p, f, b, kvh, r0);
 }

@@ -25,11 +25,11 @@ template <int DP, bool EXACT> struct Fwd {
     static constexpr int CTAS = DP == 64 ? 2 : 1;
     static constexpr bool SEP = DP == 64 && !EXACT;             // P beside S
     static constexpr int THREADS = 128 * (QT + 1);
-    static constexpr int NS = 2;
+    static constexpr int NS = 2, QB = DP == 64 ? 2 : 1;         // stages of K and V; places for a group's queries
     static constexpr uint32_t TILE = HALF * (DP / 64);
     static constexpr uint32_t TMEM = DP == 64 ? 256 : 512;
     static constexpr uint32_t P_COL = SEP ? 128 : 0, O_COL = DP == 64 ? 192 : 256;
-    static constexpr size_t SMEM = 1024 + (size_t)TILE * (QT + 2 * NS);    // then the tiles' bits
+    static constexpr size_t SMEM = 1024 + (size_t)TILE * (QT * QB + 2 * NS);    // then the tiles' bits
     static constexpr int MORE = DP == 64 ? 200 : 208, LESS = DP == 64 ? 56 : 88;   // registers: QT * MORE + LESS = the launch's
 };
 
@@ -118,35 +118,44 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                           const __grid_constant__ CUtensorMap map_v, const __grid_constant__ grf_softmax_params p)
 {
     using Sh = Fwd<DP, EXACT>;
-    constexpr int QT = Sh::QT, NS = Sh::NS;
+    constexpr int QT = Sh::QT, NS = Sh::NS, QB = Sh::QB;
     extern __shared__ unsigned char smem_dyn[];
-    __shared__ __align__(8) unsigned long long bars[5 * NS + 7 * QT];
+    constexpr int PER_GROUP = 6 + 2 * QB;
+    __shared__ __align__(8) unsigned long long bars[5 * NS + PER_GROUP * QT];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
     __shared__ float lut[BIAS == GRF_BIAS_BUCKETS ? QT * 2 * 256 : 1];
     const int tid = threadIdx.x, lane = tid & 31, warp = uniform(tid >> 5);
     const uint32_t smem = (smem_u32(smem_dyn) + 1023u) & ~1023u;
-    uint32_t* bits = reinterpret_cast<uint32_t*>(smem_dyn + (smem - smem_u32(smem_dyn)) + Sh::TILE * (QT + 2 * NS));
-    const uint32_t q_at = smem, k_at = q_at + QT * Sh::TILE, v_at = k_at + NS * Sh::TILE, bar0 = smem_u32(bars);
+    uint32_t* bits = reinterpret_cast<uint32_t*>(smem_dyn + (smem - smem_u32(smem_dyn)) + Sh::TILE * (QT * QB + 2 * NS));
+    const uint32_t q_at = smem, k_at = q_at + QT * QB * Sh::TILE, v_at = k_at + NS * Sh::TILE, bar0 = smem_u32(bars);
     auto k_full = [&](int s) { return bar0 + 8u * s; };
     auto v_full = [&](int s) { return bar0 + 8u * (NS + s); };
     auto k_empty = [&](int s) { return bar0 + 8u * (2 * NS + s); };
     auto v_empty = [&](int s) { return bar0 + 8u * (3 * NS + s); };
     auto v_clean = [&](int s) { return bar0 + 8u * (4 * NS + s); };
-    auto of_group = [&](int g, int what) { return bar0 + 8u * (5 * NS + 7 * g + what); };
-    auto q_full = [&](int g) { return of_group(g, 0); };
-    auto s_full = [&](int g) { return of_group(g, 1); };
-    auto s_read = [&](int g) { return of_group(g, 2); };
-    auto p_full = [&](int g) { return of_group(g, 3); };
-    auto pv_done = [&](int g) { return of_group(g, 4); };
-    auto drain = [&](int g) { return of_group(g, 5); };
-    auto lut_full = [&](int g) { return of_group(g, 6); };
+    auto of_group = [&](int g, int what) { return bar0 + 8u * (5 * NS + PER_GROUP * g + what); };
+    auto s_full = [&](int g) { return of_group(g, 0); };
+    auto s_read = [&](int g) { return of_group(g, 1); };
+    auto p_full = [&](int g) { return of_group(g, 2); };
+    auto pv_done = [&](int g) { return of_group(g, 3); };
+    auto lut_full = [&](int g) { return of_group(g, 4); };
+    auto o_read = [&](int g) { return of_group(g, 5); };
+    auto q_full = [&](int g, int y) { return of_group(g, 6 + y); };
+    auto q_empty = [&](int g, int y) { return of_group(g, 6 + QB + y); };
 
-    const int32_t b = (int32_t)blockIdx.x / p.H, h = (int32_t)blockIdx.x % p.H, kvh = h / p.group;
-    const grf_sight sight(p, b);
-    const int32_t i0 = ((int32_t)gridDim.y - 1 - (int32_t)blockIdx.y) * (QT * BT);           // the longest rows first
-    const int32_t tiles = (sight.end(min(i0 + QT * BT, p.Nq)) + BT - 1) / BT;
-    const forward_tiles T{p, sight, bits, i0, tiles, (tiles + 31) / 32, sight.end(p.Nq)};
+    // Blocks of queries, the longest rows first, dealt out to the CTAs forwards and backwards in turn, so that all get about the same.
+    // (With documents every CTA has one block, whose bits are made below.)
+    const int32_t heads = p.B * p.H, blocks = (p.Nq + QT * BT - 1) / (QT * BT);
+    const int64_t items = (int64_t)heads * blocks;
+    auto item = [&](int32_t round) {
+        const int64_t x = (int64_t)round * gridDim.x + ((round & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+        return x < items ? x : (int64_t)-1;
+    };
+    const int32_t rounds = (int32_t)((items + gridDim.x - 1) / gridDim.x);
+    auto bh_of = [&](int64_t x) { return (int32_t)(x % heads); };
+    auto i0_of = [&](int64_t x) { return (blocks - 1 - (int32_t)(x / heads)) * (QT * BT); };
+    auto tiles_of = [&](const grf_sight& sight, int32_t i0) { return (sight.end(min(i0 + QT * BT, p.Nq)) + BT - 1) / BT; };
     constexpr int COPY = 4 * QT, ISSUE = 4 * QT + 1, CLEAN = 4 * QT + 3;
 
     if (tid == 0) {
@@ -156,13 +165,18 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             mbar_init(k_empty(s), QT); mbar_init(v_empty(s), QT + 1);
         }
         for (int g = 0; g < QT; ++g) {
-            mbar_init(q_full(g), 1); mbar_init(s_full(g), 1); mbar_init(pv_done(g), 1); mbar_init(drain(g), 1);
-            mbar_init(s_read(g), 4); mbar_init(p_full(g), 4); mbar_init(lut_full(g), 4);
+            mbar_init(s_full(g), 1); mbar_init(pv_done(g), 1);
+            mbar_init(s_read(g), 4); mbar_init(p_full(g), 4); mbar_init(lut_full(g), 4); mbar_init(o_read(g), 4);
+            for (int y = 0; y < QB; ++y) { mbar_init(q_full(g, y), 1); mbar_init(q_empty(g, y), 1); }
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == COPY) tmem_alloc(&tmem_slot, Sh::TMEM);
-    if (sight.docs) {
+    if (p.q_doc) {
+        const int32_t b = bh_of(blockIdx.x) / p.H, i0 = i0_of(blockIdx.x);
+        const grf_sight sight(p, b);
+        const int32_t tiles = tiles_of(sight, i0);
+        const forward_tiles T{p, sight, bits, i0, tiles, (tiles + 31) / 32, 0};
         const int32_t kblocks = (p.Nk + BT - 1) / BT, qblocks = (p.Nq + BT - 1) / BT;
         for (int32_t w = warp; w < T.words; w += Sh::THREADS / 32) {
             const int32_t t = w * 32 + lane;
@@ -190,296 +204,353 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Sh::LESS));
         if (warp == COPY) {
             // ------------------------------------------------------------ copies
-            const int32_t qb = p.qs[0] ? b : 0, qh = p.qs[1] ? h : 0, kb = p.ks[0] ? b : 0, kh = p.ks[1] ? kvh : 0, vb = p.vs[0] ? b : 0, vh = p.vs[1] ? kvh : 0;
             bool ok = true;
-            int32_t n = 0;
-            for (int g = 0; g < QT; ++g) {
-                if (T.from(g) >= p.Nq || tiles == 0) continue;
-                expect_tx_elected(q_full(g), Sh::TILE);
-                for (int y = 0; y < DP / 64; ++y) load_box(q_at + g * Sh::TILE + y * HALF, &map_q, 64 * y, T.from(g), qh, qb, q_full(g));
-            }
-            for (int32_t t = T.next<QT>(0); t < tiles && ok; t = T.next<QT>(t + 1), ++n) {
-                const int s = n % NS;
-                const uint32_t before = (uint32_t)(n / NS - 1) & 1u;
-                if (n >= NS && !(ok = wait(k_empty(s), before))) break;
-                expect_tx_elected(k_full(s), Sh::TILE);
-                for (int y = 0; y < DP / 64; ++y) load_box(k_at + s * Sh::TILE + y * HALF, &map_k, 64 * y, t * BT, kh, kb, k_full(s));
-                if (n >= NS && !(ok = wait(v_empty(s), before))) {
-                    mbar_drain(k_full(s), (uint32_t)(n / NS) & 1u, 20000000ll);
-                    break;
+            int32_t n = 0, qn[QT] = {};
+            for (int32_t round = 0; round < rounds && ok; ++round) {
+                const int64_t x = item(round);
+                if (x < 0) break;
+                const int32_t bh = bh_of(x), b = bh / p.H, h = bh % p.H, kvh = h / p.group, i0 = i0_of(x);
+                const grf_sight sight(p, b);
+                const int32_t tiles = tiles_of(sight, i0);
+                const forward_tiles T{p, sight, bits, i0, tiles, (tiles + 31) / 32, 0};
+                const int32_t kb = p.ks[0] ? b : 0, kh = p.ks[1] ? kvh : 0, vb = p.vs[0] ? b : 0, vh = p.vs[1] ? kvh : 0;
+                const int32_t t0 = T.next<QT>(0);
+                for (int32_t t = t0; t < tiles && ok; t = T.next<QT>(t + 1), ++n) {
+                    const int s = n % NS;
+                    const uint32_t before = (uint32_t)(n / NS - 1) & 1u;
+                    if (n >= NS && !(ok = wait(k_empty(s), before) && wait(v_empty(s), before))) break;
+                    expect_tx_elected(k_full(s), Sh::TILE);
+                    expect_tx_elected(v_full(s), Sh::TILE);
+                    for (int y = 0; y < DP / 64; ++y) load_box(k_at + s * Sh::TILE + y * HALF, &map_k, 64 * y, t * BT, kh, kb, k_full(s));
+                    if (t == t0) {
+                        for (int g = 0; g < QT; ++g) {
+                            if (T.from(g) >= p.Nq) continue;
+                            const int y = qn[g] % QB;
+                            if (qn[g] >= QB && !wait(q_empty(g, y), (uint32_t)(qn[g] / QB - 1) & 1u)) { ok = false; break; }
+                            expect_tx_elected(q_full(g, y), Sh::TILE);
+                            for (int z = 0; z < DP / 64; ++z)
+                                load_box(q_at + (g * QB + y) * Sh::TILE + z * HALF, &map_q, 64 * z, T.from(g), p.qs[1] ? h : 0, p.qs[0] ? b : 0, q_full(g, y));
+                            ++qn[g];
+                        }
+                    }
+                    for (int y = 0; y < DP / 64; ++y) load_box(v_at + s * Sh::TILE + y * HALF, &map_v, 64 * y, t * BT, vh, vb, v_full(s));
                 }
-                expect_tx_elected(v_full(s), Sh::TILE);
-                for (int y = 0; y < DP / 64; ++y) load_box(v_at + s * Sh::TILE + y * HALF, &map_v, 64 * y, t * BT, vh, vb, v_full(s));
             }
             // after an abort nobody may have waited for the last copies: they end before the CTA does
             if (!ok || *(volatile int*)&abort_flag) {
-                for (int32_t x = max(0, n - NS); x < n; ++x) {
+                for (int32_t x = max(0, n - NS); x <= n; ++x) {
                     mbar_drain(k_full(x % NS), (uint32_t)(x / NS) & 1u, 20000000ll);
                     mbar_drain(v_full(x % NS), (uint32_t)(x / NS) & 1u, 20000000ll);
                 }
                 for (int g = 0; g < QT; ++g)
-                    if (T.from(g) < p.Nq && tiles > 0) mbar_drain(q_full(g), 0u, 20000000ll);
+                    for (int32_t x = max(0, qn[g] - QB); x < qn[g]; ++x) mbar_drain(q_full(g, x % QB), (uint32_t)(x / QB) & 1u, 20000000ll);
             }
         } else if (warp >= ISSUE && warp < ISSUE + QT) {
             // ------------------------------------------------------------ products of one group
             const int g = warp - ISSUE;
             const int32_t steps = (p.d + 15) / 16;
-            const uint64_t q_op = rows_operand(q_at + g * Sh::TILE), k_op = rows_operand(k_at), v_op = columns_operand(v_at);
+            const uint64_t q_op = rows_operand(q_at + g * QB * Sh::TILE), k_op = rows_operand(k_at), v_op = columns_operand(v_at);
             const uint32_t scores = tmem + g * BT, probs = scores + Sh::P_COL, acc = tmem + Sh::O_COL + g * DP;
             bool ok = true;
-            int32_t n = 0, c = 0;
+            int32_t n = 0, made = 0, used = 0, qn = 0, outs = 0;        // tiles, S and P of this group, its queries, its outputs
             uint32_t cleaned = 0u;                              // parity of each stage's cleanings
-            auto make_scores = [&](int s, int32_t n_) {
+            auto make_scores = [&](int32_t n_) {
+                const int s = n_ % NS;
+                if (Sh::SEP && made > 0 && !wait(s_read(g), (uint32_t)(made - 1) & 1u)) return false;
                 if (!wait(k_full(s), (uint32_t)(n_ / NS) & 1u)) return false;
                 fence_after_sync();
-                product_over_columns<DP>(scores, lo32(q_op), hi32(q_op), lo32(k_op) + s * (Sh::TILE / 16), hi32(k_op), steps);
+                product_over_columns<DP>(scores, lo32(q_op) + (qn % QB) * (Sh::TILE / 16), hi32(q_op), lo32(k_op) + s * (Sh::TILE / 16), hi32(k_op), steps);
                 mma_commit(s_full(g));
                 mma_commit(k_empty(s));
+                ++made;
                 return true;
             };
-            auto values_ready = [&](int s, int32_t n_, int32_t t) {
-                if (!wait(v_full(s), (uint32_t)(n_ / NS) & 1u)) return false;
+            auto values_ready = [&](const forward_tiles& T, int32_t t) {
+                const int s = n % NS;
+                if (!wait(v_full(s), (uint32_t)(n / NS) & 1u)) return false;
                 if (T.unclean<QT>(t)) {
                     if (!wait(v_clean(s), cleaned >> s & 1u)) return false;
                     cleaned ^= 1u << s;
                 }
                 return true;
             };
-            int32_t t = T.next<QT>(0);
-            if (t < tiles && T.from(g) < p.Nq) ok = wait(q_full(g), 0u);
-            if (Sh::SEP && t < tiles && ok) ok = make_scores(0, 0);
-            for (; t < tiles && ok; ++n) {
-                const int s = n % NS;
-                const int32_t t_next = T.next<QT>(t + 1);
-                if (!Sh::SEP) {
-                    if (T.what(g, t) == 0) {
-                        if (!(ok = wait(k_full(s), (uint32_t)(n / NS) & 1u))) break;
-                        arrive_elected(k_empty(s));
-                        if (!(ok = values_ready(s, n, t))) break;
-                        arrive_elected(v_empty(s));
-                        t = t_next;
-                        continue;
-                    }
-                    if (!(ok = make_scores(s, n))) break;
-                } else if (t_next < tiles) {
-                    if (!(ok = wait(s_read(g), (uint32_t)c & 1u))) break;
+            for (int32_t round = 0; round < rounds && ok; ++round) {
+                const int64_t x = item(round);
+                if (x < 0) break;
+                const int32_t b = bh_of(x) / p.H, i0 = i0_of(x);
+                const grf_sight sight(p, b);
+                const int32_t tiles = tiles_of(sight, i0);
+                const forward_tiles T{p, sight, bits, i0, tiles, (tiles + 31) / 32, sight.end(p.Nq)};
+                int32_t t = T.next<QT>(0), c = 0;
+                const bool queries = t < tiles && T.from(g) < p.Nq;
+                if (queries && !(ok = wait(q_full(g, qn % QB), (uint32_t)(qn / QB) & 1u))) break;
+                if (Sh::SEP && t < tiles && !(ok = make_scores(n))) break;
+                for (; t < tiles && ok; ++n) {
+                    const int s = n % NS;
+                    const int32_t t_next = T.next<QT>(t + 1);
+                    if (!Sh::SEP) {
+                        if (T.what(g, t) == 0) {
+                            if (!(ok = wait(k_full(s), (uint32_t)(n / NS) & 1u))) break;
+                            arrive_elected(k_empty(s));
+                            if (!(ok = values_ready(T, t))) break;
+                            arrive_elected(v_empty(s));
+                            t = t_next;
+                            continue;
+                        }
+                        if (!(ok = make_scores(n))) break;
+                    } else if (t_next < tiles && !(ok = make_scores(n + 1))) break;
+                    if (c == 0 && outs > 0 && !(ok = wait(o_read(g), (uint32_t)(outs - 1) & 1u))) break;
+                    if (!(ok = wait(p_full(g), (uint32_t)used & 1u))) break;
+                    if (!(ok = values_ready(T, t))) break;
                     fence_after_sync();
-                    if (!(ok = make_scores((n + 1) % NS, n + 1))) break;
+                    product_over_rows<DP>(acc, probs, lo32(v_op) + s * (Sh::TILE / 16), hi32(v_op), c > 0 ? 1u : 0u);
+                    if (EXACT) product_over_rows<DP>(acc, probs + 64, lo32(v_op) + s * (Sh::TILE / 16), hi32(v_op), 1u);
+                    mma_commit(v_empty(s));
+                    mma_commit(pv_done(g));
+                    ++c;
+                    ++used;
+                    t = t_next;
                 }
-                if (!(ok = wait(p_full(g), (uint32_t)c & 1u))) break;
-                if (!(ok = values_ready(s, n, t))) break;
-                fence_after_sync();
-                product_over_rows<DP>(acc, probs, lo32(v_op) + s * (Sh::TILE / 16), hi32(v_op), c > 0 ? 1u : 0u);
-                if (EXACT) product_over_rows<DP>(acc, probs + 64, lo32(v_op) + s * (Sh::TILE / 16), hi32(v_op), 1u);
-                mma_commit(v_empty(s));
-                mma_commit(pv_done(g));
-                ++c;
-                t = t_next;
+                if (queries && ok) {
+                    mma_commit(q_empty(g, qn % QB));
+                    ++qn;
+                }
+                if (c > 0) ++outs;
             }
             if (!ok) {
-                mma_commit(drain(g));
-                mbar_drain(drain(g), 0u, 20000000ll);
+                // products under way end before the CTA does (a barrier that nobody else needs any more)
+                mma_commit(pv_done(g));
+                mbar_drain(pv_done(g), (uint32_t)used & 1u, 20000000ll);
             }
         } else if (warp == CLEAN) {
             // ------------------------------------------------------------ rows of V that nobody sees
             int32_t n = 0;
-            for (int32_t t = T.next<QT>(0); t < tiles; t = T.next<QT>(t + 1), ++n) {
-                // (it waits for every tile, and holds the stage until then: a parity only tells a phase from the one before it)
-                const int s = n % NS;
-                if (!wait(v_full(s), (uint32_t)(n / NS) & 1u)) break;
-                if (!T.unclean<QT>(t)) {
+            bool ok = true;
+            for (int32_t round = 0; round < rounds && ok; ++round) {
+                const int64_t x = item(round);
+                if (x < 0) break;
+                const int32_t b = bh_of(x) / p.H, i0 = i0_of(x);
+                const grf_sight sight(p, b);
+                const int32_t tiles = tiles_of(sight, i0);
+                const forward_tiles T{p, sight, bits, i0, tiles, (tiles + 31) / 32, sight.end(p.Nq)};
+                for (int32_t t = T.next<QT>(0); t < tiles; t = T.next<QT>(t + 1), ++n) {
+                    // (it waits for every tile, and holds the stage until then: a parity only tells a phase from the one before it)
+                    const int s = n % NS;
+                    if (!(ok = wait(v_full(s), (uint32_t)(n / NS) & 1u))) break;
+                    if (T.unclean<QT>(t)) {
+                        for (int r = lane; r < BT; r += 32) {
+                            const int32_t j = t * BT + r;
+                            if (j >= p.Nk || (j < T.last && !(sight.docs && p.k_doc[(int64_t)b * p.Nk + j] < 0))) continue;
+                            for (int y = 0; y < DP / 64; ++y)
+                                for (int z = 0; z < 8; ++z)
+                                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(v_at + s * Sh::TILE + y * HALF + r * 128 + z * 16), "r"(0u) : "memory");
+                        }
+                        fence_async_smem();                     // the products read through the asynchronous proxy
+                        __syncwarp();
+                        arrive_elected(v_clean(s));
+                    }
                     arrive_elected(v_empty(s));
-                    continue;
                 }
-                for (int r = lane; r < BT; r += 32) {
-                    const int32_t j = t * BT + r;
-                    if (j >= p.Nk || (j < T.last && !(sight.docs && p.k_doc[(int64_t)b * p.Nk + j] < 0))) continue;
-                    for (int y = 0; y < DP / 64; ++y)
-                        for (int x = 0; x < 8; ++x)
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(v_at + s * Sh::TILE + y * HALF + r * 128 + x * 16), "r"(0u) : "memory");
-                }
-                fence_async_smem();                             // the products read through the asynchronous proxy
-                __syncwarp();
-                arrive_elected(v_clean(s));
-                arrive_elected(v_empty(s));
             }
         }
     } else {
         // ---------------------------------------------------------------- a thread per query
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Sh::MORE));
         const int g = warp >> 2, r = (warp & 3) * 32 + lane;
-        const int32_t i = T.from(g) + r, pos = sight.position(i), pos0 = sight.position(T.from(g));
-        const int32_t limit = sight.order == GRF_ORDER_FULL ? sight.len : min(sight.len, max(pos + 1, sight.prefix));
-        const int32_t doc = sight.docs && i < p.Nq ? p.q_doc[(int64_t)b * p.Nq + i] : -1;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t s_addr = tmem + g * BT + lanes, p_addr = s_addr + Sh::P_COL, o_addr = tmem + Sh::O_COL + g * DP + lanes;
         const float to2 = p.scale * GRF_LOG2E, by_cap = CAP ? p.scale / p.cap : 0.0f, cap2 = p.cap * GRF_LOG2E;
-        const float slope2 = BIAS == GRF_BIAS_SLOPES ? p.slopes[h] * GRF_LOG2E : 0.0f;
-        float m = -CUDART_INF_F;
-        uint64_t sum2[2] = {0ull, 0ull};
-        int32_t c = 0, luts = 0;
+        int32_t done = 0, luts = 0;                             // tiles of this group, tiles with a bias per diagonal
         bool ok = true;
-        for (int32_t t = T.next<QT>(0); t < tiles; t = T.next<QT>(t + 1)) {
-            const int what = T.what(g, t);
-            if (what == 0) continue;
-            const int32_t j0 = t * BT;
-            // the bias of this tile: one value, or one per diagonal
-            float bias2 = 0.0f;
-            bool diagonals = false;
-            const float* mine = lut;
-            if (BIAS == GRF_BIAS_BUCKETS) {
-                const int32_t near = grf_bucket(p, j0 - pos0 - (BT - 1)), far = grf_bucket(p, j0 + BT - 1 - pos0);
-                diagonals = near != far;
-                if (diagonals) {
-                    float* at = lut + (g * 2 + (luts & 1)) * 256;
-                    at[r] = grf_bias2<__nv_bfloat16>(p, h, j0 - pos0 + r - (BT - 1));
-                    at[r + BT] = grf_bias2<__nv_bfloat16>(p, h, j0 - pos0 + r + 1);
-                    mine = at + (BT - 1 - r);
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(lut_full(g));
-                    if (!(ok = wait(lut_full(g), (uint32_t)luts & 1u))) break;
-                    ++luts;
-                } else bias2 = grf_bias2<__nv_bfloat16>(p, h, j0 - pos0);
-            }
-            if (!(ok = wait(s_full(g), (uint32_t)c & 1u))) break;
-            fence_after_sync();
-            uint32_t sv[8][16];
+        for (int32_t round = 0; round < rounds; ++round) {
+            const int64_t which = item(round);
+            if (which < 0) break;
+            const int32_t bh = bh_of(which), b = bh / p.H, h = bh % p.H, i0 = i0_of(which);
+            const grf_sight sight(p, b);
+            const int32_t tiles = tiles_of(sight, i0);
+            const forward_tiles T{p, sight, bits, i0, tiles, (tiles + 31) / 32, 0};
+            const int32_t i = T.from(g) + r, pos = sight.position(i), pos0 = sight.position(T.from(g));
+            const int32_t limit = sight.order == GRF_ORDER_FULL ? sight.len : min(sight.len, max(pos + 1, sight.prefix));
+            const int32_t doc = sight.docs && i < p.Nq ? p.q_doc[(int64_t)b * p.Nq + i] : -1;
+            const float slope2 = BIAS == GRF_BIAS_SLOPES ? p.slopes[h] * GRF_LOG2E : 0.0f;
+            float m = -CUDART_INF_F;
+            uint64_t sum2[2] = {0ull, 0ull};
+            int32_t c = 0;
+            for (int32_t t = T.next<QT>(0); t < tiles; t = T.next<QT>(t + 1)) {
+                const int what = T.what(g, t);
+                if (what == 0) continue;
+                const int32_t j0 = t * BT;
+                // the bias of this tile: one value, or one per diagonal
+                float bias2 = 0.0f;
+                bool diagonals = false;
+                const float* mine = lut;
+                if (BIAS == GRF_BIAS_BUCKETS) {
+                    const int32_t near = grf_bucket(p, j0 - pos0 - (BT - 1)), far = grf_bucket(p, j0 + BT - 1 - pos0);
+                    diagonals = near != far;
+                    if (diagonals) {
+                        float* at = lut + (g * 2 + (luts & 1)) * 256;
+                        at[r] = grf_bias2<__nv_bfloat16>(p, h, j0 - pos0 + r - (BT - 1));
+                        at[r + BT] = grf_bias2<__nv_bfloat16>(p, h, j0 - pos0 + r + 1);
+                        mine = at + (BT - 1 - r);
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(lut_full(g));
+                        if (!(ok = wait(lut_full(g), (uint32_t)luts & 1u))) break;
+                        ++luts;
+                    } else bias2 = grf_bias2<__nv_bfloat16>(p, h, j0 - pos0);
+                }
+                if (!(ok = wait(s_full(g), (uint32_t)done & 1u))) break;
+                fence_after_sync();
+                uint32_t sv[8][16];
 #pragma unroll
-            for (int y = 0; y < 8; ++y) tmem_ld16_nowait(s_addr + 16 * y, sv[y]);
-            tmem_ld_wait();
-            if (Sh::SEP) {
+                for (int y = 0; y < 8; ++y) tmem_ld16_nowait(s_addr + 16 * y, sv[y]);
+                tmem_ld_wait();
+                if (Sh::SEP) {
+                    fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(s_read(g));
+                }
+                float top = -CUDART_INF_F;
+                const float ahead = (float)(j0 - pos);          // (exact, as are its sums, below 2^24; beyond, off by half a step as the distance itself)
+                const uint64_t to22 = pack2(to2, to2), bias22 = pack2(bias2, bias2);
+#pragma unroll
+                for (int y = 0; y < 8; ++y)
+#pragma unroll
+                    for (int e = 0; e < 16; e += 2) {
+                        const int col = 16 * y + e;
+                        float x0, x1;
+                        if (CAP) {
+                            x0 = cap2 * tanh_any(__uint_as_float(sv[y][e]) * by_cap) + bias2;
+                            x1 = cap2 * tanh_any(__uint_as_float(sv[y][e + 1]) * by_cap) + bias2;
+                        } else unpack2(fma2(pack2(sv[y][e], sv[y][e + 1]), to22, bias22), x0, x1);
+                        if (BIAS == GRF_BIAS_SLOPES) {
+                            x0 = fmaf(-slope2, fabsf(ahead + (float)col), x0);
+                            x1 = fmaf(-slope2, fabsf(ahead + (float)(col + 1)), x1);
+                        }
+                        if (BIAS == GRF_BIAS_BUCKETS) {
+                            if (diagonals) { x0 += mine[col]; x1 += mine[col + 1]; }
+                        }
+                        sv[y][e] = __float_as_uint(x0);
+                        sv[y][e + 1] = __float_as_uint(x1);
+                    }
+                if (what == 1) {
+                    if (sight.docs) {
+                        const int32_t* kd = p.k_doc + (int64_t)b * p.Nk + j0;
+#pragma unroll
+                        for (int y = 0; y < 8; ++y)
+#pragma unroll
+                            for (int e = 0; e < 16; ++e)
+                                if (!(j0 + 16 * y + e < limit && doc >= 0 && __ldg(kd + 16 * y + e) == doc)) sv[y][e] = 0xff800000u;
+                    } else {
+#pragma unroll
+                        for (int y = 0; y < 8; ++y)
+#pragma unroll
+                            for (int e = 0; e < 16; ++e)
+                                if (j0 + 16 * y + e >= limit) sv[y][e] = 0xff800000u;
+                    }
+                }
+#pragma unroll
+                for (int y = 0; y < 8; ++y)
+#pragma unroll
+                    for (int e = 0; e < 16; e += 2) top = max3(top, __uint_as_float(sv[y][e]), __uint_as_float(sv[y][e + 1]));
+                // a new maximum only when it matters: 2^8 above the one in use (or the first)
+                const bool grow = top > m + 8.0f;
+                if (__any_sync(0xffffffffu, grow)) {
+                    const float alpha = grow ? ex2(m - top) : 1.0f;
+                    if (grow) m = top;
+                    if (c > 0) {
+                        if (!(ok = wait(pv_done(g), (uint32_t)(done - 1) & 1u))) break;
+                        fence_after_sync();
+                        const uint64_t a2 = pack2(alpha, alpha);
+                        sum2[0] = mul2(sum2[0], a2);
+                        sum2[1] = mul2(sum2[1], a2);
+#pragma unroll
+                        for (int y = 0; y < DP / 16; ++y) {
+                            uint32_t o[16];
+                            tmem_ld16(o_addr + 16 * y, o);
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+                            tmem_st16(o_addr + 16 * y, o);
+                        }
+                    }
+                }
+                if (Sh::SEP && done > 0) {
+                    if (!(ok = wait(pv_done(g), (uint32_t)(done - 1) & 1u))) break;
+                    fence_after_sync();
+                }
+                const float base = m == -CUDART_INF_F ? 0.0f : m;
+                const uint64_t minus = pack2(-base, -base);
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    uint32_t w[16], u[EXACT ? 16 : 1];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int a = 2 * y + (e >> 3), z = (2 * e) & 15;
+                        float x0, x1;
+                        unpack2(add2(pack2(sv[a][z], sv[a][z + 1]), minus), x0, x1);
+                        x0 = ex2(x0);
+                        x1 = ex2(x1);
+                        sum2[e & 1] = add2(sum2[e & 1], pack2(x0, x1));
+                        w[e] = pack_bf16(x0, x1);
+                        if (EXACT) u[EXACT ? e : 0] = pack_bf16(x0 - __uint_as_float(w[e] << 16), x1 - __uint_as_float(w[e] & 0xffff0000u));
+                    }
+                    tmem_st16(p_addr + 16 * y, w);
+                    if constexpr (EXACT) tmem_st16(p_addr + 64 + 16 * y, u);
+                }
+                tmem_st_wait();
                 fence_before_sync();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(s_read(g));
+                if (lane == 0) mbar_arrive(p_full(g));
+                ++c;
+                ++done;
             }
-            float top = -CUDART_INF_F;
-            const float ahead = (float)(j0 - pos);              // (exact, as are its sums: below 2^24; beyond, off by half a step as the distance itself)
-            const uint64_t to22 = pack2(to2, to2), bias22 = pack2(bias2, bias2);
-#pragma unroll
-            for (int y = 0; y < 8; ++y)
-#pragma unroll
-                for (int e = 0; e < 16; e += 2) {
-                    const int col = 16 * y + e;
-                    float x0, x1;
-                    if (CAP) {
-                        x0 = cap2 * tanh_any(__uint_as_float(sv[y][e]) * by_cap) + bias2;
-                        x1 = cap2 * tanh_any(__uint_as_float(sv[y][e + 1]) * by_cap) + bias2;
-                    } else unpack2(fma2(pack2(sv[y][e], sv[y][e + 1]), to22, bias22), x0, x1);
-                    if (BIAS == GRF_BIAS_SLOPES) {
-                        x0 = fmaf(-slope2, fabsf(ahead + (float)col), x0);
-                        x1 = fmaf(-slope2, fabsf(ahead + (float)(col + 1)), x1);
-                    }
-                    if (BIAS == GRF_BIAS_BUCKETS) {
-                        if (diagonals) { x0 += mine[col]; x1 += mine[col + 1]; }
-                    }
-                    sv[y][e] = __float_as_uint(x0);
-                    sv[y][e + 1] = __float_as_uint(x1);
-                }
-            if (what == 1) {
-                if (sight.docs) {
-                    const int32_t* kd = p.k_doc + (int64_t)b * p.Nk + j0;
-#pragma unroll
-                    for (int y = 0; y < 8; ++y)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e)
-                            if (!(j0 + 16 * y + e < limit && doc >= 0 && __ldg(kd + 16 * y + e) == doc)) sv[y][e] = 0xff800000u;
-                } else {
-#pragma unroll
-                    for (int y = 0; y < 8; ++y)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e)
-                            if (j0 + 16 * y + e >= limit) sv[y][e] = 0xff800000u;
-                }
-            }
-#pragma unroll
-            for (int y = 0; y < 8; ++y)
-#pragma unroll
-                for (int e = 0; e < 16; e += 2) top = max3(top, __uint_as_float(sv[y][e]), __uint_as_float(sv[y][e + 1]));
-            // a new maximum only when it matters: 2^8 above the one in use (or the first)
-            const bool grow = top > m + 8.0f;
-            if (__any_sync(0xffffffffu, grow)) {
-                const float alpha = grow ? ex2(m - top) : 1.0f;
-                if (grow) m = top;
-                if (c > 0) {
-                    if (!(ok = wait(pv_done(g), (uint32_t)(c - 1) & 1u))) break;
-                    fence_after_sync();
-                    const uint64_t a2 = pack2(alpha, alpha);
-                    sum2[0] = mul2(sum2[0], a2);
-                    sum2[1] = mul2(sum2[1], a2);
-#pragma unroll
-                    for (int y = 0; y < DP / 16; ++y) {
-                        uint32_t o[16];
-                        tmem_ld16(o_addr + 16 * y, o);
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
-                        tmem_st16(o_addr + 16 * y, o);
-                    }
-                }
-            }
-            if (Sh::SEP && c > 0) {
-                if (!(ok = wait(pv_done(g), (uint32_t)(c - 1) & 1u))) break;
-                fence_after_sync();
-            }
-            const float base = m == -CUDART_INF_F ? 0.0f : m;
-            const uint64_t minus = pack2(-base, -base);
-#pragma unroll
-            for (int y = 0; y < 4; ++y) {
-                uint32_t w[16], u[EXACT ? 16 : 1];
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int a = 2 * y + (e >> 3), z = (2 * e) & 15;
-                    float x0, x1;
-                    unpack2(add2(pack2(sv[a][z], sv[a][z + 1]), minus), x0, x1);
-                    x0 = ex2(x0);
-                    x1 = ex2(x1);
-                    sum2[e & 1] = add2(sum2[e & 1], pack2(x0, x1));
-                    w[e] = pack_bf16(x0, x1);
-                    if (EXACT) u[EXACT ? e : 0] = pack_bf16(x0 - __uint_as_float(w[e] << 16), x1 - __uint_as_float(w[e] & 0xffff0000u));
-                }
-                tmem_st16(p_addr + 16 * y, w);
-                if constexpr (EXACT) tmem_st16(p_addr + 64 + 16 * y, u);
-            }
-            tmem_st_wait();
-            fence_before_sync();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(p_full(g));
-            ++c;
-        }
-        ok = __all_sync(0xffffffffu, ok) != 0;
-        if (ok && c > 0) ok = wait(pv_done(g), (uint32_t)(c - 1) & 1u);
-        fence_after_sync();
-        float l0, l1, l2, l3;
-        unpack2(sum2[0], l0, l1);
-        unpack2(sum2[1], l2, l3);
-        const float l = (l0 + l1) + (l2 + l3), inv = l == 0.0f ? 0.0f : 1.0f / l;
-        bool spoilt = false;
-        if (ok) {
+            ok = __all_sync(0xffffffffu, ok) != 0;
+            if (ok && c > 0) ok = wait(pv_done(g), (uint32_t)(done - 1) & 1u);
+            if (!ok) break;
+            fence_after_sync();
+            float l0, l1, l2, l3;
+            unpack2(sum2[0], l0, l1);
+            unpack2(sum2[1], l2, l3);
+            const float l = (l0 + l1) + (l2 + l3), inv = l == 0.0f ? 0.0f : 1.0f / l;
+            bool spoilt = false;
             __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.out_w) + b * p.os[0] + h * p.os[1] + (int64_t)i * p.os[2];
             __nv_bfloat16* rest = p.rest_w ? p.rest_w + (((int64_t)b * p.H + h) * p.Nq + i) * p.d : nullptr;
 #pragma unroll
-            for (int y = 0; y < DP / 16; ++y) {
-                uint32_t o[16];
+            for (int y = 0; y < DP / 32; ++y) {
+                uint32_t o[2][16];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) o[e] = 0u;
-                if (c > 0) tmem_ld16(o_addr + 16 * y, o);
+                for (int e = 0; e < 16; ++e) o[0][e] = o[1][e] = 0u;
+                if (c > 0) {
+                    tmem_ld16_nowait(o_addr + 32 * y, o[0]);
+                    tmem_ld16_nowait(o_addr + 32 * y + 16, o[1]);
+                    tmem_ld_wait();
+                    if (y == DP / 32 - 1) {
+                        // the accumulator may be written again
+                        fence_before_sync();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(o_read(g));
+                    }
+                }
                 if (i >= p.Nq) continue;
 #pragma unroll
-                for (int z = 0; z < 2; ++z) {
-                    if (16 * y + 8 * z >= p.d) continue;
+                for (int z = 0; z < 4; ++z) {
+                    const int col = 32 * y + 8 * z;
+                    if (col >= p.d) continue;
                     uint32_t w[4], u[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         // (no key seen: 0, whatever the accumulator holds)
-                        const float x0 = l == 0.0f ? 0.0f : __uint_as_float(o[8 * z + 2 * e]) * inv, x1 = l == 0.0f ? 0.0f : __uint_as_float(o[8 * z + 2 * e + 1]) * inv;
+                        const uint32_t (&v)[16] = o[z >> 1];
+                        const int at = 8 * (z & 1) + 2 * e;
+                        const float x0 = l == 0.0f ? 0.0f : __uint_as_float(v[at]) * inv, x1 = l == 0.0f ? 0.0f : __uint_as_float(v[at + 1]) * inv;
                         spoilt |= !(fabsf(x0) <= 3.4028235e38f) || !(fabsf(x1) <= 3.4028235e38f);
                         w[e] = pack_bf16(x0, x1);
-                        if (rest) {
+                        if (EXACT) {
                             const __nv_bfloat16 r0 = grf_rest(x0, __float2bfloat16_rn(x0)), r1 = grf_rest(x1, __float2bfloat16_rn(x1));
                             u[e] = pack_bf16(__bfloat162float(r0), __bfloat162float(r1));
                         }
                     }
-                    *reinterpret_cast<uint4*>(out + 16 * y + 8 * z) = make_uint4(w[0], w[1], w[2], w[3]);
-                    if (rest) *reinterpret_cast<uint4*>(rest + 16 * y + 8 * z) = make_uint4(u[0], u[1], u[2], u[3]);
+                    *reinterpret_cast<uint4*>(out + col) = make_uint4(w[0], w[1], w[2], w[3]);
+                    if (EXACT) *reinterpret_cast<uint4*>(rest + col) = make_uint4(u[0], u[1], u[2], u[3]);
                 }
             }
             if (p.lse_w && i < p.Nq) p.lse_w[((int64_t)b * p.H + h) * p.Nq + i] = l == 0.0f ? -CUDART_INF_F : (m + log2f(l)) * GRF_LN2;
@@ -509,7 +580,9 @@ template <int DP, bool CAP, int BIAS, bool EXACT> int launch(grf_ctx* ctx, const
     const size_t smem = Sh::SMEM + (p.q_doc ? 4 * (size_t)(2 * Sh::QT + 2) * (grf_ceil_div(p.Nk, BT) / 32 + 1) : 0);
     GRF_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     grf_softmax_scope scope(ctx, "grf:softmax_attention");
-    kernel<<<dim3(p.B * p.H, grf_ceil_div(p.Nq, Sh::QT * BT)), Sh::THREADS, smem, ctx->stream>>>(m.q, m.k, m.v, p);
+    // as many CTAs as the device holds at once, which take block after block; with documents a CTA per block
+    const int64_t items = (int64_t)p.B * p.H * grf_ceil_div(p.Nq, Sh::QT * BT), room = (int64_t)ctx->sm_count * Sh::CTAS;
+    kernel<<<(unsigned)(p.q_doc || items < room ? items : room), Sh::THREADS, smem, ctx->stream>>>(m.q, m.k, m.v, p);
     return cudaGetLastError() == cudaSuccess ? GRF_OK : GRF_ERR_CUDA;
 }
 

@@ -93,7 +93,7 @@ def test_calls_that_are_taken(fake, fields):
     (dict(dim=136), -1), (dict(dtype=2), -1), (dict(scale=float("inf")), -1), (dict(scale=float("nan")), -1), (dict(cap=-1.0), -1), (dict(cap=float("inf")), -1),
     (dict(order=3), -1), (dict(order=-1), -1), (dict(order=2), -1), (dict(prefix=SOME), -1), (dict(bias=3), -1), (dict(bias=1), -1), (dict(slopes=SOME), -1),
     (dict(bias=2), -1), (dict(BUCKETS, n_buckets=0), -1), (dict(BUCKETS, n_buckets=65), -1), (dict(BUCKETS, first=[1, 2, 5]), -1),
-    (dict(BUCKETS, first=[0, 5, 5]), -1), (dict(BUCKETS, two_sided=2), -1), (dict(q_doc=SOME), -1), (dict(k_doc=SOME), -1),
+    (dict(BUCKETS, first=[0, 5, 5]), -1), (dict(BUCKETS, first=[0, 5, (1 << 29) + 1]), -1), (dict(BUCKETS, two_sided=2), -1), (dict(q_doc=SOME), -1), (dict(k_doc=SOME), -1),
     (dict(q_stride=[4, 64, 64]), -1), (dict(q_stride=[64, 64, -64]), -1), (dict(k_stride=[1 << 37, 64, 64]), -1), (dict(out_stride=[25600, 0, 64]), -1),
     (dict(out_stride=[25600, 6400, 56]), -1), (dict(out_stride=[6400, 6400, 64]), -1), (dict(out_stride=[64, 64, 128]), -1),
     (dict(n_q=(1 << 22) + 1), -2), (dict(n_k=(1 << 22) + 1), -2), (dict(batch=40000), -2)], ids=str)
