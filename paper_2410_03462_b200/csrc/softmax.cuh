@@ -34,17 +34,38 @@ __host__ __device__ static inline int grf_softmax_columns(const grf_softmax_para
 #define GRF_LOG2E 1.4426950408889634f
 #define GRF_LN2 0.6931471805599453f
 
-__device__ __forceinline__ int32_t grf_bucket(const grf_softmax_params& p, int32_t delta)
-{
-    const int32_t n = p.two_sided ? abs(delta) : max(-delta, 0);
-    int lo = 0, hi = p.n_first;             // the last y with first[y] <= n
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (p.first[mid] <= n) lo = mid;
-        else hi = mid;
+// Buckets of distances, in shared memory: parameters indexed by a thread's own distance are read one address at a time.
+struct grf_buckets {
+    static constexpr int NEAR = 1024;
+    int32_t first[GRF_MAX_BUCKETS];
+    unsigned char near[NEAR];               // of distances below NEAR, where the last bucket starts there
+    __device__ __forceinline__ int32_t searched(const grf_softmax_params& p, int32_t n) const
+    {
+        int lo = 0, hi = p.n_first;         // the last y with first[y] <= n
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (first[mid] <= n) lo = mid;
+            else hi = mid;
+        }
+        return lo;
     }
-    return p.two_sided && delta > 0 ? lo + p.n_first : lo;
-}
+    // by the whole block; a barrier of the block follows
+    __device__ __forceinline__ void fill(const grf_softmax_params& p)
+    {
+        if (p.bias != GRF_BIAS_BUCKETS) return;
+        for (int x = threadIdx.x; x < p.n_first; x += blockDim.x) first[x] = p.first[x];
+        __syncthreads();
+        const int32_t far = p.first[p.n_first - 1];
+        if (far < NEAR)
+            for (int x = threadIdx.x; x <= far; x += blockDim.x) near[x] = (unsigned char)searched(p, x);
+    }
+    __device__ __forceinline__ int32_t operator()(const grf_softmax_params& p, int32_t delta) const
+    {
+        const int32_t n = p.two_sided ? abs(delta) : max(-delta, 0), far = p.first[p.n_first - 1];
+        const int32_t y = far < NEAR ? near[min(n, far)] : searched(p, n);
+        return p.two_sided && delta > 0 ? y + p.n_first : y;
+    }
+};
 
 __device__ __forceinline__ float grf_to_float(float x) { return x; }
 __device__ __forceinline__ float grf_to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
@@ -61,11 +82,11 @@ template <typename T> __device__ __forceinline__ __nv_bfloat16 grf_rest(float x,
 
 // The bias of relative position delta for head h, in units of log 2.
 template <typename T>
-__device__ __forceinline__ float grf_bias2(const grf_softmax_params& p, int32_t h, int32_t delta)
+__device__ __forceinline__ float grf_bias2(const grf_softmax_params& p, const grf_buckets& bucket, int32_t h, int32_t delta)
 {
     float b;
     if (p.bias == GRF_BIAS_SLOPES) b = -p.slopes[h] * fabsf((float)delta);
-    else b = grf_to_float(reinterpret_cast<const T*>(p.table)[(size_t)h * grf_softmax_columns(p) + grf_bucket(p, delta)]);
+    else b = grf_to_float(reinterpret_cast<const T*>(p.table)[(size_t)h * grf_softmax_columns(p) + bucket(p, delta)]);
     // an infinity and NaN stay what they are
     const float b2 = b * GRF_LOG2E;
     return fabsf(b) <= 3.4028235e38f ? fminf(fmaxf(b2, -GRF_BIAS_MOST), GRF_BIAS_MOST) : b2;

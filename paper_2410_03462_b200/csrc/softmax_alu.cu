@@ -142,10 +142,10 @@ template <typename T> __device__ __forceinline__ T* at_head_w(void* base, const 
 __device__ __forceinline__ int4 all_docs() { return make_int4(0, 0, 0, 0); }
 
 // Bias of every diagonal of a tile, index (j - j0) - (i - i0) + BT - 1.
-template <typename T> __device__ __forceinline__ void load_bias(float* lut, const grf_softmax_params& p, int32_t h, int32_t j0, int32_t pos0)
+template <typename T> __device__ __forceinline__ void load_bias(float* lut, const grf_softmax_params& p, const grf_buckets& bucket, int32_t h, int32_t j0, int32_t pos0)
 {
     if (p.bias == GRF_BIAS_NONE) return;
-    for (int x = threadIdx.x; x < 2 * BT - 1; x += THREADS) lut[x] = grf_bias2<T>(p, h, j0 - pos0 + x - (BT - 1));
+    for (int x = threadIdx.x; x < 2 * BT - 1; x += THREADS) lut[x] = grf_bias2<T>(p, bucket, h, j0 - pos0 + x - (BT - 1));
 }
 
 template <typename T, int DP>
@@ -155,8 +155,10 @@ __global__ void __launch_bounds__(THREADS) softmax_alu_forward_kernel(const __gr
     extern __shared__ float smem[];
     float *qs = smem, *ks = qs + A::TILE, *vs = ks + A::TILE, *pt = vs + A::TILE;
     __shared__ float lut[2 * BT];
+    __shared__ grf_buckets bucket;
     __shared__ int bad;
     const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
+    bucket.fill(p);
     const int32_t b = blockIdx.y / p.H, h = blockIdx.y % p.H, i0 = (gridDim.x - 1 - blockIdx.x) * BT, kvh = h / p.group;
     const grf_sight sight(p, b);
     const int32_t *qdoc = sight.docs ? p.q_doc + (int64_t)b * p.Nq : nullptr, *kdoc = sight.docs ? p.k_doc + (int64_t)b * p.Nk : nullptr;
@@ -183,7 +185,7 @@ __global__ void __launch_bounds__(THREADS) softmax_alu_forward_kernel(const __gr
         __syncthreads();
         load_rows<T, DP>(ks, K, p.ks[2], j0, sight.len, p.d, kdoc, false, nullptr);
         load_rows<T, DP>(vs, V, p.vs[2], j0, sight.len, p.d, kdoc, what == 1, &bad);
-        load_bias<T>(lut, p, h, j0, sight.position(i0));
+        load_bias<T>(lut, p, bucket, h, j0, sight.position(i0));
         __syncthreads();
         float s[4][4];
         products<DP>(s, qs, ks, ty, tx);
@@ -304,8 +306,10 @@ __global__ void __launch_bounds__(THREADS) softmax_alu_dq_kernel(const __grid_co
     using A = Alu<DP>;
     extern __shared__ float smem[];
     float *qs = smem, *gs = qs + A::TILE, *ks = gs + A::TILE, *vs = ks + A::TILE, *xt = vs + A::TILE, *st = xt + BT * PS;
+    __shared__ grf_buckets bucket;
     __shared__ float lut[2 * BT], bins[4][2 * GRF_MAX_BUCKETS];   // sums by bucket, of diagonals 32 w .. 32 w + 31 of each tile
     const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
+    bucket.fill(p);
     const int32_t b = blockIdx.y / p.H, h = blockIdx.y % p.H, i0 = (gridDim.x - 1 - blockIdx.x) * BT, kvh = h / p.group;
     const grf_sight sight(p, b);
     const int32_t *qdoc = sight.docs ? p.q_doc + (int64_t)b * p.Nq : nullptr, *kdoc = sight.docs ? p.k_doc + (int64_t)b * p.Nk : nullptr;
@@ -330,7 +334,7 @@ __global__ void __launch_bounds__(THREADS) softmax_alu_dq_kernel(const __grid_co
         __syncthreads();
         load_rows<T, DP>(ks, K, p.ks[2], j0, sight.len, p.d, kdoc, what == 1, nullptr);
         load_rows<T, DP>(vs, V, p.vs[2], j0, sight.len, p.d, kdoc, false, nullptr);
-        load_bias<T>(lut, p, h, j0, sight.position(i0));
+        load_bias<T>(lut, p, bucket, h, j0, sight.position(i0));
         __syncthreads();
         float s[4][4], dp[4][4];
         products<DP>(s, qs, ks, ty, tx);
@@ -354,7 +358,7 @@ __global__ void __launch_bounds__(THREADS) softmax_alu_dq_kernel(const __grid_co
                 float sum = 0.0f;
                 const int delta = tid - (BT - 1);               // j - i
                 for (int i = max(0, -delta); i < min(BT, BT - delta); ++i) sum += st[i * PS + i + delta];
-                grf_add_runs(bins[tid >> 5], tid < 2 * BT - 1 ? grf_bucket(p, j0 - sight.position(i0) + delta) : -1, sum);
+                grf_add_runs(bins[tid >> 5], tid < 2 * BT - 1 ? bucket(p, j0 - sight.position(i0) + delta) : -1, sum);
             }
         }
     }
@@ -377,7 +381,9 @@ __global__ void __launch_bounds__(THREADS) softmax_alu_dkv_kernel(const __grid_c
     extern __shared__ float smem[];
     float *qs = smem, *gs = qs + A::TILE, *ks = gs + A::TILE, *vs = ks + A::TILE, *ps = vs + A::TILE, *xs = ps + BT * PS;
     __shared__ float lut[2 * BT];
+    __shared__ grf_buckets bucket;
     const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
+    bucket.fill(p);
     const int32_t b = blockIdx.y / p.KV, kvh = blockIdx.y % p.KV, j0 = blockIdx.x * BT, j1 = j0 + BT;
     const grf_sight sight(p, b);
     const int32_t *qdoc = sight.docs ? p.q_doc + (int64_t)b * p.Nq : nullptr, *kdoc = sight.docs ? p.k_doc + (int64_t)b * p.Nk : nullptr;
@@ -397,7 +403,7 @@ __global__ void __launch_bounds__(THREADS) softmax_alu_dkv_kernel(const __grid_c
         __syncthreads();
         load_rows<T, DP>(qs, at_head<T>(p.q, p.qs, b, h), p.qs[2], i0, p.Nq, p.d, qdoc, what == 1, nullptr);
         load_rows<T, DP>(gs, at_head<T>(p.dout, p.dos, b, h), p.dos[2], i0, p.Nq, p.d, qdoc, what == 1, nullptr);
-        load_bias<T>(lut, p, h, j0, sight.position(i0));
+        load_bias<T>(lut, p, bucket, h, j0, sight.position(i0));
         __syncthreads();
         float s[4][4], dp[4][4];
         products<DP>(s, qs, ks, ty, tx);

@@ -175,6 +175,7 @@ __global__ void __launch_bounds__(THREADS) softmax_few_bf16_kernel(const __grid_
     constexpr int DP = 32 * DG, ROWS = 8 * NB;
     extern __shared__ __align__(16) unsigned char smem[];
     FewShared<ROWS, DP>& sh = *reinterpret_cast<FewShared<ROWS, DP>*>(smem);
+    __shared__ grf_buckets bucket;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int32_t unit = blockIdx.x / f.splits, split = blockIdx.x % f.splits, b = unit / (p.KV * f.row_blocks), kvh = unit / f.row_blocks % p.KV, r0 = unit % f.row_blocks * ROWS;
     const grf_sight sight(p, b);
@@ -197,6 +198,8 @@ __global__ void __launch_bounds__(THREADS) softmax_few_bf16_kernel(const __grid_
     };
     load(kr, K, p.ks[2], t0 + warp);
     load(vr, V, p.vs[2], t0 + warp);
+    bucket.fill(p);
+    __syncthreads();
     // Q as the right operand: row g of a block of eight, in the order of the keys' dimensions
     uint4 q[NB][DG];
     few_row row[NB][2];
@@ -246,7 +249,7 @@ __global__ void __launch_bounds__(THREADS) softmax_few_bf16_kernel(const __grid_
                 for (int e = 0; e < 2; ++e) {
                     const int32_t j = tile * 16 + 8 * y + g;
                     float x = capped2(p, s[n][2 * y + e]);
-                    if (p.bias != GRF_BIAS_NONE) x += grf_bias2<__nv_bfloat16>(p, row[n][e].h, j - row[n][e].pos);
+                    if (p.bias != GRF_BIAS_NONE) x += grf_bias2<__nv_bfloat16>(p, bucket, row[n][e].h, j - row[n][e].pos);
                     if (partial && !row[n][e].sees(sight, kdoc, j)) x = -CUDART_INF_F;
                     s[n][2 * y + e] = x;
                 }
@@ -340,6 +343,7 @@ __global__ void __launch_bounds__(THREADS) softmax_few_f32_kernel(const __grid_c
     constexpr int DP = 32 * DG, NC = 2 * DG, U = DG <= 2 ? 2 : 1;
     extern __shared__ __align__(16) unsigned char smem[];
     FewShared<ROWS, DP>& sh = *reinterpret_cast<FewShared<ROWS, DP>*>(smem);
+    __shared__ grf_buckets bucket;
     __shared__ float4 q[ROWS][DP / 4];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int32_t unit = blockIdx.x / f.splits, split = blockIdx.x % f.splits, b = unit / (p.KV * f.row_blocks), kvh = unit / f.row_blocks % p.KV, r0 = unit % f.row_blocks * ROWS;
@@ -365,6 +369,7 @@ __global__ void __launch_bounds__(THREADS) softmax_few_f32_kernel(const __grid_c
     };
     load(kr, K, p.ks[2], t0 + warp * U);
     load(vr, V, p.vs[2], t0 + warp * U);
+    bucket.fill(p);
     for (int x = threadIdx.x; x < ROWS * (DP / 4); x += THREADS) {
         const int r = x / (DP / 4), c = x % (DP / 4);
         few_row w;
@@ -426,7 +431,7 @@ __global__ void __launch_bounds__(THREADS) softmax_few_f32_kernel(const __grid_c
             for (int r = 0; r < ROWS; ++r) {
                 float y = capped2(p, x[u][r]);
                 if (p.bias == GRF_BIAS_SLOPES) y = fmaf(slope2[r], fabsf((float)(j - row[r].pos)), y);
-                if (p.bias == GRF_BIAS_BUCKETS) y += grf_bias2<float>(p, row[r].h, j - row[r].pos);
+                if (p.bias == GRF_BIAS_BUCKETS) y += grf_bias2<float>(p, bucket, row[r].h, j - row[r].pos);
                 if (tile + u >= t1 || (partial && !row[r].sees(sight, kdoc, j))) y = -CUDART_INF_F;
                 x[u][r] = y;
                 grow |= y > m[r] + 8.0f;

@@ -33,10 +33,12 @@ template <int DP, bool EXACT> struct Fwd {
     static constexpr int MORE = DP == 64 ? 200 : 208, LESS = DP == 64 ? 56 : 88;   // registers: QT * MORE + LESS = the launch's
 };
 
+constexpr int BIAS_NONE_SCALED = 3;     // no bias, scores scaled before anything else
+
 struct forward_tiles {
     const grf_softmax_params& p;
     const grf_sight& sight;
-    const uint32_t* bits;                                       // [seen, whole] per group, then of any group, then tiles with a token of no document
+    const uint32_t* bits;                                       // [seen, whole, one document] per group, then seen by any, then tiles with a token of no document
     int32_t i0, tiles, words;
     int32_t last;                                               // one past the last key that any query of the sequence can see
     // queries of group g
@@ -44,14 +46,16 @@ struct forward_tiles {
     __device__ __forceinline__ int what(int g, int32_t t) const
     {
         if (from(g) >= p.Nq) return 0;
-        if (sight.docs) return bit(bits + 2 * g * words, t) ? (bit(bits + (2 * g + 1) * words, t) ? 2 : 1) : 0;
+        if (sight.docs) return bit(bits + 3 * g * words, t) ? (bit(bits + (3 * g + 1) * words, t) ? 2 : 1) : 0;
         return sight.tile(from(g), min(from(g) + BT, p.Nq), t * BT, t * BT + BT, make_int4(0, 0, 0, 0), make_int4(0, 0, 0, 0));
     }
+    // whether documents have to be compared in a tile
+    __device__ __forceinline__ bool mixed(int g, int32_t t) const { return sight.docs && !bit(bits + (3 * g + 2) * words, t); }
     // the first tile from t on that any group sees
     template <int QT> __device__ __forceinline__ int32_t next(int32_t t) const
     {
         if (!sight.docs) return t;
-        const uint32_t* any = bits + 2 * QT * words;
+        const uint32_t* any = bits + 3 * QT * words;
         while (t < tiles) {
             const uint32_t w = any[t >> 5] >> (t & 31);
             if (w) return min(t + __ffs(w) - 1, tiles);
@@ -61,14 +65,14 @@ struct forward_tiles {
     }
     template <int QT> __device__ __forceinline__ bool unclean(int32_t t) const
     {
-        return (last < p.Nk && t * BT + BT > last) || (sight.docs && bit(bits + (2 * QT + 1) * words, t));
+        return (last < p.Nk && t * BT + BT > last) || (sight.docs && bit(bits + (3 * QT + 1) * words, t));
     }
 };
 
 // The outputs of row i from the keys that it sees, where a value that it does not see has spoilt them: the warp together, lanes take keys for
 // the scores and columns for the sums.  Rare, and only columns that are not finite are replaced.
 template <bool CAP>
-__device__ __noinline__ void redo_row(const grf_softmax_params& p, int32_t b, int32_t h, int32_t i, float m, float l)
+__device__ __noinline__ void redo_row(const grf_softmax_params& p, const grf_buckets& bucket, int32_t b, int32_t h, int32_t i, float m, float l)
 {
     const grf_sight sight(p, b);
     const int lane = threadIdx.x & 31;
@@ -86,7 +90,7 @@ __device__ __noinline__ void redo_row(const grf_softmax_params& p, int32_t b, in
         if (seen) {
             for (int c = 0; c < p.d; ++c) w = fmaf(__bfloat162float(Q[c]), __bfloat162float(K[(int64_t)j * p.ks[2] + c]), w);
             w = CAP ? p.cap * GRF_LOG2E * tanh_any(w * (p.scale / p.cap)) : w * (p.scale * GRF_LOG2E);
-            if (p.bias != GRF_BIAS_NONE) w += grf_bias2<__nv_bfloat16>(p, h, j - pos);
+            if (p.bias != GRF_BIAS_NONE) w += grf_bias2<__nv_bfloat16>(p, bucket, h, j - pos);
             w = __bfloat162float(__float2bfloat16_rn(ex2(w - m)));
         }
         const uint32_t who = __ballot_sync(0xffffffffu, seen);
@@ -119,12 +123,15 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
 {
     using Sh = Fwd<DP, EXACT>;
     constexpr int QT = Sh::QT, NS = Sh::NS, QB = Sh::QB;
+    constexpr bool PLAIN = BIAS == GRF_BIAS_NONE && !CAP;   // (a scale that is not positive: BIAS_NONE_SCALED)
     extern __shared__ unsigned char smem_dyn[];
     constexpr int PER_GROUP = 6 + 2 * QB;
     __shared__ __align__(8) unsigned long long bars[5 * NS + PER_GROUP * QT];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
     __shared__ float lut[BIAS == GRF_BIAS_BUCKETS ? QT * 2 * 256 : 1];
+    __shared__ __align__(16) int32_t doc_of[QT * 2 * BT];
+    __shared__ grf_buckets bucket;
     const int tid = threadIdx.x, lane = tid & 31, warp = uniform(tid >> 5);
     const uint32_t smem = (smem_u32(smem_dyn) + 1023u) & ~1023u;
     uint32_t* bits = reinterpret_cast<uint32_t*>(smem_dyn + (smem - smem_u32(smem_dyn)) + Sh::TILE * (QT * QB + 2 * NS));
@@ -172,6 +179,7 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == COPY) tmem_alloc(&tmem_slot, Sh::TMEM);
+    if (BIAS == GRF_BIAS_BUCKETS) bucket.fill(p);
     if (p.q_doc) {
         const int32_t b = bh_of(blockIdx.x) / p.H, i0 = i0_of(blockIdx.x);
         const grf_sight sight(p, b);
@@ -184,14 +192,18 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             uint32_t any = 0u;
             for (int g = 0; g < QT; ++g) {
                 int what = 0;
-                if (t < tiles && T.from(g) < p.Nq)
-                    what = sight.tile(T.from(g), min(T.from(g) + BT, p.Nq), t * BT, t * BT + BT, p.q_range[(int64_t)b * qblocks + T.from(g) / BT], kr);
-                const uint32_t seen = __ballot_sync(0xffffffffu, what != 0), whole = __ballot_sync(0xffffffffu, what == 2);
+                bool same = true;
+                if (t < tiles && T.from(g) < p.Nq) {
+                    const int4 qr = p.q_range[(int64_t)b * qblocks + T.from(g) / BT];
+                    what = sight.tile(T.from(g), min(T.from(g) + BT, p.Nq), t * BT, t * BT + BT, qr, kr);
+                    same = one_document(qr, kr);
+                }
+                const uint32_t seen = __ballot_sync(0xffffffffu, what != 0), whole = __ballot_sync(0xffffffffu, what == 2), one = __ballot_sync(0xffffffffu, same);
                 any |= seen;
-                if (lane == 0) { bits[2 * g * T.words + w] = seen; bits[(2 * g + 1) * T.words + w] = whole; }
+                if (lane == 0) { bits[3 * g * T.words + w] = seen; bits[(3 * g + 1) * T.words + w] = whole; bits[(3 * g + 2) * T.words + w] = one; }
             }
             const uint32_t hole = __ballot_sync(0xffffffffu, kr.z != 0);
-            if (lane == 0) { bits[2 * QT * T.words + w] = any; bits[(2 * QT + 1) * T.words + w] = hole; }
+            if (lane == 0) { bits[3 * QT * T.words + w] = any; bits[(3 * QT + 1) * T.words + w] = hole; }
         }
     }
     fence_before_sync();
@@ -371,32 +383,38 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             const forward_tiles T{p, sight, bits, i0, tiles, (tiles + 31) / 32, 0};
             const int32_t i = T.from(g) + r, pos = sight.position(i), pos0 = sight.position(T.from(g));
             const int32_t limit = sight.order == GRF_ORDER_FULL ? sight.len : min(sight.len, max(pos + 1, sight.prefix));
-            const int32_t doc = sight.docs && i < p.Nq ? p.q_doc[(int64_t)b * p.Nq + i] : -1;
+            int32_t doc = sight.docs && i < p.Nq ? p.q_doc[(int64_t)b * p.Nq + i] : -1;
+            if (doc < 0) doc = INT32_MIN;                       // (equal to no key's)
             const float slope2 = BIAS == GRF_BIAS_SLOPES ? p.slopes[h] * GRF_LOG2E : 0.0f;
             float m = -CUDART_INF_F;
-            uint64_t sum2[2] = {0ull, 0ull};
+            uint64_t sum2[4] = {0ull, 0ull, 0ull, 0ull};
             int32_t c = 0;
             for (int32_t t = T.next<QT>(0); t < tiles; t = T.next<QT>(t + 1)) {
                 const int what = T.what(g, t);
                 if (what == 0) continue;
                 const int32_t j0 = t * BT;
-                // the bias of this tile: one value, or one per diagonal
+                // the bias of this tile: one value, or one per diagonal; documents of its keys where they have to be compared
                 float bias2 = 0.0f;
                 bool diagonals = false;
+                const bool mixed = what == 1 && T.mixed(g, t);
                 const float* mine = lut;
+                const int32_t* docs = doc_of + (g * 2 + (luts & 1)) * BT;
                 if (BIAS == GRF_BIAS_BUCKETS) {
-                    const int32_t near = grf_bucket(p, j0 - pos0 - (BT - 1)), far = grf_bucket(p, j0 + BT - 1 - pos0);
-                    diagonals = near != far;
-                    if (diagonals) {
+                    diagonals = bucket(p, j0 - pos0 - (BT - 1)) != bucket(p, j0 + BT - 1 - pos0);
+                    if (!diagonals) bias2 = grf_bias2<__nv_bfloat16>(p, bucket, h, j0 - pos0);
+                }
+                if (diagonals || mixed) {
+                    if (BIAS == GRF_BIAS_BUCKETS && diagonals) {
                         float* at = lut + (g * 2 + (luts & 1)) * 256;
-                        at[r] = grf_bias2<__nv_bfloat16>(p, h, j0 - pos0 + r - (BT - 1));
-                        at[r + BT] = grf_bias2<__nv_bfloat16>(p, h, j0 - pos0 + r + 1);
+                        at[r] = grf_bias2<__nv_bfloat16>(p, bucket, h, j0 - pos0 + r - (BT - 1));
+                        at[r + BT] = grf_bias2<__nv_bfloat16>(p, bucket, h, j0 - pos0 + r + 1);
                         mine = at + (BT - 1 - r);
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(lut_full(g));
-                        if (!(ok = wait(lut_full(g), (uint32_t)luts & 1u))) break;
-                        ++luts;
-                    } else bias2 = grf_bias2<__nv_bfloat16>(p, h, j0 - pos0);
+                    }
+                    if (mixed) const_cast<int32_t*>(docs)[r] = j0 + r < p.Nk ? p.k_doc[(int64_t)b * p.Nk + j0 + r] : -1;
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(lut_full(g));
+                    if (!(ok = wait(lut_full(g), (uint32_t)luts & 1u))) break;
+                    ++luts;
                 }
                 if (!(ok = wait(s_full(g), (uint32_t)done & 1u))) break;
                 fence_after_sync();
@@ -409,37 +427,57 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                     __syncwarp();
                     if (lane == 0) mbar_arrive(s_read(g));
                 }
-                float top = -CUDART_INF_F;
-                const float ahead = (float)(j0 - pos);          // (exact, as are its sums, below 2^24; beyond, off by half a step as the distance itself)
-                const uint64_t to22 = pack2(to2, to2), bias22 = pack2(bias2, bias2);
-#pragma unroll
-                for (int y = 0; y < 8; ++y)
-#pragma unroll
-                    for (int e = 0; e < 16; e += 2) {
-                        const int col = 16 * y + e;
-                        float x0, x1;
-                        if (CAP) {
-                            x0 = cap2 * tanh_any(__uint_as_float(sv[y][e]) * by_cap) + bias2;
-                            x1 = cap2 * tanh_any(__uint_as_float(sv[y][e + 1]) * by_cap) + bias2;
-                        } else unpack2(fma2(pack2(sv[y][e], sv[y][e + 1]), to22, bias22), x0, x1);
-                        if (BIAS == GRF_BIAS_SLOPES) {
-                            x0 = fmaf(-slope2, fabsf(ahead + (float)col), x0);
-                            x1 = fmaf(-slope2, fabsf(ahead + (float)(col + 1)), x1);
-                        }
-                        if (BIAS == GRF_BIAS_BUCKETS) {
-                            if (diagonals) { x0 += mine[col]; x1 += mine[col + 1]; }
-                        }
-                        sv[y][e] = __float_as_uint(x0);
-                        sv[y][e + 1] = __float_as_uint(x1);
-                    }
-                if (what == 1) {
-                    if (sight.docs) {
-                        const int32_t* kd = p.k_doc + (int64_t)b * p.Nk + j0;
+                // scores in units of log 2 (PLAIN: still to be scaled, by a positive number)
+                if (CAP) capped<8>(sv, by_cap);
+                if (!PLAIN) {
+                    const uint64_t by = CAP ? pack2(cap2, cap2) : pack2(to2, to2);
+                    const float ahead = (float)(j0 - pos);      // (exact, as are its sums, below 2^24; beyond, off by half a step as the distance itself)
+                    if (BIAS == GRF_BIAS_SLOPES && __all_sync(0xffffffffu, j0 + BT - 1 <= pos)) {
+                        // every key before the query: a line
+                        const uint64_t s2 = pack2(slope2, slope2), b2 = pack2(slope2 * ahead, slope2 * ahead);
 #pragma unroll
                         for (int y = 0; y < 8; ++y)
 #pragma unroll
-                            for (int e = 0; e < 16; ++e)
-                                if (!(j0 + 16 * y + e < limit && doc >= 0 && __ldg(kd + 16 * y + e) == doc)) sv[y][e] = 0xff800000u;
+                            for (int e = 0; e < 16; e += 2) {
+                                const uint64_t line = fma2(s2, pack2((float)(16 * y + e), (float)(16 * y + e + 1)), b2);
+                                float x0, x1;
+                                unpack2(fma2(pack2(sv[y][e], sv[y][e + 1]), by, line), x0, x1);
+                                sv[y][e] = __float_as_uint(x0);
+                                sv[y][e + 1] = __float_as_uint(x1);
+                            }
+                    } else {
+                        const uint64_t bias22 = pack2(bias2, bias2);
+#pragma unroll
+                        for (int y = 0; y < 8; ++y)
+#pragma unroll
+                            for (int e = 0; e < 16; e += 2) {
+                                const int col = 16 * y + e;
+                                float x0, x1;
+                                unpack2(fma2(pack2(sv[y][e], sv[y][e + 1]), by, bias22), x0, x1);
+                                if (BIAS == GRF_BIAS_SLOPES) {
+                                    x0 = fmaf(-slope2, fabsf(ahead + (float)col), x0);
+                                    x1 = fmaf(-slope2, fabsf(ahead + (float)(col + 1)), x1);
+                                }
+                                if (BIAS == GRF_BIAS_BUCKETS) {
+                                    if (diagonals) { x0 += mine[col]; x1 += mine[col + 1]; }
+                                }
+                                sv[y][e] = __float_as_uint(x0);
+                                sv[y][e + 1] = __float_as_uint(x1);
+                            }
+                    }
+                }
+                if (what == 1) {
+                    if (mixed) {
+#pragma unroll
+                        for (int y = 0; y < 8; ++y)
+#pragma unroll
+                            for (int e = 0; e < 16; e += 4) {
+                                const int4 d4 = *reinterpret_cast<const int4*>(docs + 16 * y + e);
+                                if (!(j0 + 16 * y + e < limit && d4.x == doc)) sv[y][e] = 0xff800000u;
+                                if (!(j0 + 16 * y + e + 1 < limit && d4.y == doc)) sv[y][e + 1] = 0xff800000u;
+                                if (!(j0 + 16 * y + e + 2 < limit && d4.z == doc)) sv[y][e + 2] = 0xff800000u;
+                                if (!(j0 + 16 * y + e + 3 < limit && d4.w == doc)) sv[y][e + 3] = 0xff800000u;
+                            }
                     } else {
 #pragma unroll
                         for (int y = 0; y < 8; ++y)
@@ -448,10 +486,14 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                                 if (j0 + 16 * y + e >= limit) sv[y][e] = 0xff800000u;
                     }
                 }
+                // (four chains: one of 64 steps would take longer than the exponentials)
+                float top4[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
 #pragma unroll
                 for (int y = 0; y < 8; ++y)
 #pragma unroll
-                    for (int e = 0; e < 16; e += 2) top = max3(top, __uint_as_float(sv[y][e]), __uint_as_float(sv[y][e + 1]));
+                    for (int e = 0; e < 16; e += 2) top4[e >> 1 & 3] = max3(top4[e >> 1 & 3], __uint_as_float(sv[y][e]), __uint_as_float(sv[y][e + 1]));
+                float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3]));
+                if (PLAIN) top *= to2;
                 // a new maximum only when it matters: 2^8 above the one in use (or the first)
                 const bool grow = top > m + 8.0f;
                 if (__any_sync(0xffffffffu, grow)) {
@@ -461,8 +503,8 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                         if (!(ok = wait(pv_done(g), (uint32_t)(done - 1) & 1u))) break;
                         fence_after_sync();
                         const uint64_t a2 = pack2(alpha, alpha);
-                        sum2[0] = mul2(sum2[0], a2);
-                        sum2[1] = mul2(sum2[1], a2);
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) sum2[y] = mul2(sum2[y], a2);
 #pragma unroll
                         for (int y = 0; y < DP / 16; ++y) {
                             uint32_t o[16];
@@ -478,7 +520,7 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                     fence_after_sync();
                 }
                 const float base = m == -CUDART_INF_F ? 0.0f : m;
-                const uint64_t minus = pack2(-base, -base);
+                const uint64_t minus = pack2(-base, -base), to22 = pack2(to2, to2);
 #pragma unroll
                 for (int y = 0; y < 4; ++y) {
                     uint32_t w[16], u[EXACT ? 16 : 1];
@@ -486,10 +528,10 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                     for (int e = 0; e < 16; ++e) {
                         const int a = 2 * y + (e >> 3), z = (2 * e) & 15;
                         float x0, x1;
-                        unpack2(add2(pack2(sv[a][z], sv[a][z + 1]), minus), x0, x1);
+                        unpack2(PLAIN ? fma2(pack2(sv[a][z], sv[a][z + 1]), to22, minus) : add2(pack2(sv[a][z], sv[a][z + 1]), minus), x0, x1);
                         x0 = ex2(x0);
                         x1 = ex2(x1);
-                        sum2[e & 1] = add2(sum2[e & 1], pack2(x0, x1));
+                        sum2[e & 3] = add2(sum2[e & 3], pack2(x0, x1));
                         w[e] = pack_bf16(x0, x1);
                         if (EXACT) u[EXACT ? e : 0] = pack_bf16(x0 - __uint_as_float(w[e] << 16), x1 - __uint_as_float(w[e] & 0xffff0000u));
                     }
@@ -507,10 +549,9 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             if (ok && c > 0) ok = wait(pv_done(g), (uint32_t)(done - 1) & 1u);
             if (!ok) break;
             fence_after_sync();
-            float l0, l1, l2, l3;
-            unpack2(sum2[0], l0, l1);
-            unpack2(sum2[1], l2, l3);
-            const float l = (l0 + l1) + (l2 + l3), inv = l == 0.0f ? 0.0f : 1.0f / l;
+            float l0, l1;
+            unpack2(add2(add2(sum2[0], sum2[1]), add2(sum2[2], sum2[3])), l0, l1);
+            const float l = l0 + l1, inv = l == 0.0f ? 0.0f : 1.0f / l;
             bool spoilt = false;
             __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.out_w) + b * p.os[0] + h * p.os[1] + (int64_t)i * p.os[2];
             __nv_bfloat16* rest = p.rest_w ? p.rest_w + (((int64_t)b * p.H + h) * p.Nq + i) * p.d : nullptr;
@@ -560,7 +601,7 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             while (again) {
                 const int y = __ffs(again) - 1;
                 again &= again - 1;
-                redo_row<CAP>(p, b, h, __shfl_sync(0xffffffffu, i, y), __shfl_sync(0xffffffffu, m, y), __shfl_sync(0xffffffffu, l, y));
+                redo_row<CAP>(p, bucket, b, h, __shfl_sync(0xffffffffu, i, y), __shfl_sync(0xffffffffu, m, y), __shfl_sync(0xffffffffu, l, y));
             }
         }
         fence_before_sync();
@@ -577,7 +618,7 @@ template <int DP, bool CAP, int BIAS, bool EXACT> int launch(grf_ctx* ctx, const
 {
     using Sh = Fwd<DP, EXACT>;
     const auto kernel = softmax_tc_forward_kernel<DP, CAP, BIAS, EXACT>;
-    const size_t smem = Sh::SMEM + (p.q_doc ? 4 * (size_t)(2 * Sh::QT + 2) * (grf_ceil_div(p.Nk, BT) / 32 + 1) : 0);
+    const size_t smem = Sh::SMEM + (p.q_doc ? 4 * (size_t)(3 * Sh::QT + 2) * (grf_ceil_div(p.Nk, BT) / 32 + 1) : 0);
     GRF_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     grf_softmax_scope scope(ctx, "grf:softmax_attention");
     // as many CTAs as the device holds at once, which take block after block; with documents a CTA per block
@@ -588,6 +629,8 @@ template <int DP, bool CAP, int BIAS, bool EXACT> int launch(grf_ctx* ctx, const
 
 template <int DP, bool EXACT, bool CAP> int by_bias(grf_ctx* ctx, const grf_softmax_params& p, const forward_maps& m)
 {
+    if constexpr (!CAP)
+        if (p.bias == GRF_BIAS_NONE && !(p.scale > 0.0f)) return launch<DP, CAP, BIAS_NONE_SCALED, EXACT>(ctx, p, m);
     return p.bias == GRF_BIAS_NONE ? launch<DP, CAP, GRF_BIAS_NONE, EXACT>(ctx, p, m)
          : p.bias == GRF_BIAS_SLOPES ? launch<DP, CAP, GRF_BIAS_SLOPES, EXACT>(ctx, p, m) : launch<DP, CAP, GRF_BIAS_BUCKETS, EXACT>(ctx, p, m);
 }

@@ -27,7 +27,7 @@ template <int DP> struct Grad {
 
 // Tiles of the other side that a block sees, in order; with documents from bits in shared memory.
 struct grad_tiles {
-    const uint32_t* bits;               // seen, whole, tiles with a token of no document
+    const uint32_t* bits;               // seen, whole, tiles with a key of no document, tiles of one document
     int32_t first, tiles, words;
     bool docs;
     __device__ __forceinline__ int32_t next(int32_t t) const
@@ -42,6 +42,7 @@ struct grad_tiles {
     }
     __device__ __forceinline__ int32_t begin() const { return next(first); }
     __device__ __forceinline__ bool whole(int32_t t) const { return bit(bits + words, t); }
+    __device__ __forceinline__ bool mixed(int32_t t) const { return docs && !bit(bits + 3 * words, t); }
     __device__ __forceinline__ bool hole(int32_t t) const { return docs && bit(bits + 2 * words, t); }
 };
 
@@ -78,6 +79,8 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
     __shared__ float lut[LUTS ? 2 * 256 : 1];
+    __shared__ grf_buckets bucket;
+    __shared__ __align__(16) int32_t doc_of[2 * BT];
     __shared__ float bins[LUTS ? WORKERS * 2 * GRF_MAX_BUCKETS : 1];
     __shared__ float diag[LUTS ? WORKERS * 96 : 1];
     const int tid = threadIdx.x, lane = tid & 31, warp = uniform(tid >> 5);
@@ -110,6 +113,7 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == COPY) tmem_alloc(&tmem_slot, 512u);
+    if (LUTS) bucket.fill(p);
     if (sight.docs) {
         const int32_t kblocks = (p.Nk + BT - 1) / BT, qblocks = (p.Nq + BT - 1) / BT;
         const int4 qr = p.q_range[(int64_t)b * qblocks + qb];
@@ -117,8 +121,9 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             const int32_t t = w * 32 + lane;
             const int4 kr = t < tiles ? p.k_range[(int64_t)b * kblocks + t] : make_int4(INT32_MAX, -1, 0, 0);
             const int what = t < tiles ? sight.tile(i0, i1, t * BT, t * BT + BT, qr, kr) : 0;
-            const uint32_t seen = __ballot_sync(0xffffffffu, what != 0), whole = __ballot_sync(0xffffffffu, what == 2), hole = __ballot_sync(0xffffffffu, kr.z != 0);
-            if (lane == 0) { bits[w] = seen; bits[T.words + w] = whole; bits[2 * T.words + w] = hole; }
+            const uint32_t seen = __ballot_sync(0xffffffffu, what != 0), whole = __ballot_sync(0xffffffffu, what == 2), hole = __ballot_sync(0xffffffffu, kr.z != 0),
+                           one_doc = __ballot_sync(0xffffffffu, one_document(qr, kr));
+            if (lane == 0) { bits[w] = seen; bits[T.words + w] = whole; bits[2 * T.words + w] = hole; bits[3 * T.words + w] = one_doc; }
         }
     }
     if (LUTS)
@@ -230,7 +235,8 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         const int r = (warp & 3) * 32 + lane, part = warp >> 2, c0 = part * 64;
         const int32_t i = i0 + r, pos = sight.position(i), pos0 = sight.position(i0);
         const int32_t limit = sight.order == GRF_ORDER_FULL ? sight.len : min(sight.len, max(pos + 1, sight.prefix));
-        const int32_t doc = sight.docs && i < p.Nq ? p.q_doc[(int64_t)b * p.Nq + i] : -1;
+        int32_t doc = sight.docs && i < p.Nq ? p.q_doc[(int64_t)b * p.Nq + i] : -1;
+        if (doc < 0) doc = INT32_MIN;                           // (equal to no key's)
         const int64_t row = ((int64_t)b * p.H + h) * p.Nq + i;
         const float lse = i < p.Nq ? p.lse[row] : -CUDART_INF_F, dsum = i < p.Nq ? p.dsum[row] : 0.0f;
         const bool any = lse != -CUDART_INF_F;                  // a row without a key: P = 0
@@ -259,18 +265,24 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             bool diagonals = false;
             int32_t bucket0 = 0;
             const float* mine = lut;
+            const bool mixed = partial && T.mixed(t);           // documents have to be compared
+            int32_t* docs = doc_of + (luts & 1) * BT;
             if (LUTS) {
-                bucket0 = grf_bucket(p, j0 - pos0 - (BT - 1));
-                diagonals = bucket0 != grf_bucket(p, j0 + BT - 1 - pos0);
-                if (diagonals) {
+                bucket0 = bucket(p, j0 - pos0 - (BT - 1));
+                diagonals = bucket0 != bucket(p, j0 + BT - 1 - pos0);
+                if (!diagonals) bias2 = grf_bias2<__nv_bfloat16>(p, bucket, h, j0 - pos0);
+            }
+            if (diagonals || mixed) {
+                if (LUTS && diagonals) {
                     float* at = lut + (luts & 1) * 256;
-                    at[tid] = tid < 2 * BT - 1 ? grf_bias2<__nv_bfloat16>(p, h, j0 - pos0 + tid - (BT - 1)) : 0.0f;
+                    at[tid] = tid < 2 * BT - 1 ? grf_bias2<__nv_bfloat16>(p, bucket, h, j0 - pos0 + tid - (BT - 1)) : 0.0f;
                     mine = at + (BT - 1 - r) + c0;
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(lut_full);
-                    if (!(ok = wait(lut_full, (uint32_t)luts & 1u))) break;
-                    ++luts;
-                } else bias2 = grf_bias2<__nv_bfloat16>(p, h, j0 - pos0);
+                }
+                if (mixed && tid < BT) docs[tid] = j0 + tid < p.Nk ? p.k_doc[(int64_t)b * p.Nk + j0 + tid] : -1;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(lut_full);
+                if (!(ok = wait(lut_full, (uint32_t)luts & 1u))) break;
+                ++luts;
             }
             if (!(ok = wait(s_full0 + 8 * (n & 1), (uint32_t)(n >> 1) & 1u))) break;
             fence_after_sync();
@@ -281,14 +293,14 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
 #pragma unroll
                 for (int y = 0; y < 4; ++y) tmem_ld16_nowait(tmem + (n & 1) * BT + c0 + 16 * y + lanes, sv[y]);
                 tmem_ld_wait();
+                if (CAP) capped<4>(sv, by_cap);
 #pragma unroll
                 for (int e = 0; e < 64; ++e) {
                     const float raw = __uint_as_float(sv[e / 16][e % 16]);
                     float s;
                     if (CAP) {
-                        const float th = tanh_any(raw * by_cap);
-                        dcap[e] = fmaf(-th, th, 1.0f);
-                        s = fmaf(cap2, th, bias2);
+                        dcap[e] = fmaf(-raw, raw, 1.0f);
+                        s = fmaf(cap2, raw, bias2);
                     } else s = fmaf(raw, to2, bias2);
                     if (BIAS == GRF_BIAS_SLOPES) s = fmaf(-slope2, fabsf(ahead + (float)e), s);
                     if (LUTS) { if (diagonals) s += mine[e]; }
@@ -297,10 +309,21 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             }
             const bool careful = partial || !any;               // (of this row: nothing in it may meet an infinity or NaN)
             if (careful) {
-                const int32_t* kd = p.k_doc + (int64_t)b * p.Nk + j0 + c0;
+                const int32_t to = any ? limit - j0 - c0 : 0;
+                if (mixed) {
 #pragma unroll
-                for (int e = 0; e < 64; ++e)
-                    if (!(j0 + c0 + e < limit && any && (!sight.docs || (doc >= 0 && __ldg(kd + e) == doc)))) x[e] = 0.0f;
+                    for (int e = 0; e < 64; e += 4) {
+                        const int4 d4 = *reinterpret_cast<const int4*>(docs + c0 + e);
+                        if (!(e < to && d4.x == doc)) x[e] = 0.0f;
+                        if (!(e + 1 < to && d4.y == doc)) x[e + 1] = 0.0f;
+                        if (!(e + 2 < to && d4.z == doc)) x[e + 2] = 0.0f;
+                        if (!(e + 3 < to && d4.w == doc)) x[e + 3] = 0.0f;
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 64; ++e)
+                        if (e >= to) x[e] = 0.0f;
+                }
             }
             if (!(ok = wait(dp_full, (uint32_t)n & 1u))) break;
             fence_after_sync();
@@ -352,7 +375,7 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
 #pragma unroll
                     for (int z = 0; z < 3; ++z) {
                         const int d = lane + 32 * z;
-                        grf_add_runs(my_bins, d < 95 ? grf_bucket(p, j0 + c0 + d - 31 - sight.position(i0 + (warp & 3) * 32)) : -1, d < 95 ? at[d] : 0.0f);
+                        grf_add_runs(my_bins, d < 95 ? bucket(p, j0 + c0 + d - 31 - sight.position(i0 + (warp & 3) * 32)) : -1, d < 95 ? at[d] : 0.0f);
                     }
                     __syncwarp();
                 }
@@ -407,6 +430,7 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
     __shared__ float lut[LUTS ? 2 * 256 : 1];
+    __shared__ grf_buckets bucket;
     __shared__ __align__(16) float info[NS][2][BT];             // lse (in units of log 2; infinity where P = 0) and D of a tile's queries
     __shared__ __align__(16) int32_t info_doc[NS][BT];
     const int tid = threadIdx.x, lane = tid & 31, warp = uniform(tid >> 5);
@@ -441,14 +465,17 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == COPY) tmem_alloc(&tmem_slot, 512u);
+    if (LUTS) bucket.fill(p);
     if (sight.docs) {
         const int4 kr = p.k_range[(int64_t)b * gridDim.y + blockIdx.y];
         for (int32_t w = warp; w < T.words; w += THREADS / 32) {
             const int32_t t = w * 32 + lane;
             const bool in = t >= first && t < qblocks;
-            const int what = in ? sight.tile(t * BT, min(t * BT + BT, p.Nq), j0, j0 + BT, p.q_range[(int64_t)b * qblocks + t], kr) : 0;
-            const uint32_t seen = __ballot_sync(0xffffffffu, what != 0), whole = __ballot_sync(0xffffffffu, what == 2);
-            if (lane == 0) { bits[w] = seen; bits[T.words + w] = whole; bits[2 * T.words + w] = 0u; }
+            const int4 qr = in ? p.q_range[(int64_t)b * qblocks + t] : make_int4(INT32_MAX, -1, 0, 0);
+            const int what = in ? sight.tile(t * BT, min(t * BT + BT, p.Nq), j0, j0 + BT, qr, kr) : 0;
+            const uint32_t seen = __ballot_sync(0xffffffffu, what != 0), whole = __ballot_sync(0xffffffffu, what == 2),
+                           one_doc = __ballot_sync(0xffffffffu, one_document(qr, kr));
+            if (lane == 0) { bits[w] = seen; bits[T.words + w] = whole; bits[2 * T.words + w] = 0u; bits[3 * T.words + w] = one_doc; }
         }
     }
     fence_before_sync();
@@ -581,7 +608,8 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(MORE));
         const int r = (warp & 3) * 32 + lane, part = warp >> 2, c0 = part * 64;
         const int32_t j = j0 + r;
-        const int32_t doc = sight.docs && j < p.Nk ? p.k_doc[(int64_t)b * p.Nk + j] : -1;
+        int32_t doc = sight.docs && j < p.Nk ? p.k_doc[(int64_t)b * p.Nk + j] : -1;
+        if (doc < 0) doc = INT32_MIN;                           // (equal to no query's)
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const float to2 = p.scale * GRF_LOG2E, by_cap = CAP ? p.scale / p.cap : 0.0f, cap2 = p.cap * GRF_LOG2E;
         int32_t n = 0, luts = 0;
@@ -600,16 +628,16 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                 bool diagonals = false;
                 const float* mine = lut;
                 if (LUTS) {
-                    diagonals = grf_bucket(p, j0 - pos0 - (BT - 1)) != grf_bucket(p, j0 + BT - 1 - pos0);
+                    diagonals = bucket(p, j0 - pos0 - (BT - 1)) != bucket(p, j0 + BT - 1 - pos0);
                     if (diagonals) {
                         float* at = lut + (luts & 1) * 256;
-                        at[tid] = tid < 2 * BT - 1 ? grf_bias2<__nv_bfloat16>(p, h, j0 - pos0 + tid - (BT - 1)) : 0.0f;
+                        at[tid] = tid < 2 * BT - 1 ? grf_bias2<__nv_bfloat16>(p, bucket, h, j0 - pos0 + tid - (BT - 1)) : 0.0f;
                         mine = at + (BT - 1 + r - c0);          // column e: mine[-e]
                         __syncwarp();
                         if (lane == 0) mbar_arrive(lut_full);
                         if (!(ok = wait(lut_full, (uint32_t)luts & 1u))) break;
                         ++luts;
-                    } else bias2 = grf_bias2<__nv_bfloat16>(p, h, j0 - pos0);
+                    } else bias2 = grf_bias2<__nv_bfloat16>(p, bucket, h, j0 - pos0);
                 }
                 if (!(ok = wait(ready(s), (uint32_t)(n / NS) & 1u) && wait(s_full, (uint32_t)n & 1u))) break;
                 fence_after_sync();
@@ -620,6 +648,7 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
 #pragma unroll
                     for (int y = 0; y < 4; ++y) tmem_ld16_nowait(s_col + c0 + 16 * y + lanes, sv[y]);
                     tmem_ld_wait();
+                    if (CAP) capped<4>(sv, by_cap);
 #pragma unroll
                     for (int e4 = 0; e4 < 64; e4 += 4) {
                         const float4 l4 = *reinterpret_cast<const float4*>(&info[s][0][c0 + e4]);
@@ -630,9 +659,8 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                             const float raw = __uint_as_float(sv[e / 16][e % 16]);
                             float sc;
                             if (CAP) {
-                                const float th = tanh_any(raw * by_cap);
-                                dcap[e] = fmaf(-th, th, 1.0f);
-                                sc = fmaf(cap2, th, bias2);
+                                dcap[e] = fmaf(-raw, raw, 1.0f);
+                                sc = fmaf(cap2, raw, bias2);
                             } else sc = fmaf(raw, to2, bias2);
                             if (BIAS == GRF_BIAS_SLOPES) sc = fmaf(-slope2, fabsf(ahead - (float)e), sc);
                             if (LUTS) { if (diagonals) sc += mine[-e]; }
@@ -641,9 +669,21 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                     }
                 }
                 if (partial) {
+                    const int32_t since = from - c0;
+                    if (T.mixed(t)) {
 #pragma unroll
-                    for (int e = 0; e < 64; ++e)
-                        if (!(c0 + e >= from && (!sight.docs || (doc >= 0 && info_doc[s][c0 + e] == doc)))) x[e] = 0.0f;
+                        for (int e = 0; e < 64; e += 4) {
+                            const int4 d4 = *reinterpret_cast<const int4*>(&info_doc[s][c0 + e]);
+                            if (!(e >= since && d4.x == doc)) x[e] = 0.0f;
+                            if (!(e + 1 >= since && d4.y == doc)) x[e + 1] = 0.0f;
+                            if (!(e + 2 >= since && d4.z == doc)) x[e + 2] = 0.0f;
+                            if (!(e + 3 >= since && d4.w == doc)) x[e + 3] = 0.0f;
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 64; ++e)
+                            if (e < since) x[e] = 0.0f;
+                    }
                 }
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
@@ -726,7 +766,7 @@ struct grad_maps { CUtensorMap q, k, v, g; };
 template <int DP, bool CAP, int BIAS> int launch(grf_ctx* ctx, const grf_softmax_params& p, const grad_maps& m)
 {
     using Sh = Grad<DP>;
-    auto bits = [&](int32_t tokens) { return p.q_doc ? 12 * (size_t)(grf_ceil_div(tokens, BT) / 32 + 1) : 0; };
+    auto bits = [&](int32_t tokens) { return p.q_doc ? 16 * (size_t)(grf_ceil_div(tokens, BT) / 32 + 1) : 0; };
     const size_t dq_smem = Sh::SMEM + bits(p.Nk), dkv_smem = Sh::SMEM + bits(p.Nq);
     GRF_CUDA_TRY(cudaFuncSetAttribute(softmax_tc_dq_kernel<DP, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)dq_smem));
     GRF_CUDA_TRY(cudaFuncSetAttribute(softmax_tc_dkv_kernel<DP, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)dkv_smem));

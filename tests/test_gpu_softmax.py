@@ -125,6 +125,16 @@ def test_starts_and_lengths(lib, route, dtype, nq):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("nq", [3, 150])
+@pytest.mark.parametrize("scale", [0.0, -0.2, 0.5])
+def test_scales(lib, route, dtype, nq, scale):
+    """Scores that are all alike, or turned round; caps that many scores reach."""
+    for cap in (0.0, 0.5, 8.0):
+        x, how, dout = make(15, 2, 2, 1, nq, 150, 64, dtype, mask="causal", cap=cap)
+        check(lib, x, dict(how, scale=scale), dout)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("buckets", [(2, 2), (3, 1000), (64, 100000), (5, 7)])
 @pytest.mark.parametrize("two_sided", [False, True])
 def test_bucket_tables(lib, route, dtype, buckets, two_sided):
