@@ -35,26 +35,42 @@ template <int DP, bool EXACT> struct Fwd {
 
 constexpr int BIAS_NONE_SCALED = 3;     // no bias, scores scaled before anything else
 
-struct forward_tiles {
-    const grf_softmax_params& p;
-    const grf_sight& sight;
-    const uint32_t* bits;                                       // [seen, whole, one document] per group, then seen by any, then tiles with a token of no document
+// What a block of queries sees.
+template <int QT> struct forward_tiles {
+    const uint32_t* bits;                                       // with documents: [seen, whole, one document] per group, then seen by any, then tiles with a token of no document
+    bool docs;
     int32_t i0, tiles, words;
     int32_t last;                                               // one past the last key that any query of the sequence can see
-    // queries of group g
-    __device__ __forceinline__ int32_t from(int g) const { return i0 + g * BT; }
+    int32_t rows[QT], end[QT], whole[QT];                       // per group: whether it has queries, one past the last key seen, keys that all of them see
+    __device__ __forceinline__ forward_tiles(const grf_softmax_params& p, const grf_sight& sight, const uint32_t* bits_, int32_t i0_) : bits(bits_), docs(sight.docs), i0(i0_)
+    {
+        last = sight.end(p.Nq);
+        int32_t most = 0;
+#pragma unroll
+        for (int g = 0; g < QT; ++g) {
+            const int32_t i = i0 + g * BT;
+            rows[g] = i < p.Nq;
+            end[g] = rows[g] ? sight.end(min(i + BT, p.Nq)) : 0;
+            whole[g] = sight.order == GRF_ORDER_FULL ? sight.len : min(sight.len, max(sight.position(i) + 1, sight.prefix));
+            most = max(most, end[g]);
+        }
+        tiles = (most + BT - 1) / BT;
+        words = (tiles + 31) / 32;
+    }
+    // (chosen, not indexed: registers)
+    static __device__ __forceinline__ int32_t of(const int32_t (&x)[QT], int g) { return QT == 1 || g == 0 ? x[0] : x[QT - 1]; }
+    // group g and tile t: 0 nothing to see, 1 some of it, 2 all of it
     __device__ __forceinline__ int what(int g, int32_t t) const
     {
-        if (from(g) >= p.Nq) return 0;
-        if (sight.docs) return bit(bits + 3 * g * words, t) ? (bit(bits + (3 * g + 1) * words, t) ? 2 : 1) : 0;
-        return sight.tile(from(g), min(from(g) + BT, p.Nq), t * BT, t * BT + BT, make_int4(0, 0, 0, 0), make_int4(0, 0, 0, 0));
+        if (docs) return of(rows, g) && bit(bits + 3 * g * words, t) ? (bit(bits + (3 * g + 1) * words, t) ? 2 : 1) : 0;
+        return t * BT >= of(end, g) ? 0 : t * BT + BT <= of(whole, g) ? 2 : 1;
     }
     // whether documents have to be compared in a tile
-    __device__ __forceinline__ bool mixed(int g, int32_t t) const { return sight.docs && !bit(bits + (3 * g + 2) * words, t); }
+    __device__ __forceinline__ bool mixed(int g, int32_t t) const { return docs && !bit(bits + (3 * g + 2) * words, t); }
     // the first tile from t on that any group sees
-    template <int QT> __device__ __forceinline__ int32_t next(int32_t t) const
+    __device__ __forceinline__ int32_t next(int32_t t) const
     {
-        if (!sight.docs) return t;
+        if (!docs) return t;
         const uint32_t* any = bits + 3 * QT * words;
         while (t < tiles) {
             const uint32_t w = any[t >> 5] >> (t & 31);
@@ -63,9 +79,9 @@ struct forward_tiles {
         }
         return tiles;
     }
-    template <int QT> __device__ __forceinline__ bool unclean(int32_t t) const
+    __device__ __forceinline__ bool unclean(const grf_softmax_params& p, int32_t t) const
     {
-        return (last < p.Nk && t * BT + BT > last) || (sight.docs && bit(bits + (3 * QT + 1) * words, t));
+        return (last < p.Nk && t * BT + BT > last) || (docs && bit(bits + (3 * QT + 1) * words, t));
     }
 };
 
@@ -154,15 +170,11 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
     // Blocks of queries, the longest rows first, dealt out to the CTAs forwards and backwards in turn, so that all get about the same.
     // (With documents every CTA has one block, whose bits are made below.)
     const int32_t heads = p.B * p.H, blocks = (p.Nq + QT * BT - 1) / (QT * BT);
-    const int64_t items = (int64_t)heads * blocks;
-    auto item = [&](int32_t round) {
-        const int64_t x = (int64_t)round * gridDim.x + ((round & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
-        return x < items ? x : (int64_t)-1;
-    };
-    const int32_t rounds = (int32_t)((items + gridDim.x - 1) / gridDim.x);
-    auto bh_of = [&](int64_t x) { return (int32_t)(x % heads); };
-    auto i0_of = [&](int64_t x) { return (blocks - 1 - (int32_t)(x / heads)) * (QT * BT); };
-    auto tiles_of = [&](const grf_sight& sight, int32_t i0) { return (sight.end(min(i0 + QT * BT, p.Nq)) + BT - 1) / BT; };
+    const uint32_t items = (uint32_t)heads * (uint32_t)blocks;  // (at most 65535 * 32768)
+    auto item = [&](uint32_t round) { return round * gridDim.x + ((round & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x); };
+    const uint32_t rounds = (items - 1) / gridDim.x + 1;
+    auto bh_of = [&](uint32_t x) { return (int32_t)(x % (uint32_t)heads); };
+    auto i0_of = [&](uint32_t x) { return (blocks - 1 - (int32_t)(x / (uint32_t)heads)) * (QT * BT); };
     constexpr int COPY = 4 * QT, ISSUE = 4 * QT + 1, CLEAN = 4 * QT + 3;
 
     if (tid == 0) {
@@ -183,8 +195,8 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
     if (p.q_doc) {
         const int32_t b = bh_of(blockIdx.x) / p.H, i0 = i0_of(blockIdx.x);
         const grf_sight sight(p, b);
-        const int32_t tiles = tiles_of(sight, i0);
-        const forward_tiles T{p, sight, bits, i0, tiles, (tiles + 31) / 32, 0};
+        const forward_tiles<QT> T(p, sight, bits, i0);
+        const int32_t tiles = T.tiles;
         const int32_t kblocks = (p.Nk + BT - 1) / BT, qblocks = (p.Nq + BT - 1) / BT;
         for (int32_t w = warp; w < T.words; w += Sh::THREADS / 32) {
             const int32_t t = w * 32 + lane;
@@ -193,9 +205,9 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             for (int g = 0; g < QT; ++g) {
                 int what = 0;
                 bool same = true;
-                if (t < tiles && T.from(g) < p.Nq) {
-                    const int4 qr = p.q_range[(int64_t)b * qblocks + T.from(g) / BT];
-                    what = sight.tile(T.from(g), min(T.from(g) + BT, p.Nq), t * BT, t * BT + BT, qr, kr);
+                if (t < tiles && T.of(T.rows, g)) {
+                    const int4 qr = p.q_range[(int64_t)b * qblocks + (i0 + g * BT) / BT];
+                    what = sight.tile((i0 + g * BT), min((i0 + g * BT) + BT, p.Nq), t * BT, t * BT + BT, qr, kr);
                     same = one_document(qr, kr);
                 }
                 const uint32_t seen = __ballot_sync(0xffffffffu, what != 0), whole = __ballot_sync(0xffffffffu, what == 2), one = __ballot_sync(0xffffffffu, same);
@@ -218,33 +230,35 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             // ------------------------------------------------------------ copies
             bool ok = true;
             int32_t n = 0, qn[QT] = {};
-            for (int32_t round = 0; round < rounds && ok; ++round) {
-                const int64_t x = item(round);
-                if (x < 0) break;
+            for (uint32_t round = 0; round < rounds && ok; ++round) {
+                const uint32_t x = item(round);
+                if (x >= items) break;
                 const int32_t bh = bh_of(x), b = bh / p.H, h = bh % p.H, kvh = h / p.group, i0 = i0_of(x);
                 const grf_sight sight(p, b);
-                const int32_t tiles = tiles_of(sight, i0);
-                const forward_tiles T{p, sight, bits, i0, tiles, (tiles + 31) / 32, 0};
+                const forward_tiles<QT> T(p, sight, bits, i0);
+                const int32_t tiles = T.tiles;
                 const int32_t kb = p.ks[0] ? b : 0, kh = p.ks[1] ? kvh : 0, vb = p.vs[0] ? b : 0, vh = p.vs[1] ? kvh : 0;
-                const int32_t t0 = T.next<QT>(0);
-                for (int32_t t = t0; t < tiles && ok; t = T.next<QT>(t + 1), ++n) {
+                const int32_t t0 = T.next(0);
+                for (int32_t t = t0; t < tiles && ok; t = T.next(t + 1), ++n) {
                     const int s = n % NS;
                     const uint32_t before = (uint32_t)(n / NS - 1) & 1u;
-                    if (n >= NS && !(ok = wait(k_empty(s), before) && wait(v_empty(s), before))) break;
+                    if (n >= NS && !(ok = wait(k_empty(s), before))) break;
                     expect_tx_elected(k_full(s), Sh::TILE);
-                    expect_tx_elected(v_full(s), Sh::TILE);
                     for (int y = 0; y < DP / 64; ++y) load_box(k_at + s * Sh::TILE + y * HALF, &map_k, 64 * y, t * BT, kh, kb, k_full(s));
                     if (t == t0) {
+#pragma unroll
                         for (int g = 0; g < QT; ++g) {
-                            if (T.from(g) >= p.Nq) continue;
+                            if (!T.of(T.rows, g)) continue;
                             const int y = qn[g] % QB;
                             if (qn[g] >= QB && !wait(q_empty(g, y), (uint32_t)(qn[g] / QB - 1) & 1u)) { ok = false; break; }
                             expect_tx_elected(q_full(g, y), Sh::TILE);
                             for (int z = 0; z < DP / 64; ++z)
-                                load_box(q_at + (g * QB + y) * Sh::TILE + z * HALF, &map_q, 64 * z, T.from(g), p.qs[1] ? h : 0, p.qs[0] ? b : 0, q_full(g, y));
+                                load_box(q_at + (g * QB + y) * Sh::TILE + z * HALF, &map_q, 64 * z, (i0 + g * BT), p.qs[1] ? h : 0, p.qs[0] ? b : 0, q_full(g, y));
                             ++qn[g];
                         }
                     }
+                    if (!ok || (n >= NS && !(ok = wait(v_empty(s), before)))) break;
+                    expect_tx_elected(v_full(s), Sh::TILE);
                     for (int y = 0; y < DP / 64; ++y) load_box(v_at + s * Sh::TILE + y * HALF, &map_v, 64 * y, t * BT, vh, vb, v_full(s));
                 }
             }
@@ -254,6 +268,7 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                     mbar_drain(k_full(x % NS), (uint32_t)(x / NS) & 1u, 20000000ll);
                     mbar_drain(v_full(x % NS), (uint32_t)(x / NS) & 1u, 20000000ll);
                 }
+#pragma unroll
                 for (int g = 0; g < QT; ++g)
                     for (int32_t x = max(0, qn[g] - QB); x < qn[g]; ++x) mbar_drain(q_full(g, x % QB), (uint32_t)(x / QB) & 1u, 20000000ll);
             }
@@ -277,29 +292,29 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 ++made;
                 return true;
             };
-            auto values_ready = [&](const forward_tiles& T, int32_t t) {
+            auto values_ready = [&](const forward_tiles<QT>& T, int32_t t) {
                 const int s = n % NS;
                 if (!wait(v_full(s), (uint32_t)(n / NS) & 1u)) return false;
-                if (T.unclean<QT>(t)) {
+                if (T.unclean(p, t)) {
                     if (!wait(v_clean(s), cleaned >> s & 1u)) return false;
                     cleaned ^= 1u << s;
                 }
                 return true;
             };
-            for (int32_t round = 0; round < rounds && ok; ++round) {
-                const int64_t x = item(round);
-                if (x < 0) break;
+            for (uint32_t round = 0; round < rounds && ok; ++round) {
+                const uint32_t x = item(round);
+                if (x >= items) break;
                 const int32_t b = bh_of(x) / p.H, i0 = i0_of(x);
                 const grf_sight sight(p, b);
-                const int32_t tiles = tiles_of(sight, i0);
-                const forward_tiles T{p, sight, bits, i0, tiles, (tiles + 31) / 32, sight.end(p.Nq)};
-                int32_t t = T.next<QT>(0), c = 0;
-                const bool queries = t < tiles && T.from(g) < p.Nq;
+                const forward_tiles<QT> T(p, sight, bits, i0);
+                const int32_t tiles = T.tiles;
+                int32_t t = T.next(0), c = 0;
+                const bool queries = t < tiles && T.of(T.rows, g);
                 if (queries && !(ok = wait(q_full(g, qn % QB), (uint32_t)(qn / QB) & 1u))) break;
                 if (Sh::SEP && t < tiles && !(ok = make_scores(n))) break;
                 for (; t < tiles && ok; ++n) {
                     const int s = n % NS;
-                    const int32_t t_next = T.next<QT>(t + 1);
+                    const int32_t t_next = T.next(t + 1);
                     if (!Sh::SEP) {
                         if (T.what(g, t) == 0) {
                             if (!(ok = wait(k_full(s), (uint32_t)(n / NS) & 1u))) break;
@@ -338,18 +353,18 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             // ------------------------------------------------------------ rows of V that nobody sees
             int32_t n = 0;
             bool ok = true;
-            for (int32_t round = 0; round < rounds && ok; ++round) {
-                const int64_t x = item(round);
-                if (x < 0) break;
+            for (uint32_t round = 0; round < rounds && ok; ++round) {
+                const uint32_t x = item(round);
+                if (x >= items) break;
                 const int32_t b = bh_of(x) / p.H, i0 = i0_of(x);
                 const grf_sight sight(p, b);
-                const int32_t tiles = tiles_of(sight, i0);
-                const forward_tiles T{p, sight, bits, i0, tiles, (tiles + 31) / 32, sight.end(p.Nq)};
-                for (int32_t t = T.next<QT>(0); t < tiles; t = T.next<QT>(t + 1), ++n) {
+                const forward_tiles<QT> T(p, sight, bits, i0);
+                const int32_t tiles = T.tiles;
+                for (int32_t t = T.next(0); t < tiles; t = T.next(t + 1), ++n) {
                     // (it waits for every tile, and holds the stage until then: a parity only tells a phase from the one before it)
                     const int s = n % NS;
                     if (!(ok = wait(v_full(s), (uint32_t)(n / NS) & 1u))) break;
-                    if (T.unclean<QT>(t)) {
+                    if (T.unclean(p, t)) {
                         for (int r = lane; r < BT; r += 32) {
                             const int32_t j = t * BT + r;
                             if (j >= p.Nk || (j < T.last && !(sight.docs && p.k_doc[(int64_t)b * p.Nk + j] < 0))) continue;
@@ -374,14 +389,14 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
         const float to2 = p.scale * GRF_LOG2E, by_cap = CAP ? p.scale / p.cap : 0.0f, cap2 = p.cap * GRF_LOG2E;
         int32_t done = 0, luts = 0;                             // tiles of this group, tiles with a bias per diagonal
         bool ok = true;
-        for (int32_t round = 0; round < rounds; ++round) {
-            const int64_t which = item(round);
-            if (which < 0) break;
+        for (uint32_t round = 0; round < rounds; ++round) {
+            const uint32_t which = item(round);
+            if (which >= items) break;
             const int32_t bh = bh_of(which), b = bh / p.H, h = bh % p.H, i0 = i0_of(which);
             const grf_sight sight(p, b);
-            const int32_t tiles = tiles_of(sight, i0);
-            const forward_tiles T{p, sight, bits, i0, tiles, (tiles + 31) / 32, 0};
-            const int32_t i = T.from(g) + r, pos = sight.position(i), pos0 = sight.position(T.from(g));
+            const forward_tiles<QT> T(p, sight, bits, i0);
+            const int32_t tiles = T.tiles;
+            const int32_t i = (i0 + g * BT) + r, pos = sight.position(i), pos0 = sight.position((i0 + g * BT));
             const int32_t limit = sight.order == GRF_ORDER_FULL ? sight.len : min(sight.len, max(pos + 1, sight.prefix));
             int32_t doc = sight.docs && i < p.Nq ? p.q_doc[(int64_t)b * p.Nq + i] : -1;
             if (doc < 0) doc = INT32_MIN;                       // (equal to no key's)
@@ -389,7 +404,7 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             float m = -CUDART_INF_F;
             uint64_t sum2[4] = {0ull, 0ull, 0ull, 0ull};
             int32_t c = 0;
-            for (int32_t t = T.next<QT>(0); t < tiles; t = T.next<QT>(t + 1)) {
+            for (int32_t t = T.next(0); t < tiles; t = T.next(t + 1)) {
                 const int what = T.what(g, t);
                 if (what == 0) continue;
                 const int32_t j0 = t * BT;
@@ -432,39 +447,32 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 if (!PLAIN) {
                     const uint64_t by = CAP ? pack2(cap2, cap2) : pack2(to2, to2);
                     const float ahead = (float)(j0 - pos);      // (exact, as are its sums, below 2^24; beyond, off by half a step as the distance itself)
-                    if (BIAS == GRF_BIAS_SLOPES && __all_sync(0xffffffffu, j0 + BT - 1 <= pos)) {
-                        // every key before the query: a line
-                        const uint64_t s2 = pack2(slope2, slope2), b2 = pack2(slope2 * ahead, slope2 * ahead);
+                    const bool line = BIAS == GRF_BIAS_SLOPES && (sight.order == GRF_ORDER_CAUSAL || __all_sync(0xffffffffu, j0 + BT - 1 <= pos));
+                    // (keys behind a causal query are not seen: before it, the distance is a line)
+                    const float at0 = line ? slope2 * ahead : bias2;
+                    const uint64_t at02 = pack2(at0, at0);
 #pragma unroll
-                        for (int y = 0; y < 8; ++y)
+                    for (int y = 0; y < 8; ++y)
 #pragma unroll
-                            for (int e = 0; e < 16; e += 2) {
-                                const uint64_t line = fma2(s2, pack2((float)(16 * y + e), (float)(16 * y + e + 1)), b2);
-                                float x0, x1;
-                                unpack2(fma2(pack2(sv[y][e], sv[y][e + 1]), by, line), x0, x1);
-                                sv[y][e] = __float_as_uint(x0);
-                                sv[y][e + 1] = __float_as_uint(x1);
-                            }
-                    } else {
-                        const uint64_t bias22 = pack2(bias2, bias2);
-#pragma unroll
-                        for (int y = 0; y < 8; ++y)
-#pragma unroll
-                            for (int e = 0; e < 16; e += 2) {
-                                const int col = 16 * y + e;
-                                float x0, x1;
-                                unpack2(fma2(pack2(sv[y][e], sv[y][e + 1]), by, bias22), x0, x1);
-                                if (BIAS == GRF_BIAS_SLOPES) {
+                        for (int e = 0; e < 16; e += 2) {
+                            const int col = 16 * y + e;
+                            float x0, x1;
+                            unpack2(fma2(pack2(sv[y][e], sv[y][e + 1]), by, at02), x0, x1);
+                            if (BIAS == GRF_BIAS_SLOPES) {
+                                if (line) {
+                                    x0 = fmaf(slope2, (float)col, x0);
+                                    x1 = fmaf(slope2, (float)(col + 1), x1);
+                                } else {
                                     x0 = fmaf(-slope2, fabsf(ahead + (float)col), x0);
                                     x1 = fmaf(-slope2, fabsf(ahead + (float)(col + 1)), x1);
                                 }
-                                if (BIAS == GRF_BIAS_BUCKETS) {
-                                    if (diagonals) { x0 += mine[col]; x1 += mine[col + 1]; }
-                                }
-                                sv[y][e] = __float_as_uint(x0);
-                                sv[y][e + 1] = __float_as_uint(x1);
                             }
-                    }
+                            if (BIAS == GRF_BIAS_BUCKETS) {
+                                if (diagonals) { x0 += mine[col]; x1 += mine[col + 1]; }
+                            }
+                            sv[y][e] = __float_as_uint(x0);
+                            sv[y][e + 1] = __float_as_uint(x1);
+                        }
                 }
                 if (what == 1) {
                     if (mixed) {
@@ -491,11 +499,13 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
 #pragma unroll
                 for (int y = 0; y < 8; ++y)
 #pragma unroll
-                    for (int e = 0; e < 16; e += 2) top4[e >> 1 & 3] = max3(top4[e >> 1 & 3], __uint_as_float(sv[y][e]), __uint_as_float(sv[y][e + 1]));
-                float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3]));
+                    for (int e = 0; e < 16; e += 2) top4[e >> 1 & 3] = max3_nan(top4[e >> 1 & 3], __uint_as_float(sv[y][e]), __uint_as_float(sv[y][e + 1]));
+                float top = max_nan(max_nan(top4[0], top4[1]), max_nan(top4[2], top4[3]));
                 if (PLAIN) top *= to2;
                 // a new maximum only when it matters: 2^8 above the one in use (or the first)
-                const bool grow = top > m + 8.0f;
+                // (NaN grows too, and stays; an infinite score makes its row NaN, as infinity - infinity would)
+                const bool grow = !(top <= m + 8.0f);
+                if (top == CUDART_INF_F) top = CUDART_NAN_F;
                 if (__any_sync(0xffffffffu, grow)) {
                     const float alpha = grow ? ex2(m - top) : 1.0f;
                     if (grow) m = top;
@@ -529,8 +539,8 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                         const int a = 2 * y + (e >> 3), z = (2 * e) & 15;
                         float x0, x1;
                         unpack2(PLAIN ? fma2(pack2(sv[a][z], sv[a][z + 1]), to22, minus) : add2(pack2(sv[a][z], sv[a][z + 1]), minus), x0, x1);
-                        x0 = ex2(x0);
-                        x1 = ex2(x1);
+                        if (GRF_FMA_PAIRS(16 * y + e)) ex2_by_fma<EXACT ? 4 : 3>(pack2(x0, x1), x0, x1);
+                        else { x0 = ex2(x0); x1 = ex2(x1); }
                         sum2[e & 3] = add2(sum2[e & 3], pack2(x0, x1));
                         w[e] = pack_bf16(x0, x1);
                         if (EXACT) u[EXACT ? e : 0] = pack_bf16(x0 - __uint_as_float(w[e] << 16), x1 - __uint_as_float(w[e] & 0xffff0000u));
@@ -555,35 +565,30 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             bool spoilt = false;
             __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.out_w) + b * p.os[0] + h * p.os[1] + (int64_t)i * p.os[2];
             __nv_bfloat16* rest = p.rest_w ? p.rest_w + (((int64_t)b * p.H + h) * p.Nq + i) * p.d : nullptr;
+            // (a loop: once a block, its instructions come from afar)
+#pragma unroll 1
+            for (int y = 0; y < DP / 16; ++y) {
+                uint32_t o[16];
 #pragma unroll
-            for (int y = 0; y < DP / 32; ++y) {
-                uint32_t o[2][16];
-#pragma unroll
-                for (int e = 0; e < 16; ++e) o[0][e] = o[1][e] = 0u;
-                if (c > 0) {
-                    tmem_ld16_nowait(o_addr + 32 * y, o[0]);
-                    tmem_ld16_nowait(o_addr + 32 * y + 16, o[1]);
-                    tmem_ld_wait();
-                    if (y == DP / 32 - 1) {
-                        // the accumulator may be written again
-                        fence_before_sync();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(o_read(g));
-                    }
+                for (int e = 0; e < 16; ++e) o[e] = 0u;
+                if (c > 0) tmem_ld16(o_addr + 16 * y, o);
+                if (c > 0 && y == DP / 16 - 1) {
+                    // the accumulator may be written again
+                    fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(o_read(g));
                 }
                 if (i >= p.Nq) continue;
 #pragma unroll
-                for (int z = 0; z < 4; ++z) {
-                    const int col = 32 * y + 8 * z;
+                for (int z = 0; z < 2; ++z) {
+                    const int col = 16 * y + 8 * z;
                     if (col >= p.d) continue;
                     uint32_t w[4], u[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         // (no key seen: 0, whatever the accumulator holds)
-                        const uint32_t (&v)[16] = o[z >> 1];
-                        const int at = 8 * (z & 1) + 2 * e;
-                        const float x0 = l == 0.0f ? 0.0f : __uint_as_float(v[at]) * inv, x1 = l == 0.0f ? 0.0f : __uint_as_float(v[at + 1]) * inv;
-                        spoilt |= !(fabsf(x0) <= 3.4028235e38f) || !(fabsf(x1) <= 3.4028235e38f);
+                        const float x0 = l == 0.0f ? 0.0f : __uint_as_float(o[8 * z + 2 * e]) * inv, x1 = l == 0.0f ? 0.0f : __uint_as_float(o[8 * z + 2 * e + 1]) * inv;
+                        spoilt |= !(fabsf(x0) + fabsf(x1) <= 3.4028235e38f);
                         w[e] = pack_bf16(x0, x1);
                         if (EXACT) {
                             const __nv_bfloat16 r0 = grf_rest(x0, __float2bfloat16_rn(x0)), r1 = grf_rest(x1, __float2bfloat16_rn(x1));

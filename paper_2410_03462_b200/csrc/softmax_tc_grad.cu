@@ -52,6 +52,15 @@ __device__ __forceinline__ float min_nan(float a, float b)
     asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
+// 2^x of a row's 64 values.  (NaN in a value that takes the multiply-adds becomes 0; a row of NaN has a NaN D, which its gradients meet.)
+__device__ __forceinline__ void powers(float (&x)[64])
+{
+#pragma unroll
+    for (int e = 0; e < 64; e += 2) {
+        if (GRF_FMA_PAIRS(e / 2)) ex2_by_fma<4>(pack2(x[e], x[e + 1]), x[e], x[e + 1]);
+        else { x[e] = ex2(x[e]); x[e + 1] = ex2(x[e + 1]); }
+    }
+}
 __device__ __forceinline__ void clear_row(uint32_t tile, int r, int halves)
 {
     for (int y = 0; y < halves; ++y)
@@ -235,6 +244,7 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         const int r = (warp & 3) * 32 + lane, part = warp >> 2, c0 = part * 64;
         const int32_t i = i0 + r, pos = sight.position(i), pos0 = sight.position(i0);
         const int32_t limit = sight.order == GRF_ORDER_FULL ? sight.len : min(sight.len, max(pos + 1, sight.prefix));
+        const int32_t all_see = sight.order == GRF_ORDER_FULL ? sight.len : min(sight.len, max(pos0 + 1, sight.prefix));       // keys before it: the whole block
         int32_t doc = sight.docs && i < p.Nq ? p.q_doc[(int64_t)b * p.Nq + i] : -1;
         if (doc < 0) doc = INT32_MIN;                           // (equal to no key's)
         const int64_t row = ((int64_t)b * p.H + h) * p.Nq + i;
@@ -260,7 +270,7 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         bool ok = true;
         for (int32_t t = T.begin(); t < tiles; t = T.next(t + 1)) {
             const int32_t j0 = t * BT;
-            const bool partial = sight.docs ? !T.whole(t) : sight.tile(i0, i1, j0, j0 + BT, make_int4(0, 0, 0, 0), make_int4(0, 0, 0, 0)) == 1;
+            const bool partial = sight.docs ? !T.whole(t) : j0 + BT > all_see;
             float bias2 = 0.0f;
             bool diagonals = false;
             int32_t bucket0 = 0;
@@ -304,8 +314,9 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     } else s = fmaf(raw, to2, bias2);
                     if (BIAS == GRF_BIAS_SLOPES) s = fmaf(-slope2, fabsf(ahead + (float)e), s);
                     if (LUTS) { if (diagonals) s += mine[e]; }
-                    x[e] = ex2(min_nan(s - lse2, 0.0f));
+                    x[e] = min_nan(s - lse2, 0.0f);
                 }
+                powers(x);
             }
             const bool careful = partial || !any;               // (of this row: nothing in it may meet an infinity or NaN)
             if (careful) {
@@ -612,6 +623,7 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         if (doc < 0) doc = INT32_MIN;                           // (equal to no query's)
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const float to2 = p.scale * GRF_LOG2E, by_cap = CAP ? p.scale / p.cap : 0.0f, cap2 = p.cap * GRF_LOG2E;
+        const bool block_partial = j0 + BT > sight.len, ordered = sight.order != GRF_ORDER_FULL && j0 + BT > sight.prefix;
         int32_t n = 0, luts = 0;
         bool ok = true;
         if (some) {
@@ -619,8 +631,7 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
             do {
                 const int s = n % NS;
                 const int32_t i0 = t * BT, pos0 = sight.position(i0);
-                const bool partial = sight.docs ? !T.whole(t)
-                                                : sight.tile(i0, min(i0 + BT, p.Nq), j0, j0 + BT, make_int4(0, 0, 0, 0), make_int4(0, 0, 0, 0)) == 1;
+                const bool partial = sight.docs ? !T.whole(t) : block_partial || (ordered && pos0 < j0 + BT - 1);
                 // columns from `from` on see this key
                 const int32_t from = j >= sight.len ? BT : sight.order == GRF_ORDER_FULL || j < sight.prefix ? 0 : min(max(j - pos0, 0), BT);
                 const float slope2 = BIAS == GRF_BIAS_SLOPES ? p.slopes[h] * GRF_LOG2E : 0.0f;
@@ -664,9 +675,10 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                             } else sc = fmaf(raw, to2, bias2);
                             if (BIAS == GRF_BIAS_SLOPES) sc = fmaf(-slope2, fabsf(ahead - (float)e), sc);
                             if (LUTS) { if (diagonals) sc += mine[-e]; }
-                            x[e] = ex2(min_nan(sc - lv[z], 0.0f));
+                            x[e] = min_nan(sc - lv[z], 0.0f);
                         }
                     }
+                    powers(x);
                 }
                 if (partial) {
                     const int32_t since = from - c0;
