@@ -4,10 +4,14 @@
 // running maximum m and sum l (in units of log 2), and writes P = 2^(s - m) back to tensor memory as bf16 pairs, where it is the left operand
 // of O += P V.  O stays in tensor memory; it is rescaled only when a maximum grows by more than 2^8 (until then P <= 2^8, which costs no
 // precision: bf16 has the same relative step everywhere and l is fp32), so almost never after the first tiles.
-//   d > 64   a CTA per SM, two groups of 128 queries: while one group's softmax runs, the other one's products do.  P overwrites S
-//   d <= 64  two CTAs per SM of one group; P has its own place, so the next S is made while P is
-//   warps of the last warpgroup: copies of K and V (two stages, boxes by the copy engine), one issuing warp per group, and one that
-//   clears rows of V which nobody sees (behind a length, of no document): 0 times an infinity there would reach every query of the tile.
+// A CTA has an SM to itself and works on two groups of 128 queries in turn with the tensor cores.  Two threads share a query, 64 columns
+// each (they agree on the maximum through shared memory): with one thread a query, two warps per scheduler, the chain of a tile - load,
+// maximum, exponentials, store - bounded the kernel (2 x 16 heads x 4096, d = 128: MEASURED).
+//   d > 64   P overwrites S
+//   d <= 64  P has its own place, so the next S is made while P is
+//   warps of the last warpgroup: copies of K and V (boxes by the copy engine), one issuing warp per group, and one that clears rows of V
+//   which nobody sees (behind a length, of no document): 0 times an infinity there would reach every query of the tile.
+// CTAs take block after block of queries; barriers, tensor memory and the pipeline of copies go on from one to the next.
 // A value that some queries see and others do not, and that is not finite, does reach the others' accumulators: a row that ends up not finite
 // has its columns summed again from what it does see (redo_row).
 #include <type_traits>
@@ -18,25 +22,25 @@ namespace {
 
 using namespace grf_softmax_tc;
 
+constexpr int QT = 2;                                           // groups of a CTA
+
 // EXACT: P as the sum of two bf16 values, so that O has fp32 precision and D = dout . O of the backward pass, a difference of nearly equal terms
 // where a row looks at few keys, loses nothing (dQ of the capped case: 2.8e-3 from 64 bits without, MEASURED with).  The second values take the rest of S's place.
 template <int DP, bool EXACT> struct Fwd {
-    static constexpr int QT = DP == 64 ? 1 : 2;                 // groups
-    static constexpr int CTAS = DP == 64 ? 2 : 1;
     static constexpr bool SEP = DP == 64 && !EXACT;             // P beside S
-    static constexpr int THREADS = 128 * (QT + 1);
-    static constexpr int NS = 2, QB = DP == 64 ? 2 : 1;         // stages of K and V; places for a group's queries
+    static constexpr int NS = DP == 64 ? 3 : 2, QB = DP == 64 ? 2 : 1;     // stages of K and V; places for a group's queries
     static constexpr uint32_t TILE = HALF * (DP / 64);
-    static constexpr uint32_t TMEM = DP == 64 ? 256 : 512;
-    static constexpr uint32_t P_COL = SEP ? 128 : 0, O_COL = DP == 64 ? 192 : 256;
+    static constexpr uint32_t P_COL = SEP ? 256 : 0, P_STEP = SEP ? 64 : BT, O_COL = SEP ? 384 : 256;      // S: BT per group
     static constexpr size_t SMEM = 1024 + (size_t)TILE * (QT * QB + 2 * NS);    // then the tiles' bits
-    static constexpr int MORE = DP == 64 ? 200 : 208, LESS = DP == 64 ? 56 : 88;   // registers: QT * MORE + LESS = the launch's
 };
+constexpr int SOFT = 8 * QT;                                    // warps that make P
+constexpr int THREADS = 32 * (SOFT + 4);
+constexpr int MORE = 104, LESS = 64;                            // registers: 4 * 104 + 64 = 5 * 96, the launch's
 
 constexpr int BIAS_NONE_SCALED = 3;     // no bias, scores scaled before anything else
 
 // What a block of queries sees.
-template <int QT> struct forward_tiles {
+struct forward_tiles {
     const uint32_t* bits;                                       // with documents: [seen, whole, one document] per group, then seen by any, then tiles with a token of no document
     bool docs;
     int32_t i0, tiles, words;
@@ -58,7 +62,7 @@ template <int QT> struct forward_tiles {
         words = (tiles + 31) / 32;
     }
     // (chosen, not indexed: registers)
-    static __device__ __forceinline__ int32_t of(const int32_t (&x)[QT], int g) { return QT == 1 || g == 0 ? x[0] : x[QT - 1]; }
+    static __device__ __forceinline__ int32_t of(const int32_t (&x)[QT], int g) { return g == 0 ? x[0] : x[QT - 1]; }
     // group g and tile t: 0 nothing to see, 1 some of it, 2 all of it
     __device__ __forceinline__ int what(int g, int32_t t) const
     {
@@ -88,7 +92,7 @@ template <int QT> struct forward_tiles {
 // The outputs of row i from the keys that it sees, where a value that it does not see has spoilt them: the warp together, lanes take keys for
 // the scores and columns for the sums.  Rare, and only columns that are not finite are replaced.
 template <bool CAP>
-__device__ __noinline__ void redo_row(const grf_softmax_params& p, const grf_buckets& bucket, int32_t b, int32_t h, int32_t i, float m, float l)
+__device__ __noinline__ void redo_row(const grf_softmax_params& p, const grf_buckets& bucket, int32_t b, int32_t h, int32_t i, float m, float l, int32_t col0, int32_t col1)
 {
     const grf_sight sight(p, b);
     const int lane = threadIdx.x & 31;
@@ -125,7 +129,7 @@ __device__ __noinline__ void redo_row(const grf_softmax_params& p, const grf_buc
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
         const int c = lane + 32 * x;
-        if (c >= p.d || fabsf(__bfloat162float(out[c])) <= 3.4028235e38f) continue;
+        if (c < col0 || c >= min(col1, p.d) || fabsf(__bfloat162float(out[c])) <= 3.4028235e38f) continue;
         const float y = o[x] * inv;
         out[c] = __float2bfloat16_rn(y);
         if (p.rest_w) p.rest_w[(((int64_t)b * p.H + h) * p.Nq + i) * p.d + c] = grf_rest(y, __float2bfloat16_rn(y));
@@ -133,19 +137,21 @@ __device__ __noinline__ void redo_row(const grf_softmax_params& p, const grf_buc
 }
 
 template <int DP, bool CAP, int BIAS, bool EXACT>
-__global__ void __launch_bounds__(Fwd<DP, EXACT>::THREADS, Fwd<DP, EXACT>::CTAS)
+__global__ void __launch_bounds__(THREADS, 1)
 softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                           const __grid_constant__ CUtensorMap map_v, const __grid_constant__ grf_softmax_params p)
 {
     using Sh = Fwd<DP, EXACT>;
-    constexpr int QT = Sh::QT, NS = Sh::NS, QB = Sh::QB;
+    constexpr int NS = Sh::NS, QB = Sh::QB;
+    constexpr bool FMA = false;
     constexpr bool PLAIN = BIAS == GRF_BIAS_NONE && !CAP;   // (a scale that is not positive: BIAS_NONE_SCALED)
     extern __shared__ unsigned char smem_dyn[];
-    constexpr int PER_GROUP = 6 + 2 * QB;
+    constexpr int PER_GROUP = 5 + 2 * QB;
     __shared__ __align__(8) unsigned long long bars[5 * NS + PER_GROUP * QT];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
     __shared__ float lut[BIAS == GRF_BIAS_BUCKETS ? QT * 2 * 256 : 1];
+    __shared__ float tops[2][SOFT * 32], sums[SOFT * 32];
     __shared__ __align__(16) int32_t doc_of[QT * 2 * BT];
     __shared__ grf_buckets bucket;
     const int tid = threadIdx.x, lane = tid & 31, warp = uniform(tid >> 5);
@@ -162,10 +168,9 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
     auto s_read = [&](int g) { return of_group(g, 1); };
     auto p_full = [&](int g) { return of_group(g, 2); };
     auto pv_done = [&](int g) { return of_group(g, 3); };
-    auto lut_full = [&](int g) { return of_group(g, 4); };
-    auto o_read = [&](int g) { return of_group(g, 5); };
-    auto q_full = [&](int g, int y) { return of_group(g, 6 + y); };
-    auto q_empty = [&](int g, int y) { return of_group(g, 6 + QB + y); };
+    auto o_read = [&](int g) { return of_group(g, 4); };
+    auto q_full = [&](int g, int y) { return of_group(g, 5 + y); };
+    auto q_empty = [&](int g, int y) { return of_group(g, 5 + QB + y); };
 
     // Blocks of queries, the longest rows first, dealt out to the CTAs forwards and backwards in turn, so that all get about the same.
     // (With documents every CTA has one block, whose bits are made below.)
@@ -175,7 +180,7 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
     const uint32_t rounds = (items - 1) / gridDim.x + 1;
     auto bh_of = [&](uint32_t x) { return (int32_t)(x % (uint32_t)heads); };
     auto i0_of = [&](uint32_t x) { return (blocks - 1 - (int32_t)(x / (uint32_t)heads)) * (QT * BT); };
-    constexpr int COPY = 4 * QT, ISSUE = 4 * QT + 1, CLEAN = 4 * QT + 3;
+    constexpr int COPY = SOFT, ISSUE = SOFT + 1, CLEAN = SOFT + 3;
 
     if (tid == 0) {
         abort_flag = 0;
@@ -185,20 +190,20 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
         }
         for (int g = 0; g < QT; ++g) {
             mbar_init(s_full(g), 1); mbar_init(pv_done(g), 1);
-            mbar_init(s_read(g), 4); mbar_init(p_full(g), 4); mbar_init(lut_full(g), 4); mbar_init(o_read(g), 4);
+            mbar_init(s_read(g), 8); mbar_init(p_full(g), 8); mbar_init(o_read(g), 8);
             for (int y = 0; y < QB; ++y) { mbar_init(q_full(g, y), 1); mbar_init(q_empty(g, y), 1); }
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == COPY) tmem_alloc(&tmem_slot, Sh::TMEM);
+    if (warp == COPY) tmem_alloc(&tmem_slot, 512u);
     if (BIAS == GRF_BIAS_BUCKETS) bucket.fill(p);
     if (p.q_doc) {
         const int32_t b = bh_of(blockIdx.x) / p.H, i0 = i0_of(blockIdx.x);
         const grf_sight sight(p, b);
-        const forward_tiles<QT> T(p, sight, bits, i0);
+        const forward_tiles T(p, sight, bits, i0);
         const int32_t tiles = T.tiles;
         const int32_t kblocks = (p.Nk + BT - 1) / BT, qblocks = (p.Nq + BT - 1) / BT;
-        for (int32_t w = warp; w < T.words; w += Sh::THREADS / 32) {
+        for (int32_t w = warp; w < T.words; w += THREADS / 32) {
             const int32_t t = w * 32 + lane;
             const int4 kr = t < tiles ? p.k_range[(int64_t)b * kblocks + t] : make_int4(INT32_MAX, -1, 0, 0);
             uint32_t any = 0u;
@@ -224,8 +229,8 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
     const uint32_t tmem = (uint32_t)uniform((int32_t)tmem_slot);
     auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, &abort_flag)) != 0; };
 
-    if (warp >= 4 * QT) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Sh::LESS));
+    if (warp >= SOFT) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(LESS));
         if (warp == COPY) {
             // ------------------------------------------------------------ copies
             bool ok = true;
@@ -235,7 +240,7 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 if (x >= items) break;
                 const int32_t bh = bh_of(x), b = bh / p.H, h = bh % p.H, kvh = h / p.group, i0 = i0_of(x);
                 const grf_sight sight(p, b);
-                const forward_tiles<QT> T(p, sight, bits, i0);
+                const forward_tiles T(p, sight, bits, i0);
                 const int32_t tiles = T.tiles;
                 const int32_t kb = p.ks[0] ? b : 0, kh = p.ks[1] ? kvh : 0, vb = p.vs[0] ? b : 0, vh = p.vs[1] ? kvh : 0;
                 const int32_t t0 = T.next(0);
@@ -277,7 +282,7 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             const int g = warp - ISSUE;
             const int32_t steps = (p.d + 15) / 16;
             const uint64_t q_op = rows_operand(q_at + g * QB * Sh::TILE), k_op = rows_operand(k_at), v_op = columns_operand(v_at);
-            const uint32_t scores = tmem + g * BT, probs = scores + Sh::P_COL, acc = tmem + Sh::O_COL + g * DP;
+            const uint32_t scores = tmem + g * BT, probs = tmem + Sh::P_COL + g * Sh::P_STEP, acc = tmem + Sh::O_COL + g * DP;
             bool ok = true;
             int32_t n = 0, made = 0, used = 0, qn = 0, outs = 0;        // tiles, S and P of this group, its queries, its outputs
             uint32_t cleaned = 0u;                              // parity of each stage's cleanings
@@ -292,7 +297,7 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 ++made;
                 return true;
             };
-            auto values_ready = [&](const forward_tiles<QT>& T, int32_t t) {
+            auto values_ready = [&](const forward_tiles& T, int32_t t) {
                 const int s = n % NS;
                 if (!wait(v_full(s), (uint32_t)(n / NS) & 1u)) return false;
                 if (T.unclean(p, t)) {
@@ -306,26 +311,26 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 if (x >= items) break;
                 const int32_t b = bh_of(x) / p.H, i0 = i0_of(x);
                 const grf_sight sight(p, b);
-                const forward_tiles<QT> T(p, sight, bits, i0);
+                const forward_tiles T(p, sight, bits, i0);
                 const int32_t tiles = T.tiles;
                 int32_t t = T.next(0), c = 0;
                 const bool queries = t < tiles && T.of(T.rows, g);
                 if (queries && !(ok = wait(q_full(g, qn % QB), (uint32_t)(qn / QB) & 1u))) break;
-                if (Sh::SEP && t < tiles && !(ok = make_scores(n))) break;
+                bool ahead = false;                             // S of the present tile is already made
                 for (; t < tiles && ok; ++n) {
                     const int s = n % NS;
                     const int32_t t_next = T.next(t + 1);
-                    if (!Sh::SEP) {
-                        if (T.what(g, t) == 0) {
-                            if (!(ok = wait(k_full(s), (uint32_t)(n / NS) & 1u))) break;
-                            arrive_elected(k_empty(s));
-                            if (!(ok = values_ready(T, t))) break;
-                            arrive_elected(v_empty(s));
-                            t = t_next;
-                            continue;
-                        }
-                        if (!(ok = make_scores(n))) break;
-                    } else if (t_next < tiles && !(ok = make_scores(n + 1))) break;
+                    if (T.what(g, t) == 0) {
+                        if (!(ok = wait(k_full(s), (uint32_t)(n / NS) & 1u))) break;
+                        arrive_elected(k_empty(s));
+                        if (!(ok = values_ready(T, t))) break;
+                        arrive_elected(v_empty(s));
+                        t = t_next;
+                        continue;
+                    }
+                    if (!ahead && !(ok = make_scores(n))) break;
+                    ahead = Sh::SEP && t_next < tiles && T.what(g, t_next) != 0;
+                    if (ahead && !(ok = make_scores(n + 1))) break;
                     if (c == 0 && outs > 0 && !(ok = wait(o_read(g), (uint32_t)(outs - 1) & 1u))) break;
                     if (!(ok = wait(p_full(g), (uint32_t)used & 1u))) break;
                     if (!(ok = values_ready(T, t))) break;
@@ -358,7 +363,7 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 if (x >= items) break;
                 const int32_t b = bh_of(x) / p.H, i0 = i0_of(x);
                 const grf_sight sight(p, b);
-                const forward_tiles<QT> T(p, sight, bits, i0);
+                const forward_tiles T(p, sight, bits, i0);
                 const int32_t tiles = T.tiles;
                 for (int32_t t = T.next(0); t < tiles; t = T.next(t + 1), ++n) {
                     // (it waits for every tile, and holds the stage until then: a parity only tells a phase from the one before it)
@@ -381,28 +386,32 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             }
         }
     } else {
-        // ---------------------------------------------------------------- a thread per query
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Sh::MORE));
-        const int g = warp >> 2, r = (warp & 3) * 32 + lane;
+        // ---------------------------------------------------------------- two threads per query
+        // After a wait that gave up (the abort flag is up, every later wait returns at once) they go on to the end, as the barriers between them
+        // count all of them.
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(MORE));
+        const int g = warp >> 3, half = warp >> 2 & 1, r = (warp & 3) * 32 + lane, c0 = half * 64;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t s_addr = tmem + g * BT + lanes, p_addr = s_addr + Sh::P_COL, o_addr = tmem + Sh::O_COL + g * DP + lanes;
+        const uint32_t s_addr = tmem + g * BT + c0 + lanes, p_addr = tmem + Sh::P_COL + g * Sh::P_STEP + half * 32 + lanes,
+                       o_addr = tmem + Sh::O_COL + g * DP + half * (DP / 2) + lanes;
         const float to2 = p.scale * GRF_LOG2E, by_cap = CAP ? p.scale / p.cap : 0.0f, cap2 = p.cap * GRF_LOG2E;
-        int32_t done = 0, luts = 0;                             // tiles of this group, tiles with a bias per diagonal
-        bool ok = true;
+        auto with_other_half = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + g * 4 + (warp & 3)) : "memory"); };
+        auto with_group = [&]() { asm volatile("bar.sync %0, 256;" ::"r"(1 + 4 * QT + g) : "memory"); };
+        int32_t done = 0, luts = 0;                             // tiles of this group, tiles with a bias per diagonal or documents
         for (uint32_t round = 0; round < rounds; ++round) {
             const uint32_t which = item(round);
             if (which >= items) break;
             const int32_t bh = bh_of(which), b = bh / p.H, h = bh % p.H, i0 = i0_of(which);
             const grf_sight sight(p, b);
-            const forward_tiles<QT> T(p, sight, bits, i0);
+            const forward_tiles T(p, sight, bits, i0);
             const int32_t tiles = T.tiles;
-            const int32_t i = (i0 + g * BT) + r, pos = sight.position(i), pos0 = sight.position((i0 + g * BT));
-            const int32_t limit = sight.order == GRF_ORDER_FULL ? sight.len : min(sight.len, max(pos + 1, sight.prefix));
+            const int32_t i = i0 + g * BT + r, pos = sight.position(i), pos0 = sight.position(i0 + g * BT);
+            const int32_t limit = (sight.order == GRF_ORDER_FULL ? sight.len : min(sight.len, max(pos + 1, sight.prefix))) - c0;
             int32_t doc = sight.docs && i < p.Nq ? p.q_doc[(int64_t)b * p.Nq + i] : -1;
             if (doc < 0) doc = INT32_MIN;                       // (equal to no key's)
             const float slope2 = BIAS == GRF_BIAS_SLOPES ? p.slopes[h] * GRF_LOG2E : 0.0f;
             float m = -CUDART_INF_F;
-            uint64_t sum2[4] = {0ull, 0ull, 0ull, 0ull};
+            uint64_t sum2[2] = {0ull, 0ull};
             int32_t c = 0;
             for (int32_t t = T.next(0); t < tiles; t = T.next(t + 1)) {
                 const int what = T.what(g, t);
@@ -413,7 +422,7 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 bool diagonals = false;
                 const bool mixed = what == 1 && T.mixed(g, t);
                 const float* mine = lut;
-                const int32_t* docs = doc_of + (g * 2 + (luts & 1)) * BT;
+                int32_t* docs = doc_of + (g * 2 + (luts & 1)) * BT;
                 if (BIAS == GRF_BIAS_BUCKETS) {
                     diagonals = bucket(p, j0 - pos0 - (BT - 1)) != bucket(p, j0 + BT - 1 - pos0);
                     if (!diagonals) bias2 = grf_bias2<__nv_bfloat16>(p, bucket, h, j0 - pos0);
@@ -421,21 +430,18 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 if (diagonals || mixed) {
                     if (BIAS == GRF_BIAS_BUCKETS && diagonals) {
                         float* at = lut + (g * 2 + (luts & 1)) * 256;
-                        at[r] = grf_bias2<__nv_bfloat16>(p, bucket, h, j0 - pos0 + r - (BT - 1));
-                        at[r + BT] = grf_bias2<__nv_bfloat16>(p, bucket, h, j0 - pos0 + r + 1);
-                        mine = at + (BT - 1 - r);
+                        at[r + 128 * half] = grf_bias2<__nv_bfloat16>(p, bucket, h, j0 - pos0 + r + 128 * half - (BT - 1));
+                        mine = at + (BT - 1 - r) + c0;
                     }
-                    if (mixed) const_cast<int32_t*>(docs)[r] = j0 + r < p.Nk ? p.k_doc[(int64_t)b * p.Nk + j0 + r] : -1;
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(lut_full(g));
-                    if (!(ok = wait(lut_full(g), (uint32_t)luts & 1u))) break;
+                    if (mixed && half == 0) docs[r] = j0 + r < p.Nk ? p.k_doc[(int64_t)b * p.Nk + j0 + r] : -1;
+                    with_group();
                     ++luts;
                 }
-                if (!(ok = wait(s_full(g), (uint32_t)done & 1u))) break;
+                wait(s_full(g), (uint32_t)done & 1u);
                 fence_after_sync();
-                uint32_t sv[8][16];
+                uint32_t sv[4][16];
 #pragma unroll
-                for (int y = 0; y < 8; ++y) tmem_ld16_nowait(s_addr + 16 * y, sv[y]);
+                for (int y = 0; y < 4; ++y) tmem_ld16_nowait(s_addr + 16 * y, sv[y]);
                 tmem_ld_wait();
                 if (Sh::SEP) {
                     fence_before_sync();
@@ -443,16 +449,16 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                     if (lane == 0) mbar_arrive(s_read(g));
                 }
                 // scores in units of log 2 (PLAIN: still to be scaled, by a positive number)
-                if (CAP) capped<8>(sv, by_cap);
+                if (CAP) capped<4>(sv, by_cap);
                 if (!PLAIN) {
                     const uint64_t by = CAP ? pack2(cap2, cap2) : pack2(to2, to2);
-                    const float ahead = (float)(j0 - pos);      // (exact, as are its sums, below 2^24; beyond, off by half a step as the distance itself)
+                    const float ahead = (float)(j0 + c0 - pos); // (exact, as are its sums, below 2^24; beyond, off by half a step as the distance itself)
                     const bool line = BIAS == GRF_BIAS_SLOPES && (sight.order == GRF_ORDER_CAUSAL || __all_sync(0xffffffffu, j0 + BT - 1 <= pos));
                     // (keys behind a causal query are not seen: before it, the distance is a line)
                     const float at0 = line ? slope2 * ahead : bias2;
                     const uint64_t at02 = pack2(at0, at0);
 #pragma unroll
-                    for (int y = 0; y < 8; ++y)
+                    for (int y = 0; y < 4; ++y)
 #pragma unroll
                         for (int e = 0; e < 16; e += 2) {
                             const int col = 16 * y + e;
@@ -475,32 +481,36 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                         }
                 }
                 if (what == 1) {
+                    const int32_t to = limit - j0;
                     if (mixed) {
 #pragma unroll
-                        for (int y = 0; y < 8; ++y)
+                        for (int y = 0; y < 4; ++y)
 #pragma unroll
                             for (int e = 0; e < 16; e += 4) {
-                                const int4 d4 = *reinterpret_cast<const int4*>(docs + 16 * y + e);
-                                if (!(j0 + 16 * y + e < limit && d4.x == doc)) sv[y][e] = 0xff800000u;
-                                if (!(j0 + 16 * y + e + 1 < limit && d4.y == doc)) sv[y][e + 1] = 0xff800000u;
-                                if (!(j0 + 16 * y + e + 2 < limit && d4.z == doc)) sv[y][e + 2] = 0xff800000u;
-                                if (!(j0 + 16 * y + e + 3 < limit && d4.w == doc)) sv[y][e + 3] = 0xff800000u;
+                                const int4 d4 = *reinterpret_cast<const int4*>(docs + c0 + 16 * y + e);
+                                if (!(16 * y + e < to && d4.x == doc)) sv[y][e] = 0xff800000u;
+                                if (!(16 * y + e + 1 < to && d4.y == doc)) sv[y][e + 1] = 0xff800000u;
+                                if (!(16 * y + e + 2 < to && d4.z == doc)) sv[y][e + 2] = 0xff800000u;
+                                if (!(16 * y + e + 3 < to && d4.w == doc)) sv[y][e + 3] = 0xff800000u;
                             }
                     } else {
 #pragma unroll
-                        for (int y = 0; y < 8; ++y)
+                        for (int y = 0; y < 4; ++y)
 #pragma unroll
                             for (int e = 0; e < 16; ++e)
-                                if (j0 + 16 * y + e >= limit) sv[y][e] = 0xff800000u;
+                                if (16 * y + e >= to) sv[y][e] = 0xff800000u;
                     }
                 }
-                // (four chains: one of 64 steps would take longer than the exponentials)
+                // (four chains: one would take longer than the exponentials)
                 float top4[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
 #pragma unroll
-                for (int y = 0; y < 8; ++y)
+                for (int y = 0; y < 4; ++y)
 #pragma unroll
                     for (int e = 0; e < 16; e += 2) top4[e >> 1 & 3] = max3_nan(top4[e >> 1 & 3], __uint_as_float(sv[y][e]), __uint_as_float(sv[y][e + 1]));
                 float top = max_nan(max_nan(top4[0], top4[1]), max_nan(top4[2], top4[3]));
+                tops[done & 1][tid] = top;
+                with_other_half();                              // (by then the other half has read its S, which P may overwrite)
+                top = max_nan(top, tops[done & 1][tid ^ 128]);
                 if (PLAIN) top *= to2;
                 // a new maximum only when it matters: 2^8 above the one in use (or the first)
                 // (NaN grows too, and stays; an infinite score makes its row NaN, as infinity - infinity would)
@@ -510,13 +520,13 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                     const float alpha = grow ? ex2(m - top) : 1.0f;
                     if (grow) m = top;
                     if (c > 0) {
-                        if (!(ok = wait(pv_done(g), (uint32_t)(done - 1) & 1u))) break;
+                        wait(pv_done(g), (uint32_t)(done - 1) & 1u);
                         fence_after_sync();
                         const uint64_t a2 = pack2(alpha, alpha);
-#pragma unroll
-                        for (int y = 0; y < 4; ++y) sum2[y] = mul2(sum2[y], a2);
-#pragma unroll
-                        for (int y = 0; y < DP / 16; ++y) {
+                        sum2[0] = mul2(sum2[0], a2);
+                        sum2[1] = mul2(sum2[1], a2);
+#pragma unroll 1
+                        for (int y = 0; y < DP / 32; ++y) {
                             uint32_t o[16];
                             tmem_ld16(o_addr + 16 * y, o);
 #pragma unroll
@@ -526,22 +536,22 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                     }
                 }
                 if (Sh::SEP && done > 0) {
-                    if (!(ok = wait(pv_done(g), (uint32_t)(done - 1) & 1u))) break;
+                    wait(pv_done(g), (uint32_t)(done - 1) & 1u);
                     fence_after_sync();
                 }
                 const float base = m == -CUDART_INF_F ? 0.0f : m;
                 const uint64_t minus = pack2(-base, -base), to22 = pack2(to2, to2);
 #pragma unroll
-                for (int y = 0; y < 4; ++y) {
+                for (int y = 0; y < 2; ++y) {
                     uint32_t w[16], u[EXACT ? 16 : 1];
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
                         const int a = 2 * y + (e >> 3), z = (2 * e) & 15;
                         float x0, x1;
                         unpack2(PLAIN ? fma2(pack2(sv[a][z], sv[a][z + 1]), to22, minus) : add2(pack2(sv[a][z], sv[a][z + 1]), minus), x0, x1);
-                        if (GRF_FMA_PAIRS(16 * y + e)) ex2_by_fma<EXACT ? 4 : 3>(pack2(x0, x1), x0, x1);
+                        if (FMA && GRF_FMA_PAIRS(16 * y + e)) ex2_by_fma<EXACT ? 4 : 3>(pack2(x0, x1), x0, x1);
                         else { x0 = ex2(x0); x1 = ex2(x1); }
-                        sum2[e & 3] = add2(sum2[e & 3], pack2(x0, x1));
+                        sum2[e & 1] = add2(sum2[e & 1], pack2(x0, x1));
                         w[e] = pack_bf16(x0, x1);
                         if (EXACT) u[EXACT ? e : 0] = pack_bf16(x0 - __uint_as_float(w[e] << 16), x1 - __uint_as_float(w[e] & 0xffff0000u));
                     }
@@ -555,24 +565,24 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 ++c;
                 ++done;
             }
-            ok = __all_sync(0xffffffffu, ok) != 0;
-            if (ok && c > 0) ok = wait(pv_done(g), (uint32_t)(done - 1) & 1u);
-            if (!ok) break;
+            if (c > 0) wait(pv_done(g), (uint32_t)(done - 1) & 1u);
             fence_after_sync();
             float l0, l1;
-            unpack2(add2(add2(sum2[0], sum2[1]), add2(sum2[2], sum2[3])), l0, l1);
-            const float l = l0 + l1, inv = l == 0.0f ? 0.0f : 1.0f / l;
+            unpack2(add2(sum2[0], sum2[1]), l0, l1);
+            sums[tid] = l0 + l1;
+            with_other_half();
+            const float l = sums[tid & ~128] + sums[tid | 128], inv = l == 0.0f ? 0.0f : 1.0f / l;
             bool spoilt = false;
             __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.out_w) + b * p.os[0] + h * p.os[1] + (int64_t)i * p.os[2];
             __nv_bfloat16* rest = p.rest_w ? p.rest_w + (((int64_t)b * p.H + h) * p.Nq + i) * p.d : nullptr;
             // (a loop: once a block, its instructions come from afar)
 #pragma unroll 1
-            for (int y = 0; y < DP / 16; ++y) {
+            for (int y = 0; y < DP / 32; ++y) {
                 uint32_t o[16];
 #pragma unroll
                 for (int e = 0; e < 16; ++e) o[e] = 0u;
                 if (c > 0) tmem_ld16(o_addr + 16 * y, o);
-                if (c > 0 && y == DP / 16 - 1) {
+                if (c > 0 && y == DP / 32 - 1) {
                     // the accumulator may be written again
                     fence_before_sync();
                     __syncwarp();
@@ -581,7 +591,7 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 if (i >= p.Nq) continue;
 #pragma unroll
                 for (int z = 0; z < 2; ++z) {
-                    const int col = 16 * y + 8 * z;
+                    const int col = half * (DP / 2) + 16 * y + 8 * z;
                     if (col >= p.d) continue;
                     uint32_t w[4], u[4];
 #pragma unroll
@@ -599,21 +609,23 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                     if (EXACT) *reinterpret_cast<uint4*>(rest + col) = make_uint4(u[0], u[1], u[2], u[3]);
                 }
             }
-            if (p.lse_w && i < p.Nq) p.lse_w[((int64_t)b * p.H + h) * p.Nq + i] = l == 0.0f ? -CUDART_INF_F : (m + log2f(l)) * GRF_LN2;
-            // rows whose scores are finite but whose outputs are not
+            if (half == 0 && p.lse_w && i < p.Nq) p.lse_w[((int64_t)b * p.H + h) * p.Nq + i] = l == 0.0f ? -CUDART_INF_F : (m + log2f(l)) * GRF_LN2;
+            // rows whose scores are finite but whose outputs are not: each half its own columns
             uint32_t again = __ballot_sync(0xffffffffu, spoilt && l <= 3.4028235e38f && fabsf(m) <= 3.4028235e38f);
             __syncwarp();
             while (again) {
                 const int y = __ffs(again) - 1;
                 again &= again - 1;
-                redo_row<CAP>(p, bucket, b, h, __shfl_sync(0xffffffffu, i, y), __shfl_sync(0xffffffffu, m, y), __shfl_sync(0xffffffffu, l, y));
+                redo_row<CAP>(p, bucket, b, h, __shfl_sync(0xffffffffu, i, y), __shfl_sync(0xffffffffu, m, y), __shfl_sync(0xffffffffu, l, y), half * (DP / 2),
+                              (half + 1) * (DP / 2));
             }
+            with_other_half();                                  // (the sums are read: they may be written again)
         }
         fence_before_sync();
     }
     fence_before_sync();
     __syncthreads();
-    if (warp == COPY) tmem_dealloc(tmem, Sh::TMEM);
+    if (warp == COPY) tmem_dealloc(tmem, 512u);
     if (tid == 0 && abort_flag) atomicExch(p.error_word, 1);
 }
 
@@ -623,12 +635,12 @@ template <int DP, bool CAP, int BIAS, bool EXACT> int launch(grf_ctx* ctx, const
 {
     using Sh = Fwd<DP, EXACT>;
     const auto kernel = softmax_tc_forward_kernel<DP, CAP, BIAS, EXACT>;
-    const size_t smem = Sh::SMEM + (p.q_doc ? 4 * (size_t)(3 * Sh::QT + 2) * (grf_ceil_div(p.Nk, BT) / 32 + 1) : 0);
+    const size_t smem = Sh::SMEM + (p.q_doc ? 4 * (size_t)(3 * QT + 2) * (grf_ceil_div(p.Nk, BT) / 32 + 1) : 0);
     GRF_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     grf_softmax_scope scope(ctx, "grf:softmax_attention");
     // as many CTAs as the device holds at once, which take block after block; with documents a CTA per block
-    const int64_t items = (int64_t)p.B * p.H * grf_ceil_div(p.Nq, Sh::QT * BT), room = (int64_t)ctx->sm_count * Sh::CTAS;
-    kernel<<<(unsigned)(p.q_doc || items < room ? items : room), Sh::THREADS, smem, ctx->stream>>>(m.q, m.k, m.v, p);
+    const int64_t items = (int64_t)p.B * p.H * grf_ceil_div(p.Nq, QT * BT), room = ctx->sm_count;
+    kernel<<<(unsigned)(p.q_doc || items < room ? items : room), THREADS, smem, ctx->stream>>>(m.q, m.k, m.v, p);
     return cudaGetLastError() == cudaSuccess ? GRF_OK : GRF_ERR_CUDA;
 }
 
@@ -652,6 +664,7 @@ template <int DP> int by_rest(grf_ctx* ctx, const grf_softmax_params& p, const f
 
 int grf_softmax_tc_forward(grf_ctx* ctx, const grf_softmax_params& p)
 {
+    if (p.q_doc && p.Nk > (1 << 20)) return 1;                  // the tiles' bits: 8 KB there, more do not fit beside d = 128
     forward_maps m;
     if (!grf_make_token_box_map(&m.q, p.q, p.qs, p.B, p.H, p.Nq, p.d) || !grf_make_token_box_map(&m.k, p.k, p.ks, p.B, p.KV, p.Nk, p.d) ||
         !grf_make_token_box_map(&m.v, p.v, p.vs, p.B, p.KV, p.Nk, p.d)) return 1;
