@@ -5,20 +5,27 @@
 //          shuffles (a lane hands its sum to the next lane, which adds the next column), and the diagonals by bucket
 //   dK, dV a CTA of 128 keys goes over the query tiles of all heads that share it, transposed: S^T = K Q^T, dP^T = V dout^T (a key per lane), so
 //          that P^T and dX^T are left operands where they are made: dV += P^T dout, dK += dX^T Q
-// Seven products a tile where a single kernel would need five, but no tile of dQ travels through memory.  Two warpgroups share a tile, 64
+// Seven products a tile where a single kernel would need five, but no tile of dQ travels through memory.  Four warpgroups share a tile, 32
 // columns each, and work in turn with the products: while P of a tile is made the tensor cores finish the one before, while dS is made they
 // make the next S.  Three warps copy, issue, and prepare: lse and D of the queries (dK, dV), and rows that nobody sees cleared (0 times an
 // infinity there would reach a whole tile).
+#include <cooperative_groups.h>
+
 #include "softmax_tc.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace {
 
 using namespace grf_softmax_tc;
 
-constexpr int THREADS = 384, WORKERS = 8;           // warps that make P and dS
-constexpr int MORE = 208, LESS = 88;                // registers: 2 * 208 + 88 = 3 * 168
+constexpr int THREADS = 640, WORKERS = 16;          // warps that make P and dS
+constexpr int MORE = 104, LESS = 64;                // registers: 4 * 104 + 64 = 5 * 96
+constexpr int W = 32;                               // columns of a worker
 constexpr int COPY = WORKERS, ISSUE = WORKERS + 1, PREPARE = WORKERS + 2;
 constexpr int NS = 2;
+
+struct head_split { int32_t splits; };
 
 template <int DP> struct Grad {
     static constexpr uint32_t TILE = HALF * (DP / 64);
@@ -52,28 +59,19 @@ __device__ __forceinline__ float min_nan(float a, float b)
     asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
-// 2^x of a row's 64 values.  (NaN in a value that takes the multiply-adds becomes 0; a row of NaN has a NaN D, which its gradients meet.)
-__device__ __forceinline__ void powers(float (&x)[64])
-{
-#pragma unroll
-    for (int e = 0; e < 64; e += 2) {
-        if (GRF_FMA_PAIRS(e / 2)) ex2_by_fma<4>(pack2(x[e], x[e + 1]), x[e], x[e + 1]);
-        else { x[e] = ex2(x[e]); x[e + 1] = ex2(x[e + 1]); }
-    }
-}
 __device__ __forceinline__ void clear_row(uint32_t tile, int r, int halves)
 {
     for (int y = 0; y < halves; ++y)
         for (int x = 0; x < 8; ++x) asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(tile + y * HALF + r * 128 + x * 16), "r"(0u) : "memory");
 }
-// D[128][DP] (+)= A B: A's bf16 pairs in two halves of 32 columns, 64 columns apart.
+// D[128][DP] (+)= A B: A's bf16 pairs in the first half of every worker's columns.
 template <int DP>
-__device__ __forceinline__ void product_of_halves(uint32_t acc, uint32_t a_tmem, uint32_t b_lo, uint32_t b_hi, uint32_t accumulate)
+__device__ __forceinline__ void product_of_parts(uint32_t acc, uint32_t a_tmem, uint32_t b_lo, uint32_t b_hi, uint32_t accumulate)
 {
     constexpr uint32_t idesc = instr_desc(DP, false, true);
 #pragma unroll
     for (int y = 0; y < BT / 16; ++y)
-        mma_bf16_ts_halves(acc, a_tmem + (y / 4) * 64 + (y % 4) * 8, b_lo + y * (2048 / 16), b_hi, idesc, y > 0 ? 1u : accumulate);
+        mma_bf16_ts_halves(acc, a_tmem + (y / 2) * W + (y % 2) * 8, b_lo + y * (2048 / 16), b_hi, idesc, y > 0 ? 1u : accumulate);
 }
 
 template <int DP, bool CAP, int BIAS>
@@ -91,7 +89,7 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     __shared__ grf_buckets bucket;
     __shared__ __align__(16) int32_t doc_of[2 * BT];
     __shared__ float bins[LUTS ? WORKERS * 2 * GRF_MAX_BUCKETS : 1];
-    __shared__ float diag[LUTS ? WORKERS * 96 : 1];
+    __shared__ float diag[LUTS ? WORKERS * 64 : 1];
     const int tid = threadIdx.x, lane = tid & 31, warp = uniform(tid >> 5);
     const uint32_t smem = (smem_u32(smem_dyn) + 1023u) & ~1023u;
     uint32_t* bits = reinterpret_cast<uint32_t*>(smem_dyn + (smem - smem_u32(smem_dyn)) + Sh::TILE * (2 + 2 * NS));
@@ -211,7 +209,7 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     cleaned ^= 1u << s;
                 }
                 fence_after_sync();
-                product_of_halves<DP>(acc, dp_col, lo32(kc_op) + s * (Sh::TILE / 16), hi32(kc_op), n > 0 ? 1u : 0u);
+                product_of_parts<DP>(acc, dp_col, lo32(kc_op) + s * (Sh::TILE / 16), hi32(kc_op), n > 0 ? 1u : 0u);
                 mma_commit(k_empty(s));
                 if (t_next >= tiles) mma_commit(dq_done);
                 else ok = make_dp(n + 1);
@@ -241,7 +239,7 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(MORE));
-        const int r = (warp & 3) * 32 + lane, part = warp >> 2, c0 = part * 64;
+        const int r = (warp & 3) * 32 + lane, part = warp >> 2, c0 = part * W;
         const int32_t i = i0 + r, pos = sight.position(i), pos0 = sight.position(i0);
         const int32_t limit = sight.order == GRF_ORDER_FULL ? sight.len : min(sight.len, max(pos + 1, sight.prefix));
         const int32_t all_see = sight.order == GRF_ORDER_FULL ? sight.len : min(sight.len, max(pos0 + 1, sight.prefix));       // keys before it: the whole block
@@ -285,7 +283,7 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             if (diagonals || mixed) {
                 if (LUTS && diagonals) {
                     float* at = lut + (luts & 1) * 256;
-                    at[tid] = tid < 2 * BT - 1 ? grf_bias2<__nv_bfloat16>(p, bucket, h, j0 - pos0 + tid - (BT - 1)) : 0.0f;
+                    if (tid < 256) at[tid] = tid < 2 * BT - 1 ? grf_bias2<__nv_bfloat16>(p, bucket, h, j0 - pos0 + tid - (BT - 1)) : 0.0f;
                     mine = at + (BT - 1 - r) + c0;
                 }
                 if (mixed && tid < BT) docs[tid] = j0 + tid < p.Nk ? p.k_doc[(int64_t)b * p.Nk + j0 + tid] : -1;
@@ -297,15 +295,15 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             if (!(ok = wait(s_full0 + 8 * (n & 1), (uint32_t)(n >> 1) & 1u))) break;
             fence_after_sync();
             const float ahead = (float)(j0 + c0 - pos);
-            float x[64], dcap[CAP ? 64 : 1];
+            float x[W], dcap[CAP ? W : 1];
             {
-                uint32_t sv[4][16];
+                uint32_t sv[W / 16][16];
 #pragma unroll
-                for (int y = 0; y < 4; ++y) tmem_ld16_nowait(tmem + (n & 1) * BT + c0 + 16 * y + lanes, sv[y]);
+                for (int y = 0; y < W / 16; ++y) tmem_ld16_nowait(tmem + (n & 1) * BT + c0 + 16 * y + lanes, sv[y]);
                 tmem_ld_wait();
-                if (CAP) capped<4>(sv, by_cap);
+                if (CAP) capped<W / 16>(sv, by_cap);
 #pragma unroll
-                for (int e = 0; e < 64; ++e) {
+                for (int e = 0; e < W; ++e) {
                     const float raw = __uint_as_float(sv[e / 16][e % 16]);
                     float s;
                     if (CAP) {
@@ -314,16 +312,15 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     } else s = fmaf(raw, to2, bias2);
                     if (BIAS == GRF_BIAS_SLOPES) s = fmaf(-slope2, fabsf(ahead + (float)e), s);
                     if (LUTS) { if (diagonals) s += mine[e]; }
-                    x[e] = min_nan(s - lse2, 0.0f);
+                    x[e] = ex2(min_nan(s - lse2, 0.0f));
                 }
-                powers(x);
             }
             const bool careful = partial || !any;               // (of this row: nothing in it may meet an infinity or NaN)
             if (careful) {
                 const int32_t to = any ? limit - j0 - c0 : 0;
                 if (mixed) {
 #pragma unroll
-                    for (int e = 0; e < 64; e += 4) {
+                    for (int e = 0; e < W; e += 4) {
                         const int4 d4 = *reinterpret_cast<const int4*>(docs + c0 + e);
                         if (!(e < to && d4.x == doc)) x[e] = 0.0f;
                         if (!(e + 1 < to && d4.y == doc)) x[e + 1] = 0.0f;
@@ -332,14 +329,14 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     }
                 } else {
 #pragma unroll
-                    for (int e = 0; e < 64; ++e)
+                    for (int e = 0; e < W; ++e)
                         if (e >= to) x[e] = 0.0f;
                 }
             }
             if (!(ok = wait(dp_full, (uint32_t)n & 1u))) break;
             fence_after_sync();
 #pragma unroll
-            for (int y = 0; y < 4; ++y) {
+            for (int y = 0; y < W / 16; ++y) {
                 uint32_t dv[16];
                 tmem_ld16(dp_col + c0 + 16 * y + lanes, dv);
 #pragma unroll
@@ -349,15 +346,14 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     x[16 * y + e] = careful && x[16 * y + e] == 0.0f ? 0.0f : x[16 * y + e] * d;
                 }
             }
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
+            {
                 uint32_t w[16];
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const int a = 32 * y + 2 * e;
+                    const int a = 2 * e;
                     w[e] = CAP ? pack_bf16(x[a] * dcap[CAP ? a : 0], x[a + 1] * dcap[CAP ? a + 1 : 0]) : pack_bf16(x[a], x[a + 1]);
                 }
-                tmem_st16(dp_col + c0 + 16 * y + lanes, w);
+                tmem_st16(dp_col + c0 + lanes, w);
             }
             tmem_st_wait();
             fence_before_sync();
@@ -369,24 +365,24 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     if (bucket0 != far_bucket) { flush(); far_bucket = bucket0; }
                     float y0 = 0.0f, y1 = 0.0f, y2 = 0.0f, y3 = 0.0f;
 #pragma unroll
-                    for (int e = 0; e < 64; e += 4) { y0 += x[e]; y1 += x[e + 1]; y2 += x[e + 2]; y3 += x[e + 3]; }
+                    for (int e = 0; e < W; e += 4) { y0 += x[e]; y1 += x[e + 1]; y2 += x[e + 2]; y3 += x[e + 3]; }
                     far_sum += (y0 + y1) + (y2 + y3);
                 } else {
                     // diagonal e - lane is complete in lane 31 after column e; those that end at the last column are in the other lanes
                     float a = 0.0f;
-                    float* at = diag + warp * 96;
+                    float* at = diag + warp * 64;
 #pragma unroll
-                    for (int e = 0; e < 64; ++e) {
+                    for (int e = 0; e < W; ++e) {
                         const float up = __shfl_up_sync(0xffffffffu, a, 1);
                         a = x[e] + (lane > 0 ? up : 0.0f);
                         if (lane == 31) at[e] = a;
                     }
-                    if (lane < 31) at[64 + 30 - lane] = a;      // diagonal 63 - lane; place x holds diagonal x - 31
+                    if (lane < 31) at[W + 30 - lane] = a;       // diagonal 31 - lane; place x holds diagonal x - 31
                     __syncwarp();
 #pragma unroll
-                    for (int z = 0; z < 3; ++z) {
+                    for (int z = 0; z < 2; ++z) {
                         const int d = lane + 32 * z;
-                        grf_add_runs(my_bins, d < 95 ? bucket(p, j0 + c0 + d - 31 - sight.position(i0 + (warp & 3) * 32)) : -1, d < 95 ? at[d] : 0.0f);
+                        grf_add_runs(my_bins, d < 63 ? bucket(p, j0 + c0 + d - 31 - sight.position(i0 + (warp & 3) * 32)) : -1, d < 63 ? at[d] : 0.0f);
                     }
                     __syncwarp();
                 }
@@ -398,9 +394,9 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         fence_after_sync();
         if (ok) {
             __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.dq) + b * p.dqs[0] + h * p.dqs[1] + (int64_t)i * p.dqs[2];
-#pragma unroll
-            for (int y = 0; y < DP / 32; ++y) {
-                const int col = part * (DP / 2) + 16 * y;
+#pragma unroll 1
+            for (int y = 0; y < DP / 64; ++y) {
+                const int col = part * (DP / 4) + 16 * y;
                 uint32_t o[16];
 #pragma unroll
                 for (int e = 0; e < 16; ++e) o[e] = 0u;
@@ -432,10 +428,11 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
 template <int DP, bool CAP, int BIAS>
 __global__ void __launch_bounds__(THREADS, 1)
 softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-                      const __grid_constant__ CUtensorMap map_g, const __grid_constant__ grf_softmax_params p)
+                       const __grid_constant__ CUtensorMap map_g, const __grid_constant__ grf_softmax_params p, const head_split f)
 {
     using Sh = Grad<DP>;
     constexpr int LUTS = BIAS == GRF_BIAS_BUCKETS ? 1 : 0;
+    constexpr int SUM_ROW = DP + 4;
     extern __shared__ unsigned char smem_dyn[];
     __shared__ __align__(8) unsigned long long bars[4 * NS + 9];
     __shared__ uint32_t tmem_slot;
@@ -456,7 +453,10 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     const uint32_t keys_full = one, s_full = one + 8, dp_full = one + 16, p_full = one + 24, ds_full = one + 32, acc_done = one + 40, drain = one + 48,
                    lut_full = one + 56;
 
-    const int32_t b = (int32_t)blockIdx.x / p.KV, kvh = (int32_t)blockIdx.x % p.KV;
+    // block x: part x % splits of the heads that share key head x / splits; the parts of one make a cluster
+    const int32_t unit = (int32_t)blockIdx.x / f.splits, rank_ = (int32_t)blockIdx.x % f.splits, b = unit / p.KV, kvh = unit % p.KV;
+    const int32_t h_first = kvh * p.group + p.group * rank_ / f.splits, h_end = kvh * p.group + p.group * (rank_ + 1) / f.splits;
+    float* sums = reinterpret_cast<float*>(smem_dyn + (smem - smem_u32(smem_dyn)));       // [dV, dK][key][SUM_ROW], once the tiles are done with
     const grf_sight sight(p, b);
     const int32_t j0 = (int32_t)blockIdx.y * BT, qblocks = (p.Nq + BT - 1) / BT;
     // the first query that sees a key of the block, were there no documents
@@ -500,7 +500,7 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     auto step = [&](int32_t& t, int32_t& h) {
         t = T.next(t + 1);
         if (t >= qblocks) {
-            if (++h >= (kvh + 1) * p.group) return false;
+            if (++h >= h_end) return false;
             t = T.begin();
         }
         return true;
@@ -517,7 +517,7 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                     load_box(k_at + y * HALF, &map_k, 64 * y, j0, p.ks[1] ? kvh : 0, p.ks[0] ? b : 0, keys_full);
                     load_box(v_at + y * HALF, &map_v, 64 * y, j0, p.vs[1] ? kvh : 0, p.vs[0] ? b : 0, keys_full);
                 }
-                int32_t t = T.begin(), h = kvh * p.group;
+                int32_t t = T.begin(), h = h_first;
                 do {
                     const int s = n % NS;
                     if (n >= NS && !(ok = wait(empty(s), (uint32_t)(n / NS - 1) & 1u))) break;
@@ -559,7 +559,7 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                 return true;
             };
             if (some) {
-                int32_t t = T.begin(), h = kvh * p.group, n = 0;
+                int32_t t = T.begin(), h = h_first, n = 0;
                 ok = wait(keys_full, 0u) && make_scores(0) && make_dp(0);
                 bool more = true;
                 for (; ok && more; ++n) {
@@ -567,11 +567,11 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                     more = step(t, h);
                     if (!(ok = wait(p_full, (uint32_t)n & 1u))) break;
                     fence_after_sync();
-                    product_of_halves<DP>(dv_acc, s_col, lo32(gc_op) + s * (Sh::TILE / 16), hi32(gc_op), n > 0 ? 1u : 0u);
+                    product_of_parts<DP>(dv_acc, s_col, lo32(gc_op) + s * (Sh::TILE / 16), hi32(gc_op), n > 0 ? 1u : 0u);
                     if (more && !(ok = make_scores(n + 1))) break;
                     if (!(ok = wait(ds_full, (uint32_t)n & 1u))) break;
                     fence_after_sync();
-                    product_of_halves<DP>(dk_acc, dp_col, lo32(qc_op) + s * (Sh::TILE / 16), hi32(qc_op), n > 0 ? 1u : 0u);
+                    product_of_parts<DP>(dk_acc, dp_col, lo32(qc_op) + s * (Sh::TILE / 16), hi32(qc_op), n > 0 ? 1u : 0u);
                     mma_commit(empty(s));
                     if (!more) mma_commit(acc_done);
                     else ok = make_dp(n + 1);
@@ -582,7 +582,7 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                 }
             }
         } else if (warp == PREPARE && some) {
-            int32_t t = T.begin(), h = kvh * p.group, n = 0;
+            int32_t t = T.begin(), h = h_first, n = 0;
             do {
                 const int s = n % NS;
                 if (n >= NS && !wait(empty(s), (uint32_t)(n / NS - 1) & 1u)) break;
@@ -617,7 +617,7 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(MORE));
-        const int r = (warp & 3) * 32 + lane, part = warp >> 2, c0 = part * 64;
+        const int r = (warp & 3) * 32 + lane, part = warp >> 2, c0 = part * W;
         const int32_t j = j0 + r;
         int32_t doc = sight.docs && j < p.Nk ? p.k_doc[(int64_t)b * p.Nk + j] : -1;
         if (doc < 0) doc = INT32_MIN;                           // (equal to no query's)
@@ -627,7 +627,7 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         int32_t n = 0, luts = 0;
         bool ok = true;
         if (some) {
-            int32_t t = T.begin(), h = kvh * p.group;
+            int32_t t = T.begin(), h = h_first;
             do {
                 const int s = n % NS;
                 const int32_t i0 = t * BT, pos0 = sight.position(i0);
@@ -642,7 +642,7 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                     diagonals = bucket(p, j0 - pos0 - (BT - 1)) != bucket(p, j0 + BT - 1 - pos0);
                     if (diagonals) {
                         float* at = lut + (luts & 1) * 256;
-                        at[tid] = tid < 2 * BT - 1 ? grf_bias2<__nv_bfloat16>(p, bucket, h, j0 - pos0 + tid - (BT - 1)) : 0.0f;
+                        if (tid < 256) at[tid] = tid < 2 * BT - 1 ? grf_bias2<__nv_bfloat16>(p, bucket, h, j0 - pos0 + tid - (BT - 1)) : 0.0f;
                         mine = at + (BT - 1 + r - c0);          // column e: mine[-e]
                         __syncwarp();
                         if (lane == 0) mbar_arrive(lut_full);
@@ -653,15 +653,15 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                 if (!(ok = wait(ready(s), (uint32_t)(n / NS) & 1u) && wait(s_full, (uint32_t)n & 1u))) break;
                 fence_after_sync();
                 const float ahead = (float)(j - pos0 - c0);
-                float x[64], dcap[CAP ? 64 : 1];
+                float x[W], dcap[CAP ? W : 1];
                 {
-                    uint32_t sv[4][16];
+                    uint32_t sv[W / 16][16];
 #pragma unroll
-                    for (int y = 0; y < 4; ++y) tmem_ld16_nowait(s_col + c0 + 16 * y + lanes, sv[y]);
+                    for (int y = 0; y < W / 16; ++y) tmem_ld16_nowait(s_col + c0 + 16 * y + lanes, sv[y]);
                     tmem_ld_wait();
-                    if (CAP) capped<4>(sv, by_cap);
+                    if (CAP) capped<W / 16>(sv, by_cap);
 #pragma unroll
-                    for (int e4 = 0; e4 < 64; e4 += 4) {
+                    for (int e4 = 0; e4 < W; e4 += 4) {
                         const float4 l4 = *reinterpret_cast<const float4*>(&info[s][0][c0 + e4]);
                         const float lv[4] = {l4.x, l4.y, l4.z, l4.w};
 #pragma unroll
@@ -675,16 +675,15 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                             } else sc = fmaf(raw, to2, bias2);
                             if (BIAS == GRF_BIAS_SLOPES) sc = fmaf(-slope2, fabsf(ahead - (float)e), sc);
                             if (LUTS) { if (diagonals) sc += mine[-e]; }
-                            x[e] = min_nan(sc - lv[z], 0.0f);
+                            x[e] = ex2(min_nan(sc - lv[z], 0.0f));
                         }
                     }
-                    powers(x);
                 }
                 if (partial) {
                     const int32_t since = from - c0;
                     if (T.mixed(t)) {
 #pragma unroll
-                        for (int e = 0; e < 64; e += 4) {
+                        for (int e = 0; e < W; e += 4) {
                             const int4 d4 = *reinterpret_cast<const int4*>(&info_doc[s][c0 + e]);
                             if (!(e >= since && d4.x == doc)) x[e] = 0.0f;
                             if (!(e + 1 >= since && d4.y == doc)) x[e + 1] = 0.0f;
@@ -693,16 +692,15 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                         }
                     } else {
 #pragma unroll
-                        for (int e = 0; e < 64; ++e)
+                        for (int e = 0; e < W; ++e)
                             if (e < since) x[e] = 0.0f;
                     }
                 }
-#pragma unroll
-                for (int y = 0; y < 2; ++y) {
+                {
                     uint32_t w[16];
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) w[e] = pack_bf16(x[32 * y + 2 * e], x[32 * y + 2 * e + 1]);
-                    tmem_st16(s_col + c0 + 16 * y + lanes, w);
+                    for (int e = 0; e < 16; ++e) w[e] = pack_bf16(x[2 * e], x[2 * e + 1]);
+                    tmem_st16(s_col + c0 + lanes, w);
                 }
                 tmem_st_wait();
                 fence_before_sync();
@@ -711,7 +709,7 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                 if (!(ok = wait(dp_full, (uint32_t)n & 1u))) break;
                 fence_after_sync();
 #pragma unroll
-                for (int y = 0; y < 4; ++y) {
+                for (int y = 0; y < W / 16; ++y) {
                     uint32_t dv[16];
                     tmem_ld16(dp_col + c0 + 16 * y + lanes, dv);
 #pragma unroll
@@ -726,12 +724,11 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                         }
                     }
                 }
-#pragma unroll
-                for (int y = 0; y < 2; ++y) {
+                {
                     uint32_t w[16];
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) w[e] = pack_bf16(x[32 * y + 2 * e], x[32 * y + 2 * e + 1]);
-                    tmem_st16(dp_col + c0 + 16 * y + lanes, w);
+                    for (int e = 0; e < 16; ++e) w[e] = pack_bf16(x[2 * e], x[2 * e + 1]);
+                    tmem_st16(dp_col + c0 + lanes, w);
                 }
                 tmem_st_wait();
                 fence_before_sync();
@@ -743,26 +740,35 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         ok = __all_sync(0xffffffffu, ok) != 0;
         if (ok && n > 0) ok = wait(acc_done, 0u);
         fence_after_sync();
-        if (ok) {
-            // the first warpgroup writes dV, the second one dK
-            const int64_t (&st)[3] = part == 0 ? p.dvs : p.dks;
-            __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(part == 0 ? p.dv : p.dk) + b * st[0] + kvh * st[1] + (int64_t)j * st[2];
-            const float by = part == 0 ? 1.0f : p.scale;
+        // the first two warpgroups have dV, half of its columns each, the others dK
+        const bool is_dv = part < 2;
+        const int col0 = (part & 1) * (DP / 2);
+        const int64_t (&st)[3] = is_dv ? p.dvs : p.dks;
+        __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(is_dv ? p.dv : p.dk) + b * st[0] + kvh * st[1] + (int64_t)j * st[2];
+        const float by = is_dv ? 1.0f : p.scale;
+#pragma unroll 1
+        for (int y = 0; y < DP / 32; ++y) {
+            uint32_t o[16];
+            const int col = col0 + 16 * y;
 #pragma unroll
-            for (int y = 0; y < DP / 16; ++y) {
-                uint32_t o[16];
+            for (int e = 0; e < 16; ++e) o[e] = 0u;
+            if (ok && n > 0) tmem_ld16((is_dv ? dv_acc : dk_acc) + col + lanes, o);
+            if (f.splits > 1) {
+                // for the other CTAs of the cluster, where the tiles were
+                float4* at = reinterpret_cast<float4*>(sums + ((is_dv ? 0 : 1) * BT + r) * SUM_ROW + col);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) o[e] = 0u;
-                if (n > 0) tmem_ld16((part == 0 ? dv_acc : dk_acc) + 16 * y + lanes, o);
-                if (j >= p.Nk) continue;
+                for (int e = 0; e < 4; ++e)
+                    at[e] = make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]), __uint_as_float(o[4 * e + 3]));
+                continue;
+            }
+            if (!ok || j >= p.Nk) continue;
 #pragma unroll
-                for (int z = 0; z < 2; ++z) {
-                    if (16 * y + 8 * z >= p.d) continue;
-                    uint32_t w[4];
+            for (int z = 0; z < 2; ++z) {
+                if (col + 8 * z >= p.d) continue;
+                uint32_t w[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) w[e] = pack_bf16(__uint_as_float(o[8 * z + 2 * e]) * by, __uint_as_float(o[8 * z + 2 * e + 1]) * by);
-                    *reinterpret_cast<uint4*>(dst + 16 * y + 8 * z) = make_uint4(w[0], w[1], w[2], w[3]);
-                }
+                for (int e = 0; e < 4; ++e) w[e] = pack_bf16(__uint_as_float(o[8 * z + 2 * e]) * by, __uint_as_float(o[8 * z + 2 * e + 1]) * by);
+                *reinterpret_cast<uint4*>(dst + col + 8 * z) = make_uint4(w[0], w[1], w[2], w[3]);
             }
         }
         fence_before_sync();
@@ -770,6 +776,30 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     fence_before_sync();
     __syncthreads();
     if (warp == COPY) tmem_dealloc(tmem, 512u);
+    if (f.splits > 1) {
+        // sums over the heads' CTAs, in order; every CTA has a share of the rows
+        cg::cluster_group cluster = cg::this_cluster();
+        cluster.sync();
+        constexpr int PIECES = DP / 8;
+        const int rank = (int)cluster.block_rank(), r0 = BT * rank / f.splits, r1 = BT * (rank + 1) / f.splits;
+        for (int x = tid; x < 2 * (r1 - r0) * PIECES; x += THREADS) {
+            const int what = x / ((r1 - r0) * PIECES), r = r0 + x / PIECES % (r1 - r0), col = x % PIECES * 8;
+            if (j0 + r >= p.Nk || col >= p.d) continue;
+            float v[8] = {};
+            for (int s = 0; s < f.splits; ++s) {
+                const float4* at = reinterpret_cast<const float4*>(cluster.map_shared_rank(sums + (what * BT + r) * SUM_ROW + col, s));
+                const float4 u = at[0], w = at[1];
+                v[0] += u.x; v[1] += u.y; v[2] += u.z; v[3] += u.w;
+                v[4] += w.x; v[5] += w.y; v[6] += w.z; v[7] += w.w;
+            }
+            const int64_t (&st)[3] = what == 0 ? p.dvs : p.dks;
+            const float by = what == 0 ? 1.0f : p.scale;
+            __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(what == 0 ? p.dv : p.dk) + b * st[0] + kvh * st[1] + (int64_t)(j0 + r) * st[2] + col;
+            *reinterpret_cast<uint4*>(dst) = make_uint4(pack_bf16(v[0] * by, v[1] * by), pack_bf16(v[2] * by, v[3] * by), pack_bf16(v[4] * by, v[5] * by),
+                                                        pack_bf16(v[6] * by, v[7] * by));
+        }
+        cluster.sync();                                         // nobody's shared memory goes while it is read
+    }
     if (tid == 0 && abort_flag) atomicExch(p.error_word, 1);
 }
 
@@ -783,7 +813,23 @@ template <int DP, bool CAP, int BIAS> int launch(grf_ctx* ctx, const grf_softmax
     GRF_CUDA_TRY(cudaFuncSetAttribute(softmax_tc_dq_kernel<DP, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)dq_smem));
     GRF_CUDA_TRY(cudaFuncSetAttribute(softmax_tc_dkv_kernel<DP, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)dkv_smem));
     grf_softmax_scope scope(ctx, "grf:softmax_gradients", 2);
-    softmax_tc_dkv_kernel<DP, CAP, BIAS><<<dim3(p.B * p.KV, grf_ceil_div(p.Nk, BT)), THREADS, dkv_smem, ctx->stream>>>(m.q, m.k, m.v, m.g, p);
+    // The heads that share a key head are split over a cluster's CTAs, which add their sums through distributed shared memory, where there are
+    // too few blocks of keys to fill the device evenly (causal ones take 1 to Nq / 128 tiles a head).  MEASURED
+    head_split f = {1};
+    const int64_t blocks = (int64_t)p.B * p.KV * grf_ceil_div(p.Nk, BT);
+    while (f.splits < p.group && f.splits < 8 && blocks * f.splits < 4 * ctx->sm_count) ++f.splits;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(p.B * p.KV * f.splits, grf_ceil_div(p.Nk, BT));
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = dkv_smem;
+    cfg.stream = ctx->stream;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = (unsigned)f.splits;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    GRF_CUDA_TRY(cudaLaunchKernelEx(&cfg, softmax_tc_dkv_kernel<DP, CAP, BIAS>, m.q, m.k, m.v, m.g, p, f));
     softmax_tc_dq_kernel<DP, CAP, BIAS><<<dim3(p.B * p.H, grf_ceil_div(p.Nq, BT)), THREADS, dq_smem, ctx->stream>>>(m.q, m.k, m.v, m.g, p);
     return cudaGetLastError() == cudaSuccess ? GRF_OK : GRF_ERR_CUDA;
 }
@@ -804,6 +850,7 @@ template <int DP> int choose(grf_ctx* ctx, const grf_softmax_params& p, const gr
 
 int grf_softmax_tc_backward(grf_ctx* ctx, const grf_softmax_params& p)
 {
+    if (p.q_doc && (p.Nk > (1 << 20) || p.Nq > (1 << 20))) return 1;       // the tiles' bits
     grad_maps m;
     if (!grf_make_token_box_map(&m.q, p.q, p.qs, p.B, p.H, p.Nq, p.d) || !grf_make_token_box_map(&m.k, p.k, p.ks, p.B, p.KV, p.Nk, p.d) ||
         !grf_make_token_box_map(&m.v, p.v, p.vs, p.B, p.KV, p.Nk, p.d) || !grf_make_token_box_map(&m.g, p.dout, p.dos, p.B, p.H, p.Nq, p.d)) return 1;
