@@ -346,7 +346,7 @@ int grf_softmax_attn(grf_ctx* ctx, const grf_softmax_desc* desc, const void* Q, 
  *   dQ_i = scale sum_j dX_ij k_j,  dK_j = scale sum_i dX_ij q_i,  dV_j = sum_i P_ij dout_i,  dtable[h][y] = sum of dS_ij over bucket y
  * dK and dV are sums over the heads that share them; dtable (dtype, [heads][n_buckets * (1 + two_sided)], optional, BUCKETS only) over the
  * batch.  All outputs are overwritten, rows that nothing reaches with zeros; dQ, dK, dV are all required.  No atomic additions: equal
- * calls give equal bits.  Scores of magnitude beyond 1e30 in a row's largest place leave P_ij of that row undefined in 0 .. 1. */
+ * calls give equal bits.  A row whose lse is beyond 1e30 in magnitude (its scores tell nothing any more) has gradients of 0. */
 int grf_softmax_attn_backward(grf_ctx* ctx, const grf_softmax_desc* desc, const void* Q, const void* K, const void* V, const void* out,
                               const float* lse, const void* rest, const void* dout, void* dQ, void* dK, void* dV, void* dtable, void* workspace,
                               size_t workspace_bytes);

@@ -275,7 +275,7 @@ __device__ __forceinline__ alu_row load_alu_row(const grf_softmax_params& p, con
     const bool in = i < p.Nq;
     const int64_t x = ((int64_t)b * p.H + h) * p.Nq + i;
     const float lse = in ? p.lse[x] : -CUDART_INF_F;
-    w.any = lse != -CUDART_INF_F;
+    w.any = !(fabsf(lse) > 1.0e30f);
     w.lse2 = lse * GRF_LOG2E;
     w.dsum = in ? p.dsum[x] : 0.0f;
     w.doc = qdoc && in ? qdoc[i] : -1;
@@ -291,9 +291,7 @@ __device__ __forceinline__ void score_gradient(const grf_softmax_params& p, cons
     x += bias2;
     bool seen = w.any;
     if (what == 1) seen = seen && sight.sees(w.pos, j) && (!kdoc || (w.doc >= 0 && kdoc[j] == w.doc));
-    float e = x - w.lse2;
-    e = e > 0.0f ? 0.0f : e;                                    // (NaN stays)
-    s = seen ? exp2f(e) : 0.0f;
+    s = seen ? exp2f(x - w.lse2) : 0.0f;
     ds = seen ? s * (dp - w.dsum) : 0.0f;
     dp = p.cap > 0.0f ? (seen ? ds * (1.0f - t * t) : 0.0f) : ds;
     // a row of dout that is not finite was left out of the products of a tile that is not seen whole

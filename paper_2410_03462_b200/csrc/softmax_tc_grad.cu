@@ -53,12 +53,7 @@ struct grad_tiles {
     __device__ __forceinline__ bool hole(int32_t t) const { return docs && bit(bits + 2 * words, t); }
 };
 
-__device__ __forceinline__ float min_nan(float a, float b)
-{
-    float r;
-    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-    return r;
-}
+constexpr float LARGEST = 1.0e30f;                  // of lse
 __device__ __forceinline__ void clear_row(uint32_t tile, int r, int halves)
 {
     for (int y = 0; y < halves; ++y)
@@ -247,8 +242,8 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         if (doc < 0) doc = INT32_MIN;                           // (equal to no key's)
         const int64_t row = ((int64_t)b * p.H + h) * p.Nq + i;
         const float lse = i < p.Nq ? p.lse[row] : -CUDART_INF_F, dsum = i < p.Nq ? p.dsum[row] : 0.0f;
-        const bool any = lse != -CUDART_INF_F;                  // a row without a key: P = 0
-        const float lse2 = any ? lse * GRF_LOG2E : CUDART_INF_F;
+        const bool any = !(fabsf(lse) > LARGEST);               // a row without a key, or one whose scores tell nothing any more: P = 0
+        const float minus_lse = any ? -lse * GRF_LOG2E : -CUDART_INF_F;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const float to2 = p.scale * GRF_LOG2E, by_cap = CAP ? p.scale / p.cap : 0.0f, cap2 = p.cap * GRF_LOG2E;
         const float slope2 = BIAS == GRF_BIAS_SLOPES ? p.slopes[h] * GRF_LOG2E : 0.0f;
@@ -294,64 +289,69 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             }
             if (!(ok = wait(s_full0 + 8 * (n & 1), (uint32_t)(n >> 1) & 1u))) break;
             fence_after_sync();
-            const float ahead = (float)(j0 + c0 - pos);
-            float x[W], dcap[CAP ? W : 1];
+            uint64_t x[W / 2], slope[CAP ? W / 2 : 1];          // P, then dS; t^2 - 1 of the cap
             {
                 uint32_t sv[W / 16][16];
 #pragma unroll
                 for (int y = 0; y < W / 16; ++y) tmem_ld16_nowait(tmem + (n & 1) * BT + c0 + 16 * y + lanes, sv[y]);
                 tmem_ld_wait();
                 if (CAP) capped<W / 16>(sv, by_cap);
+                const float ahead = (float)(j0 + c0 - pos);
+                const bool line = BIAS == GRF_BIAS_SLOPES && (sight.order == GRF_ORDER_CAUSAL || __all_sync(0xffffffffu, j0 + c0 + W - 1 <= pos));
+                const float at0 = minus_lse + (BIAS == GRF_BIAS_SLOPES ? (line ? slope2 * ahead : 0.0f) : bias2);
+                const uint64_t by = CAP ? pack2(cap2, cap2) : pack2(to2, to2), at02 = pack2(at0, at0);
 #pragma unroll
-                for (int e = 0; e < W; ++e) {
-                    const float raw = __uint_as_float(sv[e / 16][e % 16]);
-                    float s;
-                    if (CAP) {
-                        dcap[e] = fmaf(-raw, raw, 1.0f);
-                        s = fmaf(cap2, raw, bias2);
-                    } else s = fmaf(raw, to2, bias2);
-                    if (BIAS == GRF_BIAS_SLOPES) s = fmaf(-slope2, fabsf(ahead + (float)e), s);
-                    if (LUTS) { if (diagonals) s += mine[e]; }
-                    x[e] = ex2(min_nan(s - lse2, 0.0f));
+                for (int e = 0; e < W; e += 2) {
+                    const uint64_t v = pack2(sv[e / 16][e % 16], sv[e / 16][e % 16 + 1]);
+                    if (CAP) slope[CAP ? e / 2 : 0] = fma2(v, v, pack2(-1.0f, -1.0f));
+                    float x0, x1;
+                    unpack2(fma2(v, by, at02), x0, x1);
+                    if (BIAS == GRF_BIAS_SLOPES) {
+                        if (line) { x0 = fmaf(slope2, (float)e, x0); x1 = fmaf(slope2, (float)(e + 1), x1); }
+                        else { x0 = fmaf(-slope2, fabsf(ahead + (float)e), x0); x1 = fmaf(-slope2, fabsf(ahead + (float)(e + 1)), x1); }
+                    }
+                    if (LUTS) { if (diagonals) { x0 += mine[e]; x1 += mine[e + 1]; } }
+                    x[e / 2] = pack2(ex2(x0), ex2(x1));
                 }
             }
             const bool careful = partial || !any;               // (of this row: nothing in it may meet an infinity or NaN)
             if (careful) {
                 const int32_t to = any ? limit - j0 - c0 : 0;
-                if (mixed) {
 #pragma unroll
-                    for (int e = 0; e < W; e += 4) {
-                        const int4 d4 = *reinterpret_cast<const int4*>(docs + c0 + e);
-                        if (!(e < to && d4.x == doc)) x[e] = 0.0f;
-                        if (!(e + 1 < to && d4.y == doc)) x[e + 1] = 0.0f;
-                        if (!(e + 2 < to && d4.z == doc)) x[e + 2] = 0.0f;
-                        if (!(e + 3 < to && d4.w == doc)) x[e + 3] = 0.0f;
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < W; ++e)
-                        if (e >= to) x[e] = 0.0f;
+                for (int e = 0; e < W; e += 4) {
+                    const int4 d4 = mixed ? *reinterpret_cast<const int4*>(docs + c0 + e) : make_int4(doc, doc, doc, doc);
+                    float y0, y1, y2, y3;
+                    unpack2(x[e / 2], y0, y1);
+                    unpack2(x[e / 2 + 1], y2, y3);
+                    x[e / 2] = pack2(e < to && d4.x == doc ? y0 : 0.0f, e + 1 < to && d4.y == doc ? y1 : 0.0f);
+                    x[e / 2 + 1] = pack2(e + 2 < to && d4.z == doc ? y2 : 0.0f, e + 3 < to && d4.w == doc ? y3 : 0.0f);
                 }
             }
             if (!(ok = wait(dp_full, (uint32_t)n & 1u))) break;
             fence_after_sync();
-#pragma unroll
-            for (int y = 0; y < W / 16; ++y) {
-                uint32_t dv[16];
-                tmem_ld16(dp_col + c0 + 16 * y + lanes, dv);
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const float d = __uint_as_float(dv[e]) - dsum;
-                    // (a place that is not seen holds 0, whatever dP is there)
-                    x[16 * y + e] = careful && x[16 * y + e] == 0.0f ? 0.0f : x[16 * y + e] * d;
-                }
-            }
             {
+                uint32_t dv[W / 16][16];
+#pragma unroll
+                for (int y = 0; y < W / 16; ++y) tmem_ld16_nowait(dp_col + c0 + 16 * y + lanes, dv[y]);
+                tmem_ld_wait();
+                const uint64_t minus_d = pack2(-dsum, -dsum);
+#pragma unroll
+                for (int e = 0; e < W; e += 2) {
+                    const uint64_t d = mul2(x[e / 2], add2(pack2(dv[e / 16][e % 16], dv[e / 16][e % 16 + 1]), minus_d));
+                    if (careful) {
+                        // a place that is not seen holds 0, whatever dP is there
+                        float y0, y1, d0, d1;
+                        unpack2(x[e / 2], y0, y1);
+                        unpack2(d, d0, d1);
+                        x[e / 2] = pack2(y0 == 0.0f ? 0.0f : d0, y1 == 0.0f ? 0.0f : d1);
+                    } else x[e / 2] = d;
+                }
                 uint32_t w[16];
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const int a = 2 * e;
-                    w[e] = CAP ? pack_bf16(x[a] * dcap[CAP ? a : 0], x[a + 1] * dcap[CAP ? a + 1 : 0]) : pack_bf16(x[a], x[a + 1]);
+                    float y0, y1;
+                    unpack2(CAP ? mul2(x[e], slope[CAP ? e : 0]) : x[e], y0, y1);
+                    w[e] = pack_bf16(y0, y1);
                 }
                 tmem_st16(dp_col + c0 + lanes, w);
             }
@@ -363,10 +363,12 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             if (sums) {
                 if (!diagonals) {
                     if (bucket0 != far_bucket) { flush(); far_bucket = bucket0; }
-                    float y0 = 0.0f, y1 = 0.0f, y2 = 0.0f, y3 = 0.0f;
+                    uint64_t y[2] = {x[0], x[1]};
 #pragma unroll
-                    for (int e = 0; e < W; e += 4) { y0 += x[e]; y1 += x[e + 1]; y2 += x[e + 2]; y3 += x[e + 3]; }
-                    far_sum += (y0 + y1) + (y2 + y3);
+                    for (int e = 2; e < W / 2; ++e) y[e & 1] = add2(y[e & 1], x[e]);
+                    float y0, y1;
+                    unpack2(add2(y[0], y[1]), y0, y1);
+                    far_sum += y0 + y1;
                 } else {
                     // diagonal e - lane is complete in lane 31 after column e; those that end at the last column are in the other lanes
                     float a = 0.0f;
@@ -374,7 +376,9 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
 #pragma unroll
                     for (int e = 0; e < W; ++e) {
                         const float up = __shfl_up_sync(0xffffffffu, a, 1);
-                        a = x[e] + (lane > 0 ? up : 0.0f);
+                        float y0, y1;
+                        unpack2(x[e / 2], y0, y1);
+                        a = (e & 1 ? y1 : y0) + (lane > 0 ? up : 0.0f);
                         if (lane == 31) at[e] = a;
                     }
                     if (lane < 31) at[W + 30 - lane] = a;       // diagonal 31 - lane; place x holds diagonal x - 31
@@ -393,6 +397,7 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         if (ok && n > 0) ok = wait(dq_done, 0u);
         fence_after_sync();
         if (ok) {
+            const float by = CAP ? -p.scale : p.scale;           // (slope of the cap with its sign turned)
             __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.dq) + b * p.dqs[0] + h * p.dqs[1] + (int64_t)i * p.dqs[2];
 #pragma unroll 1
             for (int y = 0; y < DP / 64; ++y) {
@@ -407,7 +412,7 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     if (col + 8 * z >= p.d) continue;
                     uint32_t w[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) w[e] = any ? pack_bf16(__uint_as_float(o[8 * z + 2 * e]) * p.scale, __uint_as_float(o[8 * z + 2 * e + 1]) * p.scale) : 0u;
+                    for (int e = 0; e < 4; ++e) w[e] = any ? pack_bf16(__uint_as_float(o[8 * z + 2 * e]) * by, __uint_as_float(o[8 * z + 2 * e + 1]) * by) : 0u;
                     *reinterpret_cast<uint4*>(dst + col + 8 * z) = make_uint4(w[0], w[1], w[2], w[3]);
                 }
             }
@@ -439,7 +444,7 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     __shared__ int abort_flag;
     __shared__ float lut[LUTS ? 2 * 256 : 1];
     __shared__ grf_buckets bucket;
-    __shared__ __align__(16) float info[NS][2][BT];             // lse (in units of log 2; infinity where P = 0) and D of a tile's queries
+    __shared__ __align__(16) float info[NS][2][BT];             // -lse (in units of log 2; -infinity where P = 0) and -D of a tile's queries
     __shared__ __align__(16) int32_t info_doc[NS][BT];
     const int tid = threadIdx.x, lane = tid & 31, warp = uniform(tid >> 5);
     const uint32_t smem = (smem_u32(smem_dyn) + 1023u) & ~1023u;
@@ -593,10 +598,10 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                     const int r = lane + 32 * y;
                     const bool in = t * BT + r < p.Nq;
                     const float lse = in ? p.lse[row + r] : -CUDART_INF_F, d = in ? p.dsum[row + r] : 0.0f;
-                    const bool empty_row = lse == -CUDART_INF_F;
+                    const bool empty_row = fabsf(lse) > LARGEST;
                     none[y] = __ballot_sync(0xffffffffu, in && empty_row);
-                    info[s][0][r] = empty_row ? CUDART_INF_F : lse * GRF_LOG2E;
-                    info[s][1][r] = empty_row ? 0.0f : d;
+                    info[s][0][r] = empty_row ? -CUDART_INF_F : -lse * GRF_LOG2E;
+                    info[s][1][r] = empty_row ? 0.0f : -d;
                     if (sight.docs) info_doc[s][r] = in ? p.q_doc[(int64_t)b * p.Nq + t * BT + r] : -1;
                 }
                 if (none[0] | none[1] | none[2] | none[3]) {
@@ -652,54 +657,49 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                 }
                 if (!(ok = wait(ready(s), (uint32_t)(n / NS) & 1u) && wait(s_full, (uint32_t)n & 1u))) break;
                 fence_after_sync();
-                const float ahead = (float)(j - pos0 - c0);
-                float x[W], dcap[CAP ? W : 1];
+                uint64_t x[W / 2], slope[CAP ? W / 2 : 1];      // P, then dS; t^2 - 1 of the cap
                 {
                     uint32_t sv[W / 16][16];
 #pragma unroll
                     for (int y = 0; y < W / 16; ++y) tmem_ld16_nowait(s_col + c0 + 16 * y + lanes, sv[y]);
                     tmem_ld_wait();
                     if (CAP) capped<W / 16>(sv, by_cap);
+                    const float ahead = (float)(j - pos0 - c0);
+                    const uint64_t by = CAP ? pack2(cap2, cap2) : pack2(to2, to2), bias22 = pack2(bias2, bias2);
 #pragma unroll
-                    for (int e4 = 0; e4 < W; e4 += 4) {
-                        const float4 l4 = *reinterpret_cast<const float4*>(&info[s][0][c0 + e4]);
-                        const float lv[4] = {l4.x, l4.y, l4.z, l4.w};
-#pragma unroll
-                        for (int z = 0; z < 4; ++z) {
-                            const int e = e4 + z;
-                            const float raw = __uint_as_float(sv[e / 16][e % 16]);
-                            float sc;
-                            if (CAP) {
-                                dcap[e] = fmaf(-raw, raw, 1.0f);
-                                sc = fmaf(cap2, raw, bias2);
-                            } else sc = fmaf(raw, to2, bias2);
-                            if (BIAS == GRF_BIAS_SLOPES) sc = fmaf(-slope2, fabsf(ahead - (float)e), sc);
-                            if (LUTS) { if (diagonals) sc += mine[-e]; }
-                            x[e] = ex2(min_nan(sc - lv[z], 0.0f));
-                        }
+                    for (int e = 0; e < W; e += 2) {
+                        const uint64_t v = pack2(sv[e / 16][e % 16], sv[e / 16][e % 16 + 1]);
+                        if (CAP) slope[CAP ? e / 2 : 0] = fma2(v, v, pack2(-1.0f, -1.0f));
+                        uint64_t at = *reinterpret_cast<const uint64_t*>(&info[s][0][c0 + e]);
+                        if (LUTS) at = add2(at, bias22);
+                        float x0, x1;
+                        unpack2(fma2(v, by, at), x0, x1);
+                        if (BIAS == GRF_BIAS_SLOPES) { x0 = fmaf(-slope2, fabsf(ahead - (float)e), x0); x1 = fmaf(-slope2, fabsf(ahead - (float)(e + 1)), x1); }
+                        if (LUTS) { if (diagonals) { x0 += mine[-e]; x1 += mine[-e - 1]; } }
+                        x[e / 2] = pack2(ex2(x0), ex2(x1));
                     }
                 }
                 if (partial) {
                     const int32_t since = from - c0;
-                    if (T.mixed(t)) {
+                    const bool mixed = T.mixed(t);
 #pragma unroll
-                        for (int e = 0; e < W; e += 4) {
-                            const int4 d4 = *reinterpret_cast<const int4*>(&info_doc[s][c0 + e]);
-                            if (!(e >= since && d4.x == doc)) x[e] = 0.0f;
-                            if (!(e + 1 >= since && d4.y == doc)) x[e + 1] = 0.0f;
-                            if (!(e + 2 >= since && d4.z == doc)) x[e + 2] = 0.0f;
-                            if (!(e + 3 >= since && d4.w == doc)) x[e + 3] = 0.0f;
-                        }
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < W; ++e)
-                            if (e < since) x[e] = 0.0f;
+                    for (int e = 0; e < W; e += 4) {
+                        const int4 d4 = mixed ? *reinterpret_cast<const int4*>(&info_doc[s][c0 + e]) : make_int4(doc, doc, doc, doc);
+                        float y0, y1, y2, y3;
+                        unpack2(x[e / 2], y0, y1);
+                        unpack2(x[e / 2 + 1], y2, y3);
+                        x[e / 2] = pack2(e >= since && d4.x == doc ? y0 : 0.0f, e + 1 >= since && d4.y == doc ? y1 : 0.0f);
+                        x[e / 2 + 1] = pack2(e + 2 >= since && d4.z == doc ? y2 : 0.0f, e + 3 >= since && d4.w == doc ? y3 : 0.0f);
                     }
                 }
                 {
                     uint32_t w[16];
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) w[e] = pack_bf16(x[2 * e], x[2 * e + 1]);
+                    for (int e = 0; e < 16; ++e) {
+                        float y0, y1;
+                        unpack2(x[e], y0, y1);
+                        w[e] = pack_bf16(y0, y1);
+                    }
                     tmem_st16(s_col + c0 + lanes, w);
                 }
                 tmem_st_wait();
@@ -708,26 +708,28 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                 if (lane == 0) mbar_arrive(p_full);
                 if (!(ok = wait(dp_full, (uint32_t)n & 1u))) break;
                 fence_after_sync();
-#pragma unroll
-                for (int y = 0; y < W / 16; ++y) {
-                    uint32_t dv[16];
-                    tmem_ld16(dp_col + c0 + 16 * y + lanes, dv);
-#pragma unroll
-                    for (int e4 = 0; e4 < 16; e4 += 4) {
-                        const float4 d4 = *reinterpret_cast<const float4*>(&info[s][1][c0 + 16 * y + e4]);
-                        const float d[4] = {d4.x, d4.y, d4.z, d4.w};
-#pragma unroll
-                        for (int z = 0; z < 4; ++z) {
-                            const int e = 16 * y + e4 + z;
-                            const float ds = x[e] * (__uint_as_float(dv[e4 + z]) - d[z]);
-                            x[e] = partial && x[e] == 0.0f ? 0.0f : CAP ? ds * dcap[CAP ? e : 0] : ds;
-                        }
-                    }
-                }
                 {
+                    uint32_t dv[W / 16][16];
+#pragma unroll
+                    for (int y = 0; y < W / 16; ++y) tmem_ld16_nowait(dp_col + c0 + 16 * y + lanes, dv[y]);
+                    tmem_ld_wait();
                     uint32_t w[16];
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) w[e] = pack_bf16(x[2 * e], x[2 * e + 1]);
+                    for (int e = 0; e < W; e += 2) {
+                        const uint64_t minus_d = *reinterpret_cast<const uint64_t*>(&info[s][1][c0 + e]);
+                        uint64_t d = mul2(x[e / 2], add2(pack2(dv[e / 16][e % 16], dv[e / 16][e % 16 + 1]), minus_d));
+                        if (CAP) d = mul2(d, slope[CAP ? e / 2 : 0]);
+                        float d0, d1;
+                        unpack2(d, d0, d1);
+                        if (partial) {
+                            // a place that is not seen holds 0, whatever dP is there
+                            float y0, y1;
+                            unpack2(x[e / 2], y0, y1);
+                            d0 = y0 == 0.0f ? 0.0f : d0;
+                            d1 = y1 == 0.0f ? 0.0f : d1;
+                        }
+                        w[e / 2] = pack_bf16(d0, d1);
+                    }
                     tmem_st16(dp_col + c0 + lanes, w);
                 }
                 tmem_st_wait();
@@ -745,7 +747,7 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         const int col0 = (part & 1) * (DP / 2);
         const int64_t (&st)[3] = is_dv ? p.dvs : p.dks;
         __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(is_dv ? p.dv : p.dk) + b * st[0] + kvh * st[1] + (int64_t)j * st[2];
-        const float by = is_dv ? 1.0f : p.scale;
+        const float by = is_dv ? 1.0f : CAP ? -p.scale : p.scale;       // (slope of the cap with its sign turned)
 #pragma unroll 1
         for (int y = 0; y < DP / 32; ++y) {
             uint32_t o[16];
@@ -793,7 +795,7 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                 v[4] += w.x; v[5] += w.y; v[6] += w.z; v[7] += w.w;
             }
             const int64_t (&st)[3] = what == 0 ? p.dvs : p.dks;
-            const float by = what == 0 ? 1.0f : p.scale;
+            const float by = what == 0 ? 1.0f : CAP ? -p.scale : p.scale;
             __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(what == 0 ? p.dv : p.dk) + b * st[0] + kvh * st[1] + (int64_t)(j0 + r) * st[2] + col;
             *reinterpret_cast<uint4*>(dst) = make_uint4(pack_bf16(v[0] * by, v[1] * by), pack_bf16(v[2] * by, v[3] * by), pack_bf16(v[4] * by, v[5] * by),
                                                         pack_bf16(v[6] * by, v[7] * by));
