@@ -23,11 +23,13 @@ constexpr int THREADS = 640, WORKERS = 16;          // warps that make P and dS
 constexpr int MORE = 104, LESS = 64;                // registers: 4 * 104 + 64 = 5 * 96
 constexpr int W = 32;                               // columns of a worker
 constexpr int COPY = WORKERS, ISSUE = WORKERS + 1, PREPARE = WORKERS + 2;
-constexpr int NS = 2;
 
 struct head_split { int32_t splits; };
 
 template <int DP> struct Grad {
+    // stages: a tile's place is free only once its last product is done, a tile's time before the next but one is wanted, and a copy takes
+    // about as long: two stages leave it in the open (d = 64: 1.87 us a tile and kernel with two, MEASURED with four)
+    static constexpr int NS = DP == 64 ? 4 : 2;
     static constexpr uint32_t TILE = HALF * (DP / 64);
     static constexpr size_t SMEM = 1024 + (size_t)TILE * (2 + 2 * NS);      // then the tiles' bits
 };
@@ -75,6 +77,7 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                      const __grid_constant__ CUtensorMap map_g, const __grid_constant__ grf_softmax_params p)
 {
     using Sh = Grad<DP>;
+    constexpr int NS = Sh::NS;
     constexpr int LUTS = BIAS == GRF_BIAS_BUCKETS ? 1 : 0;
     extern __shared__ unsigned char smem_dyn[];
     __shared__ __align__(8) unsigned long long bars[5 * NS + 9];
@@ -436,6 +439,7 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                        const __grid_constant__ CUtensorMap map_g, const __grid_constant__ grf_softmax_params p, const head_split f)
 {
     using Sh = Grad<DP>;
+    constexpr int NS = Sh::NS;
     constexpr int LUTS = BIAS == GRF_BIAS_BUCKETS ? 1 : 0;
     constexpr int SUM_ROW = DP + 4;
     extern __shared__ unsigned char smem_dyn[];
@@ -549,7 +553,7 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
             bool ok = true;
             auto make_scores = [&](int32_t n) {
                 const int s = n % NS;
-                if (!wait(ready(s), (uint32_t)(n / NS) & 1u) || !wait(q_full(s), (uint32_t)(n / NS) & 1u)) return false;
+                if (!wait(ready(s), (uint32_t)(n / NS) & 1u)) return false;     // (behind both copies)
                 fence_after_sync();
                 product_over_columns<DP>(s_col, lo32(k_op), hi32(k_op), lo32(q_op) + s * (Sh::TILE / 16), hi32(q_op), steps);
                 mma_commit(s_full);
@@ -557,8 +561,6 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
             };
             auto make_dp = [&](int32_t n) {
                 const int s = n % NS;
-                if (!wait(g_full(s), (uint32_t)(n / NS) & 1u)) return false;
-                fence_after_sync();
                 product_over_columns<DP>(dp_col, lo32(v_op), hi32(v_op), lo32(g_op) + s * (Sh::TILE / 16), hi32(g_op), steps);
                 mma_commit(dp_full);
                 return true;
@@ -587,26 +589,38 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                 }
             }
         } else if (warp == PREPARE && some) {
+            // (the next tile's values travel while this one's copies do; a place is free when its copies have come, as these waited for it)
             int32_t t = T.begin(), h = h_first, n = 0;
-            do {
-                const int s = n % NS;
-                if (n >= NS && !wait(empty(s), (uint32_t)(n / NS - 1) & 1u)) break;
+            float lse[4], d[4];
+            int32_t docs[4];
+            auto fetch = [&]() {
                 const int64_t row = ((int64_t)b * p.H + h) * p.Nq + t * BT;
-                uint32_t none[4];
 #pragma unroll
                 for (int y = 0; y < 4; ++y) {
                     const int r = lane + 32 * y;
                     const bool in = t * BT + r < p.Nq;
-                    const float lse = in ? p.lse[row + r] : -CUDART_INF_F, d = in ? p.dsum[row + r] : 0.0f;
-                    const bool empty_row = fabsf(lse) > LARGEST;
-                    none[y] = __ballot_sync(0xffffffffu, in && empty_row);
-                    info[s][0][r] = empty_row ? -CUDART_INF_F : -lse * GRF_LOG2E;
-                    info[s][1][r] = empty_row ? 0.0f : -d;
-                    if (sight.docs) info_doc[s][r] = in ? p.q_doc[(int64_t)b * p.Nq + t * BT + r] : -1;
+                    lse[y] = in ? p.lse[row + r] : -CUDART_INF_F;
+                    d[y] = in ? p.dsum[row + r] : 0.0f;
+                    docs[y] = in && sight.docs ? p.q_doc[(int64_t)b * p.Nq + t * BT + r] : -1;
+                }
+            };
+            fetch();
+            bool more = true;
+            while (more) {
+                const int s = n % NS;
+                if (!wait(q_full(s), (uint32_t)(n / NS) & 1u) || !wait(g_full(s), (uint32_t)(n / NS) & 1u)) break;
+                uint32_t none[4];
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    const int r = lane + 32 * y;
+                    const bool empty_row = fabsf(lse[y]) > LARGEST;
+                    none[y] = __ballot_sync(0xffffffffu, t * BT + r < p.Nq && empty_row);
+                    info[s][0][r] = empty_row ? -CUDART_INF_F : -lse[y] * GRF_LOG2E;
+                    info[s][1][r] = empty_row ? 0.0f : -d[y];
+                    if (sight.docs) info_doc[s][r] = docs[y];
                 }
                 if (none[0] | none[1] | none[2] | none[3]) {
                     // what rows of queries that see nothing hold does not matter: cleared, as 0 times it is summed below
-                    if (!wait(q_full(s), (uint32_t)(n / NS) & 1u) || !wait(g_full(s), (uint32_t)(n / NS) & 1u)) break;
 #pragma unroll
                     for (int y = 0; y < 4; ++y)
                         if (none[y] >> lane & 1u) {
@@ -618,7 +632,9 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                 __syncwarp();
                 arrive_elected(ready(s));
                 ++n;
-            } while (step(t, h));
+                more = step(t, h);
+                if (more) fetch();
+            }
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(MORE));
@@ -810,6 +826,7 @@ struct grad_maps { CUtensorMap q, k, v, g; };
 template <int DP, bool CAP, int BIAS> int launch(grf_ctx* ctx, const grf_softmax_params& p, const grad_maps& m)
 {
     using Sh = Grad<DP>;
+    constexpr int NS = Sh::NS;
     auto bits = [&](int32_t tokens) { return p.q_doc ? 16 * (size_t)(grf_ceil_div(tokens, BT) / 32 + 1) : 0; };
     const size_t dq_smem = Sh::SMEM + bits(p.Nk), dkv_smem = Sh::SMEM + bits(p.Nq);
     GRF_CUDA_TRY(cudaFuncSetAttribute(softmax_tc_dq_kernel<DP, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)dq_smem));
