@@ -56,6 +56,24 @@ struct grad_tiles {
 };
 
 constexpr float LARGEST = 1.0e30f;                  // of lse
+// a pair's values where they are to stay, else 0
+__device__ __forceinline__ void keep(uint64_t& x, bool first, bool second)
+{
+    float x0, x1;
+    unpack2(x, x0, x1);
+    x = pack2(first ? x0 : 0.0f, second ? x1 : 0.0f);
+}
+// dP is 0 where P is: a place that is not seen holds 0, whatever dP is there
+__device__ __forceinline__ void only_seen(uint32_t (&dp)[W / 16][16], const uint64_t (&p)[W / 2])
+{
+#pragma unroll
+    for (int e = 0; e < W; e += 2) {
+        float p0, p1;
+        unpack2(p[e / 2], p0, p1);
+        if (p0 == 0.0f) dp[e / 16][e % 16] = 0u;
+        if (p1 == 0.0f) dp[e / 16][e % 16 + 1] = 0u;
+    }
+}
 __device__ __forceinline__ void clear_row(uint32_t tile, int r, int halves)
 {
     for (int y = 0; y < halves; ++y)
@@ -246,6 +264,7 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         const int64_t row = ((int64_t)b * p.H + h) * p.Nq + i;
         const float lse = i < p.Nq ? p.lse[row] : -CUDART_INF_F, dsum = i < p.Nq ? p.dsum[row] : 0.0f;
         const bool any = !(fabsf(lse) > LARGEST);               // a row without a key, or one whose scores tell nothing any more: P = 0
+        const bool empties = __any_sync(0xffffffffu, !any);
         const float minus_lse = any ? -lse * GRF_LOG2E : -CUDART_INF_F;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const float to2 = p.scale * GRF_LOG2E, by_cap = CAP ? p.scale / p.cap : 0.0f, cap2 = p.cap * GRF_LOG2E;
@@ -317,17 +336,22 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     x[e / 2] = pack2(ex2(x0), ex2(x1));
                 }
             }
-            const bool careful = partial || !any;               // (of this row: nothing in it may meet an infinity or NaN)
+            // (branches that the compiler is to keep: without the barrier inside it runs a whole tile's masks under a predicate, a third of all instructions)
+            const bool careful = partial || empties;
             if (careful) {
+                __syncwarp();
                 const int32_t to = any ? limit - j0 - c0 : 0;
+                if (mixed) {
+                    __syncwarp();
 #pragma unroll
-                for (int e = 0; e < W; e += 4) {
-                    const int4 d4 = mixed ? *reinterpret_cast<const int4*>(docs + c0 + e) : make_int4(doc, doc, doc, doc);
-                    float y0, y1, y2, y3;
-                    unpack2(x[e / 2], y0, y1);
-                    unpack2(x[e / 2 + 1], y2, y3);
-                    x[e / 2] = pack2(e < to && d4.x == doc ? y0 : 0.0f, e + 1 < to && d4.y == doc ? y1 : 0.0f);
-                    x[e / 2 + 1] = pack2(e + 2 < to && d4.z == doc ? y2 : 0.0f, e + 3 < to && d4.w == doc ? y3 : 0.0f);
+                    for (int e = 0; e < W; e += 4) {
+                        const int4 d4 = *reinterpret_cast<const int4*>(docs + c0 + e);
+                        keep(x[e / 2], e < to && d4.x == doc, e + 1 < to && d4.y == doc);
+                        keep(x[e / 2 + 1], e + 2 < to && d4.z == doc, e + 3 < to && d4.w == doc);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < W; e += 2) keep(x[e / 2], e < to, e + 1 < to);
                 }
             }
             if (!(ok = wait(dp_full, (uint32_t)n & 1u))) break;
@@ -337,18 +361,13 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
 #pragma unroll
                 for (int y = 0; y < W / 16; ++y) tmem_ld16_nowait(dp_col + c0 + 16 * y + lanes, dv[y]);
                 tmem_ld_wait();
-                const uint64_t minus_d = pack2(-dsum, -dsum);
-#pragma unroll
-                for (int e = 0; e < W; e += 2) {
-                    const uint64_t d = mul2(x[e / 2], add2(pack2(dv[e / 16][e % 16], dv[e / 16][e % 16 + 1]), minus_d));
-                    if (careful) {
-                        // a place that is not seen holds 0, whatever dP is there
-                        float y0, y1, d0, d1;
-                        unpack2(x[e / 2], y0, y1);
-                        unpack2(d, d0, d1);
-                        x[e / 2] = pack2(y0 == 0.0f ? 0.0f : d0, y1 == 0.0f ? 0.0f : d1);
-                    } else x[e / 2] = d;
+                if (careful) {
+                    __syncwarp();
+                    only_seen(dv, x);
                 }
+                const uint64_t minus_d = pack2(any ? -dsum : 0.0f, any ? -dsum : 0.0f);
+#pragma unroll
+                for (int e = 0; e < W; e += 2) x[e / 2] = mul2(x[e / 2], add2(pack2(dv[e / 16][e % 16], dv[e / 16][e % 16 + 1]), minus_d));
                 uint32_t w[16];
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
@@ -696,16 +715,19 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                     }
                 }
                 if (partial) {
+                    __syncwarp();
                     const int32_t since = from - c0;
-                    const bool mixed = T.mixed(t);
+                    if (T.mixed(t)) {
+                        __syncwarp();
 #pragma unroll
-                    for (int e = 0; e < W; e += 4) {
-                        const int4 d4 = mixed ? *reinterpret_cast<const int4*>(&info_doc[s][c0 + e]) : make_int4(doc, doc, doc, doc);
-                        float y0, y1, y2, y3;
-                        unpack2(x[e / 2], y0, y1);
-                        unpack2(x[e / 2 + 1], y2, y3);
-                        x[e / 2] = pack2(e >= since && d4.x == doc ? y0 : 0.0f, e + 1 >= since && d4.y == doc ? y1 : 0.0f);
-                        x[e / 2 + 1] = pack2(e + 2 >= since && d4.z == doc ? y2 : 0.0f, e + 3 >= since && d4.w == doc ? y3 : 0.0f);
+                        for (int e = 0; e < W; e += 4) {
+                            const int4 d4 = *reinterpret_cast<const int4*>(&info_doc[s][c0 + e]);
+                            keep(x[e / 2], e >= since && d4.x == doc, e + 1 >= since && d4.y == doc);
+                            keep(x[e / 2 + 1], e + 2 >= since && d4.z == doc, e + 3 >= since && d4.w == doc);
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < W; e += 2) keep(x[e / 2], e >= since, e + 1 >= since);
                     }
                 }
                 {
@@ -729,6 +751,10 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
 #pragma unroll
                     for (int y = 0; y < W / 16; ++y) tmem_ld16_nowait(dp_col + c0 + 16 * y + lanes, dv[y]);
                     tmem_ld_wait();
+                    if (partial) {
+                        __syncwarp();
+                        only_seen(dv, x);
+                    }
                     uint32_t w[16];
 #pragma unroll
                     for (int e = 0; e < W; e += 2) {
@@ -737,13 +763,6 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                         if (CAP) d = mul2(d, slope[CAP ? e / 2 : 0]);
                         float d0, d1;
                         unpack2(d, d0, d1);
-                        if (partial) {
-                            // a place that is not seen holds 0, whatever dP is there
-                            float y0, y1;
-                            unpack2(x[e / 2], y0, y1);
-                            d0 = y0 == 0.0f ? 0.0f : d0;
-                            d1 = y1 == 0.0f ? 0.0f : d1;
-                        }
                         w[e / 2] = pack_bf16(d0, d1);
                     }
                     tmem_st16(dp_col + c0 + lanes, w);
