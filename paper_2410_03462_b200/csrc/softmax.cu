@@ -344,11 +344,10 @@ extern "C" int grf_softmax_attn_backward(grf_ctx* ctx, const grf_softmax_desc* d
 
 // ------------------------------------------------------------------------------------------------ the bias by itself
 //
-// Both directions are bound by the matrix's bytes.  The rows are written, and read, as one long run of 16-byte pieces per head (rows of
-// any length, so a piece may pass a row's end).  Beyond the distance F at which the last bucket starts there is one value to either side: most
-// pieces lie there whole and take no look-up.  The others look their distances up in shared memory (F < BIAS_NEAR; a search otherwise).
-// Gradient: pieces beyond F are added into two registers, the others into bins that every thread has for itself in shared memory, so nothing is
-// atomic; four pieces are loaded before the first is used.
+// Both directions are bound by the matrix's bytes.  A warp takes a row at a time: beyond the distance F at which the last bucket starts there is
+// one value to either side, so only the places within F of the diagonal take a look-up (in shared memory, or a search where F >= BIAS_NEAR),
+// and the others are written, or added up, 16 bytes at a time.  Gradient: the two outer buckets in registers, the others in bins that every
+// thread has for itself in shared memory, so that nothing is atomic.
 namespace {
 
 constexpr int BIAS_NEAR = 2048, BIAS_THREADS = 256;
@@ -356,8 +355,6 @@ constexpr int BIAS_NEAR = 2048, BIAS_THREADS = 256;
 struct bias_shape {
     int32_t heads, n_q, n_k, start, n_first, two_sided, near;   // near: whether distances are looked up
     int32_t strips;
-    uint32_t by_n_k;                                            // n / n_k = (t + ((n - t) >> 1)) >> shift with t the upper half of n * by_n_k
-    int32_t shift;                                              // -1: n_k = 1 or a plane that 64 bits count: divided as it is
     int32_t first[GRF_MAX_BUCKETS];
     __host__ __device__ int32_t columns() const { return n_first * (1 + two_sided); }
 };
@@ -384,135 +381,103 @@ __device__ __forceinline__ int32_t column_at(const bias_shape& s, int32_t F, con
 {
     return s.near ? near[min(max(delta + F, 0), 2 * F)] : column_of(s, delta);
 }
-// row and column of place e of a plane
-template <typename I> __device__ __forceinline__ void place_of(const bias_shape& s, I e, int32_t& i, int32_t& j)
-{
-    if (sizeof(I) == 4 && s.shift >= 0) {
-        const uint32_t n = (uint32_t)e, t = __umulhi(n, s.by_n_k), q = (t + ((n - t) >> 1)) >> s.shift;
-        i = (int32_t)q;
-        j = (int32_t)(n - q * (uint32_t)s.n_k);
-    } else {
-        i = (int32_t)(e / s.n_k);
-        j = (int32_t)(e - (I)i * s.n_k);
-    }
-}
-// A plane as pieces of 16 bytes: piece x holds the plane's places x CH - head .. + CH - 1, the first and the last one maybe not whole.
-template <typename T, typename I> struct plane_pieces {
-    static constexpr int CH = 16 / (int)sizeof(T);
-    I places, count;
-    int head;
-    __device__ __forceinline__ plane_pieces(const bias_shape& s, int64_t plane)
+// A row's three stretches: [0, left) lies beyond F before the diagonal, [right, n_k) beyond it behind.
+struct bias_row {
+    int32_t left, right, delta0;            // delta0: relative position of the row's first place
+    __device__ __forceinline__ bias_row(const bias_shape& s, int32_t F, int32_t i)
     {
-        const int64_t all = (int64_t)s.n_q * s.n_k;
-        places = (I)all;
-        head = (int)(plane * all % CH);
-        count = (I)((head + all + CH - 1) / CH);
+        delta0 = -s.start - i;
+        left = min(max(1 - F - delta0, 0), s.n_k);
+        right = min(max((s.two_sided ? max(F, 1) : 0) - delta0, left), s.n_k);
     }
-    __device__ __forceinline__ I first(I x) const { return x * CH - head; }
-    __device__ __forceinline__ bool whole(I x) const { return first(x) >= 0 && first(x) + CH <= places; }
 };
+// Places from .. to - 1 of a row of T: `each` for those before the first and behind the last 16-byte border, `piece` for the 16-byte pieces; by one warp.
+template <typename T, typename Each, typename Piece>
+__device__ __forceinline__ void by_pieces(const T* row, int32_t from, int32_t to, Each each, Piece piece)
+{
+    constexpr int CH = 16 / (int)sizeof(T);
+    const int lane = threadIdx.x & 31;
+    if (from >= to) return;
+    const int32_t ahead = (int32_t)((CH - ((uintptr_t)(row + from) / sizeof(T)) % CH) % CH), first = min(from + ahead, to), count = (to - first) / CH, last = first + count * CH;
+    if (lane < first - from) each(from + lane);
+    if (lane >= 16 && lane - 16 < to - last) each(last + lane - 16);
+#pragma unroll 4
+    for (int32_t x = lane; x < count; x += 32) piece(first + x * CH);
+}
 
-template <typename T, typename I>
+template <typename T>
 __global__ void __launch_bounds__(BIAS_THREADS) relative_rows_kernel(const __grid_constant__ bias_shape s, const T* __restrict__ table, T* __restrict__ rows)
 {
-    using P = plane_pieces<T, I>;
+    constexpr int CH = 16 / (int)sizeof(T);
     __shared__ unsigned char near[2 * BIAS_NEAR];
     __shared__ T value[2 * GRF_MAX_BUCKETS];
-    const int32_t h = blockIdx.y, F = s.first[s.n_first - 1], right = s.two_sided ? max(F, 1) : 0;
+    const int32_t h = blockIdx.y, F = s.first[s.n_first - 1], lane = threadIdx.x & 31;
     load_near(s, F, near);
     for (int x = threadIdx.x; x < s.columns(); x += BIAS_THREADS) value[x] = table[(int64_t)h * s.columns() + x];
     __syncthreads();
-    const T before = value[s.n_first - 1], behind = value[s.two_sided ? 2 * s.n_first - 1 : 0];
-    const P at(s, h);
-    T* base = rows + (int64_t)h * s.n_q * s.n_k - at.head;
-    for (I x = (I)blockIdx.x * BIAS_THREADS + threadIdx.x; x < at.count; x += (I)s.strips * BIAS_THREADS) {
-        int32_t i, j;
-        T v[P::CH];
-        if (at.whole(x)) {
-            place_of(s, at.first(x), i, j);
-            const int32_t delta = j - s.start - i;
-            if (j + P::CH <= s.n_k && (delta + P::CH - 1 <= -F || delta >= right)) {
+    const T outer[2] = {value[s.n_first - 1], value[s.two_sided ? 2 * s.n_first - 1 : 0]};
+    uint4 whole[2];
 #pragma unroll
-                for (int e = 0; e < P::CH; ++e) v[e] = delta < 0 ? before : behind;
-            } else {
+    for (int y = 0; y < 2; ++y) {
+        T v[CH];
 #pragma unroll
-                for (int e = 0; e < P::CH; ++e) {
-                    v[e] = value[column_at(s, F, near, j - s.start - i)];
-                    if (++j == s.n_k) { j = 0; ++i; }
-                }
-            }
-            uint4 w;
-            memcpy(&w, v, 16);
-            *reinterpret_cast<uint4*>(base + (int64_t)x * P::CH) = w;
-        } else {
-            for (I e = max(at.first(x), (I)0); e < min(at.first(x) + P::CH, at.places); ++e) {
-                place_of(s, e, i, j);
-                base[at.head + (int64_t)e] = value[column_at(s, F, near, j - s.start - i)];
-            }
-        }
+        for (int e = 0; e < CH; ++e) v[e] = outer[y];
+        memcpy(&whole[y], v, 16);
+    }
+    for (int32_t i = blockIdx.x * (BIAS_THREADS / 32) + (threadIdx.x >> 5); i < s.n_q; i += s.strips * (BIAS_THREADS / 32)) {
+        T* row = rows + ((int64_t)h * s.n_q + i) * s.n_k;
+        const bias_row r(s, F, i);
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+            by_pieces(row, y ? r.right : 0, y ? s.n_k : r.left, [&](int32_t j) { row[j] = outer[y]; }, [&](int32_t j) { *reinterpret_cast<uint4*>(row + j) = whole[y]; });
+        for (int32_t j = r.left + lane; j < r.right; j += 32) row[j] = value[column_at(s, F, near, r.delta0 + j)];
     }
 }
 
-template <typename T, typename I>
+template <typename T>
 __global__ void __launch_bounds__(BIAS_THREADS) relative_sums_kernel(const __grid_constant__ bias_shape s, int32_t batch, const T* __restrict__ drows, float* __restrict__ part)
 {
-    using P = plane_pieces<T, I>;
-    constexpr int AHEAD = 4;
+    constexpr int CH = 16 / (int)sizeof(T), NEAR_AHEAD = 8;
     extern __shared__ float bins[];                             // [column][thread]
     __shared__ unsigned char near[2 * BIAS_NEAR];
-    const int32_t h = blockIdx.y, columns = s.columns(), tid = threadIdx.x, F = s.first[s.n_first - 1], right = s.two_sided ? max(F, 1) : 0;
+    const int32_t h = blockIdx.y, columns = s.columns(), tid = threadIdx.x, lane = tid & 31, F = s.first[s.n_first - 1];
     load_near(s, F, near);
     for (int x = tid; x < columns * BIAS_THREADS; x += BIAS_THREADS) bins[x] = 0.0f;
     __syncthreads();
     float* mine = bins + tid;
     float far[2] = {0.0f, 0.0f};
-    for (int32_t b = 0; b < batch; ++b) {
-        const int64_t plane = (int64_t)b * s.heads + h;
-        const P at(s, plane);
-        const T* base = drows + plane * s.n_q * s.n_k - at.head;
-        const I step = (I)s.strips * BIAS_THREADS;
-        for (I x0 = (I)blockIdx.x * BIAS_THREADS + tid; x0 < at.count; x0 += AHEAD * step) {
-            uint4 w[AHEAD];
+    const int64_t all = (int64_t)batch * s.n_q, step = (int64_t)s.strips * (BIAS_THREADS / 32);
+    for (int64_t x = (int64_t)blockIdx.x * (BIAS_THREADS / 32) + (tid >> 5); x < all; x += step) {
+        const int32_t b = (int32_t)(x / s.n_q), i = (int32_t)(x - (int64_t)b * s.n_q);
+        const T* row = drows + (((int64_t)b * s.heads + h) * s.n_q + i) * s.n_k;
+        const bias_row r(s, F, i);
+        for (int32_t j0 = r.left; j0 < r.right; j0 += 32 * NEAR_AHEAD) {
+            T v[NEAR_AHEAD];
 #pragma unroll
-            for (int y = 0; y < AHEAD; ++y) {
-                const I x = x0 + y * step;
-                if (x < at.count && at.whole(x)) w[y] = __ldcs(reinterpret_cast<const uint4*>(base + (int64_t)x * P::CH));
-            }
+            for (int y = 0; y < NEAR_AHEAD; ++y)
+                if (j0 + 32 * y + lane < r.right) v[y] = row[j0 + 32 * y + lane];
 #pragma unroll
-            for (int y = 0; y < AHEAD; ++y) {
-                const I x = x0 + y * step;
-                if (x >= at.count) break;
-                int32_t i, j;
-                if (at.whole(x)) {
-                    place_of(s, at.first(x), i, j);
-                    const T* v = reinterpret_cast<const T*>(&w[y]);
-                    const int32_t delta = j - s.start - i;
-                    if (j + P::CH <= s.n_k && (delta + P::CH - 1 <= -F || delta >= right)) {
-                        float sum = 0.0f;
-#pragma unroll
-                        for (int e = 0; e < P::CH; ++e) sum += grf_to_float(v[e]);
-                        if (delta < 0) far[0] += sum;
-                        else far[1] += sum;
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < P::CH; ++e) {
-                            mine[column_at(s, F, near, j - s.start - i) * BIAS_THREADS] += grf_to_float(v[e]);
-                            if (++j == s.n_k) { j = 0; ++i; }
-                        }
-                    }
-                } else {
-                    for (I e = max(at.first(x), (I)0); e < min(at.first(x) + P::CH, at.places); ++e) {
-                        place_of(s, e, i, j);
-                        mine[column_at(s, F, near, j - s.start - i) * BIAS_THREADS] += grf_to_float(base[at.head + (int64_t)e]);
-                    }
-                }
+            for (int y = 0; y < NEAR_AHEAD; ++y) {
+                const int32_t j = j0 + 32 * y + lane;
+                if (j < r.right) mine[column_at(s, F, near, r.delta0 + j) * BIAS_THREADS] += grf_to_float(v[y]);
             }
         }
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+            by_pieces(row, y ? r.right : 0, y ? s.n_k : r.left, [&](int32_t j) { far[y] += grf_to_float(row[j]); },
+                      [&](int32_t j) {
+                          const uint4 w = __ldcs(reinterpret_cast<const uint4*>(row + j));
+                          const T* v = reinterpret_cast<const T*>(&w);
+                          float sum = 0.0f;
+#pragma unroll
+                          for (int e = 0; e < CH; ++e) sum += grf_to_float(v[e]);
+                          far[y] += sum;
+                      });
     }
     mine[(s.n_first - 1) * BIAS_THREADS] += far[0];
     mine[(s.two_sided ? 2 * s.n_first - 1 : 0) * BIAS_THREADS] += far[1];
     __syncthreads();
-    const int lane = tid & 31, warp = tid >> 5;
+    const int warp = tid >> 5;
     for (int y = warp; y < columns; y += BIAS_THREADS / 32) {
         float sum = 0.0f;
 #pragma unroll
@@ -522,9 +487,6 @@ __global__ void __launch_bounds__(BIAS_THREADS) relative_sums_kernel(const __gri
         if (lane == 0) part[((int64_t)h * s.strips + blockIdx.x) * columns + y] = sum;
     }
 }
-
-// places that 32 bits do not count (and the threads' strides behind the last one)
-bool big_plane(const bias_shape& s) { return (int64_t)s.n_q * s.n_k > ((int64_t)1 << 30); }
 
 int read_bias(bias_shape* s, int32_t heads, int32_t n_q, int32_t n_k, int32_t q_start, int32_t n_buckets, int two_sided, const int32_t* first, int dtype)
 {
@@ -537,21 +499,14 @@ int read_bias(bias_shape* s, int32_t heads, int32_t n_q, int32_t n_k, int32_t q_
     s->n_first = n_buckets; s->two_sided = two_sided;
     memcpy(s->first, first, sizeof(int32_t) * n_buckets);
     s->near = first[n_buckets - 1] < BIAS_NEAR;
-    s->shift = -1;
-    if (n_k > 1 && !big_plane(*s)) {
-        int32_t bits = 1;                                       // 2^(bits - 1) < n_k <= 2^bits
-        while (((int64_t)1 << bits) < n_k) ++bits;
-        s->by_n_k = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << bits) - n_k)) / n_k + 1);
-        s->shift = bits - 1;
-    }
     return GRF_OK;
 }
 
-// CTAs of one head: enough to fill the device, of 4096 places or more
-int32_t bias_strips(int32_t heads, int32_t n_q, int32_t n_k, int32_t most)
+// CTAs of one head: enough to fill the device, of eight rows or more
+int32_t bias_strips(int32_t heads, int32_t n_q, int32_t most)
 {
-    const int64_t by_size = ((int64_t)n_q * n_k + 4095) / 4096, by_heads = (most + heads - 1) / heads;
-    return (int32_t)(by_size < by_heads ? by_size : by_heads);
+    const int32_t by_size = (n_q + 7) / 8, by_heads = (most + heads - 1) / heads;
+    return by_size < by_heads ? by_size : by_heads;
 }
 
 constexpr int32_t ROW_CTAS = 1184, SUM_CTAS = 444;
@@ -559,17 +514,15 @@ constexpr int32_t ROW_CTAS = 1184, SUM_CTAS = 444;
 template <typename T> int bias_rows(grf_ctx* ctx, const bias_shape& s, const void* table, void* rows)
 {
     grf_softmax_scope scope(ctx, "grf:relative_rows");
-    const auto kernel = big_plane(s) ? relative_rows_kernel<T, int64_t> : relative_rows_kernel<T, int32_t>;
-    kernel<<<dim3(s.strips, s.heads), BIAS_THREADS, 0, ctx->stream>>>(s, (const T*)table, (T*)rows);
+    relative_rows_kernel<T><<<dim3(s.strips, s.heads), BIAS_THREADS, 0, ctx->stream>>>(s, (const T*)table, (T*)rows);
     return cudaGetLastError() == cudaSuccess ? GRF_OK : GRF_ERR_CUDA;
 }
 template <typename T> int bias_sums(grf_ctx* ctx, const bias_shape& s, int32_t batch, const void* drows, void* dtable, float* part)
 {
     const size_t smem = sizeof(float) * (size_t)s.columns() * BIAS_THREADS;
-    const auto kernel = big_plane(s) ? relative_sums_kernel<T, int64_t> : relative_sums_kernel<T, int32_t>;
-    GRF_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    GRF_CUDA_TRY(cudaFuncSetAttribute(relative_sums_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     grf_softmax_scope scope(ctx, "grf:relative_sums", 2);
-    kernel<<<dim3(s.strips, s.heads), BIAS_THREADS, smem, ctx->stream>>>(s, batch, (const T*)drows, part);
+    relative_sums_kernel<T><<<dim3(s.strips, s.heads), BIAS_THREADS, smem, ctx->stream>>>(s, batch, (const T*)drows, part);
     bucket_sums_kernel<T><<<dim3(s.columns(), s.heads), 256, 0, ctx->stream>>>(part, (T*)dtable, 1, s.heads, s.strips, s.columns());
     return cudaGetLastError() == cudaSuccess ? GRF_OK : GRF_ERR_CUDA;
 }
@@ -582,7 +535,7 @@ extern "C" int grf_relative_bias(grf_ctx* ctx, int32_t heads, int32_t n_q, int32
     if (!ctx || !table || !rows || !aligned(rows, 16)) return GRF_ERR_INVALID;
     bias_shape s;
     GRF_TRY(read_bias(&s, heads, n_q, n_k, q_start, n_buckets, two_sided, first, dtype));
-    s.strips = bias_strips(heads, n_q, n_k, ROW_CTAS);
+    s.strips = bias_strips(heads, n_q, ROW_CTAS);
     GRF_CUDA_TRY(cudaSetDevice(ctx->device));
     return dtype == GRF_DTYPE_F32 ? bias_rows<float>(ctx, s, table, rows) : bias_rows<__nv_bfloat16>(ctx, s, table, rows);
 }
@@ -590,7 +543,7 @@ extern "C" int grf_relative_bias(grf_ctx* ctx, int32_t heads, int32_t n_q, int32
 extern "C" size_t grf_relative_bias_workspace_bytes(int32_t heads, int32_t n_q, int32_t n_k, int32_t n_buckets, int two_sided)
 {
     if (heads <= 0 || n_q <= 0 || n_k <= 0 || n_buckets < 1 || n_buckets > GRF_MAX_BUCKETS || (two_sided & ~1) != 0) return 0;
-    return align256(sizeof(float) * (size_t)heads * bias_strips(heads, n_q, n_k, SUM_CTAS) * n_buckets * (1 + two_sided));
+    return align256(sizeof(float) * (size_t)heads * bias_strips(heads, n_q, SUM_CTAS) * n_buckets * (1 + two_sided));
 }
 
 extern "C" int grf_relative_bias_backward(grf_ctx* ctx, int32_t batch, int32_t heads, int32_t n_q, int32_t n_k, int32_t q_start,
@@ -601,7 +554,7 @@ extern "C" int grf_relative_bias_backward(grf_ctx* ctx, int32_t batch, int32_t h
     bias_shape s;
     GRF_TRY(read_bias(&s, heads, n_q, n_k, q_start, n_buckets, two_sided, first, dtype));
     if (workspace_bytes < grf_relative_bias_workspace_bytes(heads, n_q, n_k, n_buckets, two_sided)) return GRF_ERR_WORKSPACE;
-    s.strips = bias_strips(heads, n_q, n_k, SUM_CTAS);
+    s.strips = bias_strips(heads, n_q, SUM_CTAS);
     GRF_CUDA_TRY(cudaSetDevice(ctx->device));
     return dtype == GRF_DTYPE_F32 ? bias_sums<float>(ctx, s, batch, drows, dtable, (float*)workspace)
                                   : bias_sums<__nv_bfloat16>(ctx, s, batch, drows, dtable, (float*)workspace);

@@ -9,13 +9,21 @@
 //
 // 256 threads hold 4 x 4 scores each; operands lie in shared memory as rows with four words of padding, read 16 bytes at a time: two reads
 // for sixteen multiply-adds, which leaves the fp32 pipe as the bound.
+#include <cooperative_groups.h>
+
 #include "softmax.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace {
 
 constexpr int BT = 64;                  // queries, and keys, of a tile
 constexpr int THREADS = 256;
 constexpr int PS = BT + 4;              // row of a score tile
+
+// Tiles of a block's other side are dealt out to the CTAs of a cluster, which add what they have through distributed shared memory: one CTA per block
+// leaves too few warps per SM on all but the largest calls, and with causal order the longest block decides.  MEASURED
+struct alu_split { int32_t splits; };
 
 template <int DP> struct Alu {
     static constexpr int ROW = DP + 4;
@@ -149,7 +157,7 @@ template <typename T> __device__ __forceinline__ void load_bias(float* lut, cons
 }
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(THREADS) softmax_alu_forward_kernel(const __grid_constant__ grf_softmax_params p)
+__global__ void __launch_bounds__(THREADS) softmax_alu_forward_kernel(const __grid_constant__ grf_softmax_params p, const alu_split f)
 {
     using A = Alu<DP>;
     extern __shared__ float smem[];
@@ -159,11 +167,12 @@ __global__ void __launch_bounds__(THREADS) softmax_alu_forward_kernel(const __gr
     __shared__ int bad;
     const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
     bucket.fill(p);
-    const int32_t b = blockIdx.y / p.H, h = blockIdx.y % p.H, i0 = (gridDim.x - 1 - blockIdx.x) * BT, kvh = h / p.group;
+    const int32_t b = blockIdx.y / p.H, h = blockIdx.y % p.H, kvh = h / p.group, qblocks = gridDim.x / f.splits;
+    const int32_t i0 = (qblocks - 1 - (int32_t)blockIdx.x / f.splits) * BT, rank = blockIdx.x % f.splits;
     const grf_sight sight(p, b);
     const int32_t *qdoc = sight.docs ? p.q_doc + (int64_t)b * p.Nq : nullptr, *kdoc = sight.docs ? p.k_doc + (int64_t)b * p.Nk : nullptr;
     const int32_t kblocks = (p.Nk + BT - 1) / BT, i1 = min(i0 + BT, p.Nq);
-    const int4 qr = sight.docs ? p.q_range[(int64_t)b * gridDim.x + i0 / BT] : all_docs();
+    const int4 qr = sight.docs ? p.q_range[(int64_t)b * qblocks + i0 / BT] : all_docs();
     const T *K = at_head<T>(p.k, p.ks, b, kvh), *V = at_head<T>(p.v, p.vs, b, kvh);
     if (tid == 0) bad = 0;
     load_rows<T, DP>(qs, at_head<T>(p.q, p.qs, b, h), p.qs[2], i0, p.Nq, p.d, nullptr, false, nullptr);
@@ -179,7 +188,7 @@ __global__ void __launch_bounds__(THREADS) softmax_alu_forward_kernel(const __gr
     }
     const float to2 = p.scale * GRF_LOG2E, cap2 = p.cap * GRF_LOG2E, by_cap = p.cap > 0.0f ? p.scale / p.cap : 0.0f;
     const int32_t end = sight.end(i1);
-    for (int32_t j0 = 0; j0 < end; j0 += BT) {
+    for (int32_t j0 = rank * BT; j0 < end; j0 += f.splits * BT) {
         const int what = sight.tile(i0, i1, j0, j0 + BT, qr, sight.docs ? __ldg(p.k_range + (int64_t)b * kblocks + j0 / BT) : all_docs());
         if (what == 0) continue;
         __syncthreads();
@@ -233,7 +242,7 @@ __global__ void __launch_bounds__(THREADS) softmax_alu_forward_kernel(const __gr
         for (int32_t j = 0; j < end; ++j) {
             const int32_t j0 = j & ~(BT - 1);
             const int what = sight.tile(i0, i1, j0, j0 + BT, qr, sight.docs ? p.k_range[(int64_t)b * kblocks + j0 / BT] : all_docs());
-            if (what != 1) { j = j0 + BT - 1; continue; }
+            if (what != 1 || j0 / BT % f.splits != rank) { j = j0 + BT - 1; continue; }
 #pragma unroll
             for (int c = 0; c < DP / 16; ++c) {
                 const int col = c / A::W * 16 * A::W + A::W * tx + c % A::W;
@@ -245,6 +254,40 @@ __global__ void __launch_bounds__(THREADS) softmax_alu_forward_kernel(const __gr
                     if (sight.sees(sight.position(i0 + 4 * ty + r), j) && (!kdoc || (doc[r] >= 0 && kdoc[j] == doc[r]))) o[r][c] += v;
             }
         }
+    }
+    if (f.splits > 1) {
+        // maxima, sums and outputs of all parts, in order; every CTA joins a share of the rows
+        float *os = ks, *ms = pt, *ls = pt + BT;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            store_row<float, DP>(os + (4 * ty + r) * DP, o[r], tx, DP);
+            if (tx == 0) { ms[4 * ty + r] = m[r]; ls[4 * ty + r] = l[r]; }
+        }
+        cg::cluster_group cluster = cg::this_cluster();
+        cluster.sync();
+        const int r0 = BT * rank / f.splits, r1 = BT * (rank + 1) / f.splits;
+        for (int x = tid; x < (r1 - r0) * DP; x += THREADS) {
+            const int r = r0 + x / DP, c = x % DP;
+            const int32_t i = i0 + r;
+            if (i >= p.Nq || c >= p.d) continue;
+            float top = -CUDART_INF_F, sum = 0.0f, total = 0.0f;
+            for (int y = 0; y < f.splits; ++y) top = fmaxf(top, *cluster.map_shared_rank(ms + r, y));
+            for (int y = 0; y < f.splits; ++y) {
+                const float my = *cluster.map_shared_rank(ms + r, y), ly = *cluster.map_shared_rank(ls + r, y), oy = *cluster.map_shared_rank(os + r * DP + c, y);
+                // (a part without a key weighs nothing; NaN scores leave NaN sums beside a maximum that is not one)
+                const float w = my == -CUDART_INF_F ? 0.0f : exp2f(my - top), bad = ly != ly ? CUDART_NAN_F : 0.0f;
+                total += w * ly + bad;
+                sum += w * oy + bad;
+            }
+            const float y = total == 0.0f ? 0.0f : sum / total;
+            const T z = grf_from_float<T>(y);
+            (at_head_w<T>(p.out_w, p.os, b, h) + (int64_t)i * p.os[2])[c] = z;
+            const int64_t row = ((int64_t)b * p.H + h) * p.Nq + i;
+            if (p.rest_w) p.rest_w[row * p.d + c] = grf_rest(y, z);
+            if (p.lse_w && c == 0) p.lse_w[row] = total == 0.0f ? -CUDART_INF_F : (top + log2f(total)) * GRF_LN2;
+        }
+        cluster.sync();
+        return;
     }
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
@@ -263,6 +306,20 @@ __global__ void __launch_bounds__(THREADS) softmax_alu_forward_kernel(const __gr
         }
         if (p.lse_w && tx == 0)
             p.lse_w[((int64_t)b * p.H + h) * p.Nq + i] = l[r] == 0.0f ? -CUDART_INF_F : (m[r] + log2f(l[r])) * GRF_LN2;
+    }
+}
+
+// This CTA's share of a block's rows, [BT][DP] summed over the cluster in order.
+template <typename T, int DP>
+__device__ __forceinline__ void add_parts(cg::cluster_group& cluster, float* mine, int splits, int rank, T* dst, int64_t stride, int32_t rows, int32_t d, float by)
+{
+    const int r0 = BT * rank / splits, r1 = BT * (rank + 1) / splits;
+    for (int x = threadIdx.x; x < (r1 - r0) * DP; x += THREADS) {
+        const int r = r0 + x / DP, c = x % DP;
+        if (r >= rows || c >= d) continue;
+        float sum = 0.0f;
+        for (int y = 0; y < splits; ++y) sum += *cluster.map_shared_rank(mine + r * DP + c, y);
+        dst[(int64_t)r * stride + c] = grf_from_float<T>(sum * by);
     }
 }
 
@@ -299,7 +356,7 @@ __device__ __forceinline__ void score_gradient(const grf_softmax_params& p, cons
 }
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(THREADS) softmax_alu_dq_kernel(const __grid_constant__ grf_softmax_params p)
+__global__ void __launch_bounds__(THREADS) softmax_alu_dq_kernel(const __grid_constant__ grf_softmax_params p, const alu_split f)
 {
     using A = Alu<DP>;
     extern __shared__ float smem[];
@@ -308,11 +365,12 @@ __global__ void __launch_bounds__(THREADS) softmax_alu_dq_kernel(const __grid_co
     __shared__ float lut[2 * BT], bins[4][2 * GRF_MAX_BUCKETS];   // sums by bucket, of diagonals 32 w .. 32 w + 31 of each tile
     const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
     bucket.fill(p);
-    const int32_t b = blockIdx.y / p.H, h = blockIdx.y % p.H, i0 = (gridDim.x - 1 - blockIdx.x) * BT, kvh = h / p.group;
+    const int32_t b = blockIdx.y / p.H, h = blockIdx.y % p.H, kvh = h / p.group, qblocks = gridDim.x / f.splits;
+    const int32_t i0 = (qblocks - 1 - (int32_t)blockIdx.x / f.splits) * BT, rank = blockIdx.x % f.splits;
     const grf_sight sight(p, b);
     const int32_t *qdoc = sight.docs ? p.q_doc + (int64_t)b * p.Nq : nullptr, *kdoc = sight.docs ? p.k_doc + (int64_t)b * p.Nk : nullptr;
     const int32_t kblocks = (p.Nk + BT - 1) / BT, i1 = min(i0 + BT, p.Nq), columns = grf_softmax_columns(p);
-    const int4 qr = sight.docs ? p.q_range[(int64_t)b * gridDim.x + i0 / BT] : all_docs();
+    const int4 qr = sight.docs ? p.q_range[(int64_t)b * qblocks + i0 / BT] : all_docs();
     const T *K = at_head<T>(p.k, p.ks, b, kvh), *V = at_head<T>(p.v, p.vs, b, kvh);
     load_rows<T, DP>(qs, at_head<T>(p.q, p.qs, b, h), p.qs[2], i0, p.Nq, p.d, nullptr, false, nullptr);
     load_rows<T, DP>(gs, at_head<T>(p.dout, p.dos, b, h), p.dos[2], i0, p.Nq, p.d, nullptr, false, nullptr);
@@ -326,7 +384,7 @@ __global__ void __launch_bounds__(THREADS) softmax_alu_dq_kernel(const __grid_co
     }
     for (int x = tid; x < 4 * 2 * GRF_MAX_BUCKETS; x += THREADS) (&bins[0][0])[x] = 0.0f;
     const int32_t end = sight.end(i1);
-    for (int32_t j0 = 0; j0 < end; j0 += BT) {
+    for (int32_t j0 = rank * BT; j0 < end; j0 += f.splits * BT) {
         const int what = sight.tile(i0, i1, j0, j0 + BT, qr, sight.docs ? __ldg(p.k_range + (int64_t)b * kblocks + j0 / BT) : all_docs());
         if (what == 0) continue;
         __syncthreads();
@@ -361,6 +419,22 @@ __global__ void __launch_bounds__(THREADS) softmax_alu_dq_kernel(const __grid_co
         }
     }
     __syncthreads();
+    float* part = p.dtable_part ? p.dtable_part + ((int64_t)blockIdx.y * qblocks + i0 / BT) * columns : nullptr;
+    if (f.splits > 1) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) store_row<float, DP>(ks + (4 * ty + r) * DP, dq[r], tx, DP);
+        cg::cluster_group cluster = cg::this_cluster();
+        cluster.sync();
+        if (part && rank == 0 && tid < columns) {
+            float sum = 0.0f;
+            for (int y = 0; y < f.splits; ++y)
+                for (int w = 0; w < 4; ++w) sum += *cluster.map_shared_rank(&bins[w][tid], y);
+            part[tid] = sum;
+        }
+        add_parts<T, DP>(cluster, ks, f.splits, rank, at_head_w<T>(p.dq, p.dqs, b, h) + (int64_t)i0 * p.dqs[2], p.dqs[2], p.Nq - i0, p.d, p.scale);
+        cluster.sync();
+        return;
+    }
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         const int32_t i = i0 + 4 * ty + r;
@@ -369,11 +443,11 @@ __global__ void __launch_bounds__(THREADS) softmax_alu_dq_kernel(const __grid_co
         for (int c = 0; c < DP / 16; ++c) dq[r][c] *= p.scale;
         store_row<T, DP>(at_head_w<T>(p.dq, p.dqs, b, h) + (int64_t)i * p.dqs[2], dq[r], tx, p.d);
     }
-    if (p.dtable_part && tid < columns) p.dtable_part[((int64_t)blockIdx.y * gridDim.x + i0 / BT) * columns + tid] = (bins[0][tid] + bins[1][tid]) + (bins[2][tid] + bins[3][tid]);
+    if (part && tid < columns) part[tid] = (bins[0][tid] + bins[1][tid]) + (bins[2][tid] + bins[3][tid]);
 }
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(THREADS) softmax_alu_dkv_kernel(const __grid_constant__ grf_softmax_params p)
+__global__ void __launch_bounds__(THREADS) softmax_alu_dkv_kernel(const __grid_constant__ grf_softmax_params p, const alu_split f)
 {
     using A = Alu<DP>;
     extern __shared__ float smem[];
@@ -382,11 +456,11 @@ __global__ void __launch_bounds__(THREADS) softmax_alu_dkv_kernel(const __grid_c
     __shared__ grf_buckets bucket;
     const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
     bucket.fill(p);
-    const int32_t b = blockIdx.y / p.KV, kvh = blockIdx.y % p.KV, j0 = blockIdx.x * BT, j1 = j0 + BT;
+    const int32_t b = blockIdx.y / p.KV, kvh = blockIdx.y % p.KV, j0 = (int32_t)blockIdx.x / f.splits * BT, j1 = j0 + BT, rank = blockIdx.x % f.splits;
     const grf_sight sight(p, b);
     const int32_t *qdoc = sight.docs ? p.q_doc + (int64_t)b * p.Nq : nullptr, *kdoc = sight.docs ? p.k_doc + (int64_t)b * p.Nk : nullptr;
     const int32_t qblocks = (p.Nq + BT - 1) / BT;
-    const int4 kr = sight.docs ? p.k_range[(int64_t)b * gridDim.x + blockIdx.x] : all_docs();
+    const int4 kr = sight.docs ? p.k_range[(int64_t)b * (gridDim.x / f.splits) + j0 / BT] : all_docs();
     load_rows<T, DP>(ks, at_head<T>(p.k, p.ks, b, kvh), p.ks[2], j0, sight.len, p.d, kdoc, false, nullptr);
     load_rows<T, DP>(vs, at_head<T>(p.v, p.vs, b, kvh), p.vs[2], j0, sight.len, p.d, kdoc, false, nullptr);
     float dk[4][DP / 16], dv[4][DP / 16];
@@ -394,7 +468,7 @@ __global__ void __launch_bounds__(THREADS) softmax_alu_dkv_kernel(const __grid_c
     for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int c = 0; c < DP / 16; ++c) dk[r][c] = dv[r][c] = 0.0f;
-    for (int32_t x = 0; x < p.group * qblocks; ++x) {
+    for (int32_t x = rank; x < p.group * qblocks; x += f.splits) {
         const int32_t h = kvh * p.group + x / qblocks, i0 = x % qblocks * BT;
         const int what = sight.tile(i0, min(i0 + BT, p.Nq), j0, j1, sight.docs ? __ldg(p.q_range + (int64_t)b * qblocks + i0 / BT) : all_docs(), kr);
         if (what == 0) continue;
@@ -423,6 +497,21 @@ __global__ void __launch_bounds__(THREADS) softmax_alu_dkv_kernel(const __grid_c
         accumulate<DP>(dv, ps, gs, ty, tx);
         accumulate<DP>(dk, xs, qs, ty, tx);
     }
+    if (f.splits > 1) {
+        __syncthreads();
+        float *dks = qs, *dvs = ks;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            store_row<float, DP>(dks + (4 * ty + r) * DP, dk[r], tx, DP);
+            store_row<float, DP>(dvs + (4 * ty + r) * DP, dv[r], tx, DP);
+        }
+        cg::cluster_group cluster = cg::this_cluster();
+        cluster.sync();
+        add_parts<T, DP>(cluster, dks, f.splits, rank, at_head_w<T>(p.dk, p.dks, b, kvh) + (int64_t)j0 * p.dks[2], p.dks[2], p.Nk - j0, p.d, p.scale);
+        add_parts<T, DP>(cluster, dvs, f.splits, rank, at_head_w<T>(p.dv, p.dvs, b, kvh) + (int64_t)j0 * p.dvs[2], p.dvs[2], p.Nk - j0, p.d, 1.0f);
+        cluster.sync();
+        return;
+    }
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         const int32_t j = j0 + 4 * ty + r;
@@ -434,24 +523,47 @@ __global__ void __launch_bounds__(THREADS) softmax_alu_dkv_kernel(const __grid_c
     }
 }
 
+// one CTA per block, or a cluster of up to eight where the blocks fill the device less than four times over and every CTA gets two tiles or more
+alu_split split_of(const grf_ctx* ctx, int64_t blocks, int64_t tiles)
+{
+    alu_split f = {1};
+    while (f.splits < 8 && blocks * f.splits < 4 * ctx->sm_count && tiles >= 2 * (f.splits + 1)) ++f.splits;
+    return f;
+}
+
+template <typename Kernel> int launch(grf_ctx* ctx, Kernel kernel, const grf_softmax_params& p, int32_t blocks, int32_t heads, int64_t tiles, size_t smem)
+{
+    GRF_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    const alu_split f = split_of(ctx, (int64_t)blocks * heads, tiles);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(blocks * f.splits, heads);
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = ctx->stream;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = (unsigned)f.splits;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    GRF_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, p, f));
+    return GRF_OK;
+}
+
 template <typename T, int DP> int forward(grf_ctx* ctx, const grf_softmax_params& p)
 {
-    const size_t smem = sizeof(float) * (3 * Alu<DP>::TILE + BT * PS);
-    GRF_CUDA_TRY(cudaFuncSetAttribute(softmax_alu_forward_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    const int32_t qb = grf_ceil_div(p.Nq, BT), kb = grf_ceil_div(p.Nk, BT);
     grf_softmax_scope scope(ctx, "grf:softmax_attention");
-    softmax_alu_forward_kernel<T, DP><<<dim3(grf_ceil_div(p.Nq, BT), p.B * p.H), THREADS, smem, ctx->stream>>>(p);
-    return cudaGetLastError() == cudaSuccess ? GRF_OK : GRF_ERR_CUDA;
+    return launch(ctx, softmax_alu_forward_kernel<T, DP>, p, qb, p.B * p.H, kb, sizeof(float) * (3 * Alu<DP>::TILE + BT * PS));
 }
 
 template <typename T, int DP> int backward(grf_ctx* ctx, const grf_softmax_params& p)
 {
+    const int32_t qb = grf_ceil_div(p.Nq, BT), kb = grf_ceil_div(p.Nk, BT);
     const size_t smem = sizeof(float) * (4 * Alu<DP>::TILE + 2 * BT * PS);
-    GRF_CUDA_TRY(cudaFuncSetAttribute(softmax_alu_dq_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    GRF_CUDA_TRY(cudaFuncSetAttribute(softmax_alu_dkv_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     grf_softmax_scope scope(ctx, "grf:softmax_gradients", 2);
-    softmax_alu_dq_kernel<T, DP><<<dim3(grf_ceil_div(p.Nq, BT), p.B * p.H), THREADS, smem, ctx->stream>>>(p);
-    softmax_alu_dkv_kernel<T, DP><<<dim3(grf_ceil_div(p.Nk, BT), p.B * p.KV), THREADS, smem, ctx->stream>>>(p);
-    return cudaGetLastError() == cudaSuccess ? GRF_OK : GRF_ERR_CUDA;
+    GRF_TRY(launch(ctx, softmax_alu_dq_kernel<T, DP>, p, qb, p.B * p.H, kb, smem));
+    return launch(ctx, softmax_alu_dkv_kernel<T, DP>, p, kb, p.B * p.KV, (int64_t)qb * p.group, smem);
 }
 
 }  // namespace

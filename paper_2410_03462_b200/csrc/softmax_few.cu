@@ -61,6 +61,8 @@ __device__ __forceinline__ uint32_t only_finite(uint32_t x, bool& found)
     return x & keep;
 }
 
+__device__ __forceinline__ float unless_finite(float x) { return fabsf(x) <= 3.4028235e38f ? 0.0f : x; }
+
 // A row of the block: head and query, what it sees.
 struct few_row {
     int32_t h, i, pos, doc;
@@ -471,15 +473,14 @@ __global__ void __launch_bounds__(THREADS) softmax_few_f32_kernel(const __grid_c
                 const int32_t j = tile * 8 + g;
                 if (tile * 8 + 8 <= whole || j >= end) continue;
 #pragma unroll
-                for (int c = 0; c < NC; ++c)
-                    for (int e = 0; e < 4; ++e) {
-                        if (16 * c + 4 * t >= p.d) continue;
-                        const float v = V[(int64_t)j * p.vs[2] + 16 * c + e];
-                        if (fabsf(v) <= 3.4028235e38f) continue;
+                for (int c = 0; c < NC; ++c) {
+                    if (16 * c + 4 * t >= p.d) continue;
+                    const float* v = V + (int64_t)j * p.vs[2] + 16 * c;
+                    const float4 add = make_float4(unless_finite(v[0]), unless_finite(v[1]), unless_finite(v[2]), unless_finite(v[3]));
 #pragma unroll
-                        for (int r = 0; r < ROWS; ++r)
-                            if (row[r].sees(sight, kdoc, j)) (&o[r][c].x)[e] += v;
-                    }
+                    for (int r = 0; r < ROWS; ++r)
+                        if (row[r].sees(sight, kdoc, j)) { o[r][c].x += add.x; o[r][c].y += add.y; o[r][c].z += add.z; o[r][c].w += add.w; }
+                }
             }
     }
 #pragma unroll
