@@ -14,6 +14,7 @@ class Context:
 
     def __init__(self, device: int = 0):
         self.device = device
+        self.torch_device = torch.device("cuda", device)
         torch.cuda.set_device(device)
         self.stream = torch.cuda.current_stream(device)
         self.handle = B.grf_ctx_create(device, self.stream.cuda_stream)
@@ -149,9 +150,7 @@ class SoftmaxSaved(NamedTuple):
 
 
 def _tokens(t, device, shape, name):
-    """Address of an int32 device array of the given shape; None -> None."""
-    if t is None:
-        return None
+    """Address of an int32 device array of the given shape."""
     if t.dtype != torch.int32 or t.device != device or tuple(t.shape) != shape or not t.is_contiguous():
         raise ValueError(f"{name}: expected a contiguous int32 tensor {shape} on {device}")
     return t.data_ptr()
@@ -160,33 +159,39 @@ def _tokens(t, device, shape, name):
 def _stride3(t, name):
     """Strides of [batch, heads, tokens, dim] whose last axis is contiguous."""
     s = t.stride()
+    if len(s) != 4:
+        raise ValueError(f"{name}: expected four axes")
     if s[3] != 1 and t.shape[3] > 1:
         raise ValueError(f"{name}: the last axis must be contiguous")
     # (all zeros would mean "contiguous": an axis of one token, head or sequence is never stepped over, so any stride does)
     if s[0] == s[1] == s[2] == 0 and t.shape[0] * t.shape[1] * t.shape[2] > 1:
         raise ValueError(f"{name}: a tensor broadcast along every axis")
-    return s[:3]
+    return B.Stride3(s[0], s[1], s[2])
 
 
 def _softmax_desc(ctx, q, k, v, scale, cap, mask, k_len, q_start, prefix, q_doc, k_doc, slopes, table, first, two_sided):
-    if q.dim() != 4 or k.dim() != 4 or v.shape != k.shape:
+    q_shape, k_shape = q.shape, k.shape
+    if len(q_shape) != 4 or len(k_shape) != 4 or v.shape != k_shape:
         raise ValueError("expected q [B, H, Nq, d] and k, v [B, KV, Nk, d]")
-    batch, heads, n_q, dim = q.shape
-    kv_heads, n_k = k.shape[1], k.shape[2]
-    device = torch.device("cuda", ctx.device)
-    if k.shape[0] != batch or k.shape[3] != dim or k.dtype != q.dtype or v.dtype != q.dtype:
+    batch, heads, n_q, dim = q_shape
+    kv_heads, n_k = k_shape[1], k_shape[2]
+    dtype, device = q.dtype, ctx.torch_device
+    if k_shape[0] != batch or k_shape[3] != dim or k.dtype != dtype or v.dtype != dtype:
         raise ValueError("q, k and v disagree in batch, dim or type")
-    if q.device != device or k.device != device or v.device != device:
+    if not (q.is_cuda and k.is_cuda and v.is_cuda and q.get_device() == k.get_device() == v.get_device() == ctx.device):
         raise ValueError(f"expected tensors on {device}")
-    s = B.SoftmaxDesc()
-    s.batch, s.heads, s.kv_heads, s.n_q, s.n_k, s.dim, s.dtype = batch, heads, kv_heads, n_q, n_k, dim, B.dtype_code(q)
-    s.scale, s.cap, s.order = dim ** -0.5 if scale is None else scale, cap, ORDERS[mask]
-    s.q_stride[:], s.k_stride[:], s.v_stride[:] = _stride3(q, "q"), _stride3(k, "k"), _stride3(v, "v")
-    s.k_len = _tokens(k_len, device, (batch,), "k_len")
-    s.q_start = _tokens(q_start, device, (batch,), "q_start")
-    s.prefix = _tokens(prefix, device, (batch,), "prefix")
-    s.q_doc = _tokens(q_doc, device, (batch, n_q), "q_doc")
-    s.k_doc = _tokens(k_doc, device, (batch, n_k), "k_doc")
+    s = B.SoftmaxDesc(batch, heads, kv_heads, n_q, n_k, dim, B.dtype_code(q), dim ** -0.5 if scale is None else scale, cap, ORDERS[mask])
+    s.q_stride, s.k_stride, s.v_stride = _stride3(q, "q"), _stride3(k, "k"), _stride3(v, "v")
+    if k_len is not None:
+        s.k_len = _tokens(k_len, device, (batch,), "k_len")
+    if q_start is not None:
+        s.q_start = _tokens(q_start, device, (batch,), "q_start")
+    if prefix is not None:
+        s.prefix = _tokens(prefix, device, (batch,), "prefix")
+    if q_doc is not None:
+        s.q_doc = _tokens(q_doc, device, (batch, n_q), "q_doc")
+    if k_doc is not None:
+        s.k_doc = _tokens(k_doc, device, (batch, n_k), "k_doc")
     if slopes is not None and table is not None:
         raise ValueError("slopes or a table, not both")
     if slopes is not None:
@@ -198,10 +203,10 @@ def _softmax_desc(ctx, q, k, v, scale, cap, mask, k_len, q_start, prefix, q_doc,
             raise ValueError(f"a table needs first, the smallest distance of each of 1 .. {B.GRF_MAX_BUCKETS} buckets")
         n = len(first)
         shape = (heads, n * (2 if two_sided else 1))
-        if table.dtype != q.dtype or table.device != device or tuple(table.shape) != shape or not table.is_contiguous():
-            raise ValueError(f"table: expected a contiguous {q.dtype} tensor {shape} on {device}")
+        if table.dtype != dtype or table.device != device or tuple(table.shape) != shape or not table.is_contiguous():
+            raise ValueError(f"table: expected a contiguous {dtype} tensor {shape} on {device}")
         s.bias, s.table, s.n_buckets, s.two_sided = B.GRF_BIAS_BUCKETS, table.data_ptr(), n, int(two_sided)
-        s.first[:n] = [int(y) for y in first]
+        s.first[:n] = first if type(first) is list else [int(y) for y in first]
     return s
 
 
@@ -222,7 +227,7 @@ def softmax_attn(ctx: Context, q, k, v, scale=None, cap=0.0, mask="full", k_len=
     elif out.shape != q.shape or out.dtype != q.dtype or out.device != q.device:
         raise ValueError("out: expected the shape, type and device of q")
     else:
-        s.out_stride[:] = _stride3(out, "out")
+        s.out_stride = _stride3(out, "out")
     lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device) if want_lse else None
     if workspace is None:
         workspace = _scratch(B.grf_softmax_attn_workspace_bytes(ctx.handle, s, False), q.device)
@@ -245,7 +250,7 @@ def softmax_attn_backward(ctx: Context, q, k, v, out, saved, dout, scale=None, c
         raise ValueError("lse: expected float32 [B, H, Nq]")
     if rest is not None and (rest.shape != q.shape or rest.dtype != q.dtype or rest.device != q.device):
         raise ValueError("rest: expected the shape, type and device of q")
-    s.out_stride[:], s.dout_stride[:] = _stride3(out, "out"), _stride3(dout, "dout")
+    s.out_stride, s.dout_stride = _stride3(out, "out"), _stride3(dout, "dout")
     dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
     dtable = torch.empty_like(table) if table is not None and want_dtable else None
     if workspace is None:

@@ -30,13 +30,16 @@ _vp, _i32, _i64, _u64, _f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, c
 _sz, _int = ctypes.c_size_t, ctypes.c_int
 
 
+Stride3 = _i64 * 3
+
+
 class SoftmaxDesc(ctypes.Structure):
     """grf_softmax_desc; pointers as device addresses."""
     _fields_ = [("batch", _i32), ("heads", _i32), ("kv_heads", _i32), ("n_q", _i32), ("n_k", _i32), ("dim", _i32), ("dtype", _i32),
                 ("scale", _f32), ("cap", _f32), ("order", _i32), ("bias", _i32), ("n_buckets", _i32), ("two_sided", _i32),
                 ("first", _i32 * GRF_MAX_BUCKETS), ("slopes", _vp), ("table", _vp), ("k_len", _vp), ("q_start", _vp),
                 ("prefix", _vp), ("q_doc", _vp), ("k_doc", _vp)] + [
-                    (name + "_stride", _i64 * 3) for name in ("q", "k", "v", "out", "dout", "dq", "dk", "dv")]
+                    (name + "_stride", Stride3) for name in ("q", "k", "v", "out", "dout", "dq", "dk", "dv")]
 
 
 _desc = ctypes.POINTER(SoftmaxDesc)

@@ -391,19 +391,23 @@ struct bias_row {
         right = min(max((s.two_sided ? max(F, 1) : 0) - delta0, left), s.n_k);
     }
 };
-// Places from .. to - 1 of a row of T: `each` for those before the first and behind the last 16-byte border, `piece` for the 16-byte pieces; by one warp.
-template <typename T, typename Each, typename Piece>
-__device__ __forceinline__ void by_pieces(const T* row, int32_t from, int32_t to, Each each, Piece piece)
-{
-    constexpr int CH = 16 / (int)sizeof(T);
-    const int lane = threadIdx.x & 31;
-    if (from >= to) return;
-    const int32_t ahead = (int32_t)((CH - ((uintptr_t)(row + from) / sizeof(T)) % CH) % CH), first = min(from + ahead, to), count = (to - first) / CH, last = first + count * CH;
-    if (lane < first - from) each(from + lane);
-    if (lane >= 16 && lane - 16 < to - last) each(last + lane - 16);
-#pragma unroll 4
-    for (int32_t x = lane; x < count; x += 32) piece(first + x * CH);
-}
+// A stretch from .. to - 1 of a row of T as whole 16-byte pieces and what lies before the first and behind the last border.
+template <typename T> struct stretch {
+    static constexpr int CH = 16 / (int)sizeof(T);
+    int32_t from, to, first, count, last;
+    __device__ __forceinline__ stretch(const T* row, int32_t from_, int32_t to_) : from(from_), to(max(from_, to_))
+    {
+        const int32_t ahead = (int32_t)((CH - ((uintptr_t)(row + from) / sizeof(T)) % CH) % CH);
+        first = min(from + ahead, to);
+        count = (to - first) / CH;
+        last = first + count * CH;
+    }
+    // the place beside the pieces that this lane has, or -1 (fewer than 16 before, and behind)
+    __device__ __forceinline__ int32_t beside(int lane) const
+    {
+        return lane < 16 ? (lane < first - from ? from + lane : -1) : (lane - 16 < to - last ? last + lane - 16 : -1);
+    }
+};
 
 template <typename T>
 __global__ void __launch_bounds__(BIAS_THREADS) relative_rows_kernel(const __grid_constant__ bias_shape s, const T* __restrict__ table, T* __restrict__ rows)
@@ -428,8 +432,11 @@ __global__ void __launch_bounds__(BIAS_THREADS) relative_rows_kernel(const __gri
         T* row = rows + ((int64_t)h * s.n_q + i) * s.n_k;
         const bias_row r(s, F, i);
 #pragma unroll
-        for (int y = 0; y < 2; ++y)
-            by_pieces(row, y ? r.right : 0, y ? s.n_k : r.left, [&](int32_t j) { row[j] = outer[y]; }, [&](int32_t j) { *reinterpret_cast<uint4*>(row + j) = whole[y]; });
+        for (int y = 0; y < 2; ++y) {
+            const stretch<T> w(row, y ? r.right : 0, y ? s.n_k : r.left);
+            if (w.beside(lane) >= 0) row[w.beside(lane)] = outer[y];
+            for (int32_t x = lane; x < w.count; x += 32) *reinterpret_cast<uint4*>(row + w.first + x * CH) = whole[y];
+        }
         for (int32_t j = r.left + lane; j < r.right; j += 32) row[j] = value[column_at(s, F, near, r.delta0 + j)];
     }
 }
@@ -437,7 +444,7 @@ __global__ void __launch_bounds__(BIAS_THREADS) relative_rows_kernel(const __gri
 template <typename T>
 __global__ void __launch_bounds__(BIAS_THREADS) relative_sums_kernel(const __grid_constant__ bias_shape s, int32_t batch, const T* __restrict__ drows, float* __restrict__ part)
 {
-    constexpr int CH = 16 / (int)sizeof(T), NEAR_AHEAD = 8;
+    constexpr int CH = 16 / (int)sizeof(T), NEAR_AHEAD = 8, FAR_AHEAD = 4;
     extern __shared__ float bins[];                             // [column][thread]
     __shared__ unsigned char near[2 * BIAS_NEAR];
     const int32_t h = blockIdx.y, columns = s.columns(), tid = threadIdx.x, lane = tid & 31, F = s.first[s.n_first - 1];
@@ -446,33 +453,42 @@ __global__ void __launch_bounds__(BIAS_THREADS) relative_sums_kernel(const __gri
     __syncthreads();
     float* mine = bins + tid;
     float far[2] = {0.0f, 0.0f};
+    auto add = [&](int32_t delta, T v) { mine[column_at(s, F, near, delta) * BIAS_THREADS] += grf_to_float(v); };
     const int64_t all = (int64_t)batch * s.n_q, step = (int64_t)s.strips * (BIAS_THREADS / 32);
     for (int64_t x = (int64_t)blockIdx.x * (BIAS_THREADS / 32) + (tid >> 5); x < all; x += step) {
-        const int32_t b = (int32_t)(x / s.n_q), i = (int32_t)(x - (int64_t)b * s.n_q);
+        const int32_t b = all <= INT32_MAX ? (int32_t)((uint32_t)x / (uint32_t)s.n_q) : (int32_t)(x / s.n_q), i = (int32_t)(x - (int64_t)b * s.n_q);
         const T* row = drows + (((int64_t)b * s.heads + h) * s.n_q + i) * s.n_k;
         const bias_row r(s, F, i);
-        for (int32_t j0 = r.left; j0 < r.right; j0 += 32 * NEAR_AHEAD) {
-            T v[NEAR_AHEAD];
+        const stretch<T> before(row, 0, r.left), behind(row, r.right, s.n_k);
+        const int32_t pieces = before.count + behind.count;
+        auto piece_at = [&](int32_t y) { return reinterpret_cast<const uint4*>(row + (y < before.count ? before.first + y * CH : behind.first + (y - before.count) * CH)); };
+        // everything of the row that fits is under way before the first of it is used
+        uint4 w[FAR_AHEAD];
+        T v[NEAR_AHEAD], e0 = grf_from_float<T>(0.0f), e1 = e0;
 #pragma unroll
-            for (int y = 0; y < NEAR_AHEAD; ++y)
-                if (j0 + 32 * y + lane < r.right) v[y] = row[j0 + 32 * y + lane];
+        for (int y = 0; y < FAR_AHEAD; ++y) w[y] = lane + 32 * y < pieces ? __ldcs(piece_at(lane + 32 * y)) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-            for (int y = 0; y < NEAR_AHEAD; ++y) {
-                const int32_t j = j0 + 32 * y + lane;
-                if (j < r.right) mine[column_at(s, F, near, r.delta0 + j) * BIAS_THREADS] += grf_to_float(v[y]);
-            }
-        }
+        for (int y = 0; y < NEAR_AHEAD; ++y)
+            if (r.left + 32 * y + lane < r.right) v[y] = row[r.left + 32 * y + lane];
+        if (before.beside(lane) >= 0) e0 = row[before.beside(lane)];
+        if (behind.beside(lane) >= 0) e1 = row[behind.beside(lane)];
+        auto add_piece = [&](int32_t y, const uint4& u) {
+            const T* t = reinterpret_cast<const T*>(&u);
+            float sum = 0.0f;
 #pragma unroll
-        for (int y = 0; y < 2; ++y)
-            by_pieces(row, y ? r.right : 0, y ? s.n_k : r.left, [&](int32_t j) { far[y] += grf_to_float(row[j]); },
-                      [&](int32_t j) {
-                          const uint4 w = __ldcs(reinterpret_cast<const uint4*>(row + j));
-                          const T* v = reinterpret_cast<const T*>(&w);
-                          float sum = 0.0f;
+            for (int e = 0; e < CH; ++e) sum += grf_to_float(t[e]);
+            far[0] += y < before.count ? sum : 0.0f;
+            far[1] += y < before.count ? 0.0f : sum;
+        };
 #pragma unroll
-                          for (int e = 0; e < CH; ++e) sum += grf_to_float(v[e]);
-                          far[y] += sum;
-                      });
+        for (int y = 0; y < FAR_AHEAD; ++y) add_piece(lane + 32 * y, w[y]);
+        for (int32_t y = lane + 32 * FAR_AHEAD; y < pieces; y += 32) add_piece(y, __ldcs(piece_at(y)));
+        far[0] += grf_to_float(e0);
+        far[1] += grf_to_float(e1);
+#pragma unroll
+        for (int y = 0; y < NEAR_AHEAD; ++y)
+            if (r.left + 32 * y + lane < r.right) add(r.delta0 + r.left + 32 * y + lane, v[y]);
+        for (int32_t j = r.left + 32 * NEAR_AHEAD + lane; j < r.right; j += 32) add(r.delta0 + j, row[j]);
     }
     mine[(s.n_first - 1) * BIAS_THREADS] += far[0];
     mine[(s.two_sided ? 2 * s.n_first - 1 : 0) * BIAS_THREADS] += far[1];

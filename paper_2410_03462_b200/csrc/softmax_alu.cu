@@ -11,6 +11,7 @@
 // for sixteen multiply-adds, which leaves the fp32 pipe as the bound.
 #include <cooperative_groups.h>
 
+#include "packed.cuh"
 #include "softmax.cuh"
 
 namespace cg = cooperative_groups;
@@ -63,32 +64,71 @@ __device__ __forceinline__ void load_rows(float* tile, const T* base, int64_t st
     }
 }
 
-// acc[r][c] = sum over d of a[4 ty + r][.] b[tx + 16 c][.]
+// The same in two steps, so that a tile's loads are under way while the one before is computed (d <= 64: they fit in registers).
+template <typename T, int DP> struct rows_ahead {
+    static constexpr int CH = 16 / (int)sizeof(T), PER = DP / CH, N = (BT * PER + THREADS - 1) / THREADS;
+    uint4 w[N];
+    __device__ __forceinline__ void fetch(const T* base, int64_t stride, int32_t r0, int32_t rows, int32_t d, const int32_t* doc)
+    {
+#pragma unroll
+        for (int y = 0; y < N; ++y) {
+            const int x = threadIdx.x + y * THREADS, r = x / PER, c = x % PER * CH;
+            w[y] = x < BT * PER && r0 + r < rows && c < d && (!doc || doc[r0 + r] >= 0) ? *reinterpret_cast<const uint4*>(base + (int64_t)(r0 + r) * stride + c)
+                                                                                          : make_uint4(0, 0, 0, 0);
+        }
+    }
+    __device__ __forceinline__ void store(float* tile, bool clean, int* bad) const
+    {
+#pragma unroll
+        for (int y = 0; y < N; ++y) {
+            const int x = threadIdx.x + y * THREADS, r = x / PER, c = x % PER * CH;
+            if (x >= BT * PER) continue;
+            const T* t = reinterpret_cast<const T*>(&w[y]);
+            float v[CH];
+#pragma unroll
+            for (int e = 0; e < CH; ++e) {
+                v[e] = grf_to_float(t[e]);
+                if (clean && !finite(v[e])) {
+                    v[e] = 0.0f;
+                    if (bad) *bad = 1;
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < CH; e += 4) *reinterpret_cast<float4*>(tile + r * Alu<DP>::ROW + c + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+        }
+    }
+};
+
+// acc[r][c] = sum over d of a[4 ty + r][.] b[tx + 16 c][.], even and odd d by themselves: packed multiply-adds on values as they are read
 template <int DP>
 __device__ __forceinline__ void products(float (&acc)[4][4], const float* a, const float* b, int ty, int tx)
 {
     constexpr int ROW = Alu<DP>::ROW;
+    uint64_t sum[4][4];
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) acc[r][c] = 0.0f;
+        for (int c = 0; c < 4; ++c) sum[r][c] = 0ull;
 #pragma unroll 4
     for (int k = 0; k < DP; k += 4) {
-        float4 x[4], y[4];
+        ulonglong2 x[4], y[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) x[r] = *reinterpret_cast<const float4*>(a + (4 * ty + r) * ROW + k);
+        for (int r = 0; r < 4; ++r) x[r] = *reinterpret_cast<const ulonglong2*>(a + (4 * ty + r) * ROW + k);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) y[c] = *reinterpret_cast<const float4*>(b + (tx + 16 * c) * ROW + k);
+        for (int c = 0; c < 4; ++c) y[c] = *reinterpret_cast<const ulonglong2*>(b + (tx + 16 * c) * ROW + k);
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                acc[r][c] = fmaf(x[r].x, y[c].x, acc[r][c]);
-                acc[r][c] = fmaf(x[r].y, y[c].y, acc[r][c]);
-                acc[r][c] = fmaf(x[r].z, y[c].z, acc[r][c]);
-                acc[r][c] = fmaf(x[r].w, y[c].w, acc[r][c]);
-            }
+            for (int c = 0; c < 4; ++c) sum[r][c] = fma2(x[r].y, y[c].y, fma2(x[r].x, y[c].x, sum[r][c]));
     }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            float lo, hi;
+            unpack2(sum[r][c], lo, hi);
+            acc[r][c] = lo + hi;
+        }
 }
 
 template <int W> __device__ __forceinline__ void load_w(float (&v)[W], const float* at)
@@ -107,10 +147,15 @@ template <int DP>
 __device__ __forceinline__ void accumulate(float (&acc)[4][DP / 16], const float* w, const float* rows, int ty, int tx)
 {
     using A = Alu<DP>;
+    uint64_t sum[4][DP / 32];
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int c = 0; c < DP / 32; ++c) sum[r][c] = pack2(acc[r][2 * c], acc[r][2 * c + 1]);
 #pragma unroll 4
     for (int x = 0; x < BT; ++x) {
         const float4 p = *reinterpret_cast<const float4*>(w + x * PS + 4 * ty);
-        const float pr[4] = {p.x, p.y, p.z, p.w};
+        const uint64_t pr[4] = {pack2(p.x, p.x), pack2(p.y, p.y), pack2(p.z, p.z), pack2(p.w, p.w)};
 #pragma unroll
         for (int g = 0; g < A::NC; ++g) {
             float v[A::W];
@@ -118,9 +163,13 @@ __device__ __forceinline__ void accumulate(float (&acc)[4][DP / 16], const float
 #pragma unroll
             for (int r = 0; r < 4; ++r)
 #pragma unroll
-                for (int e = 0; e < A::W; ++e) acc[r][g * A::W + e] = fmaf(pr[r], v[e], acc[r][g * A::W + e]);
+                for (int e = 0; e < A::W; e += 2) sum[r][(g * A::W + e) / 2] = fma2(pr[r], pack2(v[e], v[e + 1]), sum[r][(g * A::W + e) / 2]);
         }
     }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int c = 0; c < DP / 32; ++c) unpack2(sum[r][c], acc[r][2 * c], acc[r][2 * c + 1]);
 }
 
 template <typename T, int DP>
@@ -188,12 +237,34 @@ __global__ void __launch_bounds__(THREADS) softmax_alu_forward_kernel(const __gr
     }
     const float to2 = p.scale * GRF_LOG2E, cap2 = p.cap * GRF_LOG2E, by_cap = p.cap > 0.0f ? p.scale / p.cap : 0.0f;
     const int32_t end = sight.end(i1);
-    for (int32_t j0 = rank * BT; j0 < end; j0 += f.splits * BT) {
-        const int what = sight.tile(i0, i1, j0, j0 + BT, qr, sight.docs ? __ldg(p.k_range + (int64_t)b * kblocks + j0 / BT) : all_docs());
-        if (what == 0) continue;
+    constexpr bool AHEAD = DP <= 64;
+    rows_ahead<T, AHEAD ? DP : 32> ka, va;
+    auto what_of = [&](int32_t j) { return sight.tile(i0, i1, j, j + BT, qr, sight.docs ? __ldg(p.k_range + (int64_t)b * kblocks + j / BT) : all_docs()); };
+    auto seen_from = [&](int32_t j) {
+        while (j < end && what_of(j) == 0) j += f.splits * BT;
+        return j;
+    };
+    auto fetch = [&](int32_t j) {
+        if constexpr (AHEAD)
+            if (j < end) {
+                ka.fetch(K, p.ks[2], j, sight.len, p.d, kdoc);
+                va.fetch(V, p.vs[2], j, sight.len, p.d, kdoc);
+            }
+    };
+    int32_t j_next = seen_from(rank * BT);
+    fetch(j_next);
+    for (int32_t j0 = j_next; j0 < end; j0 = j_next) {
+        const int what = what_of(j0);
+        j_next = seen_from(j0 + f.splits * BT);
         __syncthreads();
-        load_rows<T, DP>(ks, K, p.ks[2], j0, sight.len, p.d, kdoc, false, nullptr);
-        load_rows<T, DP>(vs, V, p.vs[2], j0, sight.len, p.d, kdoc, what == 1, &bad);
+        if constexpr (AHEAD) {
+            ka.store(ks, false, nullptr);
+            va.store(vs, what == 1, &bad);
+            fetch(j_next);
+        } else {
+            load_rows<T, DP>(ks, K, p.ks[2], j0, sight.len, p.d, kdoc, false, nullptr);
+            load_rows<T, DP>(vs, V, p.vs[2], j0, sight.len, p.d, kdoc, what == 1, &bad);
+        }
         load_bias<T>(lut, p, bucket, h, j0, sight.position(i0));
         __syncthreads();
         float s[4][4];
@@ -384,12 +455,34 @@ __global__ void __launch_bounds__(THREADS) softmax_alu_dq_kernel(const __grid_co
     }
     for (int x = tid; x < 4 * 2 * GRF_MAX_BUCKETS; x += THREADS) (&bins[0][0])[x] = 0.0f;
     const int32_t end = sight.end(i1);
-    for (int32_t j0 = rank * BT; j0 < end; j0 += f.splits * BT) {
-        const int what = sight.tile(i0, i1, j0, j0 + BT, qr, sight.docs ? __ldg(p.k_range + (int64_t)b * kblocks + j0 / BT) : all_docs());
-        if (what == 0) continue;
+    constexpr bool AHEAD = DP <= 64;
+    rows_ahead<T, AHEAD ? DP : 32> ka, va;
+    auto what_of = [&](int32_t j) { return sight.tile(i0, i1, j, j + BT, qr, sight.docs ? __ldg(p.k_range + (int64_t)b * kblocks + j / BT) : all_docs()); };
+    auto seen_from = [&](int32_t j) {
+        while (j < end && what_of(j) == 0) j += f.splits * BT;
+        return j;
+    };
+    auto fetch = [&](int32_t j) {
+        if constexpr (AHEAD)
+            if (j < end) {
+                ka.fetch(K, p.ks[2], j, sight.len, p.d, kdoc);
+                va.fetch(V, p.vs[2], j, sight.len, p.d, kdoc);
+            }
+    };
+    int32_t j_next = seen_from(rank * BT);
+    fetch(j_next);
+    for (int32_t j0 = j_next; j0 < end; j0 = j_next) {
+        const int what = what_of(j0);
+        j_next = seen_from(j0 + f.splits * BT);
         __syncthreads();
-        load_rows<T, DP>(ks, K, p.ks[2], j0, sight.len, p.d, kdoc, what == 1, nullptr);
-        load_rows<T, DP>(vs, V, p.vs[2], j0, sight.len, p.d, kdoc, false, nullptr);
+        if constexpr (AHEAD) {
+            ka.store(ks, what == 1, nullptr);
+            va.store(vs, false, nullptr);
+            fetch(j_next);
+        } else {
+            load_rows<T, DP>(ks, K, p.ks[2], j0, sight.len, p.d, kdoc, what == 1, nullptr);
+            load_rows<T, DP>(vs, V, p.vs[2], j0, sight.len, p.d, kdoc, false, nullptr);
+        }
         load_bias<T>(lut, p, bucket, h, j0, sight.position(i0));
         __syncthreads();
         float s[4][4], dp[4][4];
@@ -468,13 +561,40 @@ __global__ void __launch_bounds__(THREADS) softmax_alu_dkv_kernel(const __grid_c
     for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int c = 0; c < DP / 16; ++c) dk[r][c] = dv[r][c] = 0.0f;
-    for (int32_t x = rank; x < p.group * qblocks; x += f.splits) {
+    constexpr bool AHEAD = DP <= 64;
+    rows_ahead<T, AHEAD ? DP : 32> qa, ga;
+    const int32_t all = p.group * qblocks;
+    auto what_of = [&](int32_t x) {
+        const int32_t i = x % qblocks * BT;
+        return sight.tile(i, min(i + BT, p.Nq), j0, j1, sight.docs ? __ldg(p.q_range + (int64_t)b * qblocks + i / BT) : all_docs(), kr);
+    };
+    auto seen_from = [&](int32_t x) {
+        while (x < all && what_of(x) == 0) x += f.splits;
+        return x;
+    };
+    auto fetch = [&](int32_t x) {
+        if constexpr (AHEAD)
+            if (x < all) {
+                const int32_t h = kvh * p.group + x / qblocks, i = x % qblocks * BT;
+                qa.fetch(at_head<T>(p.q, p.qs, b, h), p.qs[2], i, p.Nq, p.d, qdoc);
+                ga.fetch(at_head<T>(p.dout, p.dos, b, h), p.dos[2], i, p.Nq, p.d, qdoc);
+            }
+    };
+    int32_t x_next = seen_from(rank);
+    fetch(x_next);
+    for (int32_t x = x_next; x < all; x = x_next) {
         const int32_t h = kvh * p.group + x / qblocks, i0 = x % qblocks * BT;
-        const int what = sight.tile(i0, min(i0 + BT, p.Nq), j0, j1, sight.docs ? __ldg(p.q_range + (int64_t)b * qblocks + i0 / BT) : all_docs(), kr);
-        if (what == 0) continue;
+        const int what = what_of(x);
+        x_next = seen_from(x + f.splits);
         __syncthreads();
-        load_rows<T, DP>(qs, at_head<T>(p.q, p.qs, b, h), p.qs[2], i0, p.Nq, p.d, qdoc, what == 1, nullptr);
-        load_rows<T, DP>(gs, at_head<T>(p.dout, p.dos, b, h), p.dos[2], i0, p.Nq, p.d, qdoc, what == 1, nullptr);
+        if constexpr (AHEAD) {
+            qa.store(qs, what == 1, nullptr);
+            ga.store(gs, what == 1, nullptr);
+            fetch(x_next);
+        } else {
+            load_rows<T, DP>(qs, at_head<T>(p.q, p.qs, b, h), p.qs[2], i0, p.Nq, p.d, qdoc, what == 1, nullptr);
+            load_rows<T, DP>(gs, at_head<T>(p.dout, p.dos, b, h), p.dos[2], i0, p.Nq, p.d, qdoc, what == 1, nullptr);
+        }
         load_bias<T>(lut, p, bucket, h, j0, sight.position(i0));
         __syncthreads();
         float s[4][4], dp[4][4];
