@@ -206,7 +206,7 @@ template <typename T> __device__ __forceinline__ void load_bias(float* lut, cons
 }
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(THREADS) softmax_alu_forward_kernel(const __grid_constant__ grf_softmax_params p, const alu_split f)
+__global__ void __launch_bounds__(THREADS, DP <= 64 ? 2 : 1) softmax_alu_forward_kernel(const __grid_constant__ grf_softmax_params p, const alu_split f)
 {
     using A = Alu<DP>;
     extern __shared__ float smem[];
@@ -427,7 +427,7 @@ __device__ __forceinline__ void score_gradient(const grf_softmax_params& p, cons
 }
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(THREADS) softmax_alu_dq_kernel(const __grid_constant__ grf_softmax_params p, const alu_split f)
+__global__ void __launch_bounds__(THREADS, DP <= 64 ? 2 : 1) softmax_alu_dq_kernel(const __grid_constant__ grf_softmax_params p, const alu_split f)
 {
     using A = Alu<DP>;
     extern __shared__ float smem[];
@@ -540,7 +540,7 @@ __global__ void __launch_bounds__(THREADS) softmax_alu_dq_kernel(const __grid_co
 }
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(THREADS) softmax_alu_dkv_kernel(const __grid_constant__ grf_softmax_params p, const alu_split f)
+__global__ void __launch_bounds__(THREADS, DP <= 64 ? 2 : 1) softmax_alu_dkv_kernel(const __grid_constant__ grf_softmax_params p, const alu_split f)
 {
     using A = Alu<DP>;
     extern __shared__ float smem[];

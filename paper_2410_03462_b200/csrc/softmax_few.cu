@@ -542,7 +542,7 @@ few_shape shape_of(const grf_ctx* ctx, const grf_softmax_params& p, int dtype)
     f.part = nullptr;
     // as many CTAs as keep the memory busy, of 128 keys or more; more than a cluster's only where its CTAs would have over 1024
     const int64_t units = (int64_t)p.B * p.KV * f.row_blocks;
-    int64_t s = (4 * (int64_t)ctx->sm_count + units - 1) / units;
+    int64_t s = (8 * (int64_t)ctx->sm_count + units - 1) / units;
     const int64_t most = (p.Nk + 127) / 128;
     if (s > most) s = most;
     if (s > MAX_CLUSTER && p.Nk <= MAX_CLUSTER * 1024) s = MAX_CLUSTER;

@@ -37,6 +37,7 @@ constexpr int SOFT = 8 * QT;                                    // warps that ma
 constexpr int THREADS = 32 * (SOFT + 4);
 constexpr int MORE = 104, LESS = 64;                            // registers: 4 * 104 + 64 = 5 * 96, the launch's
 
+#define FMA_PAIRS(n) ((n) % 8 == 2 || (n) % 8 == 5)             // of a thread's 32 pairs of columns
 constexpr int BIAS_NONE_SCALED = 3;     // no bias, scores scaled before anything else
 
 // What a block of queries sees.
@@ -143,7 +144,9 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
 {
     using Sh = Fwd<DP, EXACT>;
     constexpr int NS = Sh::NS, QB = Sh::QB;
-    constexpr bool FMA = false;
+    // some exponentials by multiply-adds: at d > 64, where nothing else is done to the scores, 4096 causal keys 165 -> 161 us (and 4096 seen ones 353 ->
+    // 345); with d = 64, caps or biases, whose own arithmetic fills that pipe, it costs up to a tenth
+    constexpr bool FMA = DP == 128 && BIAS == GRF_BIAS_NONE && !CAP && !EXACT;
     constexpr bool PLAIN = BIAS == GRF_BIAS_NONE && !CAP;   // (a scale that is not positive: BIAS_NONE_SCALED)
     extern __shared__ unsigned char smem_dyn[];
     constexpr int PER_GROUP = 5 + 2 * QB;
@@ -437,6 +440,7 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                     with_group();
                     ++luts;
                 }
+                const int32_t to = limit - j0;
                 wait(s_full(g), (uint32_t)done & 1u);
                 fence_after_sync();
                 uint32_t sv[4][16];
@@ -481,7 +485,6 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                         }
                 }
                 if (what == 1) {
-                    const int32_t to = limit - j0;
                     if (mixed) {
 #pragma unroll
                         for (int y = 0; y < 4; ++y)
@@ -548,8 +551,9 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                     for (int e = 0; e < 16; ++e) {
                         const int a = 2 * y + (e >> 3), z = (2 * e) & 15;
                         float x0, x1;
-                        unpack2(PLAIN ? fma2(pack2(sv[a][z], sv[a][z + 1]), to22, minus) : add2(pack2(sv[a][z], sv[a][z + 1]), minus), x0, x1);
-                        if (FMA && GRF_FMA_PAIRS(16 * y + e)) ex2_by_fma<EXACT ? 4 : 3>(pack2(x0, x1), x0, x1);
+                        const uint64_t v = pack2(sv[a][z], sv[a][z + 1]);
+                        unpack2(PLAIN ? fma2(v, to22, minus) : add2(v, minus), x0, x1);
+                        if (FMA && FMA_PAIRS(16 * y + e)) ex2_by_fma(pack2(x0, x1), x0, x1);
                         else { x0 = ex2(x0); x1 = ex2(x1); }
                         sum2[e & 1] = add2(sum2[e & 1], pack2(x0, x1));
                         w[e] = pack_bf16(x0, x1);

@@ -71,25 +71,18 @@ __device__ __forceinline__ float ex2(float x)
     return r;
 }
 // 2^x of two values by multiply-adds, for some of a tile's values, as the pipe of ex2 (a warp in eight cycles) bounds a softmax: x = i + f with i the
-// nearest integer (a sum with 1.5 * 2^23 rounds to it), 2^f by a polynomial whose largest relative error over -1/2 .. 1/2 is least, constant term 1
-// (measured 1.0e-4 at degree 3, 2.9e-6 at degree 4), and i added to the exponent.  x <= 127 - 1/2; what is below -127, -infinity with it, becomes 0.
-// NaN becomes 0: callers let it reach a row by its maximum.
-template <int DEGREE> __device__ __forceinline__ void ex2_by_fma(uint64_t x, float& y0, float& y1)
+// nearest integer (a sum with 1.5 * 2^23 rounds to it), 2^f by a cubic whose largest relative error over -1/2 .. 1/2 is least, constant term 1
+// (measured 1.0e-4: a fortieth of what rounding to bf16 takes), and i added to the exponent.  x <= 127 - 1/2; what is below -127, -infinity with it,
+// becomes 0.  NaN becomes 0: callers let it reach a row by its maximum.
+__device__ __forceinline__ void ex2_by_fma(uint64_t x, float& y0, float& y1)
 {
     constexpr float MAGIC = 12582912.0f;
     float x0, x1;
     unpack2(x, x0, x1);
     x = pack2(fmaxf(x0, -127.0f), fmaxf(x1, -127.0f));
     const uint64_t r = add2(x, pack2(MAGIC, MAGIC)), f = fma2(add2(r, pack2(-MAGIC, -MAGIC)), pack2(-1.0f, -1.0f), x);
-    uint64_t q;
-    if (DEGREE == 3) {
-        q = fma2(f, pack2(0.055008933f, 0.055008933f), pack2(0.24221097f, 0.24221097f));
-        q = fma2(q, f, pack2(0.69328290f, 0.69328290f));
-    } else {
-        q = fma2(f, pack2(0.0095828529f, 0.0095828529f), pack2(0.055906426f, 0.055906426f));
-        q = fma2(q, f, pack2(0.24024099f, 0.24024099f));
-        q = fma2(q, f, pack2(0.69312418f, 0.69312418f));
-    }
+    uint64_t q = fma2(f, pack2(0.055008933f, 0.055008933f), pack2(0.24221097f, 0.24221097f));
+    q = fma2(q, f, pack2(0.69328290f, 0.69328290f));
     q = fma2(q, f, pack2(1.0f, 1.0f));
     float r0, r1, q0, q1;
     unpack2(r, r0, r1);
@@ -97,10 +90,6 @@ template <int DEGREE> __device__ __forceinline__ void ex2_by_fma(uint64_t x, flo
     y0 = __uint_as_float(__float_as_uint(q0) + (__float_as_uint(r0) << 23));
     y1 = __uint_as_float(__float_as_uint(q1) + (__float_as_uint(r1) << 23));
 }
-// Which pairs of a tile's columns (numbered from 0) take it.
-#ifndef GRF_FMA_PAIRS
-#define GRF_FMA_PAIRS(n) ((n) % 8 == 2 || (n) % 8 == 5)
-#endif
 __device__ __forceinline__ float max3_nan(float a, float b, float c)
 {
     float r;

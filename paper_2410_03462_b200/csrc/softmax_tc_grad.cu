@@ -30,8 +30,9 @@ template <int DP> struct Grad {
     // stages: a tile's place is free only once its last product is done, a tile's time before the next but one is wanted, and a copy takes
     // about as long: two stages leave it in the open (d = 64: 1.87 us a tile and kernel with two, MEASURED with four)
     static constexpr int NS = DP == 64 ? 4 : 2;
+    static constexpr int QB = DP == 64 ? 2 : 1;        // places for what a block keeps
     static constexpr uint32_t TILE = HALF * (DP / 64);
-    static constexpr size_t SMEM = 1024 + (size_t)TILE * (2 + 2 * NS);      // then the tiles' bits
+    static constexpr size_t SMEM = 1024 + (size_t)TILE * (2 * QB + 2 * NS);        // then the tiles' bits
 };
 
 // Tiles of the other side that a block sees, in order; with documents from bits in shared memory.
@@ -95,10 +96,10 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                      const __grid_constant__ CUtensorMap map_g, const __grid_constant__ grf_softmax_params p)
 {
     using Sh = Grad<DP>;
-    constexpr int NS = Sh::NS;
+    constexpr int NS = Sh::NS, QB = Sh::QB;
     constexpr int LUTS = BIAS == GRF_BIAS_BUCKETS ? 1 : 0;
     extern __shared__ unsigned char smem_dyn[];
-    __shared__ __align__(8) unsigned long long bars[5 * NS + 9];
+    __shared__ __align__(8) unsigned long long bars[5 * NS + 7 + 2 * QB];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
     __shared__ float lut[LUTS ? 2 * 256 : 1];
@@ -108,22 +109,36 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     __shared__ float diag[LUTS ? WORKERS * 64 : 1];
     const int tid = threadIdx.x, lane = tid & 31, warp = uniform(tid >> 5);
     const uint32_t smem = (smem_u32(smem_dyn) + 1023u) & ~1023u;
-    uint32_t* bits = reinterpret_cast<uint32_t*>(smem_dyn + (smem - smem_u32(smem_dyn)) + Sh::TILE * (2 + 2 * NS));
-    const uint32_t q_at = smem, g_at = q_at + Sh::TILE, k_at = g_at + Sh::TILE, v_at = k_at + NS * Sh::TILE, bar0 = smem_u32(bars);
+    uint32_t* bits = reinterpret_cast<uint32_t*>(smem_dyn + (smem - smem_u32(smem_dyn)) + Sh::TILE * (2 * QB + 2 * NS));
+    const uint32_t q_at = smem, g_at = q_at + QB * Sh::TILE, k_at = g_at + QB * Sh::TILE, v_at = k_at + NS * Sh::TILE, bar0 = smem_u32(bars);
     auto k_full = [&](int s) { return bar0 + 8u * s; };
     auto v_full = [&](int s) { return bar0 + 8u * (NS + s); };
     auto k_empty = [&](int s) { return bar0 + 8u * (2 * NS + s); };
     auto v_empty = [&](int s) { return bar0 + 8u * (3 * NS + s); };
     auto k_clean = [&](int s) { return bar0 + 8u * (4 * NS + s); };
     const uint32_t one = bar0 + 8u * (5 * NS);
-    const uint32_t rows_full = one, s_full0 = one + 8, dp_full = one + 24, ds_full = one + 32, dq_done = one + 40, drain = one + 48, lut_full = one + 56;
+    const uint32_t s_full0 = one, dp_full = one + 16, ds_full = one + 24, dq_done = one + 32, acc_read = one + 40, drain = one + 48;
+    auto rows_full = [&](int y) { return one + 56 + 8u * y; };
+    auto rows_empty = [&](int y) { return one + 56 + 8u * (QB + y); };
 
-    const int32_t b = (int32_t)blockIdx.x / p.H, h = (int32_t)blockIdx.x % p.H, kvh = h / p.group;
-    const grf_sight sight(p, b);
-    const int32_t qb = (int32_t)gridDim.y - 1 - (int32_t)blockIdx.y, i0 = qb * BT, i1 = min(i0 + BT, p.Nq);
-    const int32_t tiles = (sight.end(i1) + BT - 1) / BT, last = sight.end(p.Nq);
-    const grad_tiles T{bits, 0, tiles, (tiles + 31) / 32, sight.docs};
-    auto unclean = [&](int32_t t) { return (last < p.Nk && t * BT + BT > last) || T.hole(t); };
+    // Blocks of queries dealt out as in the forward pass; with documents a CTA per block, whose bits are made below.
+    const int32_t heads = p.B * p.H, blocks = (p.Nq + BT - 1) / BT;
+    const uint32_t items = (uint32_t)heads * (uint32_t)blocks, rounds = (items - 1) / gridDim.x + 1;
+    auto item = [&](uint32_t round) { return round * gridDim.x + ((round & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x); };
+    struct block_of {
+        int32_t b, h, kvh, qb, i0, last;
+        grf_sight sight;
+        grad_tiles T;
+        __device__ __forceinline__ block_of(const grf_softmax_params& p, const uint32_t* bits, int32_t heads, int32_t blocks, uint32_t x)
+            : b((int32_t)(x % (uint32_t)heads) / p.H), h((int32_t)(x % (uint32_t)heads) % p.H), kvh(h / p.group), qb(blocks - 1 - (int32_t)(x / (uint32_t)heads)),
+              i0(qb * BT), sight(p, b)
+        {
+            const int32_t tiles = (sight.end(min(i0 + BT, p.Nq)) + BT - 1) / BT;
+            T = grad_tiles{bits, 0, tiles, (tiles + 31) / 32, sight.docs};
+            last = sight.end(p.Nq);
+        }
+        __device__ __forceinline__ bool unclean(const grf_softmax_params& p, int32_t t) const { return (last < p.Nk && t * BT + BT > last) || T.hole(t); }
+    };
 
     if (tid == 0) {
         abort_flag = 0;
@@ -131,19 +146,23 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             mbar_init(k_full(s), 1); mbar_init(v_full(s), 1); mbar_init(k_clean(s), 1);
             mbar_init(k_empty(s), 2); mbar_init(v_empty(s), 1);
         }
-        mbar_init(rows_full, 1); mbar_init(s_full0, 1); mbar_init(s_full0 + 8, 1); mbar_init(dp_full, 1); mbar_init(ds_full, WORKERS);
-        mbar_init(dq_done, 1); mbar_init(drain, 1); mbar_init(lut_full, WORKERS);
+        mbar_init(s_full0, 1); mbar_init(s_full0 + 8, 1); mbar_init(dp_full, 1); mbar_init(ds_full, WORKERS);
+        mbar_init(dq_done, 1); mbar_init(acc_read, WORKERS); mbar_init(drain, 1);
+        for (int y = 0; y < QB; ++y) { mbar_init(rows_full(y), 1); mbar_init(rows_empty(y), 1); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == COPY) tmem_alloc(&tmem_slot, 512u);
     if (LUTS) bucket.fill(p);
-    if (sight.docs) {
+    if (p.q_doc) {
+        const block_of I(p, bits, heads, blocks, blockIdx.x);
+        const grad_tiles& T = I.T;
+        const int32_t b = I.b, tiles = T.tiles, i1 = min(I.i0 + BT, p.Nq);
         const int32_t kblocks = (p.Nk + BT - 1) / BT, qblocks = (p.Nq + BT - 1) / BT;
-        const int4 qr = p.q_range[(int64_t)b * qblocks + qb];
+        const int4 qr = p.q_range[(int64_t)b * qblocks + I.qb];
         for (int32_t w = warp; w < T.words; w += THREADS / 32) {
             const int32_t t = w * 32 + lane;
             const int4 kr = t < tiles ? p.k_range[(int64_t)b * kblocks + t] : make_int4(INT32_MAX, -1, 0, 0);
-            const int what = t < tiles ? sight.tile(i0, i1, t * BT, t * BT + BT, qr, kr) : 0;
+            const int what = t < tiles ? I.sight.tile(I.i0, i1, t * BT, t * BT + BT, qr, kr) : 0;
             const uint32_t seen = __ballot_sync(0xffffffffu, what != 0), whole = __ballot_sync(0xffffffffu, what == 2), hole = __ballot_sync(0xffffffffu, kr.z != 0),
                            one_doc = __ballot_sync(0xffffffffu, one_document(qr, kr));
             if (lane == 0) { bits[w] = seen; bits[T.words + w] = whole; bits[2 * T.words + w] = hole; bits[3 * T.words + w] = one_doc; }
@@ -161,26 +180,34 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     if (warp >= WORKERS) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(LESS));
         if (warp == COPY) {
-            const int32_t qbt = p.qs[0] ? b : 0, qh = p.qs[1] ? h : 0, gb = p.dos[0] ? b : 0, gh = p.dos[1] ? h : 0;
-            const int32_t kb = p.ks[0] ? b : 0, kh = p.ks[1] ? kvh : 0, vb = p.vs[0] ? b : 0, vh = p.vs[1] ? kvh : 0;
             bool ok = true;
-            int32_t n = 0;
-            if (T.begin() < tiles) {
-                expect_tx_elected(rows_full, 2 * Sh::TILE);
-                for (int y = 0; y < DP / 64; ++y) {
-                    load_box(q_at + y * HALF, &map_q, 64 * y, i0, qh, qbt, rows_full);
-                    load_box(g_at + y * HALF, &map_g, 64 * y, i0, gh, gb, rows_full);
-                }
-            }
-            for (int32_t t = T.begin(); t < tiles && ok; t = T.next(t + 1), ++n) {
-                const int s = n % NS;
-                const uint32_t before = (uint32_t)(n / NS - 1) & 1u;
-                if (n >= NS && !(ok = wait(k_empty(s), before) && wait(v_empty(s), before))) break;
-                expect_tx_elected(k_full(s), Sh::TILE);
-                expect_tx_elected(v_full(s), Sh::TILE);
-                for (int y = 0; y < DP / 64; ++y) {
-                    load_box(k_at + s * Sh::TILE + y * HALF, &map_k, 64 * y, t * BT, kh, kb, k_full(s));
-                    load_box(v_at + s * Sh::TILE + y * HALF, &map_v, 64 * y, t * BT, vh, vb, v_full(s));
+            int32_t n = 0, kept = 0;
+            for (uint32_t round = 0; round < rounds && ok; ++round) {
+                const uint32_t which = item(round);
+                if (which >= items) break;
+                const block_of I(p, bits, heads, blocks, which);
+                const grad_tiles& T = I.T;
+                const int32_t kb = p.ks[0] ? I.b : 0, kh = p.ks[1] ? I.kvh : 0, vb = p.vs[0] ? I.b : 0, vh = p.vs[1] ? I.kvh : 0;
+                for (int32_t t = T.begin(); t < T.tiles && ok; t = T.next(t + 1), ++n) {
+                    const int s = n % NS;
+                    const uint32_t before = (uint32_t)(n / NS - 1) & 1u;
+                    if (n >= NS && !(ok = wait(k_empty(s), before) && wait(v_empty(s), before))) break;
+                    expect_tx_elected(k_full(s), Sh::TILE);
+                    expect_tx_elected(v_full(s), Sh::TILE);
+                    for (int y = 0; y < DP / 64; ++y) {
+                        load_box(k_at + s * Sh::TILE + y * HALF, &map_k, 64 * y, t * BT, kh, kb, k_full(s));
+                        load_box(v_at + s * Sh::TILE + y * HALF, &map_v, 64 * y, t * BT, vh, vb, v_full(s));
+                    }
+                    if (t == T.begin()) {
+                        const int y = kept % QB;
+                        if (kept >= QB && !(ok = wait(rows_empty(y), (uint32_t)(kept / QB - 1) & 1u))) { ++n; break; }
+                        expect_tx_elected(rows_full(y), 2 * Sh::TILE);
+                        for (int z = 0; z < DP / 64; ++z) {
+                            load_box(q_at + y * Sh::TILE + z * HALF, &map_q, 64 * z, I.i0, p.qs[1] ? I.h : 0, p.qs[0] ? I.b : 0, rows_full(y));
+                            load_box(g_at + y * Sh::TILE + z * HALF, &map_g, 64 * z, I.i0, p.dos[1] ? I.h : 0, p.dos[0] ? I.b : 0, rows_full(y));
+                        }
+                        ++kept;
+                    }
                 }
             }
             if (!ok || *(volatile int*)&abort_flag) {
@@ -188,74 +215,110 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     mbar_drain(k_full(x % NS), (uint32_t)(x / NS) & 1u, 20000000ll);
                     mbar_drain(v_full(x % NS), (uint32_t)(x / NS) & 1u, 20000000ll);
                 }
-                if (T.begin() < tiles) mbar_drain(rows_full, 0u, 20000000ll);
+                for (int32_t x = max(0, kept - QB); x < kept; ++x) mbar_drain(rows_full(x % QB), (uint32_t)(x / QB) & 1u, 20000000ll);
             }
         } else if (warp == ISSUE) {
             const int32_t steps = (p.d + 15) / 16;
             const uint64_t q_op = rows_operand(q_at), g_op = rows_operand(g_at), k_op = rows_operand(k_at), v_op = rows_operand(v_at), kc_op = columns_operand(k_at);
             uint32_t cleaned = 0u;
             bool ok = true;
-            auto make_scores = [&](int32_t n) {
-                const int s = n % NS;
-                if (!wait(k_full(s), (uint32_t)(n / NS) & 1u)) return false;
+            int32_t n = 0, kept = 0;                            // tiles, blocks that saw any
+            auto make_scores = [&](int32_t n_) {
+                const int s = n_ % NS;
+                if (!wait(k_full(s), (uint32_t)(n_ / NS) & 1u)) return false;
                 fence_after_sync();
-                product_over_columns<DP>(tmem + (n & 1) * BT, lo32(q_op), hi32(q_op), lo32(k_op) + s * (Sh::TILE / 16), hi32(k_op), steps);
-                mma_commit(s_full0 + 8 * (n & 1));
+                product_over_columns<DP>(tmem + (n_ & 1) * BT, lo32(q_op) + (kept % QB) * (Sh::TILE / 16), hi32(q_op), lo32(k_op) + s * (Sh::TILE / 16), hi32(k_op), steps);
+                mma_commit(s_full0 + 8 * (n_ & 1));
                 return true;
             };
-            auto make_dp = [&](int32_t n) {
-                const int s = n % NS;
-                if (!wait(v_full(s), (uint32_t)(n / NS) & 1u)) return false;
+            auto make_dp = [&](int32_t n_) {
+                const int s = n_ % NS;
+                if (!wait(v_full(s), (uint32_t)(n_ / NS) & 1u)) return false;
                 fence_after_sync();
-                product_over_columns<DP>(dp_col, lo32(g_op), hi32(g_op), lo32(v_op) + s * (Sh::TILE / 16), hi32(v_op), steps);
+                product_over_columns<DP>(dp_col, lo32(g_op) + (kept % QB) * (Sh::TILE / 16), hi32(g_op), lo32(v_op) + s * (Sh::TILE / 16), hi32(v_op), steps);
                 mma_commit(dp_full);
                 mma_commit(v_empty(s));
                 return true;
             };
-            int32_t t = T.begin(), n = 0;
-            if (t < tiles) ok = wait(rows_full, 0u) && make_scores(0) && make_dp(0);
-            for (; t < tiles && ok; ++n) {
-                const int s = n % NS;
-                const int32_t t_next = T.next(t + 1);
-                // (its place was read before the last tile's dS arrived)
-                if (t_next < tiles && !(ok = make_scores(n + 1))) break;
-                if (!(ok = wait(ds_full, (uint32_t)n & 1u))) break;
-                if (unclean(t)) {
-                    if (!(ok = wait(k_clean(s), cleaned >> s & 1u))) break;
-                    cleaned ^= 1u << s;
+            for (uint32_t round = 0; round < rounds && ok; ++round) {
+                const uint32_t which = item(round);
+                if (which >= items) break;
+                const block_of I(p, bits, heads, blocks, which);
+                const grad_tiles& T = I.T;
+                int32_t t = T.begin();
+                if (t >= T.tiles) continue;
+                bool first = true;
+                if (!(ok = wait(rows_full(kept % QB), (uint32_t)(kept / QB) & 1u) && make_scores(n) && make_dp(n))) break;
+                for (; t < T.tiles && ok; ++n) {
+                    const int s = n % NS;
+                    const int32_t t_next = T.next(t + 1);
+                    // (its place was read before the last tile's dS arrived)
+                    if (t_next < T.tiles && !(ok = make_scores(n + 1))) break;
+                    if (!(ok = wait(ds_full, (uint32_t)n & 1u))) break;
+                    if (I.unclean(p, t)) {
+                        if (!(ok = wait(k_clean(s), cleaned >> s & 1u))) break;
+                        cleaned ^= 1u << s;
+                    }
+                    // (the accumulator is the last block's until it is read)
+                    if (first && kept > 0 && !(ok = wait(acc_read, (uint32_t)(kept - 1) & 1u))) break;
+                    fence_after_sync();
+                    product_of_parts<DP>(acc, dp_col, lo32(kc_op) + s * (Sh::TILE / 16), hi32(kc_op), first ? 0u : 1u);
+                    first = false;
+                    mma_commit(k_empty(s));
+                    if (t_next >= T.tiles) {
+                        mma_commit(dq_done);
+                        mma_commit(rows_empty(kept % QB));
+                    } else ok = make_dp(n + 1);
+                    t = t_next;
                 }
-                fence_after_sync();
-                product_of_parts<DP>(acc, dp_col, lo32(kc_op) + s * (Sh::TILE / 16), hi32(kc_op), n > 0 ? 1u : 0u);
-                mma_commit(k_empty(s));
-                if (t_next >= tiles) mma_commit(dq_done);
-                else ok = make_dp(n + 1);
-                t = t_next;
+                ++kept;
             }
             if (!ok) {
                 mma_commit(drain);
                 mbar_drain(drain, 0u, 20000000ll);
             }
         } else if (warp == PREPARE) {
-            // rows of K that nobody sees, once S is made of them (before that, dQ's product alone reads them summed over rows)
+            // rows of K that nobody sees, once they have come (dQ's product sums over rows; of S they make columns that are not looked at)
             int32_t n = 0;
-            for (int32_t t = T.begin(); t < tiles; t = T.next(t + 1), ++n) {
-                const int s = n % NS;
-                if (!wait(k_full(s), (uint32_t)(n / NS) & 1u)) break;
-                if (unclean(t)) {
-                    for (int r = lane; r < BT; r += 32) {
-                        const int32_t j = t * BT + r;
-                        if (j < p.Nk && (j >= last || (sight.docs && p.k_doc[(int64_t)b * p.Nk + j] < 0))) clear_row(k_at + s * Sh::TILE, r, DP / 64);
+            bool ok = true;
+            for (uint32_t round = 0; round < rounds && ok; ++round) {
+                const uint32_t which = item(round);
+                if (which >= items) break;
+                const block_of I(p, bits, heads, blocks, which);
+                for (int32_t t = I.T.begin(); t < I.T.tiles; t = I.T.next(t + 1), ++n) {
+                    const int s = n % NS;
+                    if (!(ok = wait(k_full(s), (uint32_t)(n / NS) & 1u))) break;
+                    if (I.unclean(p, t)) {
+                        for (int r = lane; r < BT; r += 32) {
+                            const int32_t j = t * BT + r;
+                            if (j < p.Nk && (j >= I.last || (I.sight.docs && p.k_doc[(int64_t)I.b * p.Nk + j] < 0))) clear_row(k_at + s * Sh::TILE, r, DP / 64);
+                        }
+                        fence_async_smem();
+                        __syncwarp();
+                        arrive_elected(k_clean(s));
                     }
-                    fence_async_smem();
-                    __syncwarp();
-                    arrive_elected(k_clean(s));
+                    arrive_elected(k_empty(s));
                 }
-                arrive_elected(k_empty(s));
             }
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(MORE));
+        // After a wait that gave up (the abort flag is up, every later wait returns at once) they go on to the end, as the barriers between them
+        // count all of them.
         const int r = (warp & 3) * 32 + lane, part = warp >> 2, c0 = part * W;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const float to2 = p.scale * GRF_LOG2E, by_cap = CAP ? p.scale / p.cap : 0.0f, cap2 = p.cap * GRF_LOG2E;
+        const bool sums = LUTS && p.dtable_part != nullptr;
+        float* my_bins = bins + warp * 2 * GRF_MAX_BUCKETS;
+        auto with_workers = [&]() { asm volatile("bar.sync 1, 512;" ::: "memory"); };
+        int32_t n = 0, luts = 0, kept = 0;
+        for (uint32_t round = 0; round < rounds; ++round) {
+        const uint32_t which = item(round);
+        if (which >= items) break;
+        const block_of I(p, bits, heads, blocks, which);
+        const grad_tiles& T = I.T;
+        const grf_sight& sight = I.sight;
+        const int32_t b = I.b, h = I.h, i0 = I.i0, tiles = T.tiles;
         const int32_t i = i0 + r, pos = sight.position(i), pos0 = sight.position(i0);
         const int32_t limit = sight.order == GRF_ORDER_FULL ? sight.len : min(sight.len, max(pos + 1, sight.prefix));
         const int32_t all_see = sight.order == GRF_ORDER_FULL ? sight.len : min(sight.len, max(pos0 + 1, sight.prefix));       // keys before it: the whole block
@@ -266,11 +329,7 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         const bool any = !(fabsf(lse) > LARGEST);               // a row without a key, or one whose scores tell nothing any more: P = 0
         const bool empties = __any_sync(0xffffffffu, !any);
         const float minus_lse = any ? -lse * GRF_LOG2E : -CUDART_INF_F;
-        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const float to2 = p.scale * GRF_LOG2E, by_cap = CAP ? p.scale / p.cap : 0.0f, cap2 = p.cap * GRF_LOG2E;
         const float slope2 = BIAS == GRF_BIAS_SLOPES ? p.slopes[h] * GRF_LOG2E : 0.0f;
-        const bool sums = LUTS && p.dtable_part != nullptr;
-        float* my_bins = bins + warp * 2 * GRF_MAX_BUCKETS;
         float far_sum = 0.0f;                                   // of dS in tiles of one bucket, until the bucket changes
         int32_t far_bucket = -1;
         auto flush = [&]() {
@@ -281,8 +340,7 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             far_sum = 0.0f;
             __syncwarp();
         };
-        int32_t n = 0, luts = 0;
-        bool ok = true;
+        bool some = false;
         for (int32_t t = T.begin(); t < tiles; t = T.next(t + 1)) {
             const int32_t j0 = t * BT;
             const bool partial = sight.docs ? !T.whole(t) : j0 + BT > all_see;
@@ -304,12 +362,13 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     mine = at + (BT - 1 - r) + c0;
                 }
                 if (mixed && tid < BT) docs[tid] = j0 + tid < p.Nk ? p.k_doc[(int64_t)b * p.Nk + j0 + tid] : -1;
-                __syncwarp();
-                if (lane == 0) mbar_arrive(lut_full);
-                if (!(ok = wait(lut_full, (uint32_t)luts & 1u))) break;
+                with_workers();
                 ++luts;
             }
-            if (!(ok = wait(s_full0 + 8 * (n & 1), (uint32_t)(n >> 1) & 1u))) break;
+            // (branches that the compiler is to keep: without the barrier inside it runs a whole tile's masks under a predicate, a third of all instructions)
+            const bool careful = partial || empties;
+            const int32_t to = any ? limit - j0 - c0 : 0;
+            wait(s_full0 + 8 * (n & 1), (uint32_t)(n >> 1) & 1u);
             fence_after_sync();
             uint64_t x[W / 2], slope[CAP ? W / 2 : 1];          // P, then dS; t^2 - 1 of the cap
             {
@@ -336,11 +395,8 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     x[e / 2] = pack2(ex2(x0), ex2(x1));
                 }
             }
-            // (branches that the compiler is to keep: without the barrier inside it runs a whole tile's masks under a predicate, a third of all instructions)
-            const bool careful = partial || empties;
             if (careful) {
                 __syncwarp();
-                const int32_t to = any ? limit - j0 - c0 : 0;
                 if (mixed) {
                     __syncwarp();
 #pragma unroll
@@ -354,7 +410,7 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     for (int e = 0; e < W; e += 2) keep(x[e / 2], e < to, e + 1 < to);
                 }
             }
-            if (!(ok = wait(dp_full, (uint32_t)n & 1u))) break;
+            wait(dp_full, (uint32_t)n & 1u);
             fence_after_sync();
             {
                 uint32_t dv[W / 16][16];
@@ -382,6 +438,7 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             __syncwarp();
             if (lane == 0) mbar_arrive(ds_full);
             ++n;
+            some = true;
             if (sums) {
                 if (!diagonals) {
                     if (bucket0 != far_bucket) { flush(); far_bucket = bucket0; }
@@ -415,10 +472,9 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             }
         }
         if (sums) flush();
-        ok = __all_sync(0xffffffffu, ok) != 0;
-        if (ok && n > 0) ok = wait(dq_done, 0u);
+        if (some) wait(dq_done, (uint32_t)kept & 1u);
         fence_after_sync();
-        if (ok) {
+        {
             const float by = CAP ? -p.scale : p.scale;           // (slope of the cap with its sign turned)
             __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.dq) + b * p.dqs[0] + h * p.dqs[1] + (int64_t)i * p.dqs[2];
 #pragma unroll 1
@@ -427,7 +483,7 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 uint32_t o[16];
 #pragma unroll
                 for (int e = 0; e < 16; ++e) o[e] = 0u;
-                if (n > 0) tmem_ld16(acc + col + lanes, o);
+                if (some) tmem_ld16(acc + col + lanes, o);
                 if (i >= p.Nq) continue;
 #pragma unroll
                 for (int z = 0; z < 2; ++z) {
@@ -439,16 +495,30 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 }
             }
         }
+        if (some) {
+            fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(acc_read);
+            ++kept;
+        }
+        if (sums) {
+            with_workers();
+            if (tid < grf_softmax_columns(p)) {
+                float sum = 0.0f;
+                for (int w = 0; w < WORKERS; ++w) {
+                    sum += bins[w * 2 * GRF_MAX_BUCKETS + tid];
+                    bins[w * 2 * GRF_MAX_BUCKETS + tid] = 0.0f;
+                }
+                p.dtable_part[(((int64_t)b * p.H + h) * blocks + I.qb) * grf_softmax_columns(p) + tid] = sum;
+            }
+            with_workers();
+        }
+        }
         fence_before_sync();
     }
     fence_before_sync();
     __syncthreads();
     if (warp == COPY) tmem_dealloc(tmem, 512u);
-    if (LUTS && p.dtable_part && tid < grf_softmax_columns(p)) {
-        float sum = 0.0f;
-        for (int w = 0; w < WORKERS; ++w) sum += bins[w * 2 * GRF_MAX_BUCKETS + tid];
-        p.dtable_part[((int64_t)blockIdx.x * gridDim.y + qb) * grf_softmax_columns(p) + tid] = sum;
-    }
     if (tid == 0 && abort_flag) atomicExch(p.error_word, 1);
 }
 
@@ -458,11 +528,11 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                        const __grid_constant__ CUtensorMap map_g, const __grid_constant__ grf_softmax_params p, const head_split f)
 {
     using Sh = Grad<DP>;
-    constexpr int NS = Sh::NS;
+    constexpr int NS = Sh::NS, QB = Sh::QB;
     constexpr int LUTS = BIAS == GRF_BIAS_BUCKETS ? 1 : 0;
     constexpr int SUM_ROW = DP + 4;
     extern __shared__ unsigned char smem_dyn[];
-    __shared__ __align__(8) unsigned long long bars[4 * NS + 9];
+    __shared__ __align__(8) unsigned long long bars[4 * NS + 7 + 2 * QB];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
     __shared__ float lut[LUTS ? 2 * 256 : 1];
@@ -471,42 +541,76 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     __shared__ __align__(16) int32_t info_doc[NS][BT];
     const int tid = threadIdx.x, lane = tid & 31, warp = uniform(tid >> 5);
     const uint32_t smem = (smem_u32(smem_dyn) + 1023u) & ~1023u;
-    uint32_t* bits = reinterpret_cast<uint32_t*>(smem_dyn + (smem - smem_u32(smem_dyn)) + Sh::TILE * (2 + 2 * NS));
-    const uint32_t k_at = smem, v_at = k_at + Sh::TILE, q_at = v_at + Sh::TILE, g_at = q_at + NS * Sh::TILE, bar0 = smem_u32(bars);
+    uint32_t* bits = reinterpret_cast<uint32_t*>(smem_dyn + (smem - smem_u32(smem_dyn)) + Sh::TILE * (2 * QB + 2 * NS));
+    const uint32_t k_at = smem, v_at = k_at + QB * Sh::TILE, q_at = v_at + QB * Sh::TILE, g_at = q_at + NS * Sh::TILE, bar0 = smem_u32(bars);
     auto q_full = [&](int s) { return bar0 + 8u * s; };
     auto g_full = [&](int s) { return bar0 + 8u * (NS + s); };
     auto empty = [&](int s) { return bar0 + 8u * (2 * NS + s); };
     auto ready = [&](int s) { return bar0 + 8u * (3 * NS + s); };
     const uint32_t one = bar0 + 8u * (4 * NS);
-    const uint32_t keys_full = one, s_full = one + 8, dp_full = one + 16, p_full = one + 24, ds_full = one + 32, acc_done = one + 40, drain = one + 48,
-                   lut_full = one + 56;
-
-    // block x: part x % splits of the heads that share key head x / splits; the parts of one make a cluster
-    const int32_t unit = (int32_t)blockIdx.x / f.splits, rank_ = (int32_t)blockIdx.x % f.splits, b = unit / p.KV, kvh = unit % p.KV;
-    const int32_t h_first = kvh * p.group + p.group * rank_ / f.splits, h_end = kvh * p.group + p.group * (rank_ + 1) / f.splits;
+    const uint32_t s_full = one, dp_full = one + 8, p_full = one + 16, ds_full = one + 24, acc_done = one + 32, acc_read = one + 40, drain = one + 48;
+    auto keys_full = [&](int y) { return one + 56 + 8u * y; };
+    auto keys_empty = [&](int y) { return one + 56 + 8u * (QB + y); };
     float* sums = reinterpret_cast<float*>(smem_dyn + (smem - smem_u32(smem_dyn)));       // [dV, dK][key][SUM_ROW], once the tiles are done with
-    const grf_sight sight(p, b);
-    const int32_t j0 = (int32_t)blockIdx.y * BT, qblocks = (p.Nq + BT - 1) / BT;
-    // the first query that sees a key of the block, were there no documents
-    int32_t first = 0;
-    if (sight.order != GRF_ORDER_FULL && j0 >= sight.prefix) {
-        const int64_t x = (int64_t)j0 - sight.start;
-        first = x <= 0 ? 0 : x >= p.Nq ? qblocks : (int32_t)x / BT;
-    }
-    if (j0 >= sight.len) first = qblocks;
-    const grad_tiles T{bits, first, qblocks, (qblocks + 31) / 32, sight.docs};
+
+    // Blocks of keys, those that most queries see first, dealt out forwards and backwards in turn.  With documents, and where the heads that share keys
+    // are split over a cluster (CTA x: part x % splits of block x / splits), every CTA has one.
+    const int32_t units = p.B * p.KV, kblocks = (p.Nk + BT - 1) / BT, qblocks = (p.Nq + BT - 1) / BT;
+    const bool alone = f.splits > 1 || p.q_doc;
+    const uint32_t items = (uint32_t)units * (uint32_t)kblocks, rounds = alone ? 1u : (items - 1) / gridDim.x + 1;
+    auto item = [&](uint32_t round) {
+        return alone ? blockIdx.x / (uint32_t)f.splits : round * gridDim.x + ((round & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+    };
+    struct block_of {
+        int32_t b, kvh, kb, j0, h_first, h_end;
+        grf_sight sight;
+        grad_tiles T;
+        bool some;
+        __device__ __forceinline__ block_of(const grf_softmax_params& p, const uint32_t* bits, int32_t units, int32_t qblocks, int splits, uint32_t x)
+            : b((int32_t)(x % (uint32_t)units) / p.KV), kvh((int32_t)(x % (uint32_t)units) % p.KV), kb((int32_t)(x / (uint32_t)units)), j0(kb * BT), sight(p, b)
+        {
+            const int32_t part = (int32_t)blockIdx.x % splits;
+            h_first = kvh * p.group + p.group * part / splits;
+            h_end = kvh * p.group + p.group * (part + 1) / splits;
+            // the first query that sees a key of the block, were there no documents
+            int32_t first = 0;
+            if (sight.order != GRF_ORDER_FULL && j0 >= sight.prefix) {
+                const int64_t y = (int64_t)j0 - sight.start;
+                first = y <= 0 ? 0 : y >= p.Nq ? qblocks : (int32_t)y / BT;
+            }
+            if (j0 >= sight.len) first = qblocks;
+            T = grad_tiles{bits, first, qblocks, (qblocks + 31) / 32, sight.docs};
+        }
+        // (once the bits are there)
+        __device__ __forceinline__ void look() { some = T.begin() < T.tiles; }
+        // the block's tiles, head after head: true while there is one, with t and h advanced to it
+        __device__ __forceinline__ bool step(int32_t& t, int32_t& h) const
+        {
+            t = T.next(t + 1);
+            if (t >= T.tiles) {
+                if (++h >= h_end) return false;
+                t = T.begin();
+            }
+            return true;
+        }
+    };
 
     if (tid == 0) {
         abort_flag = 0;
         for (int s = 0; s < NS; ++s) { mbar_init(q_full(s), 1); mbar_init(g_full(s), 1); mbar_init(empty(s), 1); mbar_init(ready(s), 1); }
-        mbar_init(keys_full, 1); mbar_init(s_full, 1); mbar_init(dp_full, 1); mbar_init(p_full, WORKERS); mbar_init(ds_full, WORKERS);
-        mbar_init(acc_done, 1); mbar_init(drain, 1); mbar_init(lut_full, WORKERS);
+        for (int y = 0; y < QB; ++y) { mbar_init(keys_full(y), 1); mbar_init(keys_empty(y), 1); }
+        mbar_init(s_full, 1); mbar_init(dp_full, 1); mbar_init(p_full, WORKERS); mbar_init(ds_full, WORKERS);
+        mbar_init(acc_done, 1); mbar_init(acc_read, WORKERS); mbar_init(drain, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == COPY) tmem_alloc(&tmem_slot, 512u);
     if (LUTS) bucket.fill(p);
-    if (sight.docs) {
-        const int4 kr = p.k_range[(int64_t)b * gridDim.y + blockIdx.y];
+    if (p.q_doc) {
+        const block_of I(p, bits, units, qblocks, f.splits, item(0));
+        const grad_tiles& T = I.T;
+        const int32_t b = I.b, first = T.first, j0 = I.j0;
+        const grf_sight& sight = I.sight;
+        const int4 kr = p.k_range[(int64_t)b * kblocks + I.kb];
         for (int32_t w = warp; w < T.words; w += THREADS / 32) {
             const int32_t t = w * 32 + lane;
             const bool in = t >= first && t < qblocks;
@@ -522,152 +626,183 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     fence_after_sync();
     const uint32_t tmem = (uint32_t)uniform((int32_t)tmem_slot);
     const uint32_t s_col = tmem, dp_col = tmem + 128, dv_acc = tmem + 256, dk_acc = tmem + 256 + DP;
-    const bool some = T.begin() < qblocks;
     auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, &abort_flag)) != 0; };
-    // the block's tiles, head after head: true while there is one, with t and h advanced to it
-    auto step = [&](int32_t& t, int32_t& h) {
-        t = T.next(t + 1);
-        if (t >= qblocks) {
-            if (++h >= h_end) return false;
-            t = T.begin();
-        }
-        return true;
-    };
 
     if (warp >= WORKERS) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(LESS));
         if (warp == COPY) {
             bool ok = true;
-            int32_t n = 0;
-            if (some) {
-                expect_tx_elected(keys_full, 2 * Sh::TILE);
-                for (int y = 0; y < DP / 64; ++y) {
-                    load_box(k_at + y * HALF, &map_k, 64 * y, j0, p.ks[1] ? kvh : 0, p.ks[0] ? b : 0, keys_full);
-                    load_box(v_at + y * HALF, &map_v, 64 * y, j0, p.vs[1] ? kvh : 0, p.vs[0] ? b : 0, keys_full);
-                }
-                int32_t t = T.begin(), h = h_first;
+            int32_t n = 0, kept = 0;
+            for (uint32_t round = 0; round < rounds && ok; ++round) {
+                const uint32_t which = item(round);
+                if (which >= items) break;
+                block_of I(p, bits, units, qblocks, f.splits, which);
+                I.look();
+                if (!I.some) continue;
+                int32_t t = I.T.begin(), h = I.h_first;
+                bool first = true;
                 do {
                     const int s = n % NS;
                     if (n >= NS && !(ok = wait(empty(s), (uint32_t)(n / NS - 1) & 1u))) break;
                     expect_tx_elected(q_full(s), Sh::TILE);
                     expect_tx_elected(g_full(s), Sh::TILE);
                     for (int y = 0; y < DP / 64; ++y) {
-                        load_box(q_at + s * Sh::TILE + y * HALF, &map_q, 64 * y, t * BT, p.qs[1] ? h : 0, p.qs[0] ? b : 0, q_full(s));
-                        load_box(g_at + s * Sh::TILE + y * HALF, &map_g, 64 * y, t * BT, p.dos[1] ? h : 0, p.dos[0] ? b : 0, g_full(s));
+                        load_box(q_at + s * Sh::TILE + y * HALF, &map_q, 64 * y, t * BT, p.qs[1] ? h : 0, p.qs[0] ? I.b : 0, q_full(s));
+                        load_box(g_at + s * Sh::TILE + y * HALF, &map_g, 64 * y, t * BT, p.dos[1] ? h : 0, p.dos[0] ? I.b : 0, g_full(s));
                     }
                     ++n;
-                } while (step(t, h));
-                if (!ok || *(volatile int*)&abort_flag) {
-                    for (int32_t x = max(0, n - NS); x < n; ++x) {
-                        mbar_drain(q_full(x % NS), (uint32_t)(x / NS) & 1u, 20000000ll);
-                        mbar_drain(g_full(x % NS), (uint32_t)(x / NS) & 1u, 20000000ll);
+                    if (first) {
+                        first = false;
+                        const int y = kept % QB;
+                        if (kept >= QB && !(ok = wait(keys_empty(y), (uint32_t)(kept / QB - 1) & 1u))) break;
+                        expect_tx_elected(keys_full(y), 2 * Sh::TILE);
+                        for (int z = 0; z < DP / 64; ++z) {
+                            load_box(k_at + y * Sh::TILE + z * HALF, &map_k, 64 * z, I.j0, p.ks[1] ? I.kvh : 0, p.ks[0] ? I.b : 0, keys_full(y));
+                            load_box(v_at + y * Sh::TILE + z * HALF, &map_v, 64 * z, I.j0, p.vs[1] ? I.kvh : 0, p.vs[0] ? I.b : 0, keys_full(y));
+                        }
+                        ++kept;
                     }
-                    mbar_drain(keys_full, 0u, 20000000ll);
+                } while (I.step(t, h));
+            }
+            if (!ok || *(volatile int*)&abort_flag) {
+                for (int32_t x = max(0, n - NS); x < n; ++x) {
+                    mbar_drain(q_full(x % NS), (uint32_t)(x / NS) & 1u, 20000000ll);
+                    mbar_drain(g_full(x % NS), (uint32_t)(x / NS) & 1u, 20000000ll);
                 }
+                for (int32_t x = max(0, kept - QB); x < kept; ++x) mbar_drain(keys_full(x % QB), (uint32_t)(x / QB) & 1u, 20000000ll);
             }
         } else if (warp == ISSUE) {
             const int32_t steps = (p.d + 15) / 16;
             const uint64_t k_op = rows_operand(k_at), v_op = rows_operand(v_at), q_op = rows_operand(q_at), g_op = rows_operand(g_at), qc_op = columns_operand(q_at),
                            gc_op = columns_operand(g_at);
             bool ok = true;
-            auto make_scores = [&](int32_t n) {
-                const int s = n % NS;
-                if (!wait(ready(s), (uint32_t)(n / NS) & 1u)) return false;     // (behind both copies)
+            int32_t n = 0, kept = 0;                            // tiles, blocks that were seen
+            auto make_scores = [&](int32_t n_) {
+                const int s = n_ % NS;
+                if (!wait(ready(s), (uint32_t)(n_ / NS) & 1u)) return false;    // (behind both copies)
                 fence_after_sync();
-                product_over_columns<DP>(s_col, lo32(k_op), hi32(k_op), lo32(q_op) + s * (Sh::TILE / 16), hi32(q_op), steps);
+                product_over_columns<DP>(s_col, lo32(k_op) + (kept % QB) * (Sh::TILE / 16), hi32(k_op), lo32(q_op) + s * (Sh::TILE / 16), hi32(q_op), steps);
                 mma_commit(s_full);
                 return true;
             };
-            auto make_dp = [&](int32_t n) {
-                const int s = n % NS;
-                product_over_columns<DP>(dp_col, lo32(v_op), hi32(v_op), lo32(g_op) + s * (Sh::TILE / 16), hi32(g_op), steps);
+            auto make_dp = [&](int32_t n_) {
+                const int s = n_ % NS;
+                product_over_columns<DP>(dp_col, lo32(v_op) + (kept % QB) * (Sh::TILE / 16), hi32(v_op), lo32(g_op) + s * (Sh::TILE / 16), hi32(g_op), steps);
                 mma_commit(dp_full);
                 return true;
             };
-            if (some) {
-                int32_t t = T.begin(), h = h_first, n = 0;
-                ok = wait(keys_full, 0u) && make_scores(0) && make_dp(0);
-                bool more = true;
+            for (uint32_t round = 0; round < rounds && ok; ++round) {
+                const uint32_t which = item(round);
+                if (which >= items) break;
+                block_of I(p, bits, units, qblocks, f.splits, which);
+                I.look();
+                if (!I.some) continue;
+                int32_t t = I.T.begin(), h = I.h_first;
+                if (!(ok = wait(keys_full(kept % QB), (uint32_t)(kept / QB) & 1u) && make_scores(n) && make_dp(n))) break;
+                bool more = true, first = true;
                 for (; ok && more; ++n) {
                     const int s = n % NS;
-                    more = step(t, h);
+                    more = I.step(t, h);
                     if (!(ok = wait(p_full, (uint32_t)n & 1u))) break;
+                    // (the accumulators are the last block's until they are read)
+                    if (first && kept > 0 && !(ok = wait(acc_read, (uint32_t)(kept - 1) & 1u))) break;
                     fence_after_sync();
-                    product_of_parts<DP>(dv_acc, s_col, lo32(gc_op) + s * (Sh::TILE / 16), hi32(gc_op), n > 0 ? 1u : 0u);
+                    product_of_parts<DP>(dv_acc, s_col, lo32(gc_op) + s * (Sh::TILE / 16), hi32(gc_op), first ? 0u : 1u);
                     if (more && !(ok = make_scores(n + 1))) break;
                     if (!(ok = wait(ds_full, (uint32_t)n & 1u))) break;
                     fence_after_sync();
-                    product_of_parts<DP>(dk_acc, dp_col, lo32(qc_op) + s * (Sh::TILE / 16), hi32(qc_op), n > 0 ? 1u : 0u);
+                    product_of_parts<DP>(dk_acc, dp_col, lo32(qc_op) + s * (Sh::TILE / 16), hi32(qc_op), first ? 0u : 1u);
+                    first = false;
                     mma_commit(empty(s));
-                    if (!more) mma_commit(acc_done);
-                    else ok = make_dp(n + 1);
+                    if (!more) {
+                        mma_commit(acc_done);
+                        mma_commit(keys_empty(kept % QB));
+                    } else ok = make_dp(n + 1);
                 }
-                if (!ok) {
-                    mma_commit(drain);
-                    mbar_drain(drain, 0u, 20000000ll);
-                }
+                ++kept;
             }
-        } else if (warp == PREPARE && some) {
+            if (!ok) {
+                mma_commit(drain);
+                mbar_drain(drain, 0u, 20000000ll);
+            }
+        } else if (warp == PREPARE) {
             // (the next tile's values travel while this one's copies do; a place is free when its copies have come, as these waited for it)
-            int32_t t = T.begin(), h = h_first, n = 0;
-            float lse[4], d[4];
-            int32_t docs[4];
-            auto fetch = [&]() {
-                const int64_t row = ((int64_t)b * p.H + h) * p.Nq + t * BT;
+            int32_t n = 0;
+            bool ok = true;
+            for (uint32_t round = 0; round < rounds && ok; ++round) {
+                const uint32_t which = item(round);
+                if (which >= items) break;
+                block_of I(p, bits, units, qblocks, f.splits, which);
+                I.look();
+                if (!I.some) continue;
+                int32_t t = I.T.begin(), h = I.h_first;
+                float lse[4], d[4];
+                int32_t docs[4];
+                auto fetch = [&]() {
+                    const int64_t row = ((int64_t)I.b * p.H + h) * p.Nq + t * BT;
 #pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    const int r = lane + 32 * y;
-                    const bool in = t * BT + r < p.Nq;
-                    lse[y] = in ? p.lse[row + r] : -CUDART_INF_F;
-                    d[y] = in ? p.dsum[row + r] : 0.0f;
-                    docs[y] = in && sight.docs ? p.q_doc[(int64_t)b * p.Nq + t * BT + r] : -1;
-                }
-            };
-            fetch();
-            bool more = true;
-            while (more) {
-                const int s = n % NS;
-                if (!wait(q_full(s), (uint32_t)(n / NS) & 1u) || !wait(g_full(s), (uint32_t)(n / NS) & 1u)) break;
-                uint32_t none[4];
+                    for (int y = 0; y < 4; ++y) {
+                        const int r = lane + 32 * y;
+                        const bool in = t * BT + r < p.Nq;
+                        lse[y] = in ? p.lse[row + r] : -CUDART_INF_F;
+                        d[y] = in ? p.dsum[row + r] : 0.0f;
+                        docs[y] = in && I.sight.docs ? p.q_doc[(int64_t)I.b * p.Nq + t * BT + r] : -1;
+                    }
+                };
+                fetch();
+                bool more = true;
+                while (more) {
+                    const int s = n % NS;
+                    if (!(ok = wait(q_full(s), (uint32_t)(n / NS) & 1u) && wait(g_full(s), (uint32_t)(n / NS) & 1u))) break;
+                    uint32_t none[4];
 #pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    const int r = lane + 32 * y;
-                    const bool empty_row = fabsf(lse[y]) > LARGEST;
-                    none[y] = __ballot_sync(0xffffffffu, t * BT + r < p.Nq && empty_row);
-                    info[s][0][r] = empty_row ? -CUDART_INF_F : -lse[y] * GRF_LOG2E;
-                    info[s][1][r] = empty_row ? 0.0f : -d[y];
-                    if (sight.docs) info_doc[s][r] = docs[y];
-                }
-                if (none[0] | none[1] | none[2] | none[3]) {
-                    // what rows of queries that see nothing hold does not matter: cleared, as 0 times it is summed below
+                    for (int y = 0; y < 4; ++y) {
+                        const int r = lane + 32 * y;
+                        const bool empty_row = fabsf(lse[y]) > LARGEST;
+                        none[y] = __ballot_sync(0xffffffffu, t * BT + r < p.Nq && empty_row);
+                        info[s][0][r] = empty_row ? -CUDART_INF_F : -lse[y] * GRF_LOG2E;
+                        info[s][1][r] = empty_row ? 0.0f : -d[y];
+                        if (I.sight.docs) info_doc[s][r] = docs[y];
+                    }
+                    if (none[0] | none[1] | none[2] | none[3]) {
+                        // what rows of queries that see nothing hold does not matter: cleared, as 0 times it is summed below
 #pragma unroll
-                    for (int y = 0; y < 4; ++y)
-                        if (none[y] >> lane & 1u) {
-                            clear_row(q_at + s * Sh::TILE, lane + 32 * y, DP / 64);
-                            clear_row(g_at + s * Sh::TILE, lane + 32 * y, DP / 64);
-                        }
-                    fence_async_smem();
+                        for (int y = 0; y < 4; ++y)
+                            if (none[y] >> lane & 1u) {
+                                clear_row(q_at + s * Sh::TILE, lane + 32 * y, DP / 64);
+                                clear_row(g_at + s * Sh::TILE, lane + 32 * y, DP / 64);
+                            }
+                        fence_async_smem();
+                    }
+                    __syncwarp();
+                    arrive_elected(ready(s));
+                    ++n;
+                    more = I.step(t, h);
+                    if (more) fetch();
                 }
-                __syncwarp();
-                arrive_elected(ready(s));
-                ++n;
-                more = step(t, h);
-                if (more) fetch();
             }
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(MORE));
+        // (after a wait that gave up they go on, as in the other kernel)
         const int r = (warp & 3) * 32 + lane, part = warp >> 2, c0 = part * W;
-        const int32_t j = j0 + r;
-        int32_t doc = sight.docs && j < p.Nk ? p.k_doc[(int64_t)b * p.Nk + j] : -1;
-        if (doc < 0) doc = INT32_MIN;                           // (equal to no query's)
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const float to2 = p.scale * GRF_LOG2E, by_cap = CAP ? p.scale / p.cap : 0.0f, cap2 = p.cap * GRF_LOG2E;
+        auto with_workers = [&]() { asm volatile("bar.sync 1, 512;" ::: "memory"); };
+        int32_t n = 0, luts = 0, kept = 0;
+        for (uint32_t round = 0; round < rounds; ++round) {
+        const uint32_t which = item(round);
+        if (which >= items) break;
+        block_of I(p, bits, units, qblocks, f.splits, which);
+        I.look();
+        const grad_tiles& T = I.T;
+        const grf_sight& sight = I.sight;
+        const int32_t b = I.b, kvh = I.kvh, j0 = I.j0, j = j0 + r;
+        int32_t doc = sight.docs && j < p.Nk ? p.k_doc[(int64_t)b * p.Nk + j] : -1;
+        if (doc < 0) doc = INT32_MIN;                           // (equal to no query's)
         const bool block_partial = j0 + BT > sight.len, ordered = sight.order != GRF_ORDER_FULL && j0 + BT > sight.prefix;
-        int32_t n = 0, luts = 0;
-        bool ok = true;
-        if (some) {
-            int32_t t = T.begin(), h = h_first;
+        if (I.some) {
+            int32_t t = T.begin(), h = I.h_first;
             do {
                 const int s = n % NS;
                 const int32_t i0 = t * BT, pos0 = sight.position(i0);
@@ -684,13 +819,13 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                         float* at = lut + (luts & 1) * 256;
                         if (tid < 256) at[tid] = tid < 2 * BT - 1 ? grf_bias2<__nv_bfloat16>(p, bucket, h, j0 - pos0 + tid - (BT - 1)) : 0.0f;
                         mine = at + (BT - 1 + r - c0);          // column e: mine[-e]
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(lut_full);
-                        if (!(ok = wait(lut_full, (uint32_t)luts & 1u))) break;
+                        with_workers();
                         ++luts;
                     } else bias2 = grf_bias2<__nv_bfloat16>(p, bucket, h, j0 - pos0);
                 }
-                if (!(ok = wait(ready(s), (uint32_t)(n / NS) & 1u) && wait(s_full, (uint32_t)n & 1u))) break;
+                const int32_t since = from - c0;
+                wait(ready(s), (uint32_t)(n / NS) & 1u);
+                wait(s_full, (uint32_t)n & 1u);
                 fence_after_sync();
                 uint64_t x[W / 2], slope[CAP ? W / 2 : 1];      // P, then dS; t^2 - 1 of the cap
                 {
@@ -716,7 +851,6 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                 }
                 if (partial) {
                     __syncwarp();
-                    const int32_t since = from - c0;
                     if (T.mixed(t)) {
                         __syncwarp();
 #pragma unroll
@@ -744,7 +878,7 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                 fence_before_sync();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(p_full);
-                if (!(ok = wait(dp_full, (uint32_t)n & 1u))) break;
+                wait(dp_full, (uint32_t)n & 1u);
                 fence_after_sync();
                 {
                     uint32_t dv[W / 16][16];
@@ -772,10 +906,9 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                 __syncwarp();
                 if (lane == 0) mbar_arrive(ds_full);
                 ++n;
-            } while (step(t, h));
+            } while (I.step(t, h));
+            wait(acc_done, (uint32_t)kept & 1u);
         }
-        ok = __all_sync(0xffffffffu, ok) != 0;
-        if (ok && n > 0) ok = wait(acc_done, 0u);
         fence_after_sync();
         // the first two warpgroups have dV, half of its columns each, the others dK
         const bool is_dv = part < 2;
@@ -789,7 +922,7 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
             const int col = col0 + 16 * y;
 #pragma unroll
             for (int e = 0; e < 16; ++e) o[e] = 0u;
-            if (ok && n > 0) tmem_ld16((is_dv ? dv_acc : dk_acc) + col + lanes, o);
+            if (I.some) tmem_ld16((is_dv ? dv_acc : dk_acc) + col + lanes, o);
             if (f.splits > 1) {
                 // for the other CTAs of the cluster, where the tiles were
                 float4* at = reinterpret_cast<float4*>(sums + ((is_dv ? 0 : 1) * BT + r) * SUM_ROW + col);
@@ -798,7 +931,7 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                     at[e] = make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]), __uint_as_float(o[4 * e + 3]));
                 continue;
             }
-            if (!ok || j >= p.Nk) continue;
+            if (j >= p.Nk) continue;
 #pragma unroll
             for (int z = 0; z < 2; ++z) {
                 if (col + 8 * z >= p.d) continue;
@@ -808,6 +941,13 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                 *reinterpret_cast<uint4*>(dst + col + 8 * z) = make_uint4(w[0], w[1], w[2], w[3]);
             }
         }
+        if (I.some) {
+            fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(acc_read);
+            ++kept;
+        }
+        }
         fence_before_sync();
     }
     fence_before_sync();
@@ -815,6 +955,8 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     if (warp == COPY) tmem_dealloc(tmem, 512u);
     if (f.splits > 1) {
         // sums over the heads' CTAs, in order; every CTA has a share of the rows
+        const block_of I(p, bits, units, qblocks, f.splits, item(0));
+        const int32_t b = I.b, kvh = I.kvh, j0 = I.j0;
         cg::cluster_group cluster = cg::this_cluster();
         cluster.sync();
         constexpr int PIECES = DP / 8;
@@ -857,7 +999,8 @@ template <int DP, bool CAP, int BIAS> int launch(grf_ctx* ctx, const grf_softmax
     const int64_t blocks = (int64_t)p.B * p.KV * grf_ceil_div(p.Nk, BT);
     while (f.splits < p.group && f.splits < 8 && blocks * f.splits < 4 * ctx->sm_count) ++f.splits;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(p.B * p.KV * f.splits, grf_ceil_div(p.Nk, BT));
+    const int64_t q_blocks = (int64_t)p.B * p.H * grf_ceil_div(p.Nq, BT);
+    cfg.gridDim = dim3((unsigned)(f.splits > 1 || p.q_doc || blocks < ctx->sm_count ? blocks * f.splits : ctx->sm_count));
     cfg.blockDim = dim3(THREADS);
     cfg.dynamicSmemBytes = dkv_smem;
     cfg.stream = ctx->stream;
@@ -868,7 +1011,7 @@ template <int DP, bool CAP, int BIAS> int launch(grf_ctx* ctx, const grf_softmax
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
     GRF_CUDA_TRY(cudaLaunchKernelEx(&cfg, softmax_tc_dkv_kernel<DP, CAP, BIAS>, m.q, m.k, m.v, m.g, p, f));
-    softmax_tc_dq_kernel<DP, CAP, BIAS><<<dim3(p.B * p.H, grf_ceil_div(p.Nq, BT)), THREADS, dq_smem, ctx->stream>>>(m.q, m.k, m.v, m.g, p);
+    softmax_tc_dq_kernel<DP, CAP, BIAS><<<(unsigned)(p.q_doc || q_blocks < ctx->sm_count ? q_blocks : ctx->sm_count), THREADS, dq_smem, ctx->stream>>>(m.q, m.k, m.v, m.g, p);
     return cudaGetLastError() == cudaSuccess ? GRF_OK : GRF_ERR_CUDA;
 }
 
