@@ -285,8 +285,9 @@ int grf_masked_attn_mhat(grf_ctx* ctx, const grf_features* feat, int32_t G, int3
  * table, columns n_buckets .. 2 n_buckets - 1.  grf_relative_buckets makes the usual choice of first[].
  *
  * What a token that nobody sees holds (infinities, NaN) does not matter, and in grf_softmax_attn what a key that a query does not see
- * holds does not matter to that query.  An infinity or NaN in what it does see makes its results infinite or NaN; in a row of dout it
- * may reach all dim columns of the gradients that the row enters.
+ * holds does not matter to that query.  An infinity or NaN in what it does see makes its results infinite or NaN; in the backward pass
+ * such a value of a token that is seen may reach the gradients of every token of its sequence.
+ * Arrays that are written may overlap neither one another nor those that are read.
  */
 #define GRF_ORDER_FULL   0
 #define GRF_ORDER_CAUSAL 1
@@ -327,7 +328,8 @@ typedef struct grf_softmax_desc {
 int grf_relative_buckets(int32_t n_buckets, int32_t max_distance, int32_t* first);
 
 /* Bytes of DEVICE workspace that the call below needs for this descriptor (its pointers may still be NULL, except that it
- * matters which are): grf_softmax_attn (backward = 0) or grf_softmax_attn_backward (1).  May be 0; 0 also on invalid arguments. */
+ * matters which are) and the context's grf_ctx_use_tensor_cores: grf_softmax_attn (backward = 0) or grf_softmax_attn_backward (1).  May be 0; 0
+ * also on invalid arguments. */
 size_t grf_softmax_attn_workspace_bytes(const grf_ctx* ctx, const grf_softmax_desc* desc, int backward);
 
 /* Q, K, V, out: DEVICE, 16-byte aligned.  lse: optional DEVICE fp32 [batch][heads][n_q].  rest: optional, bf16 only: DEVICE [batch][heads]

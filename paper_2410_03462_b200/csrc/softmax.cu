@@ -4,6 +4,7 @@
 
 #include <nvtx3/nvToolsExt.h>
 
+#include "packed.cuh"
 #include "softmax.cuh"
 
 grf_softmax_scope::grf_softmax_scope(grf_ctx* ctx, const char* name, int launches)
@@ -160,7 +161,8 @@ int read_desc(grf_softmax_params* p, const grf_softmax_desc* s, bool backward)
     return GRF_OK;
 }
 
-bool by_few(const grf_softmax_params& p) { return p.Nq <= GRF_FEW_QUERIES; }
+// (bf16's few-query kernel multiplies on the tensor cores)
+bool by_few(const grf_ctx* ctx, const grf_softmax_params& p, int dtype) { return p.Nq <= GRF_FEW_QUERIES && (dtype == GRF_DTYPE_F32 || ctx->use_tensor_cores); }
 
 // Places inside the workspace.
 struct room {
@@ -196,7 +198,7 @@ struct doc_room {
 
 size_t forward_bytes(const grf_ctx* ctx, const grf_softmax_params& p, int dtype)
 {
-    if (by_few(p)) return grf_softmax_few_workspace(ctx, p, dtype);
+    if (by_few(ctx, p, dtype)) return grf_softmax_few_workspace(ctx, p, dtype);
     room r;
     doc_room docs(r, p);
     return r.bytes;
@@ -275,7 +277,7 @@ extern "C" int grf_softmax_attn(grf_ctx* ctx, const grf_softmax_desc* desc, cons
     GRF_CUDA_TRY(cudaSetDevice(ctx->device));
     p.q = Q; p.k = K; p.v = V; p.out_w = out; p.lse_w = lse; p.rest_w = (__nv_bfloat16*)rest;
     p.error_word = ctx->error_word;
-    if (by_few(p)) return grf_softmax_few(ctx, p, desc->dtype, workspace);
+    if (by_few(ctx, p, desc->dtype)) return grf_softmax_few(ctx, p, desc->dtype, workspace);
     room r;
     const doc_room docs(r, p);
     if (desc->dtype == GRF_DTYPE_BF16 && ctx->use_tensor_cores) {
@@ -444,7 +446,7 @@ __global__ void __launch_bounds__(BIAS_THREADS) relative_rows_kernel(const __gri
 template <typename T>
 __global__ void __launch_bounds__(BIAS_THREADS) relative_sums_kernel(const __grid_constant__ bias_shape s, int32_t batch, const T* __restrict__ drows, float* __restrict__ part)
 {
-    constexpr int CH = 16 / (int)sizeof(T), NEAR_AHEAD = 8, FAR_AHEAD = 4;
+    constexpr int CH = 16 / (int)sizeof(T), NEAR_AHEAD = 8, FAR_AHEAD = 2;
     extern __shared__ float bins[];                             // [column][thread]
     __shared__ unsigned char near[2 * BIAS_NEAR];
     const int32_t h = blockIdx.y, columns = s.columns(), tid = threadIdx.x, lane = tid & 31, F = s.first[s.n_first - 1];
@@ -452,46 +454,65 @@ __global__ void __launch_bounds__(BIAS_THREADS) relative_sums_kernel(const __gri
     for (int x = tid; x < columns * BIAS_THREADS; x += BIAS_THREADS) bins[x] = 0.0f;
     __syncthreads();
     float* mine = bins + tid;
-    float far[2] = {0.0f, 0.0f};
-    auto add = [&](int32_t delta, T v) { mine[column_at(s, F, near, delta) * BIAS_THREADS] += grf_to_float(v); };
-    const int64_t all = (int64_t)batch * s.n_q, step = (int64_t)s.strips * (BIAS_THREADS / 32);
-    for (int64_t x = (int64_t)blockIdx.x * (BIAS_THREADS / 32) + (tid >> 5); x < all; x += step) {
-        const int32_t b = all <= INT32_MAX ? (int32_t)((uint32_t)x / (uint32_t)s.n_q) : (int32_t)(x / s.n_q), i = (int32_t)(x - (int64_t)b * s.n_q);
+    uint64_t far[2] = {0ull, 0ull};                             // two sums each
+    auto add_piece = [&](uint64_t& sum, const uint4& u) {
+        if constexpr (sizeof(T) == 2) {
+            sum = add2(sum, pack2(u.x << 16, u.x & 0xffff0000u));
+            sum = add2(sum, pack2(u.y << 16, u.y & 0xffff0000u));
+            sum = add2(sum, pack2(u.z << 16, u.z & 0xffff0000u));
+            sum = add2(sum, pack2(u.w << 16, u.w & 0xffff0000u));
+        } else {
+            sum = add2(sum, pack2(u.x, u.y));
+            sum = add2(sum, pack2(u.z, u.w));
+        }
+    };
+    const int32_t step = s.strips * (BIAS_THREADS / 32);
+    int32_t b = 0, i = blockIdx.x * (BIAS_THREADS / 32) + (tid >> 5);
+    for (;; i += step) {
+        while (i >= s.n_q && b < batch) { i -= s.n_q; ++b; }
+        if (b >= batch) break;
         const T* row = drows + (((int64_t)b * s.heads + h) * s.n_q + i) * s.n_k;
         const bias_row r(s, F, i);
-        const stretch<T> before(row, 0, r.left), behind(row, r.right, s.n_k);
-        const int32_t pieces = before.count + behind.count;
-        auto piece_at = [&](int32_t y) { return reinterpret_cast<const uint4*>(row + (y < before.count ? before.first + y * CH : behind.first + (y - before.count) * CH)); };
+        const stretch<T> side[2] = {stretch<T>(row, 0, r.left), stretch<T>(row, r.right, s.n_k)};
         // everything of the row that fits is under way before the first of it is used
-        uint4 w[FAR_AHEAD];
-        T v[NEAR_AHEAD], e0 = grf_from_float<T>(0.0f), e1 = e0;
+        uint4 w[2][FAR_AHEAD];
+        T v[NEAR_AHEAD], e[2] = {grf_from_float<T>(0.0f), grf_from_float<T>(0.0f)};
 #pragma unroll
-        for (int y = 0; y < FAR_AHEAD; ++y) w[y] = lane + 32 * y < pieces ? __ldcs(piece_at(lane + 32 * y)) : make_uint4(0, 0, 0, 0);
+        for (int z = 0; z < 2; ++z) {
+            const uint4* at = reinterpret_cast<const uint4*>(row + side[z].first);
+#pragma unroll
+            for (int y = 0; y < FAR_AHEAD; ++y) w[z][y] = lane + 32 * y < side[z].count ? __ldcs(at + lane + 32 * y) : make_uint4(0, 0, 0, 0);
+            if (side[z].beside(lane) >= 0) e[z] = row[side[z].beside(lane)];
+        }
+        const int32_t count = r.right - r.left;
+        const T* middle = row + r.left;
+        const unsigned char* column = near + r.delta0 + r.left + F;     // of the middle's places, where they are looked up
 #pragma unroll
         for (int y = 0; y < NEAR_AHEAD; ++y)
-            if (r.left + 32 * y + lane < r.right) v[y] = row[r.left + 32 * y + lane];
-        if (before.beside(lane) >= 0) e0 = row[before.beside(lane)];
-        if (behind.beside(lane) >= 0) e1 = row[behind.beside(lane)];
-        auto add_piece = [&](int32_t y, const uint4& u) {
-            const T* t = reinterpret_cast<const T*>(&u);
-            float sum = 0.0f;
+            if (32 * y + lane < count) v[y] = middle[32 * y + lane];
 #pragma unroll
-            for (int e = 0; e < CH; ++e) sum += grf_to_float(t[e]);
-            far[0] += y < before.count ? sum : 0.0f;
-            far[1] += y < before.count ? 0.0f : sum;
+        for (int z = 0; z < 2; ++z) {
+            const uint4* at = reinterpret_cast<const uint4*>(row + side[z].first);
+#pragma unroll
+            for (int y = 0; y < FAR_AHEAD; ++y) add_piece(far[z], w[z][y]);
+            for (int32_t y = lane + 32 * FAR_AHEAD; y < side[z].count; y += 32) add_piece(far[z], __ldcs(at + y));
+            far[z] = add2(far[z], pack2(grf_to_float(e[z]), 0.0f));
+        }
+        auto add = [&](int32_t j, T x) {
+            const int32_t y = s.near ? column[j] : column_of(s, r.delta0 + r.left + j);
+            mine[y * BIAS_THREADS] += grf_to_float(x);
         };
 #pragma unroll
-        for (int y = 0; y < FAR_AHEAD; ++y) add_piece(lane + 32 * y, w[y]);
-        for (int32_t y = lane + 32 * FAR_AHEAD; y < pieces; y += 32) add_piece(y, __ldcs(piece_at(y)));
-        far[0] += grf_to_float(e0);
-        far[1] += grf_to_float(e1);
-#pragma unroll
         for (int y = 0; y < NEAR_AHEAD; ++y)
-            if (r.left + 32 * y + lane < r.right) add(r.delta0 + r.left + 32 * y + lane, v[y]);
-        for (int32_t j = r.left + 32 * NEAR_AHEAD + lane; j < r.right; j += 32) add(r.delta0 + j, row[j]);
+            if (32 * y + lane < count) add(32 * y + lane, v[y]);
+        for (int32_t j = 32 * NEAR_AHEAD + lane; j < count; j += 32) add(j, middle[j]);
     }
-    mine[(s.n_first - 1) * BIAS_THREADS] += far[0];
-    mine[(s.two_sided ? 2 * s.n_first - 1 : 0) * BIAS_THREADS] += far[1];
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+        float x0, x1;
+        unpack2(far[z], x0, x1);
+        mine[(z == 0 ? s.n_first - 1 : s.two_sided ? 2 * s.n_first - 1 : 0) * BIAS_THREADS] += x0 + x1;
+    }
     __syncthreads();
     const int warp = tid >> 5;
     for (int y = warp; y < columns; y += BIAS_THREADS / 32) {
