@@ -348,8 +348,7 @@ extern "C" int grf_softmax_attn_backward(grf_ctx* ctx, const grf_softmax_desc* d
 //
 // Both directions are bound by the matrix's bytes.  A warp takes a row at a time: beyond the distance F at which the last bucket starts there is
 // one value to either side, so only the places within F of the diagonal take a look-up (in shared memory, or a search where F >= BIAS_NEAR),
-// and the others are written, or added up, 16 bytes at a time.  Gradient: the two outer buckets in registers, the others in bins that every
-// thread has for itself in shared memory, so that nothing is atomic.
+// and the others are written, or added up, 16 bytes at a time.
 namespace {
 
 constexpr int BIAS_NEAR = 2048, BIAS_THREADS = 256;
@@ -399,7 +398,7 @@ template <typename T> struct stretch {
     int32_t from, to, first, count, last;
     __device__ __forceinline__ stretch(const T* row, int32_t from_, int32_t to_) : from(from_), to(max(from_, to_))
     {
-        const int32_t ahead = (int32_t)((CH - ((uintptr_t)(row + from) / sizeof(T)) % CH) % CH);
+        const int32_t ahead = (int32_t)((0u - (uint32_t)(uintptr_t)(row + from) / (uint32_t)sizeof(T)) & (uint32_t)(CH - 1));
         first = min(from + ahead, to);
         count = (to - first) / CH;
         last = first + count * CH;
@@ -443,17 +442,26 @@ __global__ void __launch_bounds__(BIAS_THREADS) relative_rows_kernel(const __gri
     }
 }
 
+// Every lane of a warp meets the same relative positions in every row: 1 - F + 32 y + lane, y < NEAR.  Their sums are registers; only where the band is
+// wider (F > 16 NEAR) are the others added into bins that every thread has for itself in shared memory.
+constexpr int NEAR = 8;
+
 template <typename T>
 __global__ void __launch_bounds__(BIAS_THREADS) relative_sums_kernel(const __grid_constant__ bias_shape s, int32_t batch, const T* __restrict__ drows, float* __restrict__ part)
 {
-    constexpr int CH = 16 / (int)sizeof(T), NEAR_AHEAD = 8, FAR_AHEAD = 2;
-    extern __shared__ float bins[];                             // [column][thread]
+    constexpr int CH = 16 / (int)sizeof(T), FAR_AHEAD = 2, WARPS = BIAS_THREADS / 32;
+    extern __shared__ float bins[];                             // [column][thread], where the band is wide
     __shared__ unsigned char near[2 * BIAS_NEAR];
-    const int32_t h = blockIdx.y, columns = s.columns(), tid = threadIdx.x, lane = tid & 31, F = s.first[s.n_first - 1];
+    __shared__ float diagonals[WARPS][32 * NEAR], outer[WARPS][2];
+    const int32_t h = blockIdx.y, columns = s.columns(), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, F = s.first[s.n_first - 1];
+    const bool wide = F > 16 * NEAR;
     load_near(s, F, near);
-    for (int x = tid; x < columns * BIAS_THREADS; x += BIAS_THREADS) bins[x] = 0.0f;
+    if (wide)
+        for (int x = tid; x < columns * BIAS_THREADS; x += BIAS_THREADS) bins[x] = 0.0f;
     __syncthreads();
-    float* mine = bins + tid;
+    float band[NEAR];
+#pragma unroll
+    for (int y = 0; y < NEAR; ++y) band[y] = 0.0f;
     uint64_t far[2] = {0ull, 0ull};                             // two sums each
     auto add_piece = [&](uint64_t& sum, const uint4& u) {
         if constexpr (sizeof(T) == 2) {
@@ -466,8 +474,8 @@ __global__ void __launch_bounds__(BIAS_THREADS) relative_sums_kernel(const __gri
             sum = add2(sum, pack2(u.z, u.w));
         }
     };
-    const int32_t step = s.strips * (BIAS_THREADS / 32);
-    int32_t b = 0, i = blockIdx.x * (BIAS_THREADS / 32) + (tid >> 5);
+    const int32_t step = s.strips * WARPS;
+    int32_t b = 0, i = blockIdx.x * WARPS + warp;
     for (;; i += step) {
         while (i >= s.n_q && b < batch) { i -= s.n_q; ++b; }
         if (b >= batch) break;
@@ -476,20 +484,18 @@ __global__ void __launch_bounds__(BIAS_THREADS) relative_sums_kernel(const __gri
         const stretch<T> side[2] = {stretch<T>(row, 0, r.left), stretch<T>(row, r.right, s.n_k)};
         // everything of the row that fits is under way before the first of it is used
         uint4 w[2][FAR_AHEAD];
-        T v[NEAR_AHEAD], e[2] = {grf_from_float<T>(0.0f), grf_from_float<T>(0.0f)};
+        T v[NEAR], e[2];
 #pragma unroll
         for (int z = 0; z < 2; ++z) {
             const uint4* at = reinterpret_cast<const uint4*>(row + side[z].first);
 #pragma unroll
             for (int y = 0; y < FAR_AHEAD; ++y) w[z][y] = lane + 32 * y < side[z].count ? __ldcs(at + lane + 32 * y) : make_uint4(0, 0, 0, 0);
-            if (side[z].beside(lane) >= 0) e[z] = row[side[z].beside(lane)];
+            const int32_t beside = side[z].beside(lane);
+            e[z] = beside >= 0 ? row[beside] : grf_from_float<T>(0.0f);
         }
-        const int32_t count = r.right - r.left;
-        const T* middle = row + r.left;
-        const unsigned char* column = near + r.delta0 + r.left + F;     // of the middle's places, where they are looked up
+        const int32_t j0 = 1 - F - r.delta0 + lane;             // may lie before the row
 #pragma unroll
-        for (int y = 0; y < NEAR_AHEAD; ++y)
-            if (32 * y + lane < count) v[y] = middle[32 * y + lane];
+        for (int y = 0; y < NEAR; ++y) v[y] = j0 + 32 * y >= r.left && j0 + 32 * y < r.right ? row[j0 + 32 * y] : grf_from_float<T>(0.0f);
 #pragma unroll
         for (int z = 0; z < 2; ++z) {
             const uint4* at = reinterpret_cast<const uint4*>(row + side[z].first);
@@ -498,30 +504,41 @@ __global__ void __launch_bounds__(BIAS_THREADS) relative_sums_kernel(const __gri
             for (int32_t y = lane + 32 * FAR_AHEAD; y < side[z].count; y += 32) add_piece(far[z], __ldcs(at + y));
             far[z] = add2(far[z], pack2(grf_to_float(e[z]), 0.0f));
         }
-        auto add = [&](int32_t j, T x) {
-            const int32_t y = s.near ? column[j] : column_of(s, r.delta0 + r.left + j);
-            mine[y * BIAS_THREADS] += grf_to_float(x);
-        };
 #pragma unroll
-        for (int y = 0; y < NEAR_AHEAD; ++y)
-            if (32 * y + lane < count) add(32 * y + lane, v[y]);
-        for (int32_t j = 32 * NEAR_AHEAD + lane; j < count; j += 32) add(j, middle[j]);
+        for (int y = 0; y < NEAR; ++y) band[y] += grf_to_float(v[y]);
+        if (wide)
+            for (int32_t j = j0 + 32 * NEAR; j < r.right; j += 32)
+                if (j >= r.left) bins[column_at(s, F, near, r.delta0 + j) * BIAS_THREADS + tid] += grf_to_float(row[j]);
     }
+#pragma unroll
+    for (int y = 0; y < NEAR; ++y) diagonals[warp][32 * y + lane] = band[y];
 #pragma unroll
     for (int z = 0; z < 2; ++z) {
         float x0, x1;
         unpack2(far[z], x0, x1);
-        mine[(z == 0 ? s.n_first - 1 : s.two_sided ? 2 * s.n_first - 1 : 0) * BIAS_THREADS] += x0 + x1;
+        x0 += x1;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) x0 += __shfl_xor_sync(0xffffffffu, x0, o);
+        if (lane == 0) outer[warp][z] = x0;
     }
     __syncthreads();
-    const int warp = tid >> 5;
-    for (int y = warp; y < columns; y += BIAS_THREADS / 32) {
-        float sum = 0.0f;
+    // one sum per diagonal, then per column, in order
+    float sum = 0.0f;
 #pragma unroll
-        for (int x = 0; x < BIAS_THREADS / 32; ++x) sum += bins[y * BIAS_THREADS + x * 32 + lane];
+    for (int x = 0; x < WARPS; ++x) sum += diagonals[x][tid];
+    __syncthreads();
+    diagonals[0][tid] = sum;
+    __syncthreads();
+    for (int y = warp; y < columns; y += WARPS) {
+        float total = 0.0f;
+        for (int x = lane; x < 32 * NEAR; x += 32)
+            if (x < 2 * F - 1 && column_at(s, F, near, 1 - F + x) == y) total += diagonals[0][x];
+        if (wide)
+            for (int x = lane; x < BIAS_THREADS; x += 32) total += bins[y * BIAS_THREADS + x];
+        if (lane < WARPS) total += (y == s.n_first - 1 ? outer[lane][0] : 0.0f) + (y == (s.two_sided ? 2 * s.n_first - 1 : 0) ? outer[lane][1] : 0.0f);
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        if (lane == 0) part[((int64_t)h * s.strips + blockIdx.x) * columns + y] = sum;
+        for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+        if (lane == 0) part[((int64_t)h * s.strips + blockIdx.x) * columns + y] = total;
     }
 }
 
@@ -542,11 +559,11 @@ int read_bias(bias_shape* s, int32_t heads, int32_t n_q, int32_t n_k, int32_t q_
 // CTAs of one head: enough to fill the device, of eight rows or more
 int32_t bias_strips(int32_t heads, int32_t n_q, int32_t most)
 {
-    const int32_t by_size = (n_q + 7) / 8, by_heads = (most + heads - 1) / heads;
+    const int32_t by_size = (n_q + 7) / 8, by_heads = most > heads ? most / heads : 1;     // (no more than are resident at once)
     return by_size < by_heads ? by_size : by_heads;
 }
 
-constexpr int32_t ROW_CTAS = 1184, SUM_CTAS = 444;
+constexpr int32_t ROW_CTAS = 1184, SUM_CTAS = 592;
 
 template <typename T> int bias_rows(grf_ctx* ctx, const bias_shape& s, const void* table, void* rows)
 {
@@ -556,7 +573,7 @@ template <typename T> int bias_rows(grf_ctx* ctx, const bias_shape& s, const voi
 }
 template <typename T> int bias_sums(grf_ctx* ctx, const bias_shape& s, int32_t batch, const void* drows, void* dtable, float* part)
 {
-    const size_t smem = sizeof(float) * (size_t)s.columns() * BIAS_THREADS;
+    const size_t smem = s.first[s.n_first - 1] > 16 * NEAR ? sizeof(float) * (size_t)s.columns() * BIAS_THREADS : 0;
     GRF_CUDA_TRY(cudaFuncSetAttribute(relative_sums_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     grf_softmax_scope scope(ctx, "grf:relative_sums", 2);
     relative_sums_kernel<T><<<dim3(s.strips, s.heads), BIAS_THREADS, smem, ctx->stream>>>(s, batch, (const T*)drows, part);

@@ -386,7 +386,7 @@ def test_bias_rows_and_table_gradient(lib, dtype, shape, two_sided, buckets):
     cols = len(first) * (2 if two_sided else 1)
     table = torch.randn(H, cols, generator=g).to(DT[dtype]).cuda()
     drows = torch.randn(B, H, nq, nk, generator=g).to(DT[dtype]).cuda()
-    for start in (None, 0, -100, 5000):
+    for start in (None, 0, -100, 5000, 2**31 - 1, -2**31):
         delta = np.arange(nk)[None, :] - (np.arange(nq)[:, None] + (nk - nq if start is None else start))
         b = R.bucket(first, delta, two_sided)
         rows = api.relative_bias(ctx, table, first, nq, nk, two_sided=two_sided, q_start=start)
