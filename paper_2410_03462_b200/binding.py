@@ -337,10 +337,14 @@ def grf_softmax_attn_backward(ctx, desc: SoftmaxDesc, Q, K, V, out, lse, rest, d
                                          workspace_bytes), "grf_softmax_attn_backward")
 
 
+def _distances(first):
+    """The smallest distance of each bucket as a C array."""
+    return (_i32 * len(first))(*(first if type(first) is list else [int(y) for y in first]))
+
+
 def grf_relative_bias(ctx, heads, n_q, n_k, q_start, first, two_sided, dtype, table, rows):
-    p, keep = _host(first, np.int32)
-    _check(lib.grf_relative_bias(ctx, heads, n_q, n_k, q_start, keep.shape[0], int(two_sided), p, dtype, _dev(table), _dev(rows)),
-           "grf_relative_bias")
+    _check(lib.grf_relative_bias(ctx, heads, n_q, n_k, q_start, len(first), int(two_sided), _distances(first), dtype, _dev(table),
+                                 _dev(rows)), "grf_relative_bias")
 
 
 def grf_relative_bias_workspace_bytes(heads, n_q, n_k, n_buckets, two_sided) -> int:
@@ -349,9 +353,8 @@ def grf_relative_bias_workspace_bytes(heads, n_q, n_k, n_buckets, two_sided) -> 
 
 def grf_relative_bias_backward(ctx, batch, heads, n_q, n_k, q_start, first, two_sided, dtype, drows, dtable, workspace,
                                workspace_bytes):
-    p, keep = _host(first, np.int32)
-    _check(lib.grf_relative_bias_backward(ctx, batch, heads, n_q, n_k, q_start, keep.shape[0], int(two_sided), p, dtype, _dev(drows),
-                                          _dev(dtable), _dev(workspace), workspace_bytes), "grf_relative_bias_backward")
+    _check(lib.grf_relative_bias_backward(ctx, batch, heads, n_q, n_k, q_start, len(first), int(two_sided), _distances(first), dtype,
+                                          _dev(drows), _dev(dtable), _dev(workspace), workspace_bytes), "grf_relative_bias_backward")
 
 
 def grf_step_host(ctx, N, rowptr, col, w, seed, n_walks, p_halt, max_len, f_phi, f_psi, G, m, d, dtype,
