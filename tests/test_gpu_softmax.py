@@ -108,6 +108,15 @@ def test_outputs_and_gradients(lib, route, shape, dtype, how):
     check(lib, *make(7, *shape, dtype, **how))
 
 
+@pytest.mark.parametrize("shape", [(40, 8, 4, 150, 170, 64), (21, 16, 2, 300, 129, 128), (100, 4, 4, 33, 257, 40)], ids=str)
+@pytest.mark.parametrize("how", [dict(), dict(mask="causal", ragged="empty", bias="table"), dict(mask="prefix", cap=10.0, start=True, bias="slopes"),
+                                 dict(mask="causal", docs="few", bias="table"), dict(start=True, ragged="empty", bias="table")],
+                         ids=lambda h: "-".join(map(str, h.values())) or "plain")
+def test_more_blocks_than_multiprocessors(lib, shape, how):
+    """CTAs that go from block to block, some of which see nothing."""
+    check(lib, *make(21, *shape, "bf16", **how))
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("docs", ["few", "many", "unsorted"])
 @pytest.mark.parametrize("mask", ["full", "causal", "prefix"])
