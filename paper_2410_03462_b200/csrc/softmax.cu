@@ -507,8 +507,8 @@ __global__ void __launch_bounds__(BIAS_THREADS) relative_sums_kernel(const __gri
 #pragma unroll
         for (int y = 0; y < NEAR; ++y) band[y] += grf_to_float(v[y]);
         if (wide)
-            for (int32_t j = j0 + 32 * NEAR; j < r.right; j += 32)
-                if (j >= r.left) bins[column_at(s, F, near, r.delta0 + j) * BIAS_THREADS + tid] += grf_to_float(row[j]);
+            for (int32_t j = max(j0 - lane + 32 * NEAR, r.left) + lane; j < r.right; j += 32)
+                bins[column_at(s, F, near, r.delta0 + j) * BIAS_THREADS + tid] += grf_to_float(row[j]);
     }
 #pragma unroll
     for (int y = 0; y < NEAR; ++y) diagonals[warp][32 * y + lane] = band[y];

@@ -408,6 +408,29 @@ def test_bias_rows_and_table_gradient(lib, dtype, shape, two_sided, buckets):
         R.assert_close(got, want, (B * nq * nk / 256 + 32) * R.U * size + R.HALF_STEP[DT[dtype]] * np.abs(want) + 1e-30, "dtable")
 
 
+@pytest.mark.parametrize("two_sided", [False, True])
+@pytest.mark.parametrize("last", [300, 5000, 1 << 29])
+def test_table_gradient_with_buckets_far_beyond_the_tokens(lib, last, two_sided):
+    """Right, and in a time that goes with the matrix, not with the distances of buckets that it does not reach."""
+    api, _, ctx = lib
+    H, nq, nk, first = 2, 300, 900, [0, 3, 200, last]
+    cols = len(first) * (2 if two_sided else 1)
+    drows = torch.randn(1, H, nq, nk, generator=torch.Generator().manual_seed(3)).cuda()
+    x = drows.double().cpu().numpy()
+    for start in (None, 0, last):
+        b = R.bucket(np.array(first), np.arange(nk)[None, :] - (np.arange(nq)[:, None] + (nk - nq if start is None else start)), two_sided)
+        for _ in range(3):
+            at = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+            at[0].record()
+            got = api.relative_bias_backward(ctx, drows, first, two_sided=two_sided, q_start=start)
+            at[1].record()
+            torch.cuda.synchronize()
+        assert at[0].elapsed_time(at[1]) < 10.0
+        sums = lambda y: np.stack([np.bincount(b.ravel(), y[:, h].sum(0).ravel(), cols) for h in range(H)])  # noqa: E731
+        want, size = sums(x), sums(np.abs(x))
+        R.assert_close(got, want, (nq * nk / 256 + 32) * R.U * size + R.HALF_STEP[torch.float32] * np.abs(want) + 1e-30, "dtable")
+
+
 def test_refusals_leave_outputs_alone(lib):
     api, B, ctx = lib
     x, how, dout = make(43, 1, 2, 1, 20, 20, 32, "bf16")
