@@ -639,8 +639,10 @@ template <int DP, bool CAP, int BIAS, bool EXACT> int launch(grf_ctx* ctx, const
 {
     using Sh = Fwd<DP, EXACT>;
     const auto kernel = softmax_tc_forward_kernel<DP, CAP, BIAS, EXACT>;
-    const size_t smem = Sh::SMEM + (p.q_doc ? 4 * (size_t)(3 * QT + 2) * (grf_ceil_div(p.Nk, BT) / 32 + 1) : 0);
-    GRF_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    auto bits = [](int32_t tokens) { return 4 * (size_t)(3 * QT + 2) * (grf_ceil_div(tokens, BT) / 32 + 1); };
+    const size_t smem = Sh::SMEM + (p.q_doc ? bits(p.Nk) : 0);
+    // (the most of any call: the attribute is the whole process's, and another thread may set it between here and the launch)
+    GRF_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(Sh::SMEM + bits(MOST_WITH_DOCS))));
     grf_softmax_scope scope(ctx, "grf:softmax_attention");
     // as many CTAs as the device holds at once, which take block after block; with documents a CTA per block
     const int64_t items = (int64_t)p.B * p.H * grf_ceil_div(p.Nq, QT * BT), room = ctx->sm_count;
@@ -668,7 +670,7 @@ template <int DP> int by_rest(grf_ctx* ctx, const grf_softmax_params& p, const f
 
 int grf_softmax_tc_forward(grf_ctx* ctx, const grf_softmax_params& p)
 {
-    if (p.q_doc && p.Nk > (1 << 20)) return 1;                  // the tiles' bits: 8 KB there, more do not fit beside d = 128
+    if (p.q_doc && p.Nk > MOST_WITH_DOCS) return 1;
     forward_maps m;
     if (!grf_make_token_box_map(&m.q, p.q, p.qs, p.B, p.H, p.Nq, p.d) || !grf_make_token_box_map(&m.k, p.k, p.ks, p.B, p.KV, p.Nk, p.d) ||
         !grf_make_token_box_map(&m.v, p.v, p.vs, p.B, p.KV, p.Nk, p.d)) return 1;

@@ -9,6 +9,7 @@ namespace grf_softmax_tc {
 using namespace grf_tc;
 
 constexpr int BT = 128;                 // queries, and keys, of a tile
+constexpr int32_t MOST_WITH_DOCS = 1 << 20;     // tokens, with documents: the tiles' bits of more do not fit beside d = 128
 constexpr uint32_t HALF = BT * 128;     // bytes of 64 columns of a tile: rows of 128 bytes, swizzled over a row
 
 // A box of 64 columns and BT rows of (columns, tokens, heads, sequences), by one elected lane of a converged warp.

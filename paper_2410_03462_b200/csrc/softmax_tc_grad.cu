@@ -988,11 +988,12 @@ struct grad_maps { CUtensorMap q, k, v, g; };
 template <int DP, bool CAP, int BIAS> int launch(grf_ctx* ctx, const grf_softmax_params& p, const grad_maps& m)
 {
     using Sh = Grad<DP>;
-    constexpr int NS = Sh::NS;
-    auto bits = [&](int32_t tokens) { return p.q_doc ? 16 * (size_t)(grf_ceil_div(tokens, BT) / 32 + 1) : 0; };
-    const size_t dq_smem = Sh::SMEM + bits(p.Nk), dkv_smem = Sh::SMEM + bits(p.Nq);
-    GRF_CUDA_TRY(cudaFuncSetAttribute(softmax_tc_dq_kernel<DP, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)dq_smem));
-    GRF_CUDA_TRY(cudaFuncSetAttribute(softmax_tc_dkv_kernel<DP, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)dkv_smem));
+    auto bits = [](int32_t tokens) { return 16 * (size_t)(grf_ceil_div(tokens, BT) / 32 + 1); };
+    const size_t dq_smem = Sh::SMEM + (p.q_doc ? bits(p.Nk) : 0), dkv_smem = Sh::SMEM + (p.q_doc ? bits(p.Nq) : 0);
+    // (the most of any call, as in the forward pass)
+    constexpr auto most = cudaFuncAttributeMaxDynamicSharedMemorySize;
+    GRF_CUDA_TRY(cudaFuncSetAttribute(softmax_tc_dq_kernel<DP, CAP, BIAS>, most, (int)(Sh::SMEM + bits(MOST_WITH_DOCS))));
+    GRF_CUDA_TRY(cudaFuncSetAttribute(softmax_tc_dkv_kernel<DP, CAP, BIAS>, most, (int)(Sh::SMEM + bits(MOST_WITH_DOCS))));
     grf_softmax_scope scope(ctx, "grf:softmax_gradients", 2);
     // The heads that share a key head are split over a cluster's CTAs, which add their sums through distributed shared memory, where there are
     // too few blocks of keys to fill the device evenly (causal ones take 1 to Nq / 128 tiles a head).  16 heads, 4 of keys,
@@ -1033,7 +1034,7 @@ template <int DP> int choose(grf_ctx* ctx, const grf_softmax_params& p, const gr
 
 int grf_softmax_tc_backward(grf_ctx* ctx, const grf_softmax_params& p)
 {
-    if (p.q_doc && (p.Nk > (1 << 20) || p.Nq > (1 << 20))) return 1;       // the tiles' bits
+    if (p.q_doc && (p.Nk > MOST_WITH_DOCS || p.Nq > MOST_WITH_DOCS)) return 1;
     grad_maps m;
     if (!grf_make_token_box_map(&m.q, p.q, p.qs, p.B, p.H, p.Nq, p.d) || !grf_make_token_box_map(&m.k, p.k, p.ks, p.B, p.KV, p.Nk, p.d) ||
         !grf_make_token_box_map(&m.v, p.v, p.vs, p.B, p.KV, p.Nk, p.d) || !grf_make_token_box_map(&m.g, p.dout, p.dos, p.B, p.H, p.Nq, p.d)) return 1;

@@ -384,6 +384,44 @@ def test_streams_and_captured_calls(lib):
         c.close()
 
 
+def test_threads_with_contexts_of_their_own(lib):
+    """Calls of the same kernels with and without what takes more shared memory, from two threads at once."""
+    import threading
+    api, B, ctx = lib
+    sides = []
+    for seed, docs, last in ((1, "few", 64), (2, None, 5000)):
+        x, how, dout = make(seed, 1, 2, 2, 130, 130, 64, "bf16", mask="causal", bias="table", docs=docs)
+        first = api.relative_buckets(32, last)
+        drows = torch.randn(1, 2, 130, 130, device="cuda")
+
+        def run(c, x=x, how=how, dout=dout, first=first, drows=drows):
+            o = api.softmax_attn(c, x["q"], x["k"], x["v"], want_lse=True, **how)
+            return (o[0], *o[1], *api.softmax_attn_backward(c, x["q"], x["k"], x["v"], *o, dout, **how), api.relative_bias_backward(c, drows, first))
+        sides.append((run, run(ctx)))
+    torch.cuda.synchronize()
+    failures = []
+
+    def work(run, want):
+        try:
+            stream = torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                c = api.Context(0)
+                for _ in range(300):
+                    got = run(c)
+                stream.synchronize()
+                assert all(torch.equal(s, t) for s, t in zip(got, want))
+                stream.synchronize()
+                c.close()
+        except Exception as e:  # noqa: BLE001
+            failures.append(e)
+    threads = [threading.Thread(target=work, args=side) for side in sides]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failures, failures
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("shape", [(1, 1, 1, 1), (1, 3, 7, 9), (2, 5, 77, 130), (3, 2, 200, 1), (1, 4, 513, 515), (2, 1, 33, 3000)], ids=str)
 @pytest.mark.parametrize("two_sided,buckets", [(False, (32, 128)), (True, (32, 128)), (True, (64, 5000)), (False, (2, 2))])
