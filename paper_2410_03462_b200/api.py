@@ -210,8 +210,15 @@ def _softmax_desc(ctx, q, k, v, scale, cap, mask, k_len, q_start, prefix, q_doc,
     return s
 
 
-def _scratch(nbytes, device):
-    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+def _scratch(nbytes, ctx):
+    """A workspace for one call.  It belongs to the context's stream, so that its memory goes to nobody else while the call runs, whichever
+    stream is the current one."""
+    if not nbytes:
+        return None
+    if torch.cuda.current_stream(ctx.device) == ctx.stream:
+        return torch.empty(nbytes, dtype=torch.uint8, device=ctx.torch_device)
+    with torch.cuda.stream(ctx.stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device=ctx.torch_device)
 
 
 def softmax_attn(ctx: Context, q, k, v, scale=None, cap=0.0, mask="full", k_len=None, q_start=None, prefix=None, q_doc=None,
@@ -230,7 +237,7 @@ def softmax_attn(ctx: Context, q, k, v, scale=None, cap=0.0, mask="full", k_len=
         s.out_stride = _stride3(out, "out")
     lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device) if want_lse else None
     if workspace is None:
-        workspace = _scratch(B.grf_softmax_attn_workspace_bytes(ctx.handle, s, False), q.device)
+        workspace = _scratch(B.grf_softmax_attn_workspace_bytes(ctx.handle, s, False), ctx)
     rest = torch.empty(q.shape, dtype=q.dtype, device=q.device) if want_lse and q.dtype == torch.bfloat16 else None
     B.grf_softmax_attn(ctx.handle, s, q, k, v, out, lse, rest, workspace, workspace.numel() if workspace is not None else 0)
     return (out, SoftmaxSaved(lse, rest)) if want_lse else out
@@ -254,7 +261,7 @@ def softmax_attn_backward(ctx: Context, q, k, v, out, saved, dout, scale=None, c
     dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
     dtable = torch.empty_like(table) if table is not None and want_dtable else None
     if workspace is None:
-        workspace = _scratch(B.grf_softmax_attn_workspace_bytes(ctx.handle, s, True), q.device)
+        workspace = _scratch(B.grf_softmax_attn_workspace_bytes(ctx.handle, s, True), ctx)
     B.grf_softmax_attn_backward(ctx.handle, s, q, k, v, out, lse, rest, dout, dq, dk, dv, dtable, workspace, workspace.numel())
     return dq, dk, dv, dtable
 
@@ -278,7 +285,7 @@ def relative_bias_backward(ctx: Context, drows, first, two_sided=False, q_start=
     batch, heads, n_q, n_k = drows.shape
     dtable = torch.empty((heads, len(first) * (2 if two_sided else 1)), dtype=drows.dtype, device=drows.device)
     if workspace is None:
-        workspace = _scratch(B.grf_relative_bias_workspace_bytes(heads, n_q, n_k, len(first), two_sided), drows.device)
+        workspace = _scratch(B.grf_relative_bias_workspace_bytes(heads, n_q, n_k, len(first), two_sided), ctx)
     B.grf_relative_bias_backward(ctx.handle, batch, heads, n_q, n_k, n_k - n_q if q_start is None else q_start, first, two_sided,
                                  B.dtype_code(drows), drows, dtable, workspace, workspace.numel())
     return dtable

@@ -384,6 +384,28 @@ def test_streams_and_captured_calls(lib):
         c.close()
 
 
+def test_workspace_of_a_call_on_a_stream_that_is_not_current(lib, monkeypatch):
+    """Memory of a call's workspace is not handed out on the current stream while the call may still run on the context's."""
+    api, B, ctx = lib
+    x, how, dout = make(8, 2, 2, 2, 300, 300, 64, "bf16", docs="few", bias="table")
+    drows = torch.randn(2, 2, 300, 300, device="cuda")
+    places = []
+    for name, at in (("grf_softmax_attn", -2), ("grf_softmax_attn_backward", -2), ("grf_relative_bias_backward", -2)):
+        call = getattr(B, name)
+        monkeypatch.setattr(B, name, lambda *a, call=call, at=at: (places.append((a[at].data_ptr(), a[at].numel())), call(*a)))
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        o = api.softmax_attn(ctx, x["q"], x["k"], x["v"], want_lse=True, **how)
+        taken = [torch.empty(places[-1][1], dtype=torch.uint8, device="cuda")]
+        api.softmax_attn_backward(ctx, x["q"], x["k"], x["v"], *o, dout, **how)
+        taken.append(torch.empty(places[-1][1], dtype=torch.uint8, device="cuda"))
+        api.relative_bias_backward(ctx, drows, how["first"])
+        taken.append(torch.empty(places[-1][1], dtype=torch.uint8, device="cuda"))
+    torch.cuda.synchronize()
+    assert len(places) == 3 and all(n > 0 for _, n in places)
+    assert not {p for p, _ in places} & {t.data_ptr() for t in taken}
+
+
 def test_threads_with_contexts_of_their_own(lib):
     """Calls of the same kernels with and without what takes more shared memory, from two threads at once."""
     import threading
