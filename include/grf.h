@@ -335,7 +335,7 @@ size_t grf_softmax_attn_workspace_bytes(const grf_ctx* ctx, const grf_softmax_de
 /* Q, K, V, out: DEVICE, 16-byte aligned.  lse: optional DEVICE fp32 [batch][heads][n_q].  rest: optional, bf16 only: DEVICE [batch][heads]
  * [n_q][dim] contiguous, 16-byte aligned, receives what rounding to bf16 took from out (rounded to bf16 itself): the backward pass uses it
  * so that D_i, a difference of nearly equal terms where a row looks at few keys, does not inherit that rounding; with rest, out itself comes
- * from probabilities held to 2^-16 (and may differ in its last bit from a call without).  workspace: DEVICE, 256-byte aligned (may be
+ * from probabilities held to 2^-16 where n_q > 16 (and may differ in its last bit from a call without).  workspace: DEVICE, 256-byte aligned (may be
  * NULL where 0 bytes are needed); its contents are scratch of this call alone, so calls that may run at the same time, captured ones
  * among them, need one each.  Few queries (n_q <= 16) are served by kernels that split the keys.  bf16 products have their probabilities
  * rounded to bf16 (by at most 2^-8 relative each), sums are fp32; summation order is fixed.  Asynchronous; can be captured.

@@ -135,6 +135,7 @@ def masked_attn_mhat(ctx: Context, feat: Features, phiQ, phiK, V, want_den=False
     return (out, den) if want_den else out
 
 
+INT32_MAX = 2**31 - 1
 ORDERS = {"full": B.GRF_ORDER_FULL, "causal": B.GRF_ORDER_CAUSAL, "prefix": B.GRF_ORDER_PREFIX}
 
 
@@ -175,6 +176,8 @@ def _softmax_desc(ctx, q, k, v, scale, cap, mask, k_len, q_start, prefix, q_doc,
         raise ValueError("expected q [B, H, Nq, d] and k, v [B, KV, Nk, d]")
     batch, heads, n_q, dim = q_shape
     kv_heads, n_k = k_shape[1], k_shape[2]
+    if n_q > INT32_MAX or n_k > INT32_MAX:
+        raise ValueError("too many tokens")
     dtype, device = q.dtype, ctx.torch_device
     if k_shape[0] != batch or k_shape[3] != dim or k.dtype != dtype or v.dtype != dtype:
         raise ValueError("q, k and v disagree in batch, dim or type")
@@ -206,7 +209,7 @@ def _softmax_desc(ctx, q, k, v, scale, cap, mask, k_len, q_start, prefix, q_doc,
         if table.dtype != dtype or table.device != device or tuple(table.shape) != shape or not table.is_contiguous():
             raise ValueError(f"table: expected a contiguous {dtype} tensor {shape} on {device}")
         s.bias, s.table, s.n_buckets, s.two_sided = B.GRF_BIAS_BUCKETS, table.data_ptr(), n, int(two_sided)
-        s.first[:n] = first if type(first) is list else [int(y) for y in first]
+        s.first[:n] = B._distances(first)
     return s
 
 
@@ -266,15 +269,25 @@ def softmax_attn_backward(ctx: Context, q, k, v, out, saved, dout, scale=None, c
     return dq, dk, dv, dtable
 
 
+def _first_position(ctx, t, n_q, n_k, q_start):
+    """Where the queries begin; checked, with the device of t."""
+    if not t.is_cuda or t.get_device() != ctx.device:
+        raise ValueError(f"expected a tensor on {ctx.torch_device}")
+    start = n_k - n_q if q_start is None else q_start
+    if n_q > INT32_MAX or n_k > INT32_MAX or not -INT32_MAX - 1 <= start <= INT32_MAX:
+        raise ValueError("n_q, n_k and q_start: expected 32-bit integers")
+    return start
+
+
 def relative_bias(ctx: Context, table, first, n_q, n_k, two_sided=False, q_start=None):
     """Rows [H, n_q, n_k] of the learned relative position bias table [H, len(first)] (twice as many columns when two_sided); the
     queries are the last of the n_k tokens unless q_start says where they begin."""
     heads = table.shape[0]
     if tuple(table.shape) != (heads, len(first) * (2 if two_sided else 1)):
         raise ValueError("table: expected one column per bucket and side")
+    start = _first_position(ctx, table, n_q, n_k, q_start)
     rows = torch.empty((heads, n_q, n_k), dtype=table.dtype, device=table.device)
-    B.grf_relative_bias(ctx.handle, heads, n_q, n_k, n_k - n_q if q_start is None else q_start, first, two_sided,
-                        B.dtype_code(table), table, rows)
+    B.grf_relative_bias(ctx.handle, heads, n_q, n_k, start, first, two_sided, B.dtype_code(table), table, rows)
     return rows
 
 
@@ -283,9 +296,10 @@ def relative_bias_backward(ctx: Context, drows, first, two_sided=False, q_start=
     if drows.dim() == 3:
         drows = drows[None]
     batch, heads, n_q, n_k = drows.shape
+    start = _first_position(ctx, drows, n_q, n_k, q_start)
     dtable = torch.empty((heads, len(first) * (2 if two_sided else 1)), dtype=drows.dtype, device=drows.device)
     if workspace is None:
         workspace = _scratch(B.grf_relative_bias_workspace_bytes(heads, n_q, n_k, len(first), two_sided), ctx)
-    B.grf_relative_bias_backward(ctx.handle, batch, heads, n_q, n_k, n_k - n_q if q_start is None else q_start, first, two_sided,
-                                 B.dtype_code(drows), drows, dtable, workspace, workspace.numel())
+    B.grf_relative_bias_backward(ctx.handle, batch, heads, n_q, n_k, start, first, two_sided, B.dtype_code(drows), drows, dtable, workspace,
+                                 workspace.numel())
     return dtable

@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from array import array
 
 import numpy as np
 
@@ -338,8 +339,11 @@ def grf_softmax_attn_backward(ctx, desc: SoftmaxDesc, Q, K, V, out, lse, rest, d
 
 
 def _distances(first):
-    """The smallest distance of each bucket as a C array."""
-    return (_i32 * len(first))(*(first if type(first) is list else [int(y) for y in first]))
+    """The smallest distance of each bucket as a C array (ctypes alone would cut larger numbers off)."""
+    try:
+        return (_i32 * len(first)).from_buffer(array("i", first if type(first) is list else [int(y) for y in first]))
+    except (OverflowError, TypeError) as e:
+        raise ValueError("expected distances as 32-bit integers") from e
 
 
 def grf_relative_bias(ctx, heads, n_q, n_k, q_start, first, two_sided, dtype, table, rows):

@@ -148,3 +148,37 @@ def test_bias_calls(fake):
     assert back(2, SOME, need) == 0
     assert back(0, SOME, need) == -1 and back(2, None, need) == -1 and back(2, SOME, need - 1) == -3 and back(2, SOME, need, SOME + 4) == -1
     assert fake.errors() == 0
+
+
+def test_numbers_that_do_not_fit_are_refused_not_cut_off():
+    import torch
+
+    from paper_2410_03462_b200 import api
+    from paper_2410_03462_b200 import binding as B
+    assert list(B._distances([0, 1, 1 << 29])) == list(B._distances(np.array([0, 1, 1 << 29]))) == [0, 1, 1 << 29]
+    for first in ([0, (1 << 32) + 1], [0, -(1 << 32) + 1], np.array([0, (1 << 32) + 1]), [0, 1.5]):
+        with pytest.raises(ValueError):
+            B._distances(first)
+
+    class Some:
+        device, torch_device, handle = 0, torch.device("cuda", 0), None
+
+    class OnDevice:
+        is_cuda = True
+
+        def get_device(self):
+            return 0
+    for n_q, n_k, start in ((4, 4, 1 << 31), (4, 4, -(1 << 31) - 1), ((1 << 32) + 4, 4, 0), (4, (1 << 32) + 4, 0)):
+        with pytest.raises(ValueError, match="32-bit"):
+            api._first_position(Some, OnDevice(), n_q, n_k, start)
+    assert api._first_position(Some, OnDevice(), 3, 7, None) == 4
+    other = OnDevice()
+    other.get_device = lambda: 1
+    for t in (torch.zeros(2, 8), other):
+        with pytest.raises(ValueError, match="cuda:0"):
+            api._first_position(Some, t, 4, 4, 0)
+    small = torch.zeros(1, 1, 1, 8)
+    many = small.expand(1, 1, (1 << 32) + 4, 8)
+    for q, k in ((many, small), (small, many)):
+        with pytest.raises(ValueError, match="too many tokens"):
+            api.softmax_attn(Some, q, k, k)
