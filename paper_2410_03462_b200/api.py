@@ -157,8 +157,8 @@ def _tokens(t, device, shape, name):
     return t.data_ptr()
 
 
-def _stride3(t, name):
-    """Strides of [batch, heads, tokens, dim] whose last axis is contiguous."""
+def _set_strides(to, t, name):
+    """A descriptor's strides of [batch, heads, tokens, dim] whose last axis is contiguous."""
     s = t.stride()
     if len(s) != 4:
         raise ValueError(f"{name}: expected four axes")
@@ -167,7 +167,7 @@ def _stride3(t, name):
     # (all zeros would mean "contiguous": an axis of one token, head or sequence is never stepped over, so any stride does)
     if s[0] == s[1] == s[2] == 0 and t.shape[0] * t.shape[1] * t.shape[2] > 1:
         raise ValueError(f"{name}: a tensor broadcast along every axis")
-    return B.Stride3(s[0], s[1], s[2])
+    to[0], to[1], to[2] = s[0], s[1], s[2]
 
 
 def _softmax_desc(ctx, q, k, v, scale, cap, mask, k_len, q_start, prefix, q_doc, k_doc, slopes, table, first, two_sided):
@@ -184,7 +184,9 @@ def _softmax_desc(ctx, q, k, v, scale, cap, mask, k_len, q_start, prefix, q_doc,
     if not (q.is_cuda and k.is_cuda and v.is_cuda and q.get_device() == k.get_device() == v.get_device() == ctx.device):
         raise ValueError(f"expected tensors on {device}")
     s = B.SoftmaxDesc(batch, heads, kv_heads, n_q, n_k, dim, B.dtype_code(q), dim ** -0.5 if scale is None else scale, cap, ORDERS[mask])
-    s.q_stride, s.k_stride, s.v_stride = _stride3(q, "q"), _stride3(k, "k"), _stride3(v, "v")
+    _set_strides(s.q_stride, q, "q")
+    _set_strides(s.k_stride, k, "k")
+    _set_strides(s.v_stride, v, "v")
     if k_len is not None:
         s.k_len = _tokens(k_len, device, (batch,), "k_len")
     if q_start is not None:
@@ -206,11 +208,16 @@ def _softmax_desc(ctx, q, k, v, scale, cap, mask, k_len, q_start, prefix, q_doc,
             raise ValueError(f"a table needs first, the smallest distance of each of 1 .. {B.GRF_MAX_BUCKETS} buckets")
         n = len(first)
         shape = (heads, n * (2 if two_sided else 1))
-        if table.dtype != dtype or table.device != device or tuple(table.shape) != shape or not table.is_contiguous():
+        if table.dtype != dtype or table.get_device() != ctx.device or tuple(table.shape) != shape or not table.is_contiguous():
             raise ValueError(f"table: expected a contiguous {dtype} tensor {shape} on {device}")
-        s.bias, s.table, s.n_buckets, s.two_sided = B.GRF_BIAS_BUCKETS, table.data_ptr(), n, int(two_sided)
-        s.first[:n] = B._distances(first)
+        s.bias, s.table, s.two_sided = B.GRF_BIAS_BUCKETS, table.data_ptr(), int(two_sided)
+        B.set_distances(s, first)
     return s
+
+
+def _like(t):
+    """Contiguous, whatever t's strides are (torch.empty takes twice as long, and a call on few tokens is bound by the host)."""
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
 def _scratch(nbytes, ctx):
@@ -233,15 +240,15 @@ def softmax_attn(ctx: Context, q, k, v, scale=None, cap=0.0, mask="full", k_len=
     which the backward pass takes."""
     s = _softmax_desc(ctx, q, k, v, scale, cap, mask, k_len, q_start, prefix, q_doc, k_doc, slopes, table, first, two_sided)
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = _like(q)
     elif out.shape != q.shape or out.dtype != q.dtype or out.device != q.device:
         raise ValueError("out: expected the shape, type and device of q")
     else:
-        s.out_stride = _stride3(out, "out")
-    lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device) if want_lse else None
+        _set_strides(s.out_stride, out, "out")
+    lse = q.new_empty(q.shape[:3], dtype=torch.float32) if want_lse else None
     if workspace is None:
         workspace = _scratch(B.grf_softmax_attn_workspace_bytes(ctx.handle, s, False), ctx)
-    rest = torch.empty(q.shape, dtype=q.dtype, device=q.device) if want_lse and q.dtype == torch.bfloat16 else None
+    rest = _like(q) if want_lse and q.dtype == torch.bfloat16 else None
     B.grf_softmax_attn(ctx.handle, s, q, k, v, out, lse, rest, workspace, workspace.numel() if workspace is not None else 0)
     return (out, SoftmaxSaved(lse, rest)) if want_lse else out
 
@@ -260,8 +267,9 @@ def softmax_attn_backward(ctx: Context, q, k, v, out, saved, dout, scale=None, c
         raise ValueError("lse: expected float32 [B, H, Nq]")
     if rest is not None and (rest.shape != q.shape or rest.dtype != q.dtype or rest.device != q.device):
         raise ValueError("rest: expected the shape, type and device of q")
-    s.out_stride, s.dout_stride = _stride3(out, "out"), _stride3(dout, "dout")
-    dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+    _set_strides(s.out_stride, out, "out")
+    _set_strides(s.dout_stride, dout, "dout")
+    dq, dk, dv = _like(q), _like(k), _like(v)
     dtable = torch.empty_like(table) if table is not None and want_dtable else None
     if workspace is None:
         workspace = _scratch(B.grf_softmax_attn_workspace_bytes(ctx.handle, s, True), ctx)
@@ -286,7 +294,7 @@ def relative_bias(ctx: Context, table, first, n_q, n_k, two_sided=False, q_start
     if tuple(table.shape) != (heads, len(first) * (2 if two_sided else 1)):
         raise ValueError("table: expected one column per bucket and side")
     start = _first_position(ctx, table, n_q, n_k, q_start)
-    rows = torch.empty((heads, n_q, n_k), dtype=table.dtype, device=table.device)
+    rows = table.new_empty((heads, n_q, n_k))
     B.grf_relative_bias(ctx.handle, heads, n_q, n_k, start, first, two_sided, B.dtype_code(table), table, rows)
     return rows
 
@@ -297,7 +305,7 @@ def relative_bias_backward(ctx: Context, drows, first, two_sided=False, q_start=
         drows = drows[None]
     batch, heads, n_q, n_k = drows.shape
     start = _first_position(ctx, drows, n_q, n_k, q_start)
-    dtable = torch.empty((heads, len(first) * (2 if two_sided else 1)), dtype=drows.dtype, device=drows.device)
+    dtable = drows.new_empty((heads, len(first) * (2 if two_sided else 1)))
     if workspace is None:
         workspace = _scratch(B.grf_relative_bias_workspace_bytes(heads, n_q, n_k, len(first), two_sided), ctx)
     B.grf_relative_bias_backward(ctx.handle, batch, heads, n_q, n_k, start, first, two_sided, B.dtype_code(drows), drows, dtable, workspace,

@@ -313,6 +313,12 @@ def grf_relative_buckets(n_buckets: int, max_distance: int) -> np.ndarray:
     return first
 
 
+def set_distances(desc: SoftmaxDesc, first):
+    first = _distances(first)
+    desc.n_buckets = len(first)
+    ctypes.memmove(desc.first, first.buffer_info()[0], 4 * len(first))
+
+
 def _strided(x):
     """Device address of a torch CUDA tensor of any strides (the descriptor states them), or an int; None -> NULL."""
     if x is None or isinstance(x, int):
@@ -339,15 +345,18 @@ def grf_softmax_attn_backward(ctx, desc: SoftmaxDesc, Q, K, V, out, lse, rest, d
 
 
 def _distances(first):
-    """The smallest distance of each bucket as a C array (ctypes alone would cut larger numbers off)."""
+    """The smallest distance of each bucket as an array of C integers (ctypes alone would cut larger numbers off)."""
+    if type(first) is np.ndarray and first.dtype == np.int32:
+        return array("i", first.tobytes())
     try:
-        return (_i32 * len(first)).from_buffer(array("i", first if type(first) is list else [int(y) for y in first]))
+        return array("i", first if type(first) is list else [int(y) for y in first])
     except (OverflowError, TypeError) as e:
         raise ValueError("expected distances as 32-bit integers") from e
 
 
 def grf_relative_bias(ctx, heads, n_q, n_k, q_start, first, two_sided, dtype, table, rows):
-    _check(lib.grf_relative_bias(ctx, heads, n_q, n_k, q_start, len(first), int(two_sided), _distances(first), dtype, _dev(table),
+    first = _distances(first)
+    _check(lib.grf_relative_bias(ctx, heads, n_q, n_k, q_start, len(first), int(two_sided), first.buffer_info()[0], dtype, _dev(table),
                                  _dev(rows)), "grf_relative_bias")
 
 
@@ -357,7 +366,8 @@ def grf_relative_bias_workspace_bytes(heads, n_q, n_k, n_buckets, two_sided) -> 
 
 def grf_relative_bias_backward(ctx, batch, heads, n_q, n_k, q_start, first, two_sided, dtype, drows, dtable, workspace,
                                workspace_bytes):
-    _check(lib.grf_relative_bias_backward(ctx, batch, heads, n_q, n_k, q_start, len(first), int(two_sided), _distances(first), dtype,
+    first = _distances(first)
+    _check(lib.grf_relative_bias_backward(ctx, batch, heads, n_q, n_k, q_start, len(first), int(two_sided), first.buffer_info()[0], dtype,
                                           _dev(drows), _dev(dtable), _dev(workspace), workspace_bytes), "grf_relative_bias_backward")
 
 

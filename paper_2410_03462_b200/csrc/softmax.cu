@@ -575,7 +575,7 @@ template <typename T> int bias_sums(grf_ctx* ctx, const bias_shape& s, int32_t b
 {
     const size_t smem = s.first[s.n_first - 1] > 16 * NEAR ? sizeof(float) * (size_t)s.columns() * BIAS_THREADS : 0;
     // (the most of any call: the attribute is the whole process's, and another thread may set it between here and the launch)
-    GRF_CUDA_TRY(cudaFuncSetAttribute(relative_sums_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(float) * 2 * GRF_MAX_BUCKETS * BIAS_THREADS));
+    if (smem > 0) GRF_CUDA_TRY(cudaFuncSetAttribute(relative_sums_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(float) * 2 * GRF_MAX_BUCKETS * BIAS_THREADS));
     grf_softmax_scope scope(ctx, "grf:relative_sums", 2);
     relative_sums_kernel<T><<<dim3(s.strips, s.heads), BIAS_THREADS, smem, ctx->stream>>>(s, batch, (const T*)drows, part);
     bucket_sums_kernel<T><<<dim3(s.columns(), s.heads), 256, 0, ctx->stream>>>(part, (T*)dtable, 1, s.heads, s.strips, s.columns());
