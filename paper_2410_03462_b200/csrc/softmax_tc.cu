@@ -90,50 +90,75 @@ struct forward_tiles {
     }
 };
 
-// The outputs of row i from the keys that it sees, where a value that it does not see has spoilt them: the warp together, lanes take keys for
-// the scores and columns for the sums.  Rare, and only columns that are not finite are replaced.
+// The outputs of row i from the keys that it sees, where a value that it does not see may have spoilt them: the warp together, lanes take keys for
+// the scores and four columns each for the sums.  Only columns that are not finite are replaced, and one whose sum is not finite either
+// stays (the row sees such a value itself): with none left the row is done.
 template <bool CAP>
 __device__ __noinline__ void redo_row(const grf_softmax_params& p, const grf_buckets& bucket, int32_t b, int32_t h, int32_t i, float m, float l, int32_t col0, int32_t col1)
 {
     const grf_sight sight(p, b);
-    const int lane = threadIdx.x & 31;
+    const int lane = threadIdx.x & 31, col = 4 * lane;
     const int32_t kvh = h / p.group, pos = sight.position(i), end = sight.end(i + 1);
     const __nv_bfloat16* Q = reinterpret_cast<const __nv_bfloat16*>(p.q) + b * p.qs[0] + h * p.qs[1] + (int64_t)i * p.qs[2];
     const __nv_bfloat16* K = reinterpret_cast<const __nv_bfloat16*>(p.k) + b * p.ks[0] + kvh * p.ks[1];
-    const __nv_bfloat16* V = reinterpret_cast<const __nv_bfloat16*>(p.v) + b * p.vs[0] + kvh * p.vs[1];
+    const __nv_bfloat16* V = reinterpret_cast<const __nv_bfloat16*>(p.v) + b * p.vs[0] + kvh * p.vs[1] + col;
+    __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.out_w) + b * p.os[0] + h * p.os[1] + (int64_t)i * p.os[2] + col;
     const int32_t doc = sight.docs ? p.q_doc[(int64_t)b * p.Nq + i] : 0;
     const int32_t* kdoc = sight.docs ? p.k_doc + (int64_t)b * p.Nk : nullptr;
     float o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    bool want[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) want[x] = col >= col0 && col < min(col1, p.d) && !(fabsf(__bfloat162float(out[x])) <= 3.4028235e38f);
     for (int32_t j0 = 0; j0 < end; j0 += 32) {
+        const bool mine = want[0] || want[1] || want[2] || want[3];
+        if (!__any_sync(0xffffffffu, mine)) return;
         const int32_t j = j0 + lane;
         const bool seen = j < end && sight.sees(pos, j) && (!kdoc || (doc >= 0 && kdoc[j] == doc));
+        const uint32_t who = __ballot_sync(0xffffffffu, seen);
         float w = 0.0f;
         if (seen) {
-            for (int c = 0; c < p.d; ++c) w = fmaf(__bfloat162float(Q[c]), __bfloat162float(K[(int64_t)j * p.ks[2] + c]), w);
+            // (loads first, here and below: most of this is their latency)
+            for (int c0 = 0; c0 < p.d; c0 += 64) {
+                uint4 k8[8];
+#pragma unroll
+                for (int x = 0; x < 8; ++x) k8[x] = c0 + 8 * x < p.d ? *reinterpret_cast<const uint4*>(K + (int64_t)j * p.ks[2] + c0 + 8 * x) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                for (int x = 0; x < 8; ++x) {
+                    const uint4 q8 = c0 + 8 * x < p.d ? *reinterpret_cast<const uint4*>(Q + c0 + 8 * x) : make_uint4(0, 0, 0, 0);
+                    const uint32_t kw[4] = {k8[x].x, k8[x].y, k8[x].z, k8[x].w}, qw[4] = {q8.x, q8.y, q8.z, q8.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        w = fmaf(__uint_as_float(qw[e] & 0xffff0000u), __uint_as_float(kw[e] & 0xffff0000u), fmaf(__uint_as_float(qw[e] << 16), __uint_as_float(kw[e] << 16), w));
+                }
+            }
             w = CAP ? p.cap * GRF_LOG2E * tanh_any(w * (p.scale / p.cap)) : w * (p.scale * GRF_LOG2E);
             if (p.bias != GRF_BIAS_NONE) w += grf_bias2<__nv_bfloat16>(p, bucket, h, j - pos);
             w = __bfloat162float(__float2bfloat16_rn(ex2(w - m)));
         }
-        const uint32_t who = __ballot_sync(0xffffffffu, seen);
-        for (int y = 0; y < 32; ++y) {
-            const float wy = __shfl_sync(0xffffffffu, w, y);
-            if (!(who >> y & 1u)) continue;
+#pragma unroll 1
+        for (int y0 = 0; y0 < 32; y0 += 16) {
+            uint2 v[16];
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const int c = lane + 32 * x;
-                if (c < p.d) o[x] = fmaf(wy, __bfloat162float(V[(int64_t)(j0 + y) * p.vs[2] + c]), o[x]);
+            for (int y = 0; y < 16; ++y) v[y] = mine && (who >> (y0 + y) & 1u) ? *reinterpret_cast<const uint2*>(V + (int64_t)(j0 + y0 + y) * p.vs[2]) : make_uint2(0, 0);
+#pragma unroll
+            for (int y = 0; y < 16; ++y) {
+                const float wy = __shfl_sync(0xffffffffu, w, y0 + y);
+                o[0] = fmaf(wy, __uint_as_float(v[y].x << 16), o[0]);
+                o[1] = fmaf(wy, __uint_as_float(v[y].x & 0xffff0000u), o[1]);
+                o[2] = fmaf(wy, __uint_as_float(v[y].y << 16), o[2]);
+                o[3] = fmaf(wy, __uint_as_float(v[y].y & 0xffff0000u), o[3]);
             }
         }
+#pragma unroll
+        for (int x = 0; x < 4; ++x) want[x] = want[x] && fabsf(o[x]) <= 3.4028235e38f;
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.out_w) + b * p.os[0] + h * p.os[1] + (int64_t)i * p.os[2];
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
-        const int c = lane + 32 * x;
-        if (c < col0 || c >= min(col1, p.d) || fabsf(__bfloat162float(out[c])) <= 3.4028235e38f) continue;
+        if (!want[x]) continue;
         const float y = o[x] * inv;
-        out[c] = __float2bfloat16_rn(y);
-        if (p.rest_w) p.rest_w[(((int64_t)b * p.H + h) * p.Nq + i) * p.d + c] = grf_rest(y, __float2bfloat16_rn(y));
+        out[x] = __float2bfloat16_rn(y);
+        if (p.rest_w) p.rest_w[(((int64_t)b * p.H + h) * p.Nq + i) * p.d + col + x] = grf_rest(y, __float2bfloat16_rn(y));
     }
 }
 
@@ -230,7 +255,10 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
     __syncthreads();
     fence_after_sync();
     const uint32_t tmem = (uint32_t)uniform((int32_t)tmem_slot);
-    auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, &abort_flag)) != 0; };
+    // (a block whose rows are all summed again takes 6 us a key: 6 s with a million, for which the other warps wait)
+    auto wait = [&](uint32_t bar, uint32_t parity) {
+        return __all_sync(0xffffffffu, mbar_wait(bar, parity, &abort_flag, p.Nk > (1 << 18) ? 16 * WAIT_CYCLES : WAIT_CYCLES)) != 0;
+    };
 
     if (warp >= SOFT) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(LESS));

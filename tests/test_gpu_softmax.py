@@ -384,6 +384,46 @@ def test_streams_and_captured_calls(lib):
         c.close()
 
 
+def test_spoilt_values_at_the_end_of_a_long_cache(lib):
+    """Infinities that some queries of a tile see and others do not, and one that all see, with keys so many that summing rows again takes long."""
+    api, B, ctx = lib
+    nq, nk, d = 256, 1 << 20, 64
+    g = torch.Generator(device="cuda").manual_seed(4)
+    q = torch.randn(1, 1, nq, d, device="cuda", generator=g).bfloat16()
+    k, v = (torch.randn(1, 1, nk, d, device="cuda", generator=g).bfloat16() for _ in range(2))
+    inf = float("inf")
+    v[0, 0, nk - 60, 7] = inf               # query nq - 60 and those behind it
+    v[0, 0, nk - 200, 9] = -inf
+    v[0, 0, 5, 11] = inf                    # everyone
+    torch.cuda.synchronize()
+    at = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+    at[0].record()
+    out = api.softmax_attn(ctx, q, k, v, mask="causal")[0, 0]
+    at[1].record()
+    torch.cuda.synchronize()
+    B.grf_ctx_check(ctx.handle)
+    print(f"{at[0].elapsed_time(at[1]):.1f} ms")
+    rows = torch.arange(nq, device="cuda")
+    assert (out[:, 11] == inf).all()
+    assert torch.equal(out[:, 7] == inf, rows >= nq - 60) and torch.equal(out[:, 9] == -inf, rows >= nq - 200)
+    other = torch.ones_like(out, dtype=torch.bool)
+    other[:, 11] = False
+    other[nq - 60:, 7] = False
+    other[nq - 200:, 9] = False
+    assert out[other].isfinite().all()
+    ones = [0, 20, 56, 57, 100, 195, 196, 255]
+    s = (q[0, 0, ones].double() @ k[0, 0].double().T) * d ** -0.5
+    s[torch.arange(nk, device="cuda")[None] > (nk - nq + rows[ones])[:, None]] = -inf
+    p = torch.softmax(s, 1)
+    w = v[0, 0].double()
+    clean = torch.where(w.isfinite(), w, 0.0)
+    want, size = p @ clean, p @ clean.abs()
+    # P and out to bf16; scores, of a size of 6 or less, and sums in 32 bits
+    bound = size * (2 * 2.0**-8 + 2.0**-16) + 1e-9
+    diff = (out[ones].double() - want).abs()
+    assert (diff <= bound)[other[ones]].all()
+
+
 def test_workspace_of_a_call_on_a_stream_that_is_not_current(lib, monkeypatch):
     """Memory of a call's workspace is not handed out on the current stream while the call may still run on the context's."""
     api, B, ctx = lib
