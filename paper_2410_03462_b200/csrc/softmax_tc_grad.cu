@@ -65,8 +65,9 @@ __device__ __forceinline__ void keep(uint64_t& x, bool first, bool second)
     unpack2(x, x0, x1);
     x = pack2(first ? x0 : 0.0f, second ? x1 : 0.0f);
 }
-// dP is 0 where P is: a place that is not seen holds 0, whatever dP is there
-__device__ __forceinline__ void only_seen(uint32_t (&dp)[W / 16][16], const uint64_t (&p)[W / 2])
+// dP, and the slope of the cap where there is one, are 0 where P is: a place that is not seen holds 0, whatever came out of the products there
+template <bool CAP>
+__device__ __forceinline__ void only_seen(uint32_t (&dp)[W / 16][16], uint64_t (&slope)[CAP ? W / 2 : 1], const uint64_t (&p)[W / 2])
 {
 #pragma unroll
     for (int e = 0; e < W; e += 2) {
@@ -74,6 +75,7 @@ __device__ __forceinline__ void only_seen(uint32_t (&dp)[W / 16][16], const uint
         unpack2(p[e / 2], p0, p1);
         if (p0 == 0.0f) dp[e / 16][e % 16] = 0u;
         if (p1 == 0.0f) dp[e / 16][e % 16 + 1] = 0u;
+        if constexpr (CAP) keep(slope[e / 2], p0 != 0.0f, p1 != 0.0f);
     }
 }
 __device__ __forceinline__ void clear_row(uint32_t tile, int r, int halves)
@@ -420,7 +422,7 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     tmem_ld_wait();
                     if (careful) {
                         __syncwarp();
-                        only_seen(dv, x);
+                        only_seen<CAP>(dv, slope, x);
                     }
                     const uint64_t minus_d = pack2(any ? -dsum : 0.0f, any ? -dsum : 0.0f);
 #pragma unroll
@@ -888,7 +890,7 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                         tmem_ld_wait();
                         if (partial) {
                             __syncwarp();
-                            only_seen(dv, x);
+                            only_seen<CAP>(dv, slope, x);
                         }
                         uint32_t w[16];
 #pragma unroll
