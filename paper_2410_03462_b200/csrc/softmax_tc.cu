@@ -439,7 +439,7 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             const int32_t i = i0 + g * BT + r, pos = sight.position(i), pos0 = sight.position(i0 + g * BT);
             const int32_t limit = (sight.order == GRF_ORDER_FULL ? sight.len : min(sight.len, max(pos + 1, sight.prefix))) - c0;
             int32_t doc = sight.docs && i < p.Nq ? p.q_doc[(int64_t)b * p.Nq + i] : -1;
-            if (doc < 0) doc = INT32_MIN;                       // (equal to no key's)
+            if (doc < 0) doc = INT32_MIN;                       // (equal to no key's: these are -1 where they are negative)
             const float slope2 = BIAS == GRF_BIAS_SLOPES ? p.slopes[h] * GRF_LOG2E : 0.0f;
             float m = -CUDART_INF_F;
             uint64_t sum2[2] = {0ull, 0ull};
@@ -464,7 +464,7 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                         at[r + 128 * half] = grf_bias2<__nv_bfloat16>(p, bucket, h, j0 - pos0 + r + 128 * half - (BT - 1));
                         mine = at + (BT - 1 - r) + c0;
                     }
-                    if (mixed && half == 0) docs[r] = j0 + r < p.Nk ? p.k_doc[(int64_t)b * p.Nk + j0 + r] : -1;
+                    if (mixed && half == 0) docs[r] = j0 + r < p.Nk ? max(p.k_doc[(int64_t)b * p.Nk + j0 + r], -1) : -1;
                     with_group();
                     ++luts;
                 }

@@ -326,7 +326,7 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             const int32_t limit = sight.order == GRF_ORDER_FULL ? sight.len : min(sight.len, max(pos + 1, sight.prefix));
             const int32_t all_see = sight.order == GRF_ORDER_FULL ? sight.len : min(sight.len, max(pos0 + 1, sight.prefix));       // keys before it: the whole block
             int32_t doc = sight.docs && i < p.Nq ? p.q_doc[(int64_t)b * p.Nq + i] : -1;
-            if (doc < 0) doc = INT32_MIN;                           // (equal to no key's)
+            if (doc < 0) doc = INT32_MIN;                           // (equal to no key's: these are -1 where they are negative)
             const int64_t row = ((int64_t)b * p.H + h) * p.Nq + i;
             const float lse = i < p.Nq ? p.lse[row] : -CUDART_INF_F, dsum = i < p.Nq ? p.dsum[row] : 0.0f;
             const bool any = !(fabsf(lse) > LARGEST);               // a row without a key, or one whose scores tell nothing any more: P = 0
@@ -364,7 +364,7 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                         if (tid < 256) at[tid] = tid < 2 * BT - 1 ? grf_bias2<__nv_bfloat16>(p, bucket, h, j0 - pos0 + tid - (BT - 1)) : 0.0f;
                         mine = at + (BT - 1 - r) + c0;
                     }
-                    if (mixed && tid < BT) docs[tid] = j0 + tid < p.Nk ? p.k_doc[(int64_t)b * p.Nk + j0 + tid] : -1;
+                    if (mixed && tid < BT) docs[tid] = j0 + tid < p.Nk ? max(p.k_doc[(int64_t)b * p.Nk + j0 + tid], -1) : -1;
                     with_workers();
                     ++luts;
                 }
@@ -749,7 +749,7 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                         const bool in = t * BT + r < p.Nq;
                         lse[y] = in ? p.lse[row + r] : -CUDART_INF_F;
                         d[y] = in ? p.dsum[row + r] : 0.0f;
-                        docs[y] = in && I.sight.docs ? p.q_doc[(int64_t)I.b * p.Nq + t * BT + r] : -1;
+                        docs[y] = in && I.sight.docs ? max(p.q_doc[(int64_t)I.b * p.Nq + t * BT + r], -1) : -1;
                     }
                 };
                 fetch();
@@ -802,7 +802,7 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
             const grf_sight& sight = I.sight;
             const int32_t b = I.b, kvh = I.kvh, j0 = I.j0, j = j0 + r;
             int32_t doc = sight.docs && j < p.Nk ? p.k_doc[(int64_t)b * p.Nk + j] : -1;
-            if (doc < 0) doc = INT32_MIN;                           // (equal to no query's)
+            if (doc < 0) doc = INT32_MIN;                           // (equal to no query's: these are -1 where they are negative)
             const bool block_partial = j0 + BT > sight.len, ordered = sight.order != GRF_ORDER_FULL && j0 + BT > sight.prefix;
             if (I.some) {
                 int32_t t = T.begin(), h = I.h_first;

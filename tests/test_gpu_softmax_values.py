@@ -47,3 +47,23 @@ def test_unseen_values_in_every_kernel(lib, route, cap, bias, mask, d):  # noqa:
     """What a token holds that nobody sees does not matter, with and without caps, biases and orders."""
     for nq in (150, 6):
         spoil_unseen(lib, *make(53, 2, 4, 2, nq, 300, d, "bf16", mask=mask, bias=bias, cap=cap, ragged=True), f"{nq} queries")
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("docs", ["few", "many", "unsorted"])
+@pytest.mark.parametrize("cap,bias,mask", [(0.0, "table", "full"), (20.0, "none", "causal"), (0.0, "slopes", "prefix")])
+def test_negative_documents(lib, route, dtype, docs, cap, bias, mask):  # noqa: F811
+    """Any negative document is none: tokens of equal negative numbers, the lowest one among them, do not see one another."""
+    if dtype == "fp32" and route == "alu":
+        pytest.skip("fp32 has one route")
+    for nq in (300, 8):
+        x, how, dout = make(59, 2, 2, 1, nq, 300, 64, dtype, mask=mask, bias=bias, cap=cap, docs=docs)
+        g = torch.Generator().manual_seed(2)
+        for name in ("q_doc", "k_doc"):
+            ids = how[name].cpu()
+            none = torch.tensor([-1, -7, -2**31, -2**31], dtype=torch.int32)[torch.randint(0, 4, ids.shape, generator=g)]
+            how[name] = torch.where((ids < 0) | (torch.rand(ids.shape, generator=g) < 0.1), none, ids).cuda()
+        check(lib, x, how, dout, f"{nq} queries: ")
+        for t, ids in ((x["k"], "k_doc"), (x["v"], "k_doc"), (dout, "q_doc")):
+            t.masked_fill_((how[ids] < 0)[:, None, :, None], NAN)
+        check(lib, x, how, dout, f"{nq} queries, NaN in padding: ")
