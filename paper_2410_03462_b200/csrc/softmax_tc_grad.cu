@@ -38,7 +38,7 @@ template <int DP> struct Grad {
 
 // Tiles of the other side that a block sees, in order; with documents from bits in shared memory.
 struct grad_tiles {
-    const uint32_t* bits;               // seen, whole, tiles with a key of no document, tiles of one document
+    const uint32_t* bits;               // seen, whole, tiles of one document
     int32_t first, tiles, words;
     bool docs;
     __device__ __forceinline__ int32_t next(int32_t t) const
@@ -53,8 +53,7 @@ struct grad_tiles {
     }
     __device__ __forceinline__ int32_t begin() const { return next(first); }
     __device__ __forceinline__ bool whole(int32_t t) const { return bit(bits + words, t); }
-    __device__ __forceinline__ bool mixed(int32_t t) const { return docs && !bit(bits + 3 * words, t); }
-    __device__ __forceinline__ bool hole(int32_t t) const { return docs && bit(bits + 2 * words, t); }
+    __device__ __forceinline__ bool mixed(int32_t t) const { return docs && !bit(bits + 2 * words, t); }
 };
 
 constexpr float LARGEST = 1.0e30f;                  // of lse
@@ -82,6 +81,24 @@ __device__ __forceinline__ void clear_row(uint32_t tile, int r, int halves)
 {
     for (int y = 0; y < halves; ++y)
         for (int x = 0; x < 8; ++x) asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(tile + y * HALF + r * 128 + x * 16), "r"(0u) : "memory");
+}
+// Rows of a tile of bf16 that hold an infinity or NaN, by a warp: bit y of lanes 8 z .. 8 z + 7 is row 4 y + z.
+template <int HALVES> __device__ __forceinline__ uint32_t not_finite(uint32_t tile, int lane)
+{
+    uint32_t rows = 0u;
+#pragma unroll 4
+    for (int y = 0; y < BT / 4; ++y)
+#pragma unroll
+        for (int x = 0; x < HALVES; ++x) {
+            uint4 v;
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(tile + x * HALF + y * 512 + lane * 16) : "memory");
+            // (an exponent of ones carries into the sign)
+            auto bad = [](uint32_t w) { return (w & 0x7f807f80u) + 0x00800080u; };
+            if ((bad(v.x) | bad(v.y) | bad(v.z) | bad(v.w)) & 0x80008000u) rows |= 1u << y;
+        }
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) rows |= __shfl_xor_sync(0xffffffffu, rows, o);
+    return rows;
 }
 // D[128][DP] (+)= A B: A's bf16 pairs in the first half of every worker's columns.
 template <int DP>
@@ -140,7 +157,8 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             T = grad_tiles{bits, 0, tiles, (tiles + 31) / 32, sight.docs};
             last = sight.end(p.Nq);
         }
-        __device__ __forceinline__ bool unclean(const grf_softmax_params& p, int32_t t) const { return (last < p.Nk && t * BT + BT > last) || T.hole(t); }
+        // a tile that may hold keys which nobody sees
+        __device__ __forceinline__ bool unclean(const grf_softmax_params& p, int32_t t) const { return (last < p.Nk && t * BT + BT > last) || (T.docs && !T.whole(t)); }
     };
 
     if (tid == 0) {
@@ -166,9 +184,9 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             const int32_t t = w * 32 + lane;
             const int4 kr = t < tiles ? p.k_range[(int64_t)b * kblocks + t] : make_int4(INT32_MAX, -1, 0, 0);
             const int what = t < tiles ? I.sight.tile(I.i0, i1, t * BT, t * BT + BT, qr, kr) : 0;
-            const uint32_t seen = __ballot_sync(0xffffffffu, what != 0), whole = __ballot_sync(0xffffffffu, what == 2), hole = __ballot_sync(0xffffffffu, kr.z != 0),
+            const uint32_t seen = __ballot_sync(0xffffffffu, what != 0), whole = __ballot_sync(0xffffffffu, what == 2),
                            one_doc = __ballot_sync(0xffffffffu, one_document(qr, kr));
-            if (lane == 0) { bits[w] = seen; bits[T.words + w] = whole; bits[2 * T.words + w] = hole; bits[3 * T.words + w] = one_doc; }
+            if (lane == 0) { bits[w] = seen; bits[T.words + w] = whole; bits[2 * T.words + w] = one_doc; }
         }
     }
     if (LUTS)
@@ -292,9 +310,28 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     const int s = n % NS;
                     if (!(ok = wait(k_full(s), (uint32_t)(n / NS) & 1u))) break;
                     if (I.unclean(p, t)) {
+                        const int32_t* kdoc = I.sight.docs ? p.k_doc + (int64_t)I.b * p.Nk : nullptr;
                         for (int r = lane; r < BT; r += 32) {
                             const int32_t j = t * BT + r;
-                            if (j < p.Nk && (j >= I.last || (I.sight.docs && p.k_doc[(int64_t)I.b * p.Nk + j] < 0))) clear_row(k_at + s * Sh::TILE, r, DP / 64);
+                            if (j < p.Nk && (j >= I.last || (kdoc && kdoc[j] < 0))) clear_row(k_at + s * Sh::TILE, r, DP / 64);
+                        }
+                        if (kdoc) {
+                            // a key of a document that no query is of, or behind the last query of its document, is seen by nobody either: which
+                            // ones these are takes a look at all queries, so only rows that hold an infinity or NaN are looked up, in this block
+                            __syncwarp();
+                            uint32_t rows = not_finite<DP / 64>(k_at + s * Sh::TILE, lane);
+                            if (__any_sync(0xffffffffu, rows != 0u)) {
+                                for (int x = 0; x < BT; ++x) {
+                                    if (!(__shfl_sync(0xffffffffu, rows, 8 * (x & 3)) >> (x >> 2) & 1u)) continue;
+                                    const int32_t j = t * BT + x;
+                                    if (j >= p.Nk) break;
+                                    const int32_t doc = kdoc[j];
+                                    bool seen = false;
+                                    for (int32_t i = I.i0 + lane; i < min(I.i0 + BT, p.Nq); i += 32)
+                                        seen |= p.q_doc[(int64_t)I.b * p.Nq + i] == doc && I.sight.sees(I.sight.position(i), j);
+                                    if (!__any_sync(0xffffffffu, seen) && lane == 0) clear_row(k_at + s * Sh::TILE, x, DP / 64);
+                                }
+                            }
                         }
                         fence_async_smem();
                         __syncwarp();
@@ -621,7 +658,7 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
             const int what = in ? sight.tile(t * BT, min(t * BT + BT, p.Nq), j0, j0 + BT, qr, kr) : 0;
             const uint32_t seen = __ballot_sync(0xffffffffu, what != 0), whole = __ballot_sync(0xffffffffu, what == 2),
                            one_doc = __ballot_sync(0xffffffffu, one_document(qr, kr));
-            if (lane == 0) { bits[w] = seen; bits[T.words + w] = whole; bits[2 * T.words + w] = 0u; bits[3 * T.words + w] = one_doc; }
+            if (lane == 0) { bits[w] = seen; bits[T.words + w] = whole; bits[2 * T.words + w] = one_doc; }
         }
     }
     fence_before_sync();
@@ -990,7 +1027,7 @@ struct grad_maps { CUtensorMap q, k, v, g; };
 template <int DP, bool CAP, int BIAS> int launch(grf_ctx* ctx, const grf_softmax_params& p, const grad_maps& m)
 {
     using Sh = Grad<DP>;
-    auto bits = [](int32_t tokens) { return 16 * (size_t)(grf_ceil_div(tokens, BT) / 32 + 1); };
+    auto bits = [](int32_t tokens) { return 12 * (size_t)(grf_ceil_div(tokens, BT) / 32 + 1); };
     const size_t dq_smem = Sh::SMEM + (p.q_doc ? bits(p.Nk) : 0), dkv_smem = Sh::SMEM + (p.q_doc ? bits(p.Nq) : 0);
     // (the most of any call, as in the forward pass)
     constexpr auto most = cudaFuncAttributeMaxDynamicSharedMemorySize;

@@ -49,6 +49,20 @@ def test_unseen_values_in_every_kernel(lib, route, cap, bias, mask, d):  # noqa:
         spoil_unseen(lib, *make(53, 2, 4, 2, nq, 300, d, "bf16", mask=mask, bias=bias, cap=cap, ragged=True), f"{nq} queries")
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("fp32", 64)])
+@pytest.mark.parametrize("nq,start", [(150, False), (300, False), (200, True)])
+@pytest.mark.parametrize("docs", ["few", "many", "unsorted"])
+@pytest.mark.parametrize("cap,bias,mask", [(0.0, "none", "full"), (20.0, "slopes", "causal"), (0.0, "table", "prefix")])
+def test_unseen_values_of_documents(lib, route, cap, bias, mask, docs, nq, start, dtype, d):  # noqa: F811
+    """Among them keys of documents that no query is of, and those behind the last query of theirs."""
+    if dtype == "fp32" and route == "alu":
+        pytest.skip("fp32 has one route")
+    x, how, dout = make(103, 2, 4, 2, nq, 300, d, dtype, mask=mask, bias=bias, cap=cap, docs=docs, start=start)
+    if start:
+        how["q_doc"] = how["q_doc"].roll(37, 1).contiguous()
+    spoil_unseen(lib, x, how, dout, "")
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("docs", ["few", "many", "unsorted"])
 @pytest.mark.parametrize("cap,bias,mask", [(0.0, "table", "full"), (20.0, "none", "causal"), (0.0, "slopes", "prefix")])
