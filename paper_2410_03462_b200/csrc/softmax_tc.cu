@@ -92,8 +92,8 @@ struct forward_tiles {
 
 // The outputs of row i from the keys that it sees, where a value that it does not see may have spoilt them: the warp together, lanes take keys for
 // the scores and four columns each for the sums.  Only columns that are not finite are replaced, and one whose sum is not finite either
-// stays (the row sees such a value itself): with none left the row is done.
-template <bool CAP>
+// stays (the row sees such a value itself): with none left the row is done.  EXACT: the weights are not rounded.
+template <bool CAP, bool EXACT>
 __device__ __noinline__ void redo_row(const grf_softmax_params& p, const grf_buckets& bucket, int32_t b, int32_t h, int32_t i, float m, float l, int32_t col0, int32_t col1)
 {
     const grf_sight sight(p, b);
@@ -133,7 +133,8 @@ __device__ __noinline__ void redo_row(const grf_softmax_params& p, const grf_buc
             }
             w = CAP ? p.cap * GRF_LOG2E * tanh_any(w * (p.scale / p.cap)) : w * (p.scale * GRF_LOG2E);
             if (p.bias != GRF_BIAS_NONE) w += grf_bias2<__nv_bfloat16>(p, bucket, h, j - pos);
-            w = __bfloat162float(__float2bfloat16_rn(ex2(w - m)));
+            w = ex2(w - m);
+            if (!EXACT) w = __bfloat162float(__float2bfloat16_rn(w));
         }
 #pragma unroll 1
         for (int y0 = 0; y0 < 32; y0 += 16) {
@@ -648,7 +649,7 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             while (again) {
                 const int y = __ffs(again) - 1;
                 again &= again - 1;
-                redo_row<CAP>(p, bucket, b, h, __shfl_sync(0xffffffffu, i, y), __shfl_sync(0xffffffffu, m, y), __shfl_sync(0xffffffffu, l, y), half * (DP / 2),
+                redo_row<CAP, EXACT>(p, bucket, b, h, __shfl_sync(0xffffffffu, i, y), __shfl_sync(0xffffffffu, m, y), __shfl_sync(0xffffffffu, l, y), half * (DP / 2),
                               (half + 1) * (DP / 2));
             }
             with_other_half();                                  // (the sums are read: they may be written again)

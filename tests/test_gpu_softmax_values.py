@@ -81,3 +81,25 @@ def test_negative_documents(lib, route, dtype, docs, cap, bias, mask):  # noqa: 
         for t, ids in ((x["k"], "k_doc"), (x["v"], "k_doc"), (dout, "q_doc")):
             t.masked_fill_((how[ids] < 0)[:, None, :, None], NAN)
         check(lib, x, how, dout, f"{nq} queries, NaN in padding: ")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("cap", [0.0, 5.0])
+@pytest.mark.parametrize("mask", ["causal", "prefix"])
+def test_rest_of_rows_that_are_summed_again(lib, mask, cap, d):  # noqa: F811
+    """An infinity in a value that a row does not see, in a tile that it does: the row's out + rest is as good as without."""
+    api, _, ctx = lib
+    nq = nk = 120
+    x, how, _ = make(67, 1, 2, 1, nq, nk, d, "bf16", mask=mask, cap=cap)
+    if mask == "prefix":
+        how["prefix"].fill_(30)
+    want = R.reference(x["q"], x["k"], x["v"], **how)
+    V = np.repeat(x["v"].double().cpu().numpy(), 2, 1)
+    r, size = R.HALF_STEP[torch.bfloat16], want["P"] @ np.abs(V)
+    bound = want["out_tol"] - r * size - r * np.abs(want["out"]) + r * r * (size + np.abs(want["out"]))
+    v = x["v"].clone()
+    v[0, 0, nk - 1, ::3] = INF                          # seen by the last query alone
+    out, saved = api.softmax_attn(ctx, x["q"], x["k"], v, want_lse=True, **how)
+    assert not out[0, :, -1, ::3].isfinite().any()
+    both = (out.double() + saved.rest.double())[:, :, :-1]
+    R.assert_close(both, want["out"][:, :, :-1], bound[:, :, :-1], "out + rest")
