@@ -83,6 +83,24 @@ def test_negative_documents(lib, route, dtype, docs, cap, bias, mask):  # noqa: 
         check(lib, x, how, dout, f"{nq} queries, NaN in padding: ")
 
 
+@pytest.mark.parametrize("nq,nk", [(40, 40), (150, 170)])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("cap,bias,mask", [(0.0, "none", "full"), (0.0, "none", "causal"), (5.0, "none", "causal"), (0.0, "table", "full"), (0.0, "slopes", "prefix")])
+def test_rest_holds_what_rounding_took(lib, cap, bias, mask, nq, nk, d):  # noqa: F811
+    """out + rest comes from probabilities of 2^-16: within a bound that probabilities rounded to bf16 do not meet."""
+    api, _, ctx = lib
+    x, how, _ = make(61, 2, 2, 1, nq, nk, d, "bf16", mask=mask, bias=bias, cap=cap)
+    want = R.reference(x["q"], x["k"], x["v"], **how)
+    V = np.repeat(x["v"].double().cpu().numpy(), 2, 1)
+    r, size = R.HALF_STEP[torch.bfloat16], want["P"] @ np.abs(V)
+    # the bound of out without the roundings of P and of out, for which each leaves a rounding of its own remainder: r r
+    bound = want["out_tol"] - r * size - r * np.abs(want["out"]) + r * r * (size + np.abs(want["out"]))
+    rounded = torch.from_numpy(want["P"] / want["P"].max(-1, keepdims=True)).bfloat16().double().numpy() * want["P"].max(-1, keepdims=True)
+    assert (np.abs(rounded @ V - want["out"]) > bound).sum() > 20
+    out, saved = api.softmax_attn(ctx, x["q"], x["k"], x["v"], want_lse=True, **how)
+    R.assert_close(out.double() + saved.rest.double(), want["out"], bound, "out + rest")
+
+
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("cap", [0.0, 5.0])
 @pytest.mark.parametrize("mask", ["causal", "prefix"])
