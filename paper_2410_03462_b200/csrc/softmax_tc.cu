@@ -92,9 +92,10 @@ struct forward_tiles {
 
 // The outputs of row i from the keys that it sees, where a value that it does not see may have spoilt them: the warp together, lanes take keys for
 // the scores and four columns each for the sums.  Only columns that are not finite are replaced, and one whose sum is not finite either
-// stays (the row sees such a value itself): with none left the row is done.  EXACT: the weights are not rounded.
+// stays (the row sees such a value itself): with none left the row is done.  EXACT: the weights are not rounded.  steps: counted up now and then.
 template <bool CAP, bool EXACT>
-__device__ __noinline__ void redo_row(const grf_softmax_params& p, const grf_buckets& bucket, int32_t b, int32_t h, int32_t i, float m, float l, int32_t col0, int32_t col1)
+__device__ __noinline__ void redo_row(const grf_softmax_params& p, const grf_buckets& bucket, int32_t b, int32_t h, int32_t i, float m, float l, int32_t col0, int32_t col1,
+                                      int* steps)
 {
     const grf_sight sight(p, b);
     const int lane = threadIdx.x & 31, col = 4 * lane;
@@ -112,6 +113,7 @@ __device__ __noinline__ void redo_row(const grf_softmax_params& p, const grf_buc
     for (int32_t j0 = 0; j0 < end; j0 += 32) {
         const bool mine = want[0] || want[1] || want[2] || want[3];
         if (!__any_sync(0xffffffffu, mine)) return;
+        if ((j0 & 1023) == 0 && lane == 0) atomicAdd(steps, 1);
         const int32_t j = j0 + lane;
         const bool seen = j < end && sight.sees(pos, j) && (!kdoc || (doc >= 0 && kdoc[j] == doc));
         const uint32_t who = __ballot_sync(0xffffffffu, seen);
@@ -163,6 +165,24 @@ __device__ __noinline__ void redo_row(const grf_softmax_params& p, const grf_buc
     }
 }
 
+// A bounded wait whose time starts anew while rows are summed again (a block all of whose rows are takes 6 us a key with
+// d = 64, 9.6 with d = 128: 2.5 s with 2^18 keys, where a wait alone gives up after 2): that is a loop over keys, so it ends, and `steps` with it.
+__device__ __forceinline__ bool wait_beside(uint32_t bar, uint32_t parity, volatile int* abort_flag, volatile int* steps)
+{
+    long long t0 = 0;
+    int last = 0;
+    for (uint32_t it = 0;; ++it) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if ((it & 63u) == 63u) {
+            if (*abort_flag) return false;
+            const long long now = clock64();
+            const int step = *steps;
+            if (t0 == 0 || step != last) { t0 = now; last = step; }
+            else if (now - t0 > WAIT_CYCLES) { *abort_flag = 1; return false; }
+        }
+    }
+}
+
 template <int DP, bool CAP, int BIAS, bool EXACT>
 __global__ void __launch_bounds__(THREADS, 1)
 softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
@@ -178,7 +198,7 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
     constexpr int PER_GROUP = 5 + 2 * QB;
     __shared__ __align__(8) unsigned long long bars[5 * NS + PER_GROUP * QT];
     __shared__ uint32_t tmem_slot;
-    __shared__ int abort_flag;
+    __shared__ int abort_flag, redo_steps;
     __shared__ float lut[BIAS == GRF_BIAS_BUCKETS ? QT * 2 * 256 : 1];
     __shared__ float tops[2][SOFT * 32], sums[SOFT * 32];
     __shared__ __align__(16) int32_t doc_of[QT * 2 * BT];
@@ -212,7 +232,7 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
     constexpr int COPY = SOFT, ISSUE = SOFT + 1, CLEAN = SOFT + 3;
 
     if (tid == 0) {
-        abort_flag = 0;
+        abort_flag = redo_steps = 0;
         for (int s = 0; s < NS; ++s) {
             mbar_init(k_full(s), 1); mbar_init(v_full(s), 1); mbar_init(v_clean(s), 1);
             mbar_init(k_empty(s), QT); mbar_init(v_empty(s), QT + 1);
@@ -256,10 +276,7 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
     __syncthreads();
     fence_after_sync();
     const uint32_t tmem = (uint32_t)uniform((int32_t)tmem_slot);
-    // (a block whose rows are all summed again takes 6 us a key: 6 s with a million, for which the other warps wait)
-    auto wait = [&](uint32_t bar, uint32_t parity) {
-        return __all_sync(0xffffffffu, mbar_wait(bar, parity, &abort_flag, p.Nk > (1 << 18) ? 16 * WAIT_CYCLES : WAIT_CYCLES)) != 0;
-    };
+    auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_beside(bar, parity, &abort_flag, &redo_steps)) != 0; };
 
     if (warp >= SOFT) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(LESS));
@@ -650,7 +667,7 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 const int y = __ffs(again) - 1;
                 again &= again - 1;
                 redo_row<CAP, EXACT>(p, bucket, b, h, __shfl_sync(0xffffffffu, i, y), __shfl_sync(0xffffffffu, m, y), __shfl_sync(0xffffffffu, l, y), half * (DP / 2),
-                              (half + 1) * (DP / 2));
+                                     (half + 1) * (DP / 2), &redo_steps);
             }
             with_other_half();                                  // (the sums are read: they may be written again)
         }

@@ -121,3 +121,34 @@ def test_rest_of_rows_that_are_summed_again(lib, mask, cap, d):  # noqa: F811
     assert not out[0, :, -1, ::3].isfinite().any()
     both = (out.double() + saved.rest.double())[:, :, :-1]
     R.assert_close(both, want["out"][:, :, :-1], bound[:, :, :-1], "out + rest")
+
+
+def test_waits_beside_rows_that_are_summed_again(lib):  # noqa: F811
+    """Every multiprocessor sums all rows of its first block again, over 2^18 keys, while its other warps wait with the second."""
+    api, B, ctx = lib
+    H, nq, nk, d = 148, 512, 1 << 18, 128
+    g = torch.Generator(device="cuda").manual_seed(6)
+    q = torch.randn(1, H, nq, d, device="cuda", generator=g).bfloat16()
+    k, v = (torch.randn(1, 1, nk, d, device="cuda", generator=g).bfloat16() for _ in range(2))
+    for x in range(4):                                  # the last key of a tile, seen by that tile's last query and later ones; a column in either half
+        v[0, 0, nk - 1 - 128 * x, [x, 64 + x]] = INF
+    torch.cuda.synchronize()
+    at = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+    at[0].record()
+    out = api.softmax_attn(ctx, q, k, v, mask="causal")
+    at[1].record()
+    torch.cuda.synchronize()
+    B.grf_ctx_check(ctx.handle)
+    print(f"{at[0].elapsed_time(at[1]):.1f} ms")
+    for h, i in ((0, 0), (1, 100), (70, 254), (71, 383), (147, 510), (147, 511)):
+        s = (k[0, 0].double() @ q[0, h, i].double()) * d ** -0.5
+        s[nk - nq + i + 1:] = -INF
+        p = torch.softmax(s, 0)
+        w = v[0, 0].double()
+        sees = (w[:nk - nq + i + 1] == INF).any(0)
+        clean = torch.where(w.isfinite(), w, 0.0)
+        want, size = p @ clean, p @ clean.abs()
+        assert torch.equal(out[0, h, i] == INF, sees) and int(sees.sum()) == 2 * ((i + 1) // 128)
+        # P and out to bf16; scores, of a size of 8 or less, and sums in 32 bits
+        bound = size * (2 * 2.0**-8 + 2.0**-16) + 1e-9
+        assert ((out[0, h, i].double() - want).abs() <= bound)[~sees].all()
