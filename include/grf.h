@@ -338,7 +338,8 @@ size_t grf_softmax_attn_workspace_bytes(const grf_ctx* ctx, const grf_softmax_de
  * from probabilities held to 2^-16 where n_q > 16 (and may differ in its last bit from a call without).  workspace: DEVICE, 256-byte aligned (may be
  * NULL where 0 bytes are needed); its contents are scratch of this call alone, so calls that may run at the same time, captured ones
  * among them, need one each.  Few queries (n_q <= 16) are served by kernels that split the keys.  bf16 products have their probabilities
- * rounded to bf16 (by at most 2^-8 relative each), sums are fp32; summation order is fixed.  Asynchronous; can be captured.
+ * rounded to bf16 (by at most 2^-8 relative each), sums are fp32; summation order is fixed.  Without lse, cap and bias, at dim > 64 in bf16, a quarter of the
+ * exponentials are within 1e-4 (relative) before that rounding.  Asynchronous; can be captured.
  * GRF_ERR_TOO_LARGE: more than GRF_MAX_TOKENS tokens, or more than 65535 (batch, head) pairs. */
 int grf_softmax_attn(grf_ctx* ctx, const grf_softmax_desc* desc, const void* Q, const void* K, const void* V, void* out, float* lse,
                      void* rest, void* workspace, size_t workspace_bytes);

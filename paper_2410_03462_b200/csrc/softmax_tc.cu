@@ -38,7 +38,7 @@ constexpr int THREADS = 32 * (SOFT + 4);
 constexpr int MORE = 104, LESS = 64;                            // registers: 4 * 104 + 64 = 5 * 96, the launch's
 
 #define FMA_PAIRS(n) ((n) % 8 == 2 || (n) % 8 == 5)             // of a thread's 32 pairs of columns
-constexpr int BIAS_NONE_SCALED = 3;     // no bias, scores scaled before anything else
+constexpr int BIAS_NONE_SCALED = 3;     // no bias, scores scaled before anything else, every exponential by its own instruction
 
 // What a block of queries sees.
 struct forward_tiles {
@@ -193,7 +193,7 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
     // some exponentials by multiply-adds: at d > 64, where nothing else is done to the scores, 4096 causal keys 165 -> 161 us (and 4096 seen ones 353 ->
     // 345); with d = 64, caps or biases, whose own arithmetic fills that pipe, it costs up to a tenth
     constexpr bool FMA = DP == 128 && BIAS == GRF_BIAS_NONE && !CAP && !EXACT;
-    constexpr bool PLAIN = BIAS == GRF_BIAS_NONE && !CAP;   // (a scale that is not positive: BIAS_NONE_SCALED)
+    constexpr bool PLAIN = BIAS == GRF_BIAS_NONE && !CAP;   // (a scale that is not positive, or lse wanted at d > 64: BIAS_NONE_SCALED)
     extern __shared__ unsigned char smem_dyn[];
     constexpr int PER_GROUP = 5 + 2 * QB;
     __shared__ __align__(8) unsigned long long bars[5 * NS + PER_GROUP * QT];
@@ -698,8 +698,9 @@ template <int DP, bool CAP, int BIAS, bool EXACT> int launch(grf_ctx* ctx, const
 
 template <int DP, bool EXACT, bool CAP> int by_bias(grf_ctx* ctx, const grf_softmax_params& p, const forward_maps& m)
 {
+    // (lse is a sum of fp32 exponentials: where it is wanted, none by multiply-adds)
     if constexpr (!CAP)
-        if (p.bias == GRF_BIAS_NONE && !(p.scale > 0.0f)) return launch<DP, CAP, BIAS_NONE_SCALED, EXACT>(ctx, p, m);
+        if (p.bias == GRF_BIAS_NONE && (!(p.scale > 0.0f) || (DP == 128 && !EXACT && p.lse_w))) return launch<DP, CAP, BIAS_NONE_SCALED, EXACT>(ctx, p, m);
     return p.bias == GRF_BIAS_NONE ? launch<DP, CAP, GRF_BIAS_NONE, EXACT>(ctx, p, m)
          : p.bias == GRF_BIAS_SLOPES ? launch<DP, CAP, GRF_BIAS_SLOPES, EXACT>(ctx, p, m) : launch<DP, CAP, GRF_BIAS_BUCKETS, EXACT>(ctx, p, m);
 }

@@ -123,6 +123,28 @@ def test_rest_of_rows_that_are_summed_again(lib, mask, cap, d):  # noqa: F811
     R.assert_close(both, want["out"][:, :, :-1], bound[:, :, :-1], "out + rest")
 
 
+@pytest.mark.parametrize("scale", [1.0, 0.5])
+def test_lse_of_a_call_without_rest(lib, scale):  # noqa: F811
+    """lse as fp32 sums of fp32 exponentials, where all of a row's weight lies on one or two keys, whichever they are."""
+    api, B, ctx = lib
+    nq = nk = 128
+    d = 128
+    q, k = torch.zeros(1, 1, nq, d), torch.zeros(1, 1, nk, d)
+    q[0, 0, :, 0] = 1 + torch.arange(nq) / 128.0        # products of eight bits by eight: exact in fp32
+    pair = torch.arange(nk) // 2
+    v = torch.randn(1, 1, nk, d, generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+    for first in range(64):
+        k[0, 0, :, 0] = torch.where(pair == first, 1.5 + (torch.arange(nk) & 1) * 0.75, torch.tensor(-30.0))
+        qc, kc = q.bfloat16().cuda(), k.bfloat16().cuda()
+        want = R.reference(qc, kc, v, scale=scale)
+        s = api._softmax_desc(ctx, qc, kc, v, scale, 0.0, "full", None, None, None, None, None, None, None, None, False)
+        out, lse = torch.empty_like(v), torch.empty(1, 1, nq, device="cuda")
+        B.grf_softmax_attn(ctx.handle, s, qc, kc, v, out, lse, None, None, 0)
+        R.assert_close(out, want["out"], want["out_tol"], "out")
+        # scores below 16 in units of log 2, three roundings; an exponential of 2^-22; a logarithm and two roundings of lse below 8
+        R.assert_close(lse, want["lse"], 3 * 8 * R.U + 2.0**-22 + 3 * 8 * R.U, f"lse, keys {2 * first} and the next")
+
+
 def test_waits_beside_rows_that_are_summed_again(lib):  # noqa: F811
     """Every multiprocessor sums all rows of its first block again, over 2^18 keys, while its other warps wait with the second."""
     api, B, ctx = lib
