@@ -80,6 +80,13 @@ template <typename T> __device__ __forceinline__ __nv_bfloat16 grf_rest(float x,
     return __float2bfloat16_rn(r == r ? r : 0.0f);              // (an infinity or NaN has none)
 }
 
+// The slope of head h in units of log 2: finite where the slope is (an infinity would make NaN of distance 0).
+__device__ __forceinline__ float grf_slope2(const grf_softmax_params& p, int32_t h)
+{
+    const float a = p.slopes[h], a2 = a * GRF_LOG2E;
+    return fabsf(a) <= 3.4028235e38f ? fminf(fmaxf(a2, -3.4028235e38f), 3.4028235e38f) : a2;
+}
+
 // The bias of relative position delta for head h, in units of log 2.
 template <typename T>
 __device__ __forceinline__ float grf_bias2(const grf_softmax_params& p, const grf_buckets& bucket, int32_t h, int32_t delta)

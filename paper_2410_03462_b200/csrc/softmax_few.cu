@@ -387,7 +387,7 @@ __global__ void __launch_bounds__(THREADS) softmax_few_f32_kernel(const __grid_c
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
         row[r].set(p, sight, qdoc, kvh, r0 + r, f.rows);
-        slope2[r] = p.bias == GRF_BIAS_SLOPES ? -p.slopes[row[r].h] * GRF_LOG2E : 0.0f;
+        slope2[r] = p.bias == GRF_BIAS_SLOPES ? -grf_slope2(p, row[r].h) : 0.0f;
         m[r] = -CUDART_INF_F;
         l[r] = 0.0f;
 #pragma unroll

@@ -458,7 +458,7 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             const int32_t limit = (sight.order == GRF_ORDER_FULL ? sight.len : min(sight.len, max(pos + 1, sight.prefix))) - c0;
             int32_t doc = sight.docs && i < p.Nq ? p.q_doc[(int64_t)b * p.Nq + i] : -1;
             if (doc < 0) doc = INT32_MIN;                       // (equal to no key's: these are -1 where they are negative)
-            const float slope2 = BIAS == GRF_BIAS_SLOPES ? p.slopes[h] * GRF_LOG2E : 0.0f;
+            const float slope2 = BIAS == GRF_BIAS_SLOPES ? grf_slope2(p, h) : 0.0f;
             float m = -CUDART_INF_F;
             uint64_t sum2[2] = {0ull, 0ull};
             int32_t c = 0;
@@ -503,8 +503,9 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 if (!PLAIN) {
                     const uint64_t by = CAP ? pack2(cap2, cap2) : pack2(to2, to2);
                     const float ahead = (float)(j0 + c0 - pos); // (exact, as are its sums, below 2^24; beyond, off by half a step as the distance itself)
-                    const bool line = BIAS == GRF_BIAS_SLOPES && (sight.order == GRF_ORDER_CAUSAL || __all_sync(0xffffffffu, j0 + BT - 1 <= pos));
-                    // (keys behind a causal query are not seen: before it, the distance is a line)
+                    // A tile's length or more before the query the distance is a line, which starts at the tile's first key; nearer than that its two parts would be
+                    // far larger than their sum, and the score be rounded to their steps (slopes of 1e4: lse off by 3e-4, and gradients with it).
+                    const bool line = BIAS == GRF_BIAS_SLOPES && __all_sync(0xffffffffu, j0 + 2 * BT - 1 <= pos);
                     const float at0 = line ? slope2 * ahead : bias2;
                     const uint64_t at02 = pack2(at0, at0);
 #pragma unroll

@@ -369,7 +369,7 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             const bool any = !(fabsf(lse) > LARGEST);               // a row without a key, or one whose scores tell nothing any more: P = 0
             const bool empties = __any_sync(0xffffffffu, !any);
             const float minus_lse = any ? -lse * GRF_LOG2E : -CUDART_INF_F;
-            const float slope2 = BIAS == GRF_BIAS_SLOPES ? p.slopes[h] * GRF_LOG2E : 0.0f;
+            const float slope2 = BIAS == GRF_BIAS_SLOPES ? grf_slope2(p, h) : 0.0f;
             float far_sum = 0.0f;                                   // of dS in tiles of one bucket, until the bucket changes
             int32_t far_bucket = -1;
             auto flush = [&]() {
@@ -418,7 +418,7 @@ softmax_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     tmem_ld_wait();
                     if (CAP) capped<W / 16>(sv, by_cap);
                     const float ahead = (float)(j0 + c0 - pos);
-                    const bool line = BIAS == GRF_BIAS_SLOPES && (sight.order == GRF_ORDER_CAUSAL || __all_sync(0xffffffffu, j0 + c0 + W - 1 <= pos));
+                    const bool line = BIAS == GRF_BIAS_SLOPES && __all_sync(0xffffffffu, j0 + c0 + 2 * W - 1 <= pos);    // (as in the forward pass)
                     const float at0 = minus_lse + (BIAS == GRF_BIAS_SLOPES ? (line ? slope2 * ahead : 0.0f) : bias2);
                     const uint64_t by = CAP ? pack2(cap2, cap2) : pack2(to2, to2), at02 = pack2(at0, at0);
 #pragma unroll
@@ -849,7 +849,7 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                     const bool partial = sight.docs ? !T.whole(t) : block_partial || (ordered && pos0 < j0 + BT - 1);
                     // columns from `from` on see this key
                     const int32_t from = j >= sight.len ? BT : sight.order == GRF_ORDER_FULL || j < sight.prefix ? 0 : min(max(j - pos0, 0), BT);
-                    const float slope2 = BIAS == GRF_BIAS_SLOPES ? p.slopes[h] * GRF_LOG2E : 0.0f;
+                    const float slope2 = BIAS == GRF_BIAS_SLOPES ? grf_slope2(p, h) : 0.0f;
                     float bias2 = 0.0f;
                     bool diagonals = false;
                     const float* mine = lut;

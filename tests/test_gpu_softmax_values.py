@@ -145,6 +145,38 @@ def test_lse_of_a_call_without_rest(lib, scale):  # noqa: F811
         R.assert_close(lse, want["lse"], 3 * 8 * R.U + 2.0**-22 + 3 * 8 * R.U, f"lse, keys {2 * first} and the next")
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("nq", [5, 300])
+@pytest.mark.parametrize("mask", ["causal", "full"])
+@pytest.mark.parametrize("slope", [1.0e4, 1.0e6, 1.0e37, 3.0e38])
+def test_steep_slopes(lib, route, dtype, mask, nq, slope):  # noqa: F811
+    """Slopes so steep that a query is left with its own position: that score is not rounded to the steps of the others' biases."""
+    if dtype == "fp32" and route == "alu":
+        pytest.skip("fp32 has one route")
+    api, _, ctx = lib
+    d = 64
+    x, _, dout = make(71, 1, 2, 1, nq, 300, d, dtype)
+    how = {"mask": mask, "slopes": torch.full((2,), slope, device="cuda")}
+    out, saved = api.softmax_attn(ctx, x["q"], x["k"], x["v"], want_lse=True, **how)
+    Q, K, V, G = (t.double().cpu().numpy() for t in (x["q"], x["k"], x["v"], dout))
+    own = slice(300 - nq, 300)
+    s = (Q * K[:, :, own]).sum(-1) * d ** -0.5
+    e = (d + 8) * R.U * ((np.abs(Q) * np.abs(K[:, :, own])).sum(-1) * d ** -0.5 + np.abs(s) + 1)
+    R.assert_close(saved.lse, s, 2 * e, "lse")
+    r = R.HALF_STEP[DT[dtype]]
+    R.assert_close(out, np.broadcast_to(V[:, :, own], out.shape), 4 * e[..., None] * np.abs(V[:, :, own]) + 1e-30, "out")
+    dq, dk, dv, _ = api.softmax_attn_backward(ctx, x["q"], x["k"], x["v"], out, saved, dout, **how)
+    # P = 1 within the error of s - lse, then rounded; dv of a key: the two heads' dout of its query
+    want = np.zeros(V.shape)
+    want[:, 0, own] = G.sum(1)
+    bound = np.zeros(V.shape)
+    bound[:, 0, own] = ((4 * e[..., None] + r) * np.abs(G)).sum(1) + (r + 8 * R.U) * np.abs(G.sum(1))
+    R.assert_close(dv, want, bound, "dv")
+    # dS = P (dP - D) of two sums of the same products
+    ds = (4 * d * R.U) * (np.abs(G) * np.abs(V[:, :, own])).sum(-1) + 1e-30
+    assert (np.abs(dq.double().cpu().numpy()) <= (1 + 2 * r) * ds[..., None] * d ** -0.5 * np.abs(K[:, :, own]) + 1e-30).all()
+
+
 def test_waits_beside_rows_that_are_summed_again(lib):  # noqa: F811
     """Every multiprocessor sums all rows of its first block again, over 2^18 keys, while its other warps wait with the second."""
     api, B, ctx = lib
