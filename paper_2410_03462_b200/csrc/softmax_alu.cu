@@ -37,67 +37,82 @@ template <int DP> struct Alu {
 
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) <= 3.4028235e38f; }
 
+// A chunk of a row as floats.  clean: what is not finite becomes 0; true if there was any.
+template <typename T> __device__ __forceinline__ bool to_floats(float (&v)[16 / sizeof(T)], const uint4& w, bool clean)
+{
+    const T* t = reinterpret_cast<const T*>(&w);
+    bool found = false;
+#pragma unroll
+    for (int e = 0; e < 16 / (int)sizeof(T); ++e) {
+        v[e] = grf_to_float(t[e]);
+        if (clean && !finite(v[e])) {
+            v[e] = 0.0f;
+            found = true;
+        }
+    }
+    return found;
+}
+// bad[r]: whether any lane of row r has found something (PER lanes a row, all of the warp here)
+template <int PER> __device__ __forceinline__ void mark_row(int* bad, int r, bool found)
+{
+    const uint32_t who = __ballot_sync(0xffffffffu, found), lane = threadIdx.x & 31u;
+    if (lane % PER == 0) bad[r] = (who >> lane & (0xffffffffu >> (32 - PER))) != 0u;
+}
+
 // Rows r0 .. r0 + 63 of [tokens][d] as floats: zeros behind `rows`, behind d, and for tokens whose document is negative.  clean: what is not
-// finite becomes 0 too and sets *bad.
+// finite becomes 0 too; true if this thread has found any, and bad (or NULL) says in which rows there is some.
 template <typename T, int DP>
-__device__ __forceinline__ void load_rows(float* tile, const T* base, int64_t stride, int32_t r0, int32_t rows, int32_t d, const int32_t* doc,
+__device__ __forceinline__ bool load_rows(float* tile, const T* base, int64_t stride, int32_t r0, int32_t rows, int32_t d, const int32_t* doc,
                                           bool clean, int* bad)
 {
     constexpr int CH = 16 / (int)sizeof(T), PER = DP / CH;
+    static_assert(BT * PER % THREADS == 0 && 32 % PER == 0, "rows are whole warps' business");
+    bool any = false;
     for (int x = threadIdx.x; x < BT * PER; x += THREADS) {
         const int r = x / PER, c = x % PER * CH;
         float v[CH];
+        bool found = false;
 #pragma unroll
         for (int e = 0; e < CH; ++e) v[e] = 0.0f;
         if (r0 + r < rows && c < d && (!doc || doc[r0 + r] >= 0)) {
-            const uint4 w = *reinterpret_cast<const uint4*>(base + (int64_t)(r0 + r) * stride + c);
-            const T* t = reinterpret_cast<const T*>(&w);
-#pragma unroll
-            for (int e = 0; e < CH; ++e) {
-                v[e] = grf_to_float(t[e]);
-                if (clean && !finite(v[e])) {
-                    v[e] = 0.0f;
-                    if (bad) *bad = 1;
-                }
-            }
+            found = to_floats<T>(v, *reinterpret_cast<const uint4*>(base + (int64_t)(r0 + r) * stride + c), clean);
         }
+        if (bad) mark_row<PER>(bad, r, found);
+        any |= found;
 #pragma unroll
         for (int e = 0; e < CH; e += 4) *reinterpret_cast<float4*>(tile + r * Alu<DP>::ROW + c + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
     }
+    return any;
 }
 
 // The same in two steps, so that a tile's loads are under way while the one before is computed (d <= 64: they fit in registers).
 template <typename T, int DP> struct rows_ahead {
-    static constexpr int CH = 16 / (int)sizeof(T), PER = DP / CH, N = (BT * PER + THREADS - 1) / THREADS;
+    static constexpr int CH = 16 / (int)sizeof(T), PER = DP / CH, N = BT * PER / THREADS;
+    static_assert(BT * PER % THREADS == 0, "no thread is left out");
     uint4 w[N];
     __device__ __forceinline__ void fetch(const T* base, int64_t stride, int32_t r0, int32_t rows, int32_t d, const int32_t* doc)
     {
 #pragma unroll
         for (int y = 0; y < N; ++y) {
             const int x = threadIdx.x + y * THREADS, r = x / PER, c = x % PER * CH;
-            w[y] = x < BT * PER && r0 + r < rows && c < d && (!doc || doc[r0 + r] >= 0) ? *reinterpret_cast<const uint4*>(base + (int64_t)(r0 + r) * stride + c)
+            w[y] = r0 + r < rows && c < d && (!doc || doc[r0 + r] >= 0) ? *reinterpret_cast<const uint4*>(base + (int64_t)(r0 + r) * stride + c)
                                                                                           : make_uint4(0, 0, 0, 0);
         }
     }
-    __device__ __forceinline__ void store(float* tile, bool clean, int* bad) const
+    __device__ __forceinline__ bool store(float* tile, bool clean, int* bad) const
     {
+        bool any = false;
 #pragma unroll
         for (int y = 0; y < N; ++y) {
             const int x = threadIdx.x + y * THREADS, r = x / PER, c = x % PER * CH;
-            if (x >= BT * PER) continue;
-            const T* t = reinterpret_cast<const T*>(&w[y]);
             float v[CH];
-#pragma unroll
-            for (int e = 0; e < CH; ++e) {
-                v[e] = grf_to_float(t[e]);
-                if (clean && !finite(v[e])) {
-                    v[e] = 0.0f;
-                    if (bad) *bad = 1;
-                }
-            }
+            const bool found = to_floats<T>(v, w[y], clean);
+            if (bad) mark_row<PER>(bad, r, found);
+            any |= found;
 #pragma unroll
             for (int e = 0; e < CH; e += 4) *reinterpret_cast<float4*>(tile + r * Alu<DP>::ROW + c + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
         }
+        return any;
     }
 };
 
@@ -261,11 +276,11 @@ __global__ void __launch_bounds__(THREADS, DP <= 64 ? 2 : 1) softmax_alu_forward
         __syncthreads();
         if constexpr (AHEAD) {
             ka.store(ks, false, nullptr);
-            va.store(vs, what == 1, &bad);
+            if (va.store(vs, what == 1, nullptr)) bad = 1;
             fetch(j_next);
         } else {
             load_rows<T, DP>(ks, K, p.ks[2], j0, sight.len, p.d, kdoc, false, nullptr);
-            load_rows<T, DP>(vs, V, p.vs[2], j0, sight.len, p.d, kdoc, what == 1, &bad);
+            if (load_rows<T, DP>(vs, V, p.vs[2], j0, sight.len, p.d, kdoc, what == 1, nullptr)) bad = 1;
         }
         load_bias<T>(lut, p, bucket, h, j0, sight.position(i0));
         __syncthreads();
@@ -413,7 +428,7 @@ __device__ __forceinline__ alu_row load_alu_row(const grf_softmax_params& p, con
     return w;
 }
 __device__ __forceinline__ void score_gradient(const grf_softmax_params& p, const grf_sight& sight, const alu_row& w, const int32_t* kdoc, int what,
-                                               int32_t j, float bias2, float& s, float& dp, float& ds)
+                                               int32_t j, float bias2, bool spoilt, float& s, float& dp, float& ds)
 {
     float t = 0.0f, x;
     if (p.cap > 0.0f) { t = tanhf(s * (p.scale / p.cap)); x = p.cap * GRF_LOG2E * t; }
@@ -426,6 +441,8 @@ __device__ __forceinline__ void score_gradient(const grf_softmax_params& p, cons
     dp = p.cap > 0.0f ? (seen ? ds * (1.0f - t * t) : 0.0f) : ds;
     // a row of dout that is not finite was left out of the products of a tile that is not seen whole
     if (seen && !finite(w.dsum)) s = CUDART_NAN_F;
+    // and so was a row of q or k that is not: its scores are not those that the row has
+    if (seen && spoilt) s = dp = ds = CUDART_NAN_F;
 }
 
 template <typename T, int DP>
@@ -435,6 +452,7 @@ __global__ void __launch_bounds__(THREADS, DP <= 64 ? 2 : 1) softmax_alu_dq_kern
     extern __shared__ float smem[];
     float *qs = smem, *gs = qs + A::TILE, *ks = gs + A::TILE, *vs = ks + A::TILE, *xt = vs + A::TILE, *st = xt + BT * PS;
     __shared__ grf_buckets bucket;
+    __shared__ int bad_key[BT];
     __shared__ float lut[2 * BT], bins[4][2 * GRF_MAX_BUCKETS];   // sums by bucket, of diagonals 32 w .. 32 w + 31 of each tile
     const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
     bucket.fill(p);
@@ -476,17 +494,18 @@ __global__ void __launch_bounds__(THREADS, DP <= 64 ? 2 : 1) softmax_alu_dq_kern
     for (int32_t j0 = j_next; j0 < end; j0 = j_next) {
         const int what = what_of(j0);
         j_next = seen_from(j0 + f.splits * BT);
+        bool found;
         __syncthreads();
         if constexpr (AHEAD) {
-            ka.store(ks, what == 1, nullptr);
+            found = ka.store(ks, what == 1, bad_key);
             va.store(vs, false, nullptr);
             fetch(j_next);
         } else {
-            load_rows<T, DP>(ks, K, p.ks[2], j0, sight.len, p.d, kdoc, what == 1, nullptr);
+            found = load_rows<T, DP>(ks, K, p.ks[2], j0, sight.len, p.d, kdoc, what == 1, bad_key);
             load_rows<T, DP>(vs, V, p.vs[2], j0, sight.len, p.d, kdoc, false, nullptr);
         }
         load_bias<T>(lut, p, bucket, h, j0, sight.position(i0));
-        __syncthreads();
+        const bool any_bad = __syncthreads_or(found);
         float s[4][4], dp[4][4];
         products<DP>(s, qs, ks, ty, tx);
         products<DP>(dp, gs, vs, ty, tx);
@@ -496,7 +515,7 @@ __global__ void __launch_bounds__(THREADS, DP <= 64 ? 2 : 1) softmax_alu_dq_kern
             for (int c = 0; c < 4; ++c) {
                 const int i = 4 * ty + r, j = tx + 16 * c;
                 float ds;
-                score_gradient(p, sight, row[r], kdoc, what, j0 + j, p.bias != GRF_BIAS_NONE ? lut[j - i + BT - 1] : 0.0f, s[r][c], dp[r][c], ds);
+                score_gradient(p, sight, row[r], kdoc, what, j0 + j, p.bias != GRF_BIAS_NONE ? lut[j - i + BT - 1] : 0.0f, any_bad && bad_key[j], s[r][c], dp[r][c], ds);
                 if (p.dtable_part) st[i * PS + j] = ds;
             }
 #pragma unroll
@@ -547,6 +566,7 @@ __global__ void __launch_bounds__(THREADS, DP <= 64 ? 2 : 1) softmax_alu_dkv_ker
     using A = Alu<DP>;
     extern __shared__ float smem[];
     float *qs = smem, *gs = qs + A::TILE, *ks = gs + A::TILE, *vs = ks + A::TILE, *ps = vs + A::TILE, *xs = ps + BT * PS;
+    __shared__ int bad_query[BT];
     __shared__ float lut[2 * BT];
     __shared__ grf_buckets bucket;
     const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
@@ -588,17 +608,18 @@ __global__ void __launch_bounds__(THREADS, DP <= 64 ? 2 : 1) softmax_alu_dkv_ker
         const int32_t h = kvh * p.group + x / qblocks, i0 = x % qblocks * BT;
         const int what = what_of(x);
         x_next = seen_from(x + f.splits);
+        bool found;
         __syncthreads();
         if constexpr (AHEAD) {
-            qa.store(qs, what == 1, nullptr);
+            found = qa.store(qs, what == 1, bad_query);
             ga.store(gs, what == 1, nullptr);
             fetch(x_next);
         } else {
-            load_rows<T, DP>(qs, at_head<T>(p.q, p.qs, b, h), p.qs[2], i0, p.Nq, p.d, qdoc, what == 1, nullptr);
+            found = load_rows<T, DP>(qs, at_head<T>(p.q, p.qs, b, h), p.qs[2], i0, p.Nq, p.d, qdoc, what == 1, bad_query);
             load_rows<T, DP>(gs, at_head<T>(p.dout, p.dos, b, h), p.dos[2], i0, p.Nq, p.d, qdoc, what == 1, nullptr);
         }
         load_bias<T>(lut, p, bucket, h, j0, sight.position(i0));
-        __syncthreads();
+        const bool any_bad = __syncthreads_or(found);
         float s[4][4], dp[4][4];
         products<DP>(s, qs, ks, ty, tx);
         products<DP>(dp, gs, vs, ty, tx);
@@ -610,7 +631,7 @@ __global__ void __launch_bounds__(THREADS, DP <= 64 ? 2 : 1) softmax_alu_dkv_ker
             for (int c = 0; c < 4; ++c) {
                 const int j = tx + 16 * c;
                 float ds;
-                score_gradient(p, sight, w, kdoc, what, j0 + j, p.bias != GRF_BIAS_NONE ? lut[j - i + BT - 1] : 0.0f, s[r][c], dp[r][c], ds);
+                score_gradient(p, sight, w, kdoc, what, j0 + j, p.bias != GRF_BIAS_NONE ? lut[j - i + BT - 1] : 0.0f, any_bad && bad_query[i], s[r][c], dp[r][c], ds);
                 ps[i * PS + j] = s[r][c];
                 xs[i * PS + j] = dp[r][c];
             }

@@ -177,6 +177,25 @@ def test_steep_slopes(lib, route, dtype, mask, nq, slope):  # noqa: F811
     assert (np.abs(dq.double().cpu().numpy()) <= (1 + 2 * r) * ds[..., None] * d ** -0.5 * np.abs(K[:, :, own]) + 1e-30).all()
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("bad", [INF, -INF, NAN])
+@pytest.mark.parametrize("who", ["q", "k"])
+def test_gradients_of_infinite_capped_scores(lib, route, dtype, bad, who):  # noqa: F811
+    """A value that is not finite in what is seen leaves no finite gradient beside it: 0 times infinity is NaN."""
+    if dtype == "fp32" and route == "alu":
+        pytest.skip("fp32 has one route")
+    api, _, ctx = lib
+    x, how, dout = make(79, 2, 2, 1, 100, 100, 64, dtype, mask="causal", cap=10.0)
+    x[who][0, 0, 50, 7] = bad
+    o = api.softmax_attn(ctx, x["q"], x["k"], x["v"], want_lse=True, **how)
+    dq, dk, dv, _ = api.softmax_attn_backward(ctx, x["q"], x["k"], x["v"], *o, dout, **how)
+    if who == "k":
+        assert not dq[0, :, 50:, 7].isfinite().any()
+    else:
+        assert not dk[0, 0, :51, 7].isfinite().any()
+    assert dq[1].isfinite().all() and dk[1].isfinite().all() and dv[1].isfinite().all()
+
+
 def test_waits_beside_rows_that_are_summed_again(lib):  # noqa: F811
     """Every multiprocessor sums all rows of its first block again, over 2^18 keys, while its other warps wait with the second."""
     api, B, ctx = lib
