@@ -439,7 +439,7 @@ __device__ __forceinline__ void score_gradient(const grf_softmax_params& p, cons
     s = seen ? exp2f(x - w.lse2) : 0.0f;
     ds = seen ? s * (dp - w.dsum) : 0.0f;
     dp = p.cap > 0.0f ? (seen ? ds * (1.0f - t * t) : 0.0f) : ds;
-    // a row of dout that is not finite was left out of the products of a tile that is not seen whole
+    // a row of dout that is not finite was left out of the products (0 times it, where it is not seen or has no scores, would be NaN)
     if (seen && !finite(w.dsum)) s = CUDART_NAN_F;
     // and so was a row of q or k that is not: its scores are not those that the row has
     if (seen && spoilt) s = dp = ds = CUDART_NAN_F;
@@ -497,11 +497,11 @@ __global__ void __launch_bounds__(THREADS, DP <= 64 ? 2 : 1) softmax_alu_dq_kern
         bool found;
         __syncthreads();
         if constexpr (AHEAD) {
-            found = ka.store(ks, what == 1, bad_key);
+            found = ka.store(ks, true, bad_key);
             va.store(vs, false, nullptr);
             fetch(j_next);
         } else {
-            found = load_rows<T, DP>(ks, K, p.ks[2], j0, sight.len, p.d, kdoc, what == 1, bad_key);
+            found = load_rows<T, DP>(ks, K, p.ks[2], j0, sight.len, p.d, kdoc, true, bad_key);
             load_rows<T, DP>(vs, V, p.vs[2], j0, sight.len, p.d, kdoc, false, nullptr);
         }
         load_bias<T>(lut, p, bucket, h, j0, sight.position(i0));
@@ -611,12 +611,12 @@ __global__ void __launch_bounds__(THREADS, DP <= 64 ? 2 : 1) softmax_alu_dkv_ker
         bool found;
         __syncthreads();
         if constexpr (AHEAD) {
-            found = qa.store(qs, what == 1, bad_query);
-            ga.store(gs, what == 1, nullptr);
+            found = qa.store(qs, true, bad_query);
+            ga.store(gs, true, nullptr);
             fetch(x_next);
         } else {
-            found = load_rows<T, DP>(qs, at_head<T>(p.q, p.qs, b, h), p.qs[2], i0, p.Nq, p.d, qdoc, what == 1, bad_query);
-            load_rows<T, DP>(gs, at_head<T>(p.dout, p.dos, b, h), p.dos[2], i0, p.Nq, p.d, qdoc, what == 1, nullptr);
+            found = load_rows<T, DP>(qs, at_head<T>(p.q, p.qs, b, h), p.qs[2], i0, p.Nq, p.d, qdoc, true, bad_query);
+            load_rows<T, DP>(gs, at_head<T>(p.dout, p.dos, b, h), p.dos[2], i0, p.Nq, p.d, qdoc, true, nullptr);
         }
         load_bias<T>(lut, p, bucket, h, j0, sight.position(i0));
         const bool any_bad = __syncthreads_or(found);

@@ -178,6 +178,38 @@ def test_steep_slopes(lib, route, dtype, mask, nq, slope):  # noqa: F811
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("cap", [0.0, 10.0])
+@pytest.mark.parametrize("d", [40, 128])
+def test_rows_whose_scores_are_all_lowest(lib, route, dtype, cap, d):  # noqa: F811
+    """Queries that only see keys with a bias of -infinity, in tiles that they see whole: nothing of theirs reaches a gradient, NaN neither."""
+    if dtype == "fp32" and route == "alu":
+        pytest.skip("fp32 has one route")
+    api, _, ctx = lib
+    nq, nk = 256, 64
+    x, how, dout = make(73, 1, 2, 1, nq, nk, d, dtype, cap=cap)
+    how.update(first=[0, 200], table=torch.tensor([[0.5, -INF], [1.0, -INF]], dtype=DT[dtype], device="cuda"), two_sided=False,
+               q_start=torch.tensor([100], dtype=torch.int32, device="cuda"))
+    o, saved = api.softmax_attn(ctx, x["q"], x["k"], x["v"], want_lse=True, **how)
+    want = api.softmax_attn_backward(ctx, x["q"], x["k"], x["v"], o, saved, dout, **how)
+    gone = torch.arange(nq) >= 163
+    assert torch.equal(saved.lse[0, 0].cpu() == -INF, gone) and (o[:, :, 163:] == 0).all()
+    dout[:, :, 163:] = NAN
+    dout[:, :, 170:] = INF
+    for y, z in zip(api.softmax_attn_backward(ctx, x["q"], x["k"], x["v"], o, saved, dout, **how), want):
+        assert torch.equal(y, z)
+    if cap:                                             # (a cap makes an infinite product finite, and -infinity of it still)
+        k, clean = x["k"].abs(), dout.clone()
+        clean[:, :, 163:] = 0
+        ref = R.reference(x["q"], k, x["v"], clean, **how)
+        o, saved = api.softmax_attn(ctx, x["q"], k, x["v"], want_lse=True, **how)
+        q = x["q"].clone()
+        q[:, :, 180:] = INF
+        for name, y in zip(("dq", "dk", "dv", "dtable"), api.softmax_attn_backward(ctx, q, k, x["v"], o, saved, dout, **how)):
+            # (out and lse are the kernel's: each bound counts once more)
+            R.assert_close(y, ref[name], 2 * ref[name + "_tol"], name)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("bad", [INF, -INF, NAN])
 @pytest.mark.parametrize("who", ["q", "k"])
 def test_gradients_of_infinite_capped_scores(lib, route, dtype, bad, who):  # noqa: F811
