@@ -303,7 +303,7 @@ typedef struct grf_softmax_desc {
     int32_t batch, heads, kv_heads, n_q, n_k;  /* kv_heads divides heads                                                     */
     int32_t dim;                       /* of Q, K and V: a multiple of 8, 8 .. 128                                           */
     int32_t dtype;                     /* of Q, K, V, out, their gradients, and the bucket table and its gradient            */
-    float scale, cap;                  /* finite; cap >= 0                                                                   */
+    float scale, cap;                  /* finite, 1.4427 times each and (with a cap) scale / cap too; cap >= 0               */
     int32_t order;                     /* GRF_ORDER_*                                                                        */
     int32_t bias;                      /* GRF_BIAS_*                                                                         */
     int32_t n_buckets, two_sided;      /* BUCKETS: 1 .. GRF_MAX_BUCKETS                                                      */

@@ -131,7 +131,8 @@ int read_desc(grf_softmax_params* p, const grf_softmax_desc* s, bool backward)
 {
     if (s->batch <= 0 || s->heads <= 0 || s->kv_heads <= 0 || s->n_q <= 0 || s->n_k <= 0 || s->heads % s->kv_heads != 0) return GRF_ERR_INVALID;
     if (s->dim < 8 || s->dim > 128 || s->dim % 8 != 0 || (s->dtype != GRF_DTYPE_F32 && s->dtype != GRF_DTYPE_BF16)) return GRF_ERR_INVALID;
-    if (!std::isfinite(s->scale) || !std::isfinite(s->cap) || s->cap < 0.0f) return GRF_ERR_INVALID;
+    if (!std::isfinite(s->scale * GRF_LOG2E) || !std::isfinite(s->cap * GRF_LOG2E) || s->cap < 0.0f) return GRF_ERR_INVALID;
+    if (s->cap > 0.0f && !std::isfinite(s->scale / s->cap)) return GRF_ERR_INVALID;         // (0 times these would be NaN)
     if (s->order < GRF_ORDER_FULL || s->order > GRF_ORDER_PREFIX || s->bias < GRF_BIAS_NONE || s->bias > GRF_BIAS_BUCKETS) return GRF_ERR_INVALID;
     if ((s->order == GRF_ORDER_PREFIX) != (s->prefix != nullptr) || (s->q_doc != nullptr) != (s->k_doc != nullptr)) return GRF_ERR_INVALID;
     if ((s->bias == GRF_BIAS_SLOPES) != (s->slopes != nullptr) || (s->bias == GRF_BIAS_BUCKETS) != (s->table != nullptr)) return GRF_ERR_INVALID;

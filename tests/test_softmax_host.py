@@ -182,3 +182,17 @@ def test_numbers_that_do_not_fit_are_refused_not_cut_off():
     for q, k in ((many, small), (small, many)):
         with pytest.raises(ValueError, match="too many tokens"):
             api.softmax_attn(Some, q, k, k)
+
+
+@pytest.mark.parametrize("fields", [dict(scale=3e38), dict(scale=-3e38), dict(cap=3e38), dict(cap=1e-40), dict(cap=1.0, scale=2.5e38), dict(cap=0.5, scale=2e38)], ids=str)
+def test_scales_and_caps_that_overflow_are_refused(fake, fields):
+    ctx = fake.context()
+    s = _desc(**fields)
+    assert _call(fake, ctx, s, ws=1 << 40) == -1 and _call(fake, ctx, s, True, ws=1 << 40) == -1
+    assert fake.launched("softmax") == 0
+
+
+@pytest.mark.parametrize("fields", [dict(scale=2e38), dict(cap=2e38), dict(cap=1e-37), dict(cap=1.0, scale=2e38), dict(cap=1e-40, scale=0.0)], ids=str)
+def test_scales_and_caps_that_do_not_overflow_are_taken(fake, fields):
+    ctx = fake.context()
+    assert _call(fake, ctx, _desc(**fields)) == 0 and _call(fake, ctx, _desc(**fields), True) == 0
