@@ -172,6 +172,8 @@ def _set_strides(to, t, name):
 
 def _softmax_desc(ctx, q, k, v, scale, cap, mask, k_len, q_start, prefix, q_doc, k_doc, slopes, table, first, two_sided):
     q_shape, k_shape = q.shape, k.shape
+    if mask not in ORDERS:
+        raise ValueError(f"mask: expected one of {', '.join(ORDERS)}")
     if len(q_shape) != 4 or len(k_shape) != 4 or v.shape != k_shape:
         raise ValueError("expected q [B, H, Nq, d] and k, v [B, KV, Nk, d]")
     batch, heads, n_q, dim = q_shape
@@ -231,6 +233,10 @@ def _scratch(nbytes, ctx):
         return torch.empty(nbytes, dtype=torch.uint8, device=ctx.torch_device)
 
 
+def _bytes(workspace):
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
 def softmax_attn(ctx: Context, q, k, v, scale=None, cap=0.0, mask="full", k_len=None, q_start=None, prefix=None, q_doc=None,
                  k_doc=None, slopes=None, table=None, first=None, two_sided=False, want_lse=False, out=None, workspace=None):
     """Softmax attention over tokens in an order (grf_softmax_attn).  q [B, H, Nq, d], k, v [B, KV, Nk, d]: CUDA tensors (fp32 or bf16)
@@ -249,7 +255,7 @@ def softmax_attn(ctx: Context, q, k, v, scale=None, cap=0.0, mask="full", k_len=
     if workspace is None:
         workspace = _scratch(B.grf_softmax_attn_workspace_bytes(ctx.handle, s, False), ctx)
     rest = _like(q) if want_lse and q.dtype == torch.bfloat16 else None
-    B.grf_softmax_attn(ctx.handle, s, q, k, v, out, lse, rest, workspace, workspace.numel() if workspace is not None else 0)
+    B.grf_softmax_attn(ctx.handle, s, q, k, v, out, lse, rest, workspace, _bytes(workspace))
     return (out, SoftmaxSaved(lse, rest)) if want_lse else out
 
 
@@ -273,7 +279,7 @@ def softmax_attn_backward(ctx: Context, q, k, v, out, saved, dout, scale=None, c
     dtable = torch.empty_like(table) if table is not None and want_dtable else None
     if workspace is None:
         workspace = _scratch(B.grf_softmax_attn_workspace_bytes(ctx.handle, s, True), ctx)
-    B.grf_softmax_attn_backward(ctx.handle, s, q, k, v, out, lse, rest, dout, dq, dk, dv, dtable, workspace, workspace.numel())
+    B.grf_softmax_attn_backward(ctx.handle, s, q, k, v, out, lse, rest, dout, dq, dk, dv, dtable, workspace, _bytes(workspace))
     return dq, dk, dv, dtable
 
 
@@ -309,5 +315,5 @@ def relative_bias_backward(ctx: Context, drows, first, two_sided=False, q_start=
     if workspace is None:
         workspace = _scratch(B.grf_relative_bias_workspace_bytes(heads, n_q, n_k, len(first), two_sided), ctx)
     B.grf_relative_bias_backward(ctx.handle, batch, heads, n_q, n_k, start, first, two_sided, B.dtype_code(drows), drows, dtable, workspace,
-                                 workspace.numel())
+                                 _bytes(workspace))
     return dtable

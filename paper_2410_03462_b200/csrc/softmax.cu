@@ -294,14 +294,14 @@ extern "C" int grf_softmax_attn_backward(grf_ctx* ctx, const grf_softmax_desc* d
                                          const float* lse, const void* rest, const void* dout, void* dQ, void* dK, void* dV, void* dtable, void* workspace,
                                          size_t workspace_bytes)
 {
-    if (!ctx || !desc || !Q || !K || !V || !out || !lse || !dout || !dQ || !dK || !dV || !workspace) return GRF_ERR_INVALID;
+    if (!ctx || !desc || !Q || !K || !V || !out || !lse || !dout || !dQ || !dK || !dV) return GRF_ERR_INVALID;
     grf_softmax_params p;
     GRF_TRY(read_desc(&p, desc, true));
     if (dtable && p.bias != GRF_BIAS_BUCKETS) return GRF_ERR_INVALID;
     if (rest && desc->dtype != GRF_DTYPE_BF16) return GRF_ERR_INVALID;
     for (const void* x : {Q, K, V, out, rest, dout, (const void*)dQ, (const void*)dK, (const void*)dV})
         if (!aligned(x, 16)) return GRF_ERR_INVALID;
-    if (!aligned(workspace, 256)) return GRF_ERR_INVALID;
+    if (!workspace || !aligned(workspace, 256)) return GRF_ERR_INVALID;
     const backward_room r(p);
     if (r.bytes > workspace_bytes) return GRF_ERR_WORKSPACE;
     GRF_CUDA_TRY(cudaSetDevice(ctx->device));
@@ -606,9 +606,10 @@ extern "C" int grf_relative_bias_backward(grf_ctx* ctx, int32_t batch, int32_t h
                                           int32_t n_buckets, int two_sided, const int32_t* first, int dtype, const void* drows, void* dtable,
                                           void* workspace, size_t workspace_bytes)
 {
-    if (!ctx || batch <= 0 || !drows || !dtable || !workspace || !aligned(drows, 16) || !aligned(workspace, 256)) return GRF_ERR_INVALID;
+    if (!ctx || batch <= 0 || !drows || !dtable || !aligned(drows, 16)) return GRF_ERR_INVALID;
     bias_shape s;
     GRF_TRY(read_bias(&s, heads, n_q, n_k, q_start, n_buckets, two_sided, first, dtype));
+    if (!workspace || !aligned(workspace, 256)) return GRF_ERR_INVALID;
     if (workspace_bytes < grf_relative_bias_workspace_bytes(heads, n_q, n_k, n_buckets, two_sided)) return GRF_ERR_WORKSPACE;
     s.strips = bias_strips(heads, n_q, SUM_CTAS);
     GRF_CUDA_TRY(cudaSetDevice(ctx->device));

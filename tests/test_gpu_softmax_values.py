@@ -228,6 +228,25 @@ def test_gradients_of_infinite_capped_scores(lib, route, dtype, bad, who):  # no
     assert dq[1].isfinite().all() and dk[1].isfinite().all() and dv[1].isfinite().all()
 
 
+def test_refusals_of_the_backward_calls(lib):  # noqa: F811
+    """What the library refuses is its error in every call, whoever brings the workspace."""
+    api, B, ctx = lib
+    x, how, dout = make(101, 1, 2, 1, 20, 20, 136, "bf16")
+    with pytest.raises(B.GrfError) as e:
+        api.softmax_attn(ctx, x["q"], x["k"], x["v"])
+    assert e.value.code == B.GRF_ERR_INVALID
+    saved = api.SoftmaxSaved(torch.zeros(1, 2, 20, device="cuda"), None)
+    with pytest.raises(B.GrfError) as e:
+        api.softmax_attn_backward(ctx, x["q"], x["k"], x["v"], x["q"], saved, dout)
+    assert e.value.code == B.GRF_ERR_INVALID
+    with pytest.raises(B.GrfError) as e:
+        api.relative_bias_backward(ctx, torch.zeros(2, 20, 20, device="cuda"), list(range(65)))
+    assert e.value.code == B.GRF_ERR_INVALID
+    x, how, dout = make(101, 1, 2, 1, 20, 20, 64, "bf16")
+    with pytest.raises(ValueError):
+        api.softmax_attn(ctx, x["q"], x["k"], x["v"], mask="casual")
+
+
 def test_waits_beside_rows_that_are_summed_again(lib):  # noqa: F811
     """Every multiprocessor sums all rows of its first block again, over 2^18 keys, while its other warps wait with the second."""
     api, B, ctx = lib

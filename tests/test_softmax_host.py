@@ -196,3 +196,26 @@ def test_scales_and_caps_that_overflow_are_refused(fake, fields):
 def test_scales_and_caps_that_do_not_overflow_are_taken(fake, fields):
     ctx = fake.context()
     assert _call(fake, ctx, _desc(**fields)) == 0 and _call(fake, ctx, _desc(**fields), True) == 0
+
+
+def test_calls_too_large_are_told_so_without_a_workspace(fake):
+    """A size of 0 is what a caller gets for them, so there is no workspace to bring."""
+    ctx = fake.context()
+    p = lambda x: C.c_void_p(x)  # noqa: E731
+    s = _desc(batch=40000)
+    fn = fake.lib.grf_softmax_attn_backward
+    assert fn(ctx, C.byref(s), *(p(x) for x in (SOME,) * 5), None, *(p(x) for x in (SOME,) * 4), None, None, C.c_size_t(0)) == -2
+    assert fn(ctx, C.byref(_desc()), *(p(x) for x in (SOME,) * 5), None, *(p(x) for x in (SOME,) * 4), None, None, C.c_size_t(0)) == -1
+    first = np.array([0, 1, 4], np.int32).ctypes.data_as(C.c_void_p)
+    assert fake.lib.grf_relative_bias_backward(ctx, 1, 65536, 1, 1, 0, 3, 1, first, 0, p(SOME), p(SOME), None, C.c_size_t(0)) == -2
+    assert fake.lib.grf_relative_bias_backward(ctx, 1, 4, 1, 1, 0, 3, 1, first, 0, p(SOME), p(SOME), None, C.c_size_t(0)) == -1
+
+
+def test_masks_that_there_are_not():
+    import torch
+
+    from paper_2410_03462_b200 import api
+    x = torch.zeros(1, 1, 1, 8)
+    for mask in ("casual", None, "PREFIX"):
+        with pytest.raises(ValueError, match="full, causal, prefix"):
+            api.softmax_attn(None, x, x, x, mask=mask)
