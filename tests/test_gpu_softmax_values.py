@@ -228,6 +228,30 @@ def test_gradients_of_infinite_capped_scores(lib, route, dtype, bad, who):  # no
     assert dq[1].isfinite().all() and dk[1].isfinite().all() and dv[1].isfinite().all()
 
 
+INFERENCE = [(19, 8, 4, 150, 170, 128), (1, 2, 1, 300, 300, 96), (2, 4, 2, 129, 500, 128), (1, 3, 1, 257, 255, 64), (2, 2, 2, 70, 70, 24)]
+
+
+@pytest.mark.parametrize("shape", INFERENCE, ids=str)
+@pytest.mark.parametrize("cap,bias,mask", MODIFIERS)
+def test_outputs_only(lib, shape, cap, bias, mask):  # noqa: F811
+    """Calls that keep nothing for a backward pass, which bf16 has kernels of its own for."""
+    for more in (dict(), dict(ragged="empty", start=True), dict(docs="few")):
+        x, how, _ = make(83, *shape, "bf16", mask=mask, bias=bias, cap=cap, **more)
+        outputs_only(lib, x, how, f"{more}: ")
+    for scale in (-0.1, 0.0):
+        x, how, _ = make(89, *shape, "bf16", mask=mask, bias=bias, cap=cap)
+        outputs_only(lib, x, dict(how, scale=scale), f"scale {scale}: ")
+
+
+@pytest.mark.parametrize("mask", ["full", "causal"])
+def test_outputs_only_of_long_rows(lib, mask):  # noqa: F811
+    """The plain call at d = 128, some of whose exponentials are sums of products: over sharp rows and flat ones."""
+    for sharp in (0.1, 1.5, 12.0):
+        x, how, _ = make(97, 1, 2, 1, 300, 2000, 128, "bf16", mask=mask)
+        x["q"] = (x["q"].float() * sharp).bfloat16()
+        outputs_only(lib, x, how, f"times {sharp}: ")
+
+
 def test_refusals_of_the_backward_calls(lib):  # noqa: F811
     """What the library refuses is its error in every call, whoever brings the workspace."""
     api, B, ctx = lib
