@@ -37,8 +37,8 @@ template <int DP> struct Alu {
 
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) <= 3.4028235e38f; }
 
-// A chunk of a row as floats.  clean: what is not finite becomes 0; true if there was any.
-template <typename T> __device__ __forceinline__ bool to_floats(float (&v)[16 / sizeof(T)], const uint4& w, bool clean)
+// A chunk of a row as floats.  clean: what is not finite becomes 0, and *some (or NULL) 1; true if there was any.
+template <typename T> __device__ __forceinline__ bool to_floats(float (&v)[16 / sizeof(T)], const uint4& w, bool clean, int* some)
 {
     const T* t = reinterpret_cast<const T*>(&w);
     bool found = false;
@@ -48,6 +48,7 @@ template <typename T> __device__ __forceinline__ bool to_floats(float (&v)[16 / 
         if (clean && !finite(v[e])) {
             v[e] = 0.0f;
             found = true;
+            if (some) *some = 1;
         }
     }
     return found;
@@ -60,10 +61,10 @@ template <int PER> __device__ __forceinline__ void mark_row(int* bad, int r, boo
 }
 
 // Rows r0 .. r0 + 63 of [tokens][d] as floats: zeros behind `rows`, behind d, and for tokens whose document is negative.  clean: what is not
-// finite becomes 0 too; true if this thread has found any, and bad (or NULL) says in which rows there is some.
+// finite becomes 0 too; true if this thread has found any, bad (or NULL) says in which rows there is some, *some (or NULL) becomes 1 then.
 template <typename T, int DP>
 __device__ __forceinline__ bool load_rows(float* tile, const T* base, int64_t stride, int32_t r0, int32_t rows, int32_t d, const int32_t* doc,
-                                          bool clean, int* bad)
+                                          bool clean, int* bad, int* some = nullptr)
 {
     constexpr int CH = 16 / (int)sizeof(T), PER = DP / CH;
     static_assert(BT * PER % THREADS == 0 && 32 % PER == 0, "rows are whole warps' business");
@@ -75,7 +76,7 @@ __device__ __forceinline__ bool load_rows(float* tile, const T* base, int64_t st
 #pragma unroll
         for (int e = 0; e < CH; ++e) v[e] = 0.0f;
         if (r0 + r < rows && c < d && (!doc || doc[r0 + r] >= 0)) {
-            found = to_floats<T>(v, *reinterpret_cast<const uint4*>(base + (int64_t)(r0 + r) * stride + c), clean);
+            found = to_floats<T>(v, *reinterpret_cast<const uint4*>(base + (int64_t)(r0 + r) * stride + c), clean, some);
         }
         if (bad) mark_row<PER>(bad, r, found);
         any |= found;
@@ -99,14 +100,14 @@ template <typename T, int DP> struct rows_ahead {
                                                                                           : make_uint4(0, 0, 0, 0);
         }
     }
-    __device__ __forceinline__ bool store(float* tile, bool clean, int* bad) const
+    __device__ __forceinline__ bool store(float* tile, bool clean, int* bad, int* some = nullptr) const
     {
         bool any = false;
 #pragma unroll
         for (int y = 0; y < N; ++y) {
             const int x = threadIdx.x + y * THREADS, r = x / PER, c = x % PER * CH;
             float v[CH];
-            const bool found = to_floats<T>(v, w[y], clean);
+            const bool found = to_floats<T>(v, w[y], clean, some);
             if (bad) mark_row<PER>(bad, r, found);
             any |= found;
 #pragma unroll
@@ -276,11 +277,11 @@ __global__ void __launch_bounds__(THREADS, DP <= 64 ? 2 : 1) softmax_alu_forward
         __syncthreads();
         if constexpr (AHEAD) {
             ka.store(ks, false, nullptr);
-            if (va.store(vs, what == 1, nullptr)) bad = 1;
+            va.store(vs, what == 1, nullptr, &bad);
             fetch(j_next);
         } else {
             load_rows<T, DP>(ks, K, p.ks[2], j0, sight.len, p.d, kdoc, false, nullptr);
-            if (load_rows<T, DP>(vs, V, p.vs[2], j0, sight.len, p.d, kdoc, what == 1, nullptr)) bad = 1;
+            load_rows<T, DP>(vs, V, p.vs[2], j0, sight.len, p.d, kdoc, what == 1, nullptr, &bad);
         }
         load_bias<T>(lut, p, bucket, h, j0, sight.position(i0));
         __syncthreads();

@@ -503,9 +503,9 @@ softmax_tc_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 if (!PLAIN) {
                     const uint64_t by = CAP ? pack2(cap2, cap2) : pack2(to2, to2);
                     const float ahead = (float)(j0 + c0 - pos); // (exact, as are its sums, below 2^24; beyond, off by half a step as the distance itself)
-                    // A tile's length or more before the query the distance is a line, which starts at the tile's first key; nearer than that its two parts would be
+                    // Where a half's last key is its 64 columns before the query, or more, the distance is a line from its first key; nearer its two parts would be
                     // far larger than their sum, and the score be rounded to their steps (slopes of 1e4: lse off by 3e-4, and gradients with it).
-                    const bool line = BIAS == GRF_BIAS_SLOPES && __all_sync(0xffffffffu, j0 + 2 * BT - 1 <= pos);
+                    const bool line = BIAS == GRF_BIAS_SLOPES && __all_sync(0xffffffffu, j0 + c0 + 127 <= pos);
                     const float at0 = line ? slope2 * ahead : bias2;
                     const uint64_t at02 = pack2(at0, at0);
 #pragma unroll
