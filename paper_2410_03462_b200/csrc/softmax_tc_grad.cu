@@ -848,7 +848,9 @@ softmax_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                     const int32_t i0 = t * BT, pos0 = sight.position(i0);
                     const bool partial = sight.docs ? !T.whole(t) : block_partial || (ordered && pos0 < j0 + BT - 1);
                     // columns from `from` on see this key
-                    const int32_t from = j >= sight.len ? BT : sight.order == GRF_ORDER_FULL || j < sight.prefix ? 0 : min(max(j - pos0, 0), BT);
+                    // (none, where those that would are behind the last query: there P is 0 only if the key's scores are numbers)
+                    int32_t from = j >= sight.len ? BT : sight.order == GRF_ORDER_FULL || j < sight.prefix ? 0 : min(max(j - pos0, 0), BT);
+                    if (i0 + from >= p.Nq) from = BT;
                     const float slope2 = BIAS == GRF_BIAS_SLOPES ? grf_slope2(p, h) : 0.0f;
                     float bias2 = 0.0f;
                     bool diagonals = false;

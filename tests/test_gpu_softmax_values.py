@@ -300,3 +300,16 @@ def test_waits_beside_rows_that_are_summed_again(lib):  # noqa: F811
         # P and out to bf16; scores, of a size of 8 or less, and sums in 32 bits
         bound = size * (2 * 2.0**-8 + 2.0**-16) + 1e-9
         assert ((out[0, h, i].double() - want).abs() <= bound)[~sees].all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("cap", [0.0, 10.0])
+@pytest.mark.parametrize("mask", ["causal", "prefix"])
+def test_unseen_values_behind_the_last_query(lib, route, mask, cap, d):  # noqa: F811
+    """Keys behind the last query, in blocks of keys that earlier ones are seen in, where the last block of queries is not full."""
+    for seed, nq, nk in ((1, 95, 225), (2, 8, 100), (3, 234, 444), (4, 128, 300)):
+        x, how, dout = make(seed, 3, 2, 1, nq, nk, d, "bf16", mask=mask, cap=cap)
+        how["q_start"] = torch.tensor([0, nk // 3, nk - nq - 5], dtype=torch.int32, device="cuda")
+        if mask == "prefix":
+            how["prefix"].clamp_(max=nk // 4)
+        spoil_unseen(lib, x, how, dout, f"{nq} queries, {nk} keys")
