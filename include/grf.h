@@ -285,8 +285,8 @@ int grf_masked_attn_mhat(grf_ctx* ctx, const grf_features* feat, int32_t G, int3
  * table, columns n_buckets .. 2 n_buckets - 1.  grf_relative_buckets makes the usual choice of first[].
  *
  * What a token that nobody sees holds (infinities, NaN) does not matter, and in grf_softmax_attn what a key that a query does not see
- * holds does not matter to that query.  An infinity or NaN in what it does see makes its results infinite or NaN; in the backward pass
- * such a value of a token that is seen may reach the gradients of every token of its sequence.
+ * holds does not matter to that query.  An infinity or NaN in what it does see makes its results infinite or NaN, unless a cap makes a number of
+ * an infinite score; in the backward pass such a value of a token that is seen may reach the gradients of every token of its sequence.
  * Arrays that are written may overlap neither one another nor those that are read.
  */
 #define GRF_ORDER_FULL   0
@@ -298,7 +298,8 @@ int grf_masked_attn_mhat(grf_ctx* ctx, const grf_features* feat, int32_t G, int3
 #define GRF_MAX_BUCKETS  64
 #define GRF_MAX_TOKENS   (1 << 22)   /* largest n_q and n_k */
 
-/* Zero the whole structure first: a zero field means "not used" (a stride triple of zeros: contiguous [batch][heads][tokens][dim]). */
+/* Zero the whole structure first: a zero field means "not used" (a stride triple of zeros: contiguous [batch][heads][tokens][dim]).
+ * GRF_ERR_INVALID unless batch, heads, kv_heads, n_q and n_k are 1 or more: there is no empty call. */
 typedef struct grf_softmax_desc {
     int32_t batch, heads, kv_heads, n_q, n_k;  /* kv_heads divides heads                                                     */
     int32_t dim;                       /* of Q, K and V: a multiple of 8, 8 .. 128                                           */
@@ -355,7 +356,8 @@ int grf_softmax_attn_backward(grf_ctx* ctx, const grf_softmax_desc* desc, const 
                               size_t workspace_bytes);
 
 /* The learned relative position bias by itself, as rows of a matrix (compare grf_mask_rows): rows[h][i][j] = table[h][bucket(j - (q_start
- * + i))], buckets as above; first: HOST [n_buckets].  table [heads][n_buckets * (1 + two_sided)] and rows [heads][n_q][n_k]: DEVICE, dtype.
+ * + i))], buckets as above; first: HOST [n_buckets].  table [heads][n_buckets * (1 + two_sided)] and rows [heads][n_q][n_k]: DEVICE, dtype,
+ * contiguous; rows and drows 16-byte aligned.
  * The backward call sums drows [batch][heads][n_q][n_k] into dtable (fp32 sums in a fixed order, one rounding to dtype), for which it
  * needs the workspace.  Asynchronous.  At most GRF_MAX_TOKENS tokens and 65535 heads. */
 int grf_relative_bias(grf_ctx* ctx, int32_t heads, int32_t n_q, int32_t n_k, int32_t q_start, int32_t n_buckets, int two_sided,

@@ -239,8 +239,8 @@ def _bytes(workspace):
 
 def softmax_attn(ctx: Context, q, k, v, scale=None, cap=0.0, mask="full", k_len=None, q_start=None, prefix=None, q_doc=None,
                  k_doc=None, slopes=None, table=None, first=None, two_sided=False, want_lse=False, out=None, workspace=None):
-    """Softmax attention over tokens in an order (grf_softmax_attn).  q [B, H, Nq, d], k, v [B, KV, Nk, d]: CUDA tensors (fp32 or bf16)
-    of any strides with a contiguous last axis; KV divides H.  mask: "full", "causal", "prefix" (with prefix [B]).  k_len, q_start,
+    """Softmax attention over tokens in an order (grf_softmax_attn).  q [B, H, Nq, d], k, v [B, KV, Nk, d]: CUDA tensors (fp32 or bf16),
+    the last axis contiguous, the others of any strides, 0 among them, that are whole 16 bytes, as addresses are; d a multiple of 8 up to 128; KV divides H.  mask: "full", "causal", "prefix" (with prefix [B]).  k_len, q_start,
     prefix [B], q_doc [B, Nq], k_doc [B, Nk]: int32.  A bias by distance: slopes [H] (fp32), or table [H, len(first)] (twice as many
     columns when two_sided) with first as relative_buckets gives it.  Returns out [B, H, Nq, d]; with want_lse (out, SoftmaxSaved),
     which the backward pass takes."""
@@ -262,7 +262,7 @@ def softmax_attn(ctx: Context, q, k, v, scale=None, cap=0.0, mask="full", k_len=
 def softmax_attn_backward(ctx: Context, q, k, v, out, saved, dout, scale=None, cap=0.0, mask="full", k_len=None, q_start=None,
                           prefix=None, q_doc=None, k_doc=None, slopes=None, table=None, first=None, two_sided=False,
                           want_dtable=True, workspace=None):
-    """Gradients of softmax_attn from its out and SoftmaxSaved and the gradient dout of out (any strides): (dq, dk, dv, dtable), dtable None
+    """Gradients of softmax_attn from its out and SoftmaxSaved and the gradient dout of out (strides as of q): (dq, dk, dv, dtable), dtable None
     without a table.  Gradients of broadcast or shared k, v are those of the tensors as they are passed."""
     s = _softmax_desc(ctx, q, k, v, scale, cap, mask, k_len, q_start, prefix, q_doc, k_doc, slopes, table, first, two_sided)
     for name, t in (("out", out), ("dout", dout)):

@@ -8,8 +8,10 @@
 // all heads that share it for dK and dV.
 //
 // 256 threads hold 4 x 4 scores each; operands lie in shared memory as rows with four words of padding, read 16 bytes at a time: two reads
-// for sixteen multiply-adds.  What bounds it is the latency of these reads: two CTAs of eight warps fit an SM and issue in two cycles of five
-// (d <= 64, where the next tile's loads wait in registers as well), about 9 TFLOP/s of visible work on 3 x 5 heads x 1003.
+// for sixteen multiply-adds.  What bounds it is latency: two CTAs of eight warps fit an SM (d <= 64, where the next tile's loads wait in registers as
+// well) and issue in 31 % of the cycles (forward, d = 32; 26 % with d = 64, gradients 21 %), waiting at a tile's barriers (1.7 .. 4.0 cycles per instruction),
+// for shared memory (1.6 .. 1.9) and for memory (0.8 .. 2.9): about 12 TFLOP/s of visible work on 3 x 5 heads x 1003.  Products run over 32, 64 or 128
+// dimensions, so others pay for the next of these.
 #include <cooperative_groups.h>
 
 #include "packed.cuh"

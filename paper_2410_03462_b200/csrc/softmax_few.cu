@@ -1,5 +1,5 @@
 // Softmax attention of a few queries per sequence (new tokens against a cache): the keys are split over CTAs and warps, and K and V are
-// read once, straight into registers.
+// read straight into registers, once for every block of rows.
 //
 // The rows of one key head are its group's heads times n_q queries, in blocks of 16 (bf16) or 4 (fp32).  A warp goes over every fourth
 // 16-key (fp32: 8-key) tile of its CTA's stretch with running maxima and sums; warps join in shared memory, CTAs of a sequence and head
@@ -9,10 +9,13 @@
 // instruction.  A thread loads 16 bytes of a key: eight consecutive values where the fragment wants four pairs eight apart.  A product over d
 // does not depend on its order, so Q is loaded in the same order; value fragments are 8 x 8 blocks transposed in registers, which
 // permutes the columns of O^T in the same known way.  No shared memory is filled, and a tile's loads are under way while the one before
-// is multiplied.  fp32: a thread holds a quarter of a key's dimensions and adds in plain arithmetic; four rows, so that their sums fit in registers.
+// is multiplied.  P is rounded to bf16 for its product (by 2^-8 relative at most, as the outputs are; l sums it unrounded).
+// fp32: a thread holds a quarter of a key's dimensions and adds in plain arithmetic; four rows, whose sums fit in registers up to d = 64 (d = 96
+// spills 96 bytes a thread, d = 128 444).
 //
-// What bounds it is the memory: 64 sequences x 32 heads (8 of keys) of up to 8192 keys, d = 128, 248 us, 5.4 TB/s; eight times as many CTAs as SMs, as
-// lengths are uneven (four times: 252, sixteen: 257).  One sequence of 1000 keys takes 8 us, latency from end to end.
+// What bounds bf16 is the memory: 64 sequences x 32 heads (8 of keys) of up to 8192 keys, d = 128, 248 .. 260 us on several cards, 5.4 .. 5.2 TB/s; eight
+// times as many CTAs as SMs, as lengths are uneven (four and sixteen times: no better).  One sequence of 1000 keys takes 8 us, latency from end to end.
+// fp32: latency and instructions, at 1.7 warps a scheduler (issue slots 20 % busy), and more than four rows read the keys again.
 #include <cooperative_groups.h>
 
 #include "softmax.cuh"

@@ -6,7 +6,7 @@
 // precision: bf16 has the same relative step everywhere and l is fp32), so almost never after the first tiles.
 // A CTA has an SM to itself and works on two groups of 128 queries in turn with the tensor cores.  Two threads share a query, 64 columns
 // each (they agree on the maximum through shared memory): with one thread a query, two warps per scheduler, the chain of a tile - load,
-// maximum, exponentials, store - bounded the kernel (2 x 16 heads x 4096 causal and capped, d = 128: 272 us, with two 234; d = 64: 207 and 182).
+// maximum, exponentials, store - bounded the kernel (2 x 16 heads x 4096 causal and capped, d = 128: 272 us, with two 234 at that time, 247 with all that came since; d = 64: 207 and 182).
 //   d > 64   P overwrites S
 //   d <= 64  P has its own place, so the next S is made while P is
 //   warps of the last warpgroup: copies of K and V (boxes by the copy engine), one issuing warp per group, and one that clears rows of V
