@@ -312,7 +312,8 @@ typedef struct grf_softmax_desc {
     const float* slopes;               /* DEVICE [heads]                                                                     */
     const void* table;                 /* DEVICE [heads][n_buckets * (1 + two_sided)], dtype                                 */
     const int32_t* k_len;              /* DEVICE [batch] or NULL: n_k each; values are clipped to 0 .. n_k                   */
-    const int32_t* q_start;            /* DEVICE [batch] or NULL: n_k - n_q each (the queries are the last tokens)           */
+    const int32_t* q_start;            /* DEVICE [batch] or NULL: n_k - n_q each (the queries are the last tokens); positions
+                                        * beyond +-2^30 count as +-2^30                                                      */
     const int32_t* prefix;             /* DEVICE [batch], with GRF_ORDER_PREFIX                                              */
     const int32_t* q_doc;              /* DEVICE [batch][n_q] and                                                            */
     const int32_t* k_doc;              /* DEVICE [batch][n_k]: both or neither; any order of documents                       */

@@ -313,3 +313,26 @@ def test_unseen_values_behind_the_last_query(lib, route, mask, cap, d):  # noqa:
         if mask == "prefix":
             how["prefix"].clamp_(max=nk // 4)
         spoil_unseen(lib, x, how, dout, f"{nq} queries, {nk} keys")
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("nq", [3, 140])
+def test_numbers_at_the_ends_of_their_range(lib, route, dtype, nq):  # noqa: F811
+    """Starts, lengths, prefixes and documents of any 32 bits."""
+    if dtype == "fp32" and route == "alu":
+        pytest.skip("fp32 has one route")
+    low, high = -2**31, 2**31 - 1
+    ends = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    for mask in ("full", "causal", "prefix"):
+        for bias, buckets in (("none", (32, 128)), ("table", (32, 128)), ("table", (64, 1 << 24))):
+            x, how, dout = make(107, 6, 2, 1, nq, 150, 64, dtype, mask=mask, bias=bias, buckets=buckets)
+            if mask == "prefix":
+                how["prefix"] = ends(low, high, 0, 40, high, low)
+            how["q_start"] = ends(low, high, -nq // 2, 100, low, high)
+            how["k_len"] = ends(high, high, 150, high, 70, low)
+            check(lib, x, how, dout, f"{mask} {bias}: ")
+            g = torch.Generator().manual_seed(1)
+            ids = ends(low, -1, 0, 1, high - 1, high)
+            pick = lambda n: ids[torch.randint(0, 6, (6, n), generator=g).cuda()]  # noqa: E731
+            x, how, dout = make(109, 6, 2, 1, nq, 150, 64, dtype, mask=mask, bias=bias, buckets=buckets)
+            check(lib, x, dict(how, q_doc=pick(nq), k_doc=pick(150)), dout, f"{mask} {bias} documents: ")
